@@ -48,9 +48,227 @@ __global__ __launch_bounds__(256) void matmul_simple(const uint8_t *__restrict__
     }
 }
 
+
+// ---- tiles through LDS
+//
+// A workgroup of WM x WN waves computes a BM x BN tile, each wave TM x TN
+// blocks of 32 x 32.  The contraction goes in stages of 128 columns (64 bytes
+// of codes a row).  Codes are copied from memory straight into LDS, sixteen
+// bytes a lane, three stages ahead of the products through four buffers;
+// scales likewise, for two groups of 256 columns at a time (16 bytes a row),
+// two such pairs ahead.  Past the end the copies repeat the last stage, so
+// that the loop has no branches: it is one run of matrix instructions with
+// everything else dealt out between them.  A stage is two rounds of matrix instructions, and the operands of each round
+// are read from LDS during the round before, the first ones of a stage before
+// its own barrier: that barrier says that the NEXT stage's codes are there.
+//
+// Of a stage's four blocks half h of the lanes takes blocks 2 h and 2 h + 1.
+// In LDS a row's four 16-byte pieces are permuted by bits 1 and 2 of the row
+// number, so that eight rows that are read together fill all banks once; the
+// copy writes LDS in lane order, so the permutation is applied to the
+// addresses that it reads.
+//
+// The operands change places in the instruction (B first), so that a lane
+// ends up with one row of the result and four columns in sequence; the
+// results of 32 rows go through LDS once more to be stored sixteen bytes a
+// lane.
+constexpr int kStageCodes = 64;  // bytes of a row
+constexpr int kBuffers = 4;
+constexpr int kScaleGroups = 2;   // groups whose scales are copied together
+constexpr int kScaleBuffers = 4;
+
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+// Sixteen bytes per lane from base + offset to LDS at dst + 16 lane.  The
+// compiler does not count these copies: whoever reads dst waits for them.
+__device__ inline void copy_to_lds(uint32_t dst, const uint8_t *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base));
+}
+__device__ inline void copy4_to_lds(uint32_t dst, const uint8_t *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base));
+}
+// All but the newest N copies (or loads) of this wave have arrived, its LDS
+// accesses are done, and so it is for the other waves.
+template <int N> __device__ inline void wait_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int T, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
+                                                            const uint8_t *__restrict__ bc, const uint8_t *__restrict__ bs,
+                                                            int64_t M, int64_t N, int groups, uint32_t tiles_m,
+                                                            uint32_t tiles_n, typename Elem<T>::type *__restrict__ out,
+                                                            int64_t stride) {
+    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, ROWS = BM + BN;
+    constexpr int COPIES = ROWS / 16 / W;  // per wave and stage: sixteen rows each
+    constexpr int A_COPIES = BM / 16 / W;  // of which rows of A
+    constexpr int SCALE_COPIES = ROWS / 16 / W;  // per wave and two groups: sixteen rows each
+    constexpr int OPS = TM + TN, PRODUCTS = TM * TN;  // of a round
+    static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0, "rows are dealt evenly");
+    static_assert(OPS <= PRODUCTS && COPIES <= PRODUCTS && SCALE_COPIES % 4 == 0, "they fit beside a round's products");
+    constexpr int STAGE_COPIES = COPIES + SCALE_COPIES / 4;
+    constexpr int SCALE_ROW = kScaleGroups * kGroupScales;
+    __shared__ __align__(16) uint8_t codes[kBuffers][ROWS * kStageCodes];
+    __shared__ __align__(16) uint8_t scales[kScaleBuffers][ROWS * SCALE_ROW];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 31, h = lane >> 5;
+    const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x % tiles_n;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int stages = groups * 2;
+
+    // rows past the end repeat the last one: their products are not stored
+    const int64_t code_pitch = (int64_t)groups * kGroupCodes, scale_pitch = (int64_t)groups * kGroupScales;
+    const uint8_t *a_base = ac + m0 * code_pitch, *b_base = bc + n0 * code_pitch;
+    const int a_last = (int)min((int64_t)BM, M - m0) - 1, b_last = (int)min((int64_t)BN, N - n0) - 1;
+    uint32_t src[COPIES];
+#pragma unroll
+    for (int i = 0; i < COPIES; i++) {
+        const bool in_a = i < A_COPIES;
+        const int row = (in_a ? wave * A_COPIES + i : wave * (COPIES - A_COPIES) + i - A_COPIES) * 16 + (lane >> 2);
+        src[i] = (uint32_t)(min(row, in_a ? a_last : b_last) * (uint32_t)code_pitch) + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)&codes[0][0];
+    const uint32_t dst_a = lds0 + wave * A_COPIES * 1024, dst_b = lds0 + BM * kStageCodes + wave * (COPIES - A_COPIES) * 1024;
+    const auto copy = [&](int i, int stage, int at) {
+        const uint32_t buffer = (uint32_t)at % kBuffers * (ROWS * kStageCodes);
+        if (i < A_COPIES) copy_to_lds(dst_a + buffer + i * 1024, a_base + (int64_t)stage * kStageCodes, src[i]);
+        else copy_to_lds(dst_b + buffer + (i - A_COPIES) * 1024, b_base + (int64_t)stage * kStageCodes, src[i]);
+    };
+
+    const uint8_t *as_base = as + m0 * scale_pitch, *bs_base = bs + n0 * scale_pitch;
+    const uint32_t sdst = (uint32_t)(uintptr_t)(lds_byte *)&scales[0][0] + wave * SCALE_COPIES * 256;
+    const auto copy_scale = [&](int i, int g) {  // of the two groups from g on, four lanes a row
+        const int first = (wave * SCALE_COPIES + i) * 16, row = first + (lane >> 2);
+        const bool in_a = first < BM;
+        const int at = in_a ? min(row, a_last) : min(row - BM, b_last);
+        const uint32_t offset = (uint32_t)at * (uint32_t)scale_pitch + min(g + ((lane & 3) >> 1), groups - 1) * kGroupScales + (lane & 1) * 4;
+        copy4_to_lds(sdst + (uint32_t)(g / kScaleGroups) % kScaleBuffers * (ROWS * SCALE_ROW) + i * 256, in_a ? as_base : bs_base, offset);
+    };
+
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) acc[i][j] = f32x16{0};
+    const int row_a = wave / WN * TM * 32 + r, row_b = BM + wave % WN * TN * 32 + r;
+
+    // operands of the round in hand and of the next; sixteen bits of scales (a byte for each round) a stage
+    u32x4 op[2][OPS];
+    int sc[2][OPS];
+    const auto row_of = [&](int i) { return i < TM ? row_a + i * 32 : row_b + (i - TM) * 32; };
+    // in the order of first use: a row block, the column blocks, the other row blocks
+    const auto nth_op = [&](int n) { return n == 0 ? 0 : n <= TN ? TM + n - 1 : n - TN; };
+    const auto read_op = [&](int i, int stage, int s) {
+        const int piece = (h * 2 + s) ^ ((lane >> 1) & 3);
+        op[s][i] = *(const u32x4 *)(codes[(uint32_t)stage % kBuffers] + row_of(i) * kStageCodes + piece * 16);
+    };
+    const auto read_scale = [&](int i, int stage, int q) {
+        const uint8_t *p = scales[(uint32_t)stage / (2 * kScaleGroups) % kScaleBuffers] + stage % (2 * kScaleGroups) * 4 + h * 2;
+        sc[q][i] = *(const uint16_t *)(p + row_of(i) * SCALE_ROW);
+    };
+    const auto product = [&](auto sel, auto parity, int n) {
+        constexpr int s = decltype(sel)::value, q = decltype(parity)::value;
+        const int i = n / TN, j = n % TN;
+        i32x8 a = {0}, b = {0};
+        *(u32x4 *)&a = op[s][i];
+        *(u32x4 *)&b = op[s][TM + j];
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, acc[i][j], 4, 4, s, sc[q][TM + j], s, sc[q][i]);
+    };
+    typedef std::integral_constant<int, 0> C0;
+    typedef std::integral_constant<int, 1> C1;
+
+#pragma unroll
+    for (int i = 0; i < SCALE_COPIES; i++) copy_scale(i, 0), copy_scale(i, kScaleGroups);
+#pragma unroll
+    for (int k = 0; k < 3; k++)
+#pragma unroll
+        for (int i = 0; i < COPIES; i++) copy(i, min(k, stages - 1), k);
+    wait_and_meet<0>();
+#pragma unroll
+    for (int n = 0; n < OPS; n++) read_op(nth_op(n), 0, 0), read_scale(nth_op(n), 0, 0);
+
+    const auto run_stage = [&](int g, auto half) {
+        constexpr int q = decltype(half)::value;
+        const int t = 2 * g + q;
+        wait_and_meet<STAGE_COPIES>();  // the codes of stage t + 1 are there, and the buffer of stage t - 1 is free
+#pragma unroll
+        for (int n = 0; n < PRODUCTS; n++) {
+            if (n < OPS) read_op(nth_op(n), t, 1);
+            if (n < SCALE_COPIES / 4)
+                copy_scale(((g & 1) * 2 + q) * (SCALE_COPIES / 4) + n, (g & ~1) + 2 * kScaleGroups);
+            if (n >= PRODUCTS - COPIES) copy(n - (PRODUCTS - COPIES), min(t + 3, stages - 1), t + 3);
+            product(C0(), half, n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int n = 0; n < PRODUCTS; n++) {
+            if (n < OPS) read_op(nth_op(n), t + 1, 0), read_scale(nth_op(n), t + 1, 1 - q);
+            product(C1(), half, n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int g = 0; g < groups; g++) {
+        run_stage(g, C0());
+        run_stage(g, C1());
+    }
+    wait_and_meet<0>();
+
+    typedef typename Elem<T>::type E;
+    constexpr int COLS = TN * 32, PITCH = COLS + 16 / sizeof(E), PER = 16 / sizeof(E), LANES = COLS / PER;
+    static_assert(W * 32 * PITCH * sizeof(E) <= sizeof(codes), "the results of 32 rows of every wave fit");
+    E *mine = (E *)&codes[0][0] + wave * 32 * PITCH;
+    const int64_t n_wave = n0 + wave % WN * COLS;
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+#pragma unroll
+        for (int j = 0; j < TN; j++)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) {
+                E e[4];
+#pragma unroll
+                for (int c = 0; c < 4; c++) e[c] = Elem<T>::put(acc[i][j][v + c]);
+                E *p = mine + r * PITCH + j * 32 + 2 * v + 4 * h;
+                if (sizeof(E) == 2) *(u32x2 *)p = *(u32x2 *)e;
+                else *(u32x4 *)p = *(u32x4 *)e;
+            }
+        __builtin_amdgcn_wave_barrier();
+        const int64_t m_first = m0 + wave / WN * TM * 32 + i * 32, n = n_wave + lane % LANES * PER;
+#pragma unroll
+        for (int k = 0; k < 32; k += 64 / LANES) {
+            const int row = k + lane / LANES;
+            const u32x4 v = *(const u32x4 *)(mine + row * PITCH + lane % LANES * PER);
+            if (m_first + row < M) {
+                E *o = out + (m_first + row) * stride + n;
+                if (n + PER <= N) *(u32x4_any *)o = v;
+                else
+#pragma unroll
+                    for (int c = 0; c < PER; c++)
+                        if (n + c < N) o[c] = ((const E *)&v)[c];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <int T, int WM, int WN, int TM, int TN>
+void launch_tile(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs, int64_t M,
+                 int64_t N, int64_t K, void *out, int64_t stride) {
+    constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
+    const uint32_t tm = (uint32_t)((M + BM - 1) / BM), tn = (uint32_t)((N + BN - 1) / BN);
+    matmul_tile<T, WM, WN, TM, TN><<<tm * tn, 64 * WM * WN, 0, st>>>(ac, as, bc, bs, M, N, (int)groups_of(K), tm, tn,
+                                                                   (typename Elem<T>::type *)out, stride);
+}
+
 template <int T>
 sim_status matmul_t(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs, int64_t M,
                     int64_t N, int64_t K, void *out, int64_t stride) {
+    if (M >= 128 && N >= 128 && K > 0 && K < (1 << 23)) {  // offsets within a tile fit in 32 bits
+        if (((M + 255) / 256) * ((N + 255) / 256) >= 200) launch_tile<T, 2, 2, 4, 4>(st, ac, as, bc, bs, M, N, K, out, stride);
+        else launch_tile<T, 2, 2, 2, 2>(st, ac, as, bc, bs, M, N, K, out, stride);
+        return SIM_OPS_LAUNCH_OK();
+    }
     const uint32_t grid = (uint32_t)(((M + 63) / 64) * ((N + 63) / 64));
     matmul_simple<T><<<grid, 256, 0, st>>>(ac, as, bc, bs, M, N, (int)groups_of(K), (typename Elem<T>::type *)out, stride);
     return SIM_OPS_LAUNCH_OK();
