@@ -4,45 +4,30 @@
 // stream.
 //
 // Both products run on 16x16x32 matrix instructions with sixteen weight rows
-// as the first operand and sixteen of the expert's tokens as the second, the
-// waves of a workgroup each taking a part of the contraction.  Activations
-// and 4-bit weights enter as bf16; values of more than 8 significant bits
-// (fp16 inputs, the hidden values between the products) enter as the sum of
-// two bf16 parts, which is free where the weights' bytes bound the time.
-#include "ops_common.h"
+// as the first operand and sixteen tokens as the second, the waves of a
+// workgroup each taking a part of the contraction in steps of 128 columns.
+// A wave keeps a ring of U steps' operands in registers and refills a place
+// as soon as it has been multiplied, weights and activations alike, since
+// loads return in the order in which they were issued.  Activations and 4-bit
+// weights enter as bf16; values of more than 8 significant bits (fp16, the
+// hidden values between the products) enter as the sum of two bf16 parts,
+// which is free where the weights' bytes bound the time.
+#include "ops_route_keys.h"
 
 namespace simops {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int kStep = 128;  // columns of one step of a wave
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// Which expert the a-th non-empty list belongs to; -1 past the last.
-__device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int a, int *shared) {
-    const int lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        int seen = 0, found = -1;
-        for (int e0 = 0; e0 < E && found < 0; e0 += 64) {
-            const int e = e0 + lane;
-            const bool some = e < E && offsets[e + 1] > offsets[e];
-            const uint64_t all = __ballot(some);
-            const bool hit = some && seen + __popcll(all & ((1ull << lane) - 1)) == a;
-            const uint64_t at = __ballot(hit);
-            if (at) found = e0 + __ffsll((unsigned long long)at) - 1;
-            seen += __popcll(all);
-        }
-        if (lane == 0) *shared = found;
-    }
-    __syncthreads();
-    return *shared;
-}
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// 16-bit elements k .. k + 7 of a row of K, zeros past its end, as raw bits.
-__device__ inline u32x4 load_row8(const uint16_t *__restrict__ row, int64_t k, int64_t K) {
-    if (k + 8 <= K) return *(const u32x4_a2 *)(row + k);
+// 16-bit elements k .. k + 7 of a row of K as raw bits, zeros past its end.
+// EDGE: K need not be a whole number of steps.
+template <bool EDGE> __device__ inline u32x4 load_row8(const uint16_t *__restrict__ row, int k, int K) {
+    if (!EDGE || k + 8 <= K) return *(const u32x4_a2 *)(row + k);
     uint16_t v[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = k + i < K ? row[k + i] : 0;
@@ -70,155 +55,548 @@ __device__ inline bf16x8 widen8(uint32_t codes, float scale) {
     return r;
 }
 
-__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// A step's elements of lane l (q = l / 16) in instruction s: 16-bit weights
+// take 32 s + 8 q .. + 7, so that an instruction's load covers 64 contiguous
+// bytes of each row; 4-bit ones 32 q + 8 s, whose 32 codes are one load.
+template <int WT> __device__ inline int step_at(int q, int s) { return WT == SIM_TYPE_MX4 ? 32 * q + 8 * s : 32 * s + 8 * q; }
 
-// A wave's step of one 16-row weight tile: lane l holds row l % 16 and, of
-// 128 columns, elements 32 (l / 16) + 8 s .. + 7 in instruction s.
-template <int WT> struct Weights;  // the four instructions' operands
-template <> struct Weights<SIM_TYPE_BF16> {
+// A step of one tile of sixteen weight rows; lane l holds row l % 16.
+template <int WT, bool EDGE> struct Weights {
     u32x4 raw[4];
-    __device__ void load(const void *base, const uint8_t *, int64_t row, int64_t K, int64_t k) {
+    // base: the weights; row: this lane's; k0: the step's first column
+    __device__ void load(const void *base, const uint8_t *, int64_t row, int K, int k0, int q) {
         const uint16_t *p = (const uint16_t *)base + row * K;
 #pragma unroll
-        for (int s = 0; s < 4; s++) raw[s] = load_row8(p, k + 8 * s, K);
+        for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(p, k0 + step_at<WT>(q, s), K);
     }
-    __device__ f32x4 mul(int s, bf16x8 x, f32x4 c) const { return mfma(__builtin_bit_cast(bf16x8, raw[s]), x, c); }
-};
-template <> struct Weights<SIM_TYPE_F16> {
-    u32x4 raw[4];
-    __device__ void load(const void *base, const uint8_t *, int64_t row, int64_t K, int64_t k) {
-        const uint16_t *p = (const uint16_t *)base + row * K;
-#pragma unroll
-        for (int s = 0; s < 4; s++) raw[s] = load_row8(p, k + 8 * s, K);
-    }
-    __device__ f32x4 mul(int s, bf16x8 x, f32x4 c) const {
+    struct Operand {
         bf16x8 hi, lo;
-        split_f16(raw[s], hi, lo);
-        return mfma(lo, x, mfma(hi, x, c));
+    };
+    __device__ Operand operand(int s) const {
+        Operand o;
+        if (WT == SIM_TYPE_F16) split_f16(raw[s], o.hi, o.lo);
+        else o.hi = __builtin_bit_cast(bf16x8, raw[s]);
+        return o;
+    }
+    static __device__ f32x4 mul(const Operand &w, bf16x8 x, f32x4 c) {
+        c = mfma(w.hi, x, c);
+        return WT == SIM_TYPE_F16 ? mfma(w.lo, x, c) : c;
     }
 };
-template <> struct Weights<SIM_TYPE_MX4> {
+template <bool EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
     u32x4 raw;
     uint32_t sb;
-    __device__ void load(const void *base, const uint8_t *scales, int64_t row, int64_t K, int64_t k) {
+    __device__ void load(const void *base, const uint8_t *scales, int64_t row, int K, int k0, int q) {
+        // rows are whole groups of 256 columns, so a step never leaves its row
         const int64_t g = groups_of(K);
-        raw = u32x4{0, 0, 0, 0};
-        sb = 0;
-        if (k < K) {  // the row's last group may end in the middle of a step
-            raw = *(const u32x4 *)((const uint8_t *)base + row * g * kGroupCodes + k / 2);
-            sb = scales[row * g * kGroupScales + k / 32];
-        }
+        raw = *(const u32x4 *)((const uint8_t *)base + row * g * kGroupCodes + k0 / 2 + q * 16);
+        sb = scales[row * g * kGroupScales + k0 / 32 + q];
     }
-    __device__ f32x4 mul(int s, bf16x8 x, f32x4 c) const { return mfma(widen8(raw[s], scale_value(sb)), x, c); }
+    struct Operand {
+        bf16x8 hi;
+    };
+    __device__ Operand operand(int s) const { return {widen8(raw[s], scale_value(sb))}; }
+    static __device__ f32x4 mul(const Operand &w, bf16x8 x, f32x4 c) { return mfma(w.hi, x, c); }
 };
 
-// Gate and up products of sixteen hidden units of one expert.
-template <int T, int WT>
-__global__ __launch_bounds__(64 * kWaves) void layer_up(const uint16_t *__restrict__ x, int64_t x_stride, int64_t D,
-                                                        const void *__restrict__ w13, const uint8_t *__restrict__ s13,
-                                                        int64_t F, int E, int k, const int32_t *__restrict__ offsets,
-                                                        const int32_t *__restrict__ order,
-                                                        const float *__restrict__ weights, uint32_t tiles,
-                                                        __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo,
-                                                        int64_t h_pitch) {
-    __shared__ int s_expert;
-    __shared__ f32x4 part[kWaves][2][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int e = nth_expert(offsets, E, blockIdx.x / tiles, &s_expert);
-    if (e < 0) return;
-    const int64_t f0 = (int64_t)(blockIdx.x % tiles) * 16;
-    const int first = offsets[e], n = offsets[e + 1] - first;
-    const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
-    for (int c0 = 0; c0 < n; c0 += 16) {
-        const int slot = order[first + min(c0 + r, n - 1)];
-        const uint16_t *xr = x + (int64_t)(slot / k) * x_stride;
-        f32x4 g = {0}, u = {0};
-        for (int64_t d = wave * kStep; d < D; d += kWaves * kStep) {
-            const int64_t kk = d + q * 32;
-            Weights<WT> wg, wu;
-            wg.load(w13, s13, row, D, kk);
-            wu.load(w13, s13, row + F, D, kk);
+// A step of sixteen inputs; lane l holds token l % 16.
+template <int T, int WT, bool EDGE> struct Inputs {
+    u32x4 raw[4];
+    __device__ void load(const uint16_t *row, int K, int k0, int q) {
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                const u32x4 raw = load_row8(xr, kk + 8 * s, D);
-                if (T == SIM_TYPE_BF16) {
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, raw);
-                    g = wg.mul(s, v, g);
-                    u = wu.mul(s, v, u);
-                } else {
-                    bf16x8 hi, lo;
-                    split_f16(raw, hi, lo);
-                    g = wg.mul(s, lo, wg.mul(s, hi, g));
-                    u = wu.mul(s, lo, wu.mul(s, hi, u));
-                }
+        for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
+    }
+    template <typename W> __device__ f32x4 mul(int s, const typename W::Operand &w, f32x4 c) const {
+        if (T == SIM_TYPE_BF16) return W::mul(w, __builtin_bit_cast(bf16x8, raw[s]), c);
+        bf16x8 hi, lo;
+        split_f16(raw[s], hi, lo);
+        return W::mul(w, lo, W::mul(w, hi, c));
+    }
+};
+
+// A step of sixteen rows of hidden values in their two parts (rows of a whole
+// number of steps), zeros where the lane has none.
+template <int WT> struct Hidden {
+    u32x4 hi[4], lo[4];
+    __device__ void load(const __bf16 *h_hi, const __bf16 *h_lo, int64_t at, bool some, int k0, int q) {
+#pragma unroll
+        for (int s = 0; s < 4; s++) {
+            hi[s] = lo[s] = u32x4{0, 0, 0, 0};
+            if (some) {
+                hi[s] = *(const u32x4 *)(h_hi + at + k0 + step_at<WT>(q, s));
+                lo[s] = *(const u32x4 *)(h_lo + at + k0 + step_at<WT>(q, s));
             }
         }
-        part[wave][0][lane] = g;
-        part[wave][1][lane] = u;
-        __syncthreads();
-        if (wave == 0) {
+    }
+    template <typename W> __device__ f32x4 mul(int s, const typename W::Operand &w, f32x4 c) const {
+        return W::mul(w, __builtin_bit_cast(bf16x8, lo[s]), W::mul(w, __builtin_bit_cast(bf16x8, hi[s]), c));
+    }
+};
+
+// n operands through a ring of U places: load(place, which), use(place).  The
+// loop that does the work has no conditions, so the waits in it count loads
+// exactly; n = 0 loads the first operand and uses nothing.
+template <int U, typename Load, typename Use> __device__ inline void ring(int n, Load &&load, Use &&use) {
 #pragma unroll
-            for (int w = 1; w < kWaves; w++) {
-                g += part[w][0][lane];
-                u += part[w][1][lane];
+    for (int i = 0; i < U; i++) load(i, max(0, min(i, n - 1)));
+    int at = 0;
+    for (; at + 2 * U <= n; at += U)
+#pragma unroll
+        for (int i = 0; i < U; i++) {
+            use(i);
+            load(i, at + U + i);
+        }
+#pragma unroll
+    for (int i = 0; i < U; i++) {
+        if (at + i < n) use(i);
+        if (at + U + i < n) load(i, at + U + i);
+    }
+#pragma unroll
+    for (int i = 0; i < U; i++)
+        if (at + U + i < n) use(i);
+}
+// of n steps dealt to W waves in turn, those of this wave
+__device__ inline int share(int n, int wave, int W) { return n > wave ? (n - wave + W - 1) / W : 0; }
+
+__device__ inline float gated(float g, float u, float w) { return g / (1.f + expf(-g)) * u * w; }
+
+__device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, const float v[4]) {
+    __bf16 hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        hi[i] = (__bf16)v[i];
+        lo[i] = (__bf16)(v[i] - (float)hi[i]);
+    }
+    *(u32x2 *)(h_hi + at) = *(u32x2 *)hi;
+    *(u32x2 *)(h_lo + at) = *(u32x2 *)lo;
+}
+
+// ------------------------------------------------------- at most 16 tokens
+//
+// Two kernels, of as many workgroups as the GPU holds at once.  The tokens
+// themselves are the sixteen columns of every product.  The first kernel
+// routes, every workgroup for itself, which costs less than a launch, and
+// then takes tiles of sixteen hidden units of the used experts in turn.  In
+// the second, the columns of tokens that did not choose an expert are zero,
+// so all experts add into one accumulator and nothing has to be joined but
+// the parts of the split contraction.
+
+constexpr int kFewTokens = 16;
+constexpr int kFewExperts = 256;
+constexpr int kFewWaves = 4;
+constexpr int kFewGroups = 768;  // workgroups: three on each of 256 compute units
+constexpr int kMaxSplits = 32;
+
+// What the first kernel leaves for the second.
+struct FewPlan {
+    int32_t *n_used;    // experts with tokens
+    int16_t *expert;    // [n_used]
+    int16_t *slot;      // [n_used][16]: token's slot, -1
+    uint32_t *arrived;  // [tiles of the second kernel]
+};
+
+struct FewRoute {
+    uint32_t key[kFewTokens * kFewExperts];
+    float weight[kFewTokens * SIM_MOE_MAX_TOPK];
+    uint8_t pos[kFewTokens][kFewExperts];  // which choice of the token the expert is
+    uint32_t tokens[kFewExperts];          // bit t: token t chose the expert
+    int16_t list[kFewExperts];             // the used experts
+    int count[kFewWaves];
+};
+
+__device__ inline float load_logit(const void *p, int type, int64_t i) {
+    if (type == SIM_TYPE_F32) return ((const float *)p)[i];
+    if (type == SIM_TYPE_F16) return (float)((const _Float16 *)p)[i];
+    return (float)((const __bf16 *)p)[i];
+}
+
+// All tokens' choices, sixteen threads a token; returns the number of used
+// experts.
+__device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
+    const int l = threadIdx.x & 15, t = threadIdx.x >> 4, n_tok = (int)a.T, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    static_assert(64 * kFewWaves == kFewExperts && 4 * kFewWaves == kFewTokens, "a thread for each expert, sixteen for each token");
+    s.tokens[threadIdx.x] = 0;
+    uint32_t *key = s.key + t * kFewExperts;
+    if (t < n_tok)
+        for (int e = l; e < a.E; e += 16) {
+            const bool ok = !a.mask || a.mask[t * a.mask_stride + e];
+            key[e] = ok ? order_key(load_logit(a.logits, a.type, t * a.stride + e)) : 0;
+        }
+    __syncthreads();
+    if (t < n_tok) {
+        float top = 0.f, z = 0.f, w[2] = {0.f, 0.f};
+        uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};
+        for (int j = 0; j < a.k; j++) {
+            uint32_t bk = 0, bi = 0xffffu;
+            for (int e = l; e < a.E; e += 16) {  // a lane's own keys only, its last choice already 0
+                const uint32_t v = key[e];
+                const bool take = v > bk;
+                bk = take ? v : bk;
+                bi = take ? (uint32_t)e : bi;
             }
-            if (c0 + r < n) {
-                const float w = weights[slot];
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const int64_t f = f0 + 4 * q + i;
-                    const float v = f < F ? g[i] / (1.f + expf(-g[i])) * u[i] * w : 0.f;
-                    const __bf16 hi = (__bf16)v;
-                    h_hi[slot * h_pitch + f] = hi;
-                    h_lo[slot * h_pitch + f] = (__bf16)(v - (float)hi);
+            best16(bk, bi);
+            if (j == 0) {
+                top = key_value(bk);
+                if (!a.renorm) {
+                    for (int e = l; e < a.E; e += 16) z += key[e] ? expf(key_value(key[e]) - top) : 0.f;
+                    z = sum16(z);
                 }
+            }
+            if (bk && (bi & 15) == (uint32_t)l) key[bi] = 0;
+            if (l == (j & 15)) {
+                if (j < 16) mine[0] = bk, mine_e[0] = bi;
+                else mine[1] = bk, mine_e[1] = bi;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 2; q++) w[q] = mine[q] ? expf(key_value(mine[q]) - top) : 0.f;
+        if (a.renorm) z = sum16(w[0] + w[1]);
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            const int j = q * 16 + l;
+            if (j < a.k && mine[q]) {
+                s.weight[t * a.k + j] = w[q] / z;
+                s.pos[t][mine_e[q]] = (uint8_t)j;
+                atomicOr(&s.tokens[mine_e[q]], 1u << t);
+            }
+        }
+    }
+    __syncthreads();
+    const uint64_t all = __ballot(s.tokens[threadIdx.x] != 0);
+    if (lane == 0) s.count[wave] = __popcll(all);
+    __syncthreads();
+    int at = __popcll(all & ((1ull << lane) - 1)), used = 0;
+    for (int w = 0; w < kFewWaves; w++) {
+        if (w < wave) at += s.count[w];
+        used += s.count[w];
+    }
+    if (s.tokens[threadIdx.x]) s.list[at] = (int16_t)threadIdx.x;
+    __syncthreads();
+    return used;
+}
+
+// Gate and up products, sixteen hidden units of one expert after another.
+template <int T, int WT, int U, bool EDGE>
+__global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, const uint16_t *__restrict__ x, int64_t x_stride,
+                                                            int D, const void *__restrict__ w13,
+                                                            const uint8_t *__restrict__ s13, int F, int tiles,
+                                                            __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo, int h_pitch,
+                                                            FewPlan plan, int down_tiles) {
+    __shared__ FewRoute rt;
+    __shared__ f32x4 part[2][kFewWaves][2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int used = few_route(route, rt);
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) *plan.n_used = used;
+        for (int i = threadIdx.x; i < down_tiles; i += blockDim.x) plan.arrived[i] = 0;
+        for (int i = threadIdx.x; i < used * 16; i += blockDim.x) {
+            const int e = rt.list[i >> 4], t = i & 15;
+            plan.slot[i] = (rt.tokens[e] >> t) & 1 ? (int16_t)(t * route.k + rt.pos[t][e]) : (int16_t)-1;
+            if (t == 0) plan.expert[i >> 4] = (int16_t)e;
+        }
+    }
+    const int steps = (D + kStep - 1) / kStep, items = used * tiles;
+    int turn = 0;
+    for (int item = blockIdx.x; item < items; item += gridDim.x, turn ^= 1) {
+        const int e = __builtin_amdgcn_readfirstlane(rt.list[item / tiles]), f0 = item % tiles * 16;
+        const uint32_t tokens = rt.tokens[e];
+        const bool has = (tokens >> r) & 1;
+        const uint16_t *xr = x + (int64_t)(has ? r : __ffs(tokens) - 1) * x_stride;  // other columns repeat one of its tokens
+        const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
+        typedef Weights<WT, EDGE> Wt;
+        Wt wg[U], wu[U];
+        Inputs<T, WT, EDGE> xi[U];
+        f32x4 g = {0}, u = {0};
+        ring<U>(
+            share(steps, wave, kFewWaves),
+            [&](int i, int n) {
+                const int k0 = min(wave + n * kFewWaves, steps - 1) * kStep;
+                wg[i].load(w13, s13, row, D, k0, q);
+                wu[i].load(w13, s13, row + F, D, k0, q);
+                xi[i].load(xr, D, k0, q);
+            },
+            [&](int i) {
+#pragma unroll
+                for (int s = 0; s < 4; s++) {
+                    g = xi[i].template mul<Wt>(s, wg[i].operand(s), g);
+                    u = xi[i].template mul<Wt>(s, wu[i].operand(s), u);
+                }
+            });
+        part[turn][wave][0][lane] = g;
+        part[turn][wave][1][lane] = u;
+        __syncthreads();
+        if (wave == 0) {  // the others go on: their next parts go to the other place
+#pragma unroll
+            for (int w = 1; w < kFewWaves; w++) {
+                g += part[turn][w][0][lane];
+                u += part[turn][w][1][lane];
+            }
+            if (has) {
+                const int slot = r * route.k + rt.pos[r][e];
+                const float weight = rt.weight[slot];
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = f0 + 4 * q + i < F ? gated(g[i], u[i], weight) : 0.f;
+                const int64_t at = (int64_t)slot * h_pitch + f0 + 4 * q;
+                store_hidden(h_hi, h_lo, at, v);
+                if (f0 + 16 >= F)  // the rest of the last step
+                    for (int f = 16; f0 + f < h_pitch; f += 16) {
+                        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                        store_hidden(h_hi, h_lo, at + f, zero);
+                    }
+            }
+        }
+    }
+}
+
+// 16 R output columns of all tokens; the steps of all used experts are one
+// list, dealt to the splits and their waves.
+template <int T, int WT, int R, int U, bool EDGE>
+__global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
+                                                              int h_pitch, int F, const void *__restrict__ w2,
+                                                              const uint8_t *__restrict__ s2, int D, int n_tok, FewPlan plan,
+                                                              int splits, float *__restrict__ parts,
+                                                              typename Elem<T>::type *__restrict__ y, int64_t y_stride) {
+    static_assert(R <= kFewWaves, "a wave for each row tile");
+    __shared__ f32x4 part[kFewWaves][R][64];
+    __shared__ int16_t s_slot[kFewExperts * 16], s_expert[kFewExperts];
+    __shared__ int last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int tile = blockIdx.x / splits, split = blockIdx.x % splits, d0 = tile * 16 * R;
+    const int per = h_pitch / kStep, total = *plan.n_used * per;
+    const int begin = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
+    typedef Weights<WT, EDGE> Wt;
+    Wt w[U][R];
+    Hidden<WT> h[U];
+    f32x4 acc[R];
+#pragma unroll
+    for (int i = 0; i < R; i++) acc[i] = f32x4{0};
+    const int a0 = begin / per, lists = end > begin ? (end - 1) / per - a0 + 1 : 0;  // the experts of these steps
+    for (int i = threadIdx.x; i < lists * 16; i += blockDim.x) {
+        s_slot[i] = plan.slot[a0 * 16 + i];
+        if (i < lists) s_expert[i] = plan.expert[a0 + i];
+    }
+    __syncthreads();
+    if (end > begin)
+        ring<U>(
+            share(end - begin, wave, kFewWaves),
+            [&](int i, int n) {
+                const int step = min(begin + wave + n * kFewWaves, end - 1), a = step / per, k0 = (step - a * per) * kStep;
+                const int e = __builtin_amdgcn_readfirstlane(s_expert[a - a0]), slot = s_slot[(a - a0) * 16 + r];
+                h[i].load(h_hi, h_lo, (int64_t)slot * h_pitch, slot >= 0, k0, q);
+#pragma unroll
+                for (int j = 0; j < R; j++)
+                    w[i][j].load(w2, s2, (int64_t)e * D + min(d0 + j * 16 + r, D - 1), F, k0, q);
+            },
+            [&](int i) {
+#pragma unroll
+                for (int s = 0; s < 4; s++)
+#pragma unroll
+                    for (int j = 0; j < R; j++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s), acc[j]);
+            });
+#pragma unroll
+    for (int j = 0; j < R; j++) part[wave][j][lane] = acc[j];
+    __syncthreads();
+    f32x4 v = {0};
+    const int j = wave;  // wave j sums and stores row tile j
+    const bool mine = j < R && r < n_tok;
+    if (mine)
+#pragma unroll
+        for (int i = 0; i < kFewWaves; i++) v += part[i][j][lane];
+    if (splits > 1) {
+        // Every split leaves its part; the one that comes last adds them up
+        // in their order, so that the result does not depend on which it is.
+        // The parts are written and read at device scope, past the caches
+        // that are not shared, so that only their order has to be kept: they
+        // have left before the count goes up, and are read after it.
+        const auto at = [&](int p, int i) { return parts + (((int64_t)tile * splits + p) * R + j) * 256 + (r * 4 + i) * 4 + q; };
+        if (mine)
+#pragma unroll
+            for (int i = 0; i < 4; i++) __hip_atomic_store(at(split, i), v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0)
+            last = __hip_atomic_fetch_add(&plan.arrived[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)splits - 1;
+        __syncthreads();
+        if (!last) return;
+        v = f32x4{0};
+        if (mine)
+            for (int p = 0; p < splits; p++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] += __hip_atomic_load(at(p, i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (mine)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int d = d0 + j * 16 + 4 * q + i;
+            if (d < D) y[r * y_stride + d] = Elem<T>::put(v[i]);
+        }
+}
+
+// ------------------------------------------------------- more tokens
+//
+// The router's lists give each expert its tokens, CT tiles of sixteen at a
+// time as columns.  The second product leaves one row per slot, and a last
+// kernel adds a token's rows up.
+
+constexpr int kWaves = 4;
+
+// Which expert the a-th non-empty list belongs to; -1 past the last.  The
+// same in every wave.
+__device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int a) {
+    const int lane = threadIdx.x & 63;
+    int seen = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        const int e = e0 + lane;
+        const bool some = e < E && offsets[e + 1] > offsets[e];
+        const uint64_t all = __ballot(some);
+        const uint64_t at = __ballot(some && seen + __popcll(all & ((1ull << lane) - 1)) == a);
+        if (at) return e0 + __ffsll((unsigned long long)at) - 1;
+        seen += __popcll(all);
+    }
+    return -1;
+}
+
+template <int T, int WT, int CT, int U, bool EDGE>
+__global__ __launch_bounds__(64 * kWaves) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
+                                                        const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
+                                                        int E, int k, const int32_t *__restrict__ offsets,
+                                                        const int32_t *__restrict__ order, const float *__restrict__ weights,
+                                                        uint32_t tiles, __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo,
+                                                        int h_pitch) {
+    __shared__ f32x4 part[kWaves][2][CT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int e = nth_expert(offsets, E, blockIdx.x / tiles);
+    if (e < 0) return;
+    const int f0 = (int)(blockIdx.x % tiles) * 16;
+    const int first = offsets[e], n = offsets[e + 1] - first;
+    const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
+    const int steps = (D + kStep - 1) / kStep;
+    for (int c0 = 0; c0 < n; c0 += 16 * CT) {
+        const uint16_t *xr[CT];
+#pragma unroll
+        for (int c = 0; c < CT; c++) xr[c] = x + (int64_t)(order[first + min(c0 + c * 16 + r, n - 1)] / k) * x_stride;
+        typedef Weights<WT, EDGE> Wt;
+        Wt wg[U], wu[U];
+        Inputs<T, WT, EDGE> xi[U][CT];
+        f32x4 g[CT], u[CT];
+#pragma unroll
+        for (int c = 0; c < CT; c++) g[c] = u[c] = f32x4{0};
+        ring<U>(
+            share(steps, wave, kWaves),
+            [&](int i, int m) {
+                const int k0 = min(wave + m * kWaves, steps - 1) * kStep;
+                wg[i].load(w13, s13, row, D, k0, q);
+                wu[i].load(w13, s13, row + F, D, k0, q);
+#pragma unroll
+                for (int c = 0; c < CT; c++) xi[i][c].load(xr[c], D, k0, q);
+            },
+            [&](int i) {
+#pragma unroll
+                for (int s = 0; s < 4; s++) {
+                    const typename Wt::Operand og = wg[i].operand(s), ou = wu[i].operand(s);
+#pragma unroll
+                    for (int c = 0; c < CT; c++) {
+                        g[c] = xi[i][c].template mul<Wt>(s, og, g[c]);
+                        u[c] = xi[i][c].template mul<Wt>(s, ou, u[c]);
+                    }
+                }
+            });
+#pragma unroll
+        for (int c = 0; c < CT; c++) {
+            part[wave][0][c][lane] = g[c];
+            part[wave][1][c][lane] = u[c];
+        }
+        __syncthreads();
+        for (int c = wave; c < CT; c += kWaves) {
+            if (c0 + c * 16 + r < n) {
+                f32x4 sg = {0}, su = {0};
+#pragma unroll
+                for (int w = 0; w < kWaves; w++) {
+                    sg += part[w][0][c][lane];
+                    su += part[w][1][c][lane];
+                }
+                const int slot = order[first + c0 + c * 16 + r];
+                const float weight = weights[slot];
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = f0 + 4 * q + i < F ? gated(sg[i], su[i], weight) : 0.f;
+                const int64_t at = (int64_t)slot * h_pitch + f0 + 4 * q;
+                store_hidden(h_hi, h_lo, at, v);
+                if (blockIdx.x % tiles == tiles - 1)
+                    for (int f = f0 + 16; f < h_pitch; f += 16) {
+                        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+                        store_hidden(h_hi, h_lo, at + f - f0, zero);
+                    }
             }
         }
         __syncthreads();
     }
 }
 
-// Sixteen output columns of one expert, for each of its slots.
-template <int WT>
-__global__ __launch_bounds__(64 * kWaves) void layer_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
-                                                          int64_t h_pitch, int64_t F, const void *__restrict__ w2,
-                                                          const uint8_t *__restrict__ s2, int64_t D, int E,
+template <int WT, int R, int CT, int U, bool EDGE>
+__global__ __launch_bounds__(64 * kWaves) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
+                                                          int h_pitch, int F, const void *__restrict__ w2,
+                                                          const uint8_t *__restrict__ s2, int D, int E,
                                                           const int32_t *__restrict__ offsets,
                                                           const int32_t *__restrict__ order, uint32_t tiles,
                                                           float *__restrict__ out) {
-    __shared__ int s_expert;
-    __shared__ f32x4 part[kWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int e = nth_expert(offsets, E, blockIdx.x / tiles, &s_expert);
+    __shared__ f32x4 part[kWaves][R][CT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int e = nth_expert(offsets, E, blockIdx.x / tiles);
     if (e < 0) return;
-    const int64_t d0 = (int64_t)(blockIdx.x % tiles) * 16;
+    const int d0 = (int)(blockIdx.x % tiles) * 16 * R;
     const int first = offsets[e], n = offsets[e + 1] - first;
-    const int64_t row = (int64_t)e * D + min(d0 + r, D - 1);
-    for (int c0 = 0; c0 < n; c0 += 16) {
-        const int slot = order[first + min(c0 + r, n - 1)];
-        const uint16_t *hr = (const uint16_t *)h_hi + slot * h_pitch, *lr = (const uint16_t *)h_lo + slot * h_pitch;
-        f32x4 y = {0};
-        for (int64_t f = wave * kStep; f < F; f += kWaves * kStep) {
-            const int64_t kk = f + q * 32;
-            Weights<WT> w;
-            w.load(w2, s2, row, F, kk);
+    const int steps = h_pitch / kStep;
+    for (int c0 = 0; c0 < n; c0 += 16 * CT) {
+        int64_t at[CT];
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                y = w.mul(s, __builtin_bit_cast(bf16x8, load_row8(hr, kk + 8 * s, F)), y);
-                y = w.mul(s, __builtin_bit_cast(bf16x8, load_row8(lr, kk + 8 * s, F)), y);
-            }
-        }
-        part[wave][lane] = y;
+        for (int c = 0; c < CT; c++) at[c] = (int64_t)order[first + min(c0 + c * 16 + r, n - 1)] * h_pitch;
+        typedef Weights<WT, EDGE> Wt;
+        Wt w[U][R];
+        Hidden<WT> h[U][CT];
+        f32x4 acc[R][CT];
+#pragma unroll
+        for (int j = 0; j < R; j++)
+#pragma unroll
+            for (int c = 0; c < CT; c++) acc[j][c] = f32x4{0};
+        ring<U>(
+            share(steps, wave, kWaves),
+            [&](int i, int m) {
+                const int k0 = min(wave + m * kWaves, steps - 1) * kStep;
+#pragma unroll
+                for (int j = 0; j < R; j++) w[i][j].load(w2, s2, (int64_t)e * D + min(d0 + j * 16 + r, D - 1), F, k0, q);
+#pragma unroll
+                for (int c = 0; c < CT; c++) h[i][c].load(h_hi, h_lo, at[c], true, k0, q);
+            },
+            [&](int i) {
+#pragma unroll
+                for (int s = 0; s < 4; s++)
+#pragma unroll
+                    for (int j = 0; j < R; j++) {
+                        const typename Wt::Operand o = w[i][j].operand(s);
+#pragma unroll
+                        for (int c = 0; c < CT; c++) acc[j][c] = h[i][c].template mul<Wt>(s, o, acc[j][c]);
+                    }
+            });
+#pragma unroll
+        for (int j = 0; j < R; j++)
+#pragma unroll
+            for (int c = 0; c < CT; c++) part[wave][j][c][lane] = acc[j][c];
         __syncthreads();
-        if (wave == 0) {
+        for (int p = wave; p < R * CT; p += kWaves) {
+            const int j = p / CT, c = p % CT;
+            if (c0 + c * 16 + r < n) {
+                f32x4 v = {0};
 #pragma unroll
-            for (int w = 1; w < kWaves; w++) y += part[w][lane];
-            if (c0 + r < n)
+                for (int w = 0; w < kWaves; w++) v += part[w][j][c][lane];
+                float *o = out + (int64_t)order[first + c0 + c * 16 + r] * D;
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
-                    const int64_t d = d0 + 4 * q + i;
-                    if (d < D) out[(int64_t)slot * D + d] = y[i];
+                    const int d = d0 + j * 16 + 4 * q + i;
+                    if (d < D) o[d] = v[i];
                 }
+            }
         }
         __syncthreads();
     }
@@ -237,31 +615,59 @@ __global__ __launch_bounds__(256) void layer_join(const float *__restrict__ part
     y[t * y_stride + d] = Elem<T>::put(s);
 }
 
-inline int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 inline size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+inline bool few(int64_t T, int E) { return T <= kFewTokens && E <= kFewExperts; }
 
 // The workspace in the order in which it is handed out.
 struct Layout {
     size_t experts, weights, offsets, order, route, hi, lo, part, end;
-    int64_t pitch;
+    size_t n_used, expert, slot, arrived;
+    int pitch;
     Layout(int64_t T, int64_t D, int E, int k, int64_t F) {
-        const size_t n = (size_t)T * k;
-        pitch = up16(F);
+        const size_t n = (size_t)T * k, lists = std::min<size_t>(E, n);
+        pitch = (int)((F + kStep - 1) / kStep * kStep);
         size_t at = 0;
         const auto take = [&](size_t bytes) { const size_t p = at; at += aligned(bytes); return p; };
-        experts = take(n * 4);
-        weights = take(n * 4);
-        offsets = take((size_t)(E + 1) * 4);
-        order = take(n * 4);
-        route = take(route_workspace(T, E, k));
         hi = take(n * pitch * 2);
         lo = take(n * pitch * 2);
-        part = take(n * D * 4);
+        if (few(T, E)) {
+            n_used = take(4);
+            expert = take(lists * 2);
+            slot = take(lists * 16 * 2);
+            arrived = take((size_t)(D + 15) / 16 * 4);
+            part = take((size_t)kMaxSplits * ((D + 63) / 64 * 64) * 16 * 4);
+        } else {
+            experts = take(n * 4);
+            weights = take(n * 4);
+            offsets = take((size_t)(E + 1) * 4);
+            order = take(n * 4);
+            route = take(route_workspace(T, E, k));
+            part = take(n * D * 4);
+        }
         end = at;
     }
 };
 
-template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
+template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
+    const RouteArgs &r = a.route;
+    const Layout at(r.T, a.D, r.E, r.k, a.F);
+    __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
+    const FewPlan plan = {(int32_t *)(ws + at.n_used), (int16_t *)(ws + at.expert), (int16_t *)(ws + at.slot),
+                          (uint32_t *)(ws + at.arrived)};
+    constexpr bool M = WT == SIM_TYPE_MX4;
+    constexpr int R = M ? 4 : 2;  // row tiles: an activation load for 2 KB of weights
+    const int64_t lists = std::min<int64_t>(r.E, r.T * r.k);
+    const int tf = (int)((a.F + 15) / 16), td = (int)((a.D + 16 * R - 1) / (16 * R));
+    few_up<T, WT, M ? 4 : 2, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
+        r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
+    const int splits = std::max(1, std::min(kMaxSplits, kFewGroups / td));
+    few_down<T, WT, R, 2, EDGE><<<td * splits, 64 * kFewWaves, 0, st>>>(
+        hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, splits, (float *)(ws + at.part),
+        (typename Elem<T>::type *)a.y, a.y_stride);
+    return SIM_OPS_LAUNCH_OK();
+}
+
+template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
     const RouteArgs &r = a.route;
     const Layout at(r.T, a.D, r.E, r.k, a.F);
     int32_t *experts = (int32_t *)(ws + at.experts), *offsets = (int32_t *)(ws + at.offsets), *order = (int32_t *)(ws + at.order);
@@ -269,16 +675,36 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
     __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
     const sim_status s = launch_route(st, r, experts, weights, offsets, order, ws + at.route);
     if (s != SIM_OK) return s;
+    constexpr bool M = WT == SIM_TYPE_MX4;
+    constexpr int R = 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
-    if (a.F > 0) {
-        const uint32_t tf = (uint32_t)((a.F + 15) / 16);
-        layer_up<T, WT><<<lists * tf, 64 * kWaves, 0, st>>>((const uint16_t *)a.x, a.x_stride, a.D, a.w13, a.s13, a.F, r.E,
-                                                           r.k, offsets, order, weights, tf, hi, lo, at.pitch);
-    }
-    const uint32_t td = (uint32_t)((a.D + 15) / 16), tj = (uint32_t)((a.D + 255) / 256);
-    layer_down<WT><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, a.F, a.w2, a.s2, a.D, r.E, offsets, order, td, part);
+    const uint32_t tf = (uint32_t)((a.F + 15) / 16), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
+    group_up<T, WT, CT, M ? 4 / CT : 2, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
+        (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
+        at.pitch);
+    group_down<WT, R, CT, CT == 1 ? 2 : 1, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2,
+                                                                                  (int)a.D, r.E, offsets, order, td, part);
     layer_join<T><<<(uint32_t)(r.T * tj), 256, 0, st>>>(part, experts, r.k, a.D, (typename Elem<T>::type *)a.y, a.y_stride, tj);
     return SIM_OPS_LAUNCH_OK();
+}
+
+template <int T>
+__global__ __launch_bounds__(256) void layer_zero(typename Elem<T>::type *y, int64_t stride, int64_t D) {
+    for (int64_t d = threadIdx.x; d < D; d += 256) y[blockIdx.x * stride + d] = Elem<T>::put(0.f);
+}
+
+template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
+    const RouteArgs &r = a.route;
+    if (a.F == 0) {
+        layer_zero<T><<<(uint32_t)r.T, 256, 0, st>>>((typename Elem<T>::type *)a.y, a.y_stride, a.D);
+        return SIM_OPS_LAUNCH_OK();
+    }
+    const bool edge = a.D % kStep || a.F % kStep;
+    if (few(r.T, r.E)) return edge ? few_t<T, WT, true>(st, a, ws) : few_t<T, WT, false>(st, a, ws);
+    // columns by the tokens of an average expert
+    const int64_t mean = r.T * r.k / r.E;
+    if (mean <= 10) return edge ? group_t<T, WT, 1, true>(st, a, ws) : group_t<T, WT, 1, false>(st, a, ws);
+    return edge ? group_t<T, WT, 2, true>(st, a, ws) : group_t<T, WT, 2, false>(st, a, ws);
 }
 
 }  // namespace
