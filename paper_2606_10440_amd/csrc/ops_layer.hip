@@ -60,11 +60,40 @@ __device__ inline bf16x8 widen8(uint32_t codes, float scale) {
 // bytes of each row; 4-bit ones 32 q + 8 s, whose 32 codes are one load.
 template <int WT> __device__ inline int step_at(int q, int s) { return WT == SIM_TYPE_MX4 ? 32 * q + 8 * s : 32 * s + 8 * q; }
 
+// The scales of a run of U steps of R tiles of 4-bit weights: sixteen bytes a
+// row for four steps, eight for two.  The rows' pieces of eight bytes lie one
+// in a lane, piece-major, and each lane asks the one that has its row: loads
+// that every lane makes for itself would cost more cache accesses than the
+// codes (measured for 459 MB of 4-bit weights: 147 us with a byte load a
+// step, 128 us with sixteen bytes a run).
+template <int WT, int R, int U> struct Scales {
+    __device__ void load(const uint8_t *, int64_t, int, int) {}
+    __device__ float get(int, int, int, int) const { return 1.f; }
+    static __device__ int tile() { return 0; }
+};
+template <int R, int U> struct Scales<SIM_TYPE_MX4, R, U> {
+    static_assert(R * 16 * (U / 2) <= 64, "a lane for each piece");
+    u32x2 v;
+    // the tile whose row (lane % 16) this lane loads
+    static __device__ int tile() { return (threadIdx.x >> 4 & 3) % R; }
+    // row: of that tile; rows are whole groups of 256 columns, two steps: a
+    // run of four may have half of it past the end, a step never
+    __device__ void load(const uint8_t *scales, int64_t row, int K, int run) {
+        const int g = (int)groups_of(K), piece = min((int)(threadIdx.x & 63) / (16 * R), U / 2 - 1);
+        v = ((const u32x2 *)scales)[row * g + min(run * (U / 2) + piece, g - 1)];
+    }
+    // of step i, tile j: row r, quarter q
+    __device__ float get(int i, int j, int r, int q) const {
+        const uint32_t four = (uint32_t)__builtin_amdgcn_ds_bpermute(((i >> 1) * 16 * R + j * 16 + r) * 4, (int)v[i & 1]);
+        return scale_value((four >> (8 * q)) & 255);
+    }
+};
+
 // A step of one tile of sixteen weight rows; lane l holds row l % 16.
 template <int WT, bool EDGE> struct Weights {
     u32x4 raw[4];
     // base: the weights; row: this lane's; k0: the step's first column
-    __device__ void load(const void *base, const uint8_t *, int64_t row, int K, int k0, int q) {
+    __device__ void load(const void *base, int64_t row, int K, int k0, int q) {
         const uint16_t *p = (const uint16_t *)base + row * K;
 #pragma unroll
         for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(p, k0 + step_at<WT>(q, s), K);
@@ -72,7 +101,7 @@ template <int WT, bool EDGE> struct Weights {
     struct Operand {
         bf16x8 hi, lo;
     };
-    __device__ Operand operand(int s) const {
+    __device__ Operand operand(int s, float) const {
         Operand o;
         if (WT == SIM_TYPE_F16) split_f16(raw[s], o.hi, o.lo);
         else o.hi = __builtin_bit_cast(bf16x8, raw[s]);
@@ -85,17 +114,13 @@ template <int WT, bool EDGE> struct Weights {
 };
 template <bool EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
     u32x4 raw;
-    uint32_t sb;
-    __device__ void load(const void *base, const uint8_t *scales, int64_t row, int K, int k0, int q) {
-        // rows are whole groups of 256 columns, so a step never leaves its row
-        const int64_t g = groups_of(K);
-        raw = *(const u32x4 *)((const uint8_t *)base + row * g * kGroupCodes + k0 / 2 + q * 16);
-        sb = scales[row * g * kGroupScales + k0 / 32 + q];
+    __device__ void load(const void *base, int64_t row, int K, int k0, int q) {
+        raw = *(const u32x4 *)((const uint8_t *)base + row * groups_of(K) * kGroupCodes + k0 / 2 + q * 16);
     }
     struct Operand {
         bf16x8 hi;
     };
-    __device__ Operand operand(int s) const { return {widen8(raw[s], scale_value(sb))}; }
+    __device__ Operand operand(int s, float scale) const { return {widen8(raw[s], scale)}; }
     static __device__ f32x4 mul(const Operand &w, bf16x8 x, f32x4 c) { return mfma(w.hi, x, c); }
 };
 
@@ -106,10 +131,10 @@ template <int T, int WT, bool EDGE> struct Inputs {
 #pragma unroll
         for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
     }
-    template <typename W> __device__ f32x4 mul(int s, const typename W::Operand &w, f32x4 c) const {
-        if (T == SIM_TYPE_BF16) return W::mul(w, __builtin_bit_cast(bf16x8, raw[s]), c);
+    template <typename W> static __device__ f32x4 mul(u32x4 v, const typename W::Operand &w, f32x4 c) {
+        if (T == SIM_TYPE_BF16) return W::mul(w, __builtin_bit_cast(bf16x8, v), c);
         bf16x8 hi, lo;
-        split_f16(raw[s], hi, lo);
+        split_f16(v, hi, lo);
         return W::mul(w, lo, W::mul(w, hi, c));
     }
 };
@@ -133,30 +158,44 @@ template <int WT> struct Hidden {
     }
 };
 
-// n operands through a ring of U places: load(place, which), use(place).  The
-// loop that does the work has no conditions, so the waits in it count loads
-// exactly; n = 0 loads the first operand and uses nothing.
-template <int U, typename Load, typename Use> __device__ inline void ring(int n, Load &&load, Use &&use) {
-#pragma unroll
-    for (int i = 0; i < U; i++) load(i, max(0, min(i, n - 1)));
-    int at = 0;
-    for (; at + 2 * U <= n; at += U)
+// Runs of U steps, this wave's of every W, through a ring of U places:
+// head(parity, run) loads what belongs to a whole run, load(place, run), use(
+// place, parity, run).  The loop that does the work has no conditions around
+// its loads, so the waits in it count them exactly.
+template <int U, int W, typename Head, typename Load, typename Use>
+__device__ inline void ring(int runs, int wave, Head &&head, Load &&load, Use &&use) {
+    if (wave >= runs) return;
+    const auto turn = [&](auto parity, int run) {  // uses one run and loads the next of this wave
+        constexpr int p = decltype(parity)::value;
+        head(1 - p, run + W);
 #pragma unroll
         for (int i = 0; i < U; i++) {
-            use(i);
-            load(i, at + U + i);
+            use(i, p, run);
+            load(i, run + W);
         }
+    };
+    const auto end = [&](auto parity, int run) {
+        constexpr int p = decltype(parity)::value;
 #pragma unroll
-    for (int i = 0; i < U; i++) {
-        if (at + i < n) use(i);
-        if (at + U + i < n) load(i, at + U + i);
+        for (int i = 0; i < U; i++) use(i, p, run);
+    };
+    typedef std::integral_constant<int, 0> P0;
+    typedef std::integral_constant<int, 1> P1;
+    int run = wave;
+    head(0, run);
+#pragma unroll
+    for (int i = 0; i < U; i++) load(i, run);
+    for (; run + 2 * W < runs; run += 2 * W) {
+        turn(P0(), run);
+        turn(P1(), run + W);
     }
-#pragma unroll
-    for (int i = 0; i < U; i++)
-        if (at + U + i < n) use(i);
+    if (run + W < runs) {
+        turn(P0(), run);
+        end(P1(), run + W);
+    } else {
+        end(P0(), run);
+    }
 }
-// of n steps dealt to W waves in turn, those of this wave
-__device__ inline int share(int n, int wave, int W) { return n > wave ? (n - wave + W - 1) / W : 0; }
 
 __device__ inline float gated(float g, float u, float w) { return g / (1.f + expf(-g)) * u * w; }
 
@@ -195,8 +234,13 @@ struct FewPlan {
     uint32_t *arrived;  // [tiles of the second kernel]
 };
 
+constexpr int kFewInputs = 24576;  // bytes of inputs that a workgroup of the first kernel keeps in LDS
+
 struct FewRoute {
-    uint32_t key[kFewTokens * kFewExperts];
+    union {
+        uint32_t key[kFewTokens * kFewExperts];
+        uint8_t inputs[kFewInputs];  // once the choices are made
+    };
     float weight[kFewTokens * SIM_MOE_MAX_TOPK];
     uint8_t pos[kFewTokens][kFewExperts];  // which choice of the token the expert is
     uint32_t tokens[kFewExperts];          // bit t: token t chose the expert
@@ -276,13 +320,13 @@ __device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
 }
 
 // Gate and up products, sixteen hidden units of one expert after another.
-template <int T, int WT, int U, bool EDGE>
+template <int T, int WT, bool EDGE>
 __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, const uint16_t *__restrict__ x, int64_t x_stride,
                                                             int D, const void *__restrict__ w13,
                                                             const uint8_t *__restrict__ s13, int F, int tiles,
                                                             __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo, int h_pitch,
                                                             FewPlan plan, int down_tiles) {
-    __shared__ FewRoute rt;
+    __shared__ __align__(16) FewRoute rt;
     __shared__ f32x4 part[2][kFewWaves][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const int used = few_route(route, rt);
@@ -296,32 +340,85 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
         }
     }
     const int steps = (D + kStep - 1) / kStep, items = used * tiles;
-    int turn = 0;
+    int turn = 0, held = -1;
+    bool in_lds = false;
+    // neighbours take neighbouring rows at the same time (measured: 109 us;
+    // 126 us with a range of items for each workgroup)
     for (int item = blockIdx.x; item < items; item += gridDim.x, turn ^= 1) {
         const int e = __builtin_amdgcn_readfirstlane(rt.list[item / tiles]), f0 = item % tiles * 16;
         const uint32_t tokens = rt.tokens[e];
         const bool has = (tokens >> r) & 1;
-        const uint16_t *xr = x + (int64_t)(has ? r : __ffs(tokens) - 1) * x_stride;  // other columns repeat one of its tokens
-        const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
-        typedef Weights<WT, EDGE> Wt;
-        Wt wg[U], wu[U];
-        Inputs<T, WT, EDGE> xi[U];
-        f32x4 g = {0}, u = {0};
-        ring<U>(
-            share(steps, wave, kFewWaves),
-            [&](int i, int n) {
-                const int k0 = min(wave + n * kFewWaves, steps - 1) * kStep;
-                wg[i].load(w13, s13, row, D, k0, q);
-                wu[i].load(w13, s13, row + F, D, k0, q);
-                xi[i].load(xr, D, k0, q);
-            },
-            [&](int i) {
-#pragma unroll
-                for (int s = 0; s < 4; s++) {
-                    g = xi[i].template mul<Wt>(s, wg[i].operand(s), g);
-                    u = xi[i].template mul<Wt>(s, wu[i].operand(s), u);
+        const int pitch = D * 2 + 16;  // so that sixteen rows start in different banks
+        if (e != held) {  // the expert's inputs to LDS, where they fit
+            held = e;
+            in_lds = !EDGE && __popc(tokens) * pitch <= kFewInputs;
+            if (in_lds) {
+                __syncthreads();
+                uint32_t left = tokens;
+                for (int n = 0; left; n++, left &= left - 1) {
+                    const uint16_t *from = x + (int64_t)(__ffs(left) - 1) * x_stride;
+                    for (int c = threadIdx.x; c < D / 8; c += 64 * kFewWaves)
+                        *(u32x4 *)(rt.inputs + n * pitch + c * 16) = *(const u32x4_a2 *)(from + c * 8);
                 }
-            });
+                __syncthreads();
+            }
+        }
+        const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1), scale_row = row + (int64_t)Scales<WT, 2, 2>::tile() * F;
+        typedef Inputs<T, WT, EDGE> In;
+        f32x4 g = {0}, u = {0};
+        if (in_lds) {
+            constexpr int U = WT == SIM_TYPE_MX4 ? 4 : 2;
+            typedef Weights<WT, EDGE> Wt;
+            Wt wg[U], wu[U];
+            Scales<WT, 2, U> sc[2];
+            // columns without a token repeat the first
+            const uint8_t *xr = rt.inputs + (has ? __popc(tokens & ((1u << r) - 1)) : 0) * pitch;
+            ring<U, kFewWaves>(
+                (steps + U - 1) / U, wave,
+                [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
+                [&](int i, int run) {  // a step past the last loads that again and is not used
+                    const int k0 = min(run * U + i, steps - 1) * kStep;
+                    wg[i].load(w13, row, D, k0, q);
+                    wu[i].load(w13, row + F, D, k0, q);
+                },
+                [&](int i, int p, int run) {
+                    if (run * U + i < steps) {
+                        const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
+#pragma unroll
+                        for (int s = 0; s < 4; s++) {
+                            const u32x4 v = *(const u32x4 *)(xr + ((run * U + i) * kStep + step_at<WT>(q, s)) * 2);
+                            g = In::template mul<Wt>(v, wg[i].operand(s, cg), g);
+                            u = In::template mul<Wt>(v, wu[i].operand(s, cu), u);
+                        }
+                    }
+                });
+        } else {
+            constexpr int U = 2;
+            typedef Weights<WT, EDGE> Wt;
+            Wt wg[U], wu[U];
+            Scales<WT, 2, U> sc[2];
+            const uint16_t *xr = x + (int64_t)(has ? r : __ffs(tokens) - 1) * x_stride;
+            In xi[U];
+            ring<U, kFewWaves>(
+                (steps + U - 1) / U, wave,
+                [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
+                [&](int i, int run) {
+                    const int k0 = min(run * U + i, steps - 1) * kStep;
+                    wg[i].load(w13, row, D, k0, q);
+                    wu[i].load(w13, row + F, D, k0, q);
+                    xi[i].load(xr, D, k0, q);
+                },
+                [&](int i, int p, int run) {
+                    if (run * U + i < steps) {
+                        const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
+#pragma unroll
+                        for (int s = 0; s < 4; s++) {
+                            g = In::template mul<Wt>(xi[i].raw[s], wg[i].operand(s, cg), g);
+                            u = In::template mul<Wt>(xi[i].raw[s], wu[i].operand(s, cu), u);
+                        }
+                    }
+                });
+        }
         part[turn][wave][0][lane] = g;
         part[turn][wave][1][lane] = u;
         __syncthreads();
@@ -351,19 +448,24 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
 
 // 16 R output columns of all tokens; the steps of all used experts are one
 // list, dealt to the splits and their waves.
-template <int T, int WT, int R, int U, bool EDGE>
+template <int T, int WT, int R, bool EDGE>
 __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
                                                               int h_pitch, int F, const void *__restrict__ w2,
                                                               const uint8_t *__restrict__ s2, int D, int n_tok, FewPlan plan,
-                                                              int splits, float *__restrict__ parts,
+                                                              int max_lists, int splits, float *__restrict__ parts,
                                                               typename Elem<T>::type *__restrict__ y, int64_t y_stride) {
     static_assert(R <= kFewWaves, "a wave for each row tile");
+    constexpr int U = 2;
     __shared__ f32x4 part[kFewWaves][R][64];
     __shared__ int16_t s_slot[kFewExperts * 16], s_expert[kFewExperts];
     __shared__ int last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
-    const int tile = blockIdx.x / splits, split = blockIdx.x % splits, d0 = tile * 16 * R;
-    const int per = h_pitch / kStep, total = *plan.n_used * per;
+    const int tiles = gridDim.x / splits, tile = blockIdx.x % tiles, split = blockIdx.x / tiles, d0 = tile * 16 * R;
+    for (int i = threadIdx.x; i < max_lists * 16; i += blockDim.x) {  // the whole plan: not one load after another
+        s_slot[i] = plan.slot[i];
+        if (i < max_lists) s_expert[i] = plan.expert[i];
+    }
+    const int steps = h_pitch / kStep, per = (steps + U - 1) / U, total = *plan.n_used * per;  // runs
     const int begin = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
     typedef Weights<WT, EDGE> Wt;
     Wt w[U][R];
@@ -371,29 +473,39 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
     f32x4 acc[R];
 #pragma unroll
     for (int i = 0; i < R; i++) acc[i] = f32x4{0};
-    const int a0 = begin / per, lists = end > begin ? (end - 1) / per - a0 + 1 : 0;  // the experts of these steps
-    for (int i = threadIdx.x; i < lists * 16; i += blockDim.x) {
-        s_slot[i] = plan.slot[a0 * 16 + i];
-        if (i < lists) s_expert[i] = plan.expert[a0 + i];
-    }
     __syncthreads();
-    if (end > begin)
-        ring<U>(
-            share(end - begin, wave, kFewWaves),
-            [&](int i, int n) {
-                const int step = min(begin + wave + n * kFewWaves, end - 1), a = step / per, k0 = (step - a * per) * kStep;
-                const int e = __builtin_amdgcn_readfirstlane(s_expert[a - a0]), slot = s_slot[(a - a0) * 16 + r];
-                h[i].load(h_hi, h_lo, (int64_t)slot * h_pitch, slot >= 0, k0, q);
+    Scales<WT, R, U> sc[2];
+    int64_t row[R], hidden = 0;  // of the run that is being loaded
+    int k0 = 0;
+    bool some = false;
+    ring<U, kFewWaves>(
+        end - begin, wave,
+        [&](int p, int run) {
+            const int a = (begin + run) / per;
+            const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane(s_expert[a]) * D;
+            const int slot = s_slot[a * 16 + r];
+            k0 = begin + run - a * per;
+            some = slot >= 0;
+            hidden = (int64_t)slot * h_pitch;
 #pragma unroll
-                for (int j = 0; j < R; j++)
-                    w[i][j].load(w2, s2, (int64_t)e * D + min(d0 + j * 16 + r, D - 1), F, k0, q);
-            },
-            [&](int i) {
+            for (int j = 0; j < R; j++) row[j] = first + min(d0 + j * 16 + r, D - 1);
+            sc[p].load(s2, first + min(d0 + sc[p].tile() * 16 + r, D - 1), F, k0);
+        },
+        [&](int i, int) {
+            const int at = min(k0 * U + i, steps - 1) * kStep;
+            h[i].load(h_hi, h_lo, hidden, some, at, q);
 #pragma unroll
-                for (int s = 0; s < 4; s++)
+            for (int j = 0; j < R; j++) w[i][j].load(w2, row[j], F, at, q);
+        },
+        [&](int i, int p, int run) {
+            if ((begin + run) % per * U + i < steps)
 #pragma unroll
-                    for (int j = 0; j < R; j++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s), acc[j]);
-            });
+                for (int j = 0; j < R; j++) {
+                    const float c = sc[p].get(i, j, r, q);
+#pragma unroll
+                    for (int s = 0; s < 4; s++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s, c), acc[j]);
+                }
+        });
 #pragma unroll
     for (int j = 0; j < R; j++) part[wave][j][lane] = acc[j];
     __syncthreads();
@@ -457,8 +569,8 @@ __device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int
     return -1;
 }
 
-template <int T, int WT, int CT, int U, bool EDGE>
-__global__ __launch_bounds__(64 * kWaves) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
+template <int T, int WT, int CT, bool EDGE>
+__global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
                                                         const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
                                                         int E, int k, const int32_t *__restrict__ offsets,
                                                         const int32_t *__restrict__ order, const float *__restrict__ weights,
@@ -471,34 +583,41 @@ __global__ __launch_bounds__(64 * kWaves) void group_up(const uint16_t *__restri
     const int f0 = (int)(blockIdx.x % tiles) * 16;
     const int first = offsets[e], n = offsets[e + 1] - first;
     const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
+    constexpr int U = 2;
     const int steps = (D + kStep - 1) / kStep;
     for (int c0 = 0; c0 < n; c0 += 16 * CT) {
         const uint16_t *xr[CT];
 #pragma unroll
         for (int c = 0; c < CT; c++) xr[c] = x + (int64_t)(order[first + min(c0 + c * 16 + r, n - 1)] / k) * x_stride;
         typedef Weights<WT, EDGE> Wt;
+        typedef Inputs<T, WT, EDGE> In;
         Wt wg[U], wu[U];
-        Inputs<T, WT, EDGE> xi[U][CT];
+        Scales<WT, 2, U> sc[2];
+        In xi[U][CT];
         f32x4 g[CT], u[CT];
 #pragma unroll
         for (int c = 0; c < CT; c++) g[c] = u[c] = f32x4{0};
-        ring<U>(
-            share(steps, wave, kWaves),
-            [&](int i, int m) {
-                const int k0 = min(wave + m * kWaves, steps - 1) * kStep;
-                wg[i].load(w13, s13, row, D, k0, q);
-                wu[i].load(w13, s13, row + F, D, k0, q);
+        ring<U, kWaves>(
+            (steps + U - 1) / U, wave,
+            [&](int p, int run) { sc[p].load(s13, row + (int64_t)sc[p].tile() * F, D, run); },
+            [&](int i, int run) {
+                const int k0 = min(run * U + i, steps - 1) * kStep;
+                wg[i].load(w13, row, D, k0, q);
+                wu[i].load(w13, row + F, D, k0, q);
 #pragma unroll
                 for (int c = 0; c < CT; c++) xi[i][c].load(xr[c], D, k0, q);
             },
-            [&](int i) {
+            [&](int i, int p, int run) {
+                if (run * U + i < steps) {
+                    const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
-                for (int s = 0; s < 4; s++) {
-                    const typename Wt::Operand og = wg[i].operand(s), ou = wu[i].operand(s);
+                    for (int s = 0; s < 4; s++) {
+                        const typename Wt::Operand og = wg[i].operand(s, cg), ou = wu[i].operand(s, cu);
 #pragma unroll
-                    for (int c = 0; c < CT; c++) {
-                        g[c] = xi[i][c].template mul<Wt>(s, og, g[c]);
-                        u[c] = xi[i][c].template mul<Wt>(s, ou, u[c]);
+                        for (int c = 0; c < CT; c++) {
+                            g[c] = In::template mul<Wt>(xi[i][c].raw[s], og, g[c]);
+                            u[c] = In::template mul<Wt>(xi[i][c].raw[s], ou, u[c]);
+                        }
                     }
                 }
             });
@@ -534,8 +653,8 @@ __global__ __launch_bounds__(64 * kWaves) void group_up(const uint16_t *__restri
     }
 }
 
-template <int WT, int R, int CT, int U, bool EDGE>
-__global__ __launch_bounds__(64 * kWaves) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
+template <int WT, int R, int CT, bool EDGE>
+__global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
                                                           int h_pitch, int F, const void *__restrict__ w2,
                                                           const uint8_t *__restrict__ s2, int D, int E,
                                                           const int32_t *__restrict__ offsets,
@@ -552,31 +671,42 @@ __global__ __launch_bounds__(64 * kWaves) void group_down(const __bf16 *__restri
         int64_t at[CT];
 #pragma unroll
         for (int c = 0; c < CT; c++) at[c] = (int64_t)order[first + min(c0 + c * 16 + r, n - 1)] * h_pitch;
+        constexpr int U = CT == 1 || WT == SIM_TYPE_MX4 ? 2 : 1;
         typedef Weights<WT, EDGE> Wt;
         Wt w[U][R];
+        Scales<WT, R, U> sc[2];
         Hidden<WT> h[U][CT];
         f32x4 acc[R][CT];
+        int64_t row[R];
 #pragma unroll
-        for (int j = 0; j < R; j++)
+        for (int j = 0; j < R; j++) {
+            row[j] = (int64_t)e * D + min(d0 + j * 16 + r, D - 1);
 #pragma unroll
             for (int c = 0; c < CT; c++) acc[j][c] = f32x4{0};
-        ring<U>(
-            share(steps, wave, kWaves),
-            [&](int i, int m) {
-                const int k0 = min(wave + m * kWaves, steps - 1) * kStep;
+        }
+        ring<U, kWaves>(
+            (steps + U - 1) / U, wave,
+            [&](int p, int run) {
+                sc[p].load(s2, (int64_t)e * D + min(d0 + sc[p].tile() * 16 + r, D - 1), F, run);
+            },
+            [&](int i, int run) {
+                const int k0 = min(run * U + i, steps - 1) * kStep;
 #pragma unroll
-                for (int j = 0; j < R; j++) w[i][j].load(w2, s2, (int64_t)e * D + min(d0 + j * 16 + r, D - 1), F, k0, q);
+                for (int j = 0; j < R; j++) w[i][j].load(w2, row[j], F, k0, q);
 #pragma unroll
                 for (int c = 0; c < CT; c++) h[i][c].load(h_hi, h_lo, at[c], true, k0, q);
             },
-            [&](int i) {
-#pragma unroll
-                for (int s = 0; s < 4; s++)
+            [&](int i, int p, int run) {
+                if (run * U + i < steps)
 #pragma unroll
                     for (int j = 0; j < R; j++) {
-                        const typename Wt::Operand o = w[i][j].operand(s);
+                        const float scale = sc[p].get(i, j, r, q);
 #pragma unroll
-                        for (int c = 0; c < CT; c++) acc[j][c] = h[i][c].template mul<Wt>(s, o, acc[j][c]);
+                        for (int s = 0; s < 4; s++) {
+                            const typename Wt::Operand o = w[i][j].operand(s, scale);
+#pragma unroll
+                            for (int c = 0; c < CT; c++) acc[j][c] = h[i][c].template mul<Wt>(s, o, acc[j][c]);
+                        }
                     }
             });
 #pragma unroll
@@ -654,15 +784,14 @@ template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const Layer
     __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
     const FewPlan plan = {(int32_t *)(ws + at.n_used), (int16_t *)(ws + at.expert), (int16_t *)(ws + at.slot),
                           (uint32_t *)(ws + at.arrived)};
-    constexpr bool M = WT == SIM_TYPE_MX4;
-    constexpr int R = M ? 4 : 2;  // row tiles: an activation load for 2 KB of weights
+    constexpr int R = WT == SIM_TYPE_MX4 ? 4 : 2;  // row tiles that share the hidden values
     const int64_t lists = std::min<int64_t>(r.E, r.T * r.k);
     const int tf = (int)((a.F + 15) / 16), td = (int)((a.D + 16 * R - 1) / (16 * R));
-    few_up<T, WT, M ? 4 : 2, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
+    few_up<T, WT, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
         r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
     const int splits = std::max(1, std::min(kMaxSplits, kFewGroups / td));
-    few_down<T, WT, R, 2, EDGE><<<td * splits, 64 * kFewWaves, 0, st>>>(
-        hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, splits, (float *)(ws + at.part),
+    few_down<T, WT, R, EDGE><<<td * splits, 64 * kFewWaves, 0, st>>>(
+        hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, (int)lists, splits, (float *)(ws + at.part),
         (typename Elem<T>::type *)a.y, a.y_stride);
     return SIM_OPS_LAUNCH_OK();
 }
@@ -675,14 +804,13 @@ template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, c
     __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
     const sim_status s = launch_route(st, r, experts, weights, offsets, order, ws + at.route);
     if (s != SIM_OK) return s;
-    constexpr bool M = WT == SIM_TYPE_MX4;
     constexpr int R = 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
     const uint32_t tf = (uint32_t)((a.F + 15) / 16), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
-    group_up<T, WT, CT, M ? 4 / CT : 2, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
+    group_up<T, WT, CT, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
         (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
         at.pitch);
-    group_down<WT, R, CT, CT == 1 ? 2 : 1, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2,
+    group_down<WT, R, CT, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2,
                                                                                   (int)a.D, r.E, offsets, order, td, part);
     layer_join<T><<<(uint32_t)(r.T * tj), 256, 0, st>>>(part, experts, r.k, a.D, (typename Elem<T>::type *)a.y, a.y_stride, tj);
     return SIM_OPS_LAUNCH_OK();

@@ -6,18 +6,17 @@
 namespace simops {
 namespace {
 
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
 // Eight consecutive elements of a row, zeros past the end of the row.
 template <int T, bool WIDE>
 __device__ inline void load8(const typename Elem<T>::type *p, int64_t left, float v[8]) {
     typedef typename Elem<T>::type E;
-    if (WIDE) {  // aligned, and the row is a whole number of eights
+    if (WIDE || left >= 8) {  // WIDE: the row is a whole number of eights
         if (left > 0) {
             E e[8];
-            if (sizeof(E) == 2) *(u32x4 *)e = *(const u32x4 *)p;
-            else {
-                ((u32x4 *)e)[0] = ((const u32x4 *)p)[0];
-                ((u32x4 *)e)[1] = ((const u32x4 *)p)[1];
-            }
+            ((u32x4 *)e)[0] = __builtin_nontemporal_load((const u32x4_any *)p);
+            if (sizeof(E) == 4) ((u32x4 *)e)[1] = __builtin_nontemporal_load((const u32x4_any *)p + 1);
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = Elem<T>::get(e[i]);
         } else {
@@ -161,10 +160,10 @@ __global__ __launch_bounds__(256) void dequantize(const uint8_t *__restrict__ co
             e[i] = Elem<T>::put(n & 8 ? -v : v);
         }
         E *p = out + row * stride + col;
-        if (WIDE) {
+        if (WIDE || col + 8 <= cols) {
             if (col < cols) {
-                ((u32x4 *)p)[0] = ((u32x4 *)e)[0];
-                if (sizeof(E) == 4) ((u32x4 *)p)[1] = ((u32x4 *)e)[1];
+                ((u32x4_any *)p)[0] = ((u32x4 *)e)[0];
+                if (sizeof(E) == 4) ((u32x4_any *)p)[1] = ((u32x4 *)e)[1];
             }
         } else {
 #pragma unroll
@@ -188,7 +187,7 @@ sim_status quantize_t(hipStream_t st, const void *xv, int64_t rows, int64_t cols
         return SIM_OPS_LAUNCH_OK();
     }
     const int64_t per = groups_of(cols), n = rows * per;
-    const bool wide = (uintptr_t)x % 16 == 0 && stride * sizeof(E) % 16 == 0 && cols % 8 == 0;
+    const bool wide = cols % 8 == 0;
     constexpr int U = 4;
     const bool many = n >= 8 * U * 1024;
     const int64_t blocks = many ? (n + 8 * U - 1) / (8 * U) : (n + 7) / 8;
@@ -207,7 +206,7 @@ sim_status dequantize_t(hipStream_t st, const uint8_t *codes, const uint8_t *sca
                         void *out, int64_t stride) {
     typedef typename Elem<T>::type E;
     const int64_t per = groups_of(cols), n = rows * per;
-    const bool wide = (uintptr_t)out % 16 == 0 && stride * sizeof(E) % 16 == 0 && cols % 8 == 0;
+    const bool wide = cols % 8 == 0;
     constexpr int U = 4;
     const bool many = n >= 8 * U * 1024;
     const uint32_t blocks = (uint32_t)(many ? (n + 8 * U - 1) / (8 * U) : (n + 7) / 8);
