@@ -116,7 +116,7 @@ sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a
 }
 
 size_t sim_mx4_linear_workspace(int64_t M, int64_t N, int64_t K) {
-    if (!dims_ok(M, K) || M == 0 || K == 0) return 0;
+    if (!dims_ok(M, K) || M == 0 || K == 0 || linear_in_one(M, K)) return 0;
     return (size_t)((M * (sim_mx4_code_pitch(K) + sim_mx4_scale_pitch(K)) + 15) / 16 * 16) + sim_mx4_matmul_workspace(M, N, K);
 }
 
@@ -133,6 +133,9 @@ sim_status sim_mx4_linear(void *stream, const void *x, int32_t x_type, int64_t x
     NEED(aligned_to(w_codes, 16) && aligned_to(w_scales, 16), "codes and scales must be 16-byte aligned");
     const size_t need = sim_mx4_linear_workspace(M, N, K);
     NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
+    if (linear_in_one(M, K))
+        return done(launch_linear((hipStream_t)stream, x, x_type, x_stride, w_codes, w_scales, M, N, K, out, type, row_stride),
+                    __func__);
     uint8_t *codes = (uint8_t *)workspace, *scales = codes + M * sim_mx4_code_pitch(K);
     if (K > 0) {
         const sim_status s = launch_quantize((hipStream_t)stream, x, x_type, M, K, x_stride, false, codes, scales);

@@ -94,6 +94,9 @@ sim_status launch_dequantize(hipStream_t st, const uint8_t *codes, const uint8_t
                              void *out, int type, int64_t stride);
 sim_status launch_matmul(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs,
                          int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride);
+bool linear_in_one(int64_t M, int64_t K);  // whether launch_linear takes these sizes
+sim_status launch_linear(hipStream_t st, const void *x, int x_type, int64_t x_stride, const uint8_t *wc, const uint8_t *ws,
+                         int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride);
 struct RouteArgs {
     const void *logits;
     int type;

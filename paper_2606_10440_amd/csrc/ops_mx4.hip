@@ -1,33 +1,10 @@
 // Quantisation to 4 bits with a shared power-of-two scale for 32 elements,
 // and back.  Both only move bytes: one pass over the input, wide loads, the
 // conversions are single instructions.
-#include "ops_common.h"
+#include "ops_quant.h"
 
 namespace simops {
 namespace {
-
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;
-
-// Eight consecutive elements of a row, zeros past the end of the row.
-template <int T, bool WIDE>
-__device__ inline void load8(const typename Elem<T>::type *p, int64_t left, float v[8]) {
-    typedef typename Elem<T>::type E;
-    if (WIDE || left >= 8) {  // WIDE: the row is a whole number of eights
-        if (left > 0) {
-            E e[8];
-            ((u32x4 *)e)[0] = __builtin_nontemporal_load((const u32x4_any *)p);
-            if (sizeof(E) == 4) ((u32x4 *)e)[1] = __builtin_nontemporal_load((const u32x4_any *)p + 1);
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = Elem<T>::get(e[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = 0.f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = i < left ? Elem<T>::get(p[i]) : 0.f;
-    }
-}
 
 // Blocks along the columns.  A lane holds 8 elements, four lanes a block, 32
 // lanes a group of 256 columns; a half wave takes U groups at a time, so that
@@ -49,13 +26,8 @@ __global__ __launch_bounds__(256) void quantize_rows(const typename Elem<T>::typ
 #pragma unroll
     for (int u = 0; u < U; u++) {
         const int64_t g = g0 + u;
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; i++) m = max(m, mag(v[u][i]));
-        m = max(m, dpp_u32<kDppXor1>(m));
-        m = max(m, dpp_u32<kDppXor2>(m));
-        const uint32_t sb = scale_byte(m);
-        const uint32_t c = sb == 255 ? 0u : pack8(v[u], scale_value(sb));
+        uint32_t sb;
+        const uint32_t c = quantize8(v[u], sb);
         if (g < n_groups) {
             *(uint32_t *)(codes + g * kGroupCodes + lane * 4) = c;
             if ((lane & 3) == 0) scales[g * kGroupScales + (lane >> 2)] = (uint8_t)sb;

@@ -8,7 +8,8 @@
 // to the sum, so of a group of 256 columns half h takes blocks 4 h .. 4 h + 3
 // in four instructions: 64 contiguous bytes of codes and one word of scales
 // per lane and group.
-#include "ops_common.h"
+#include "ops_quant.h"
+#include "ops_stream.h"
 
 namespace simops {
 namespace {
@@ -106,8 +107,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
     constexpr int SCALE_COPIES = ROWS / 16 / W;  // per wave and two groups: sixteen rows each
     constexpr int OPS = TM + TN, PRODUCTS = TM * TN;  // of a round
     static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0, "rows are dealt evenly");
-    static_assert(OPS <= PRODUCTS && COPIES <= PRODUCTS && SCALE_COPIES % 4 == 0, "they fit beside a round's products");
-    constexpr int STAGE_COPIES = COPIES + SCALE_COPIES / 4;
+    constexpr int STAGE_SCALES = (SCALE_COPIES + 3) / 4, STAGE_COPIES = COPIES + STAGE_SCALES;
+    // the slot beside a round's products from which the copies start
+    constexpr int COPY_SLOT = COPIES < PRODUCTS ? PRODUCTS - COPIES : 0;
     constexpr int SCALE_ROW = kScaleGroups * kGroupScales;
     __shared__ __align__(16) uint8_t codes[kBuffers][ROWS * kStageCodes];
     __shared__ __align__(16) uint8_t scales[kScaleBuffers][ROWS * SCALE_ROW];
@@ -195,16 +197,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
         wait_and_meet<STAGE_COPIES>();  // the codes of stage t + 1 are there, and the buffer of stage t - 1 is free
 #pragma unroll
         for (int n = 0; n < PRODUCTS; n++) {
-            if (n < OPS) read_op(nth_op(n), t, 1);
-            if (n < SCALE_COPIES / 4)
-                copy_scale(((g & 1) * 2 + q) * (SCALE_COPIES / 4) + n, (g & ~1) + 2 * kScaleGroups);
-            if (n >= PRODUCTS - COPIES) copy(n - (PRODUCTS - COPIES), min(t + 3, stages - 1), t + 3);
+#pragma unroll
+            for (int o = n; o < OPS; o += PRODUCTS) read_op(nth_op(o), t, 1);
+#pragma unroll
+            for (int o = n; o < STAGE_SCALES; o += PRODUCTS)
+                copy_scale(min(((g & 1) * 2 + q) * STAGE_SCALES + o, SCALE_COPIES - 1), (g & ~1) + 2 * kScaleGroups);
+#pragma unroll
+            for (int o = n - COPY_SLOT; o < COPIES; o += PRODUCTS)
+                if (o >= 0) copy(o, min(t + 3, stages - 1), t + 3);
             product(C0(), half, n);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int n = 0; n < PRODUCTS; n++) {
-            if (n < OPS) read_op(nth_op(n), t + 1, 0), read_scale(nth_op(n), t + 1, 1 - q);
+#pragma unroll
+            for (int o = n; o < OPS; o += PRODUCTS) read_op(nth_op(o), t + 1, 0), read_scale(nth_op(o), t + 1, 1 - q);
             product(C1(), half, n);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -261,12 +268,159 @@ void launch_tile(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uin
                                                                    (typename Elem<T>::type *)out, stride);
 }
 
+// ---- few rows of A
+//
+// At most 32 rows: the time is that of reading B once.  A workgroup takes 16 R
+// rows of B, its waves each a part of the contraction, with 16x16x128
+// instructions, B's rows as the first operand: lane l holds row l % 16 and
+// block l / 16 of 128 columns.  The rows of A lie in LDS, where they are put
+// into 4 bits first if they are not (XT).
+constexpr int kSkinnyRows = 32;
+constexpr int kSkinnyLds = 49152;  // bytes of A
+constexpr int kSkinnyWaves = 8;
+constexpr int64_t kOwnQuantize = 32768;  // elements
+
+template <int T, int XT, int R, int MT>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *__restrict__ x, const uint8_t *__restrict__ xs,
+                                                                   int64_t x_stride, const uint8_t *__restrict__ bc,
+                                                                   const uint8_t *__restrict__ bs, int M, int64_t N, int K,
+                                                                   typename Elem<T>::type *__restrict__ out, int64_t stride) {
+    constexpr int U = 4, W = kSkinnyWaves;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int groups = (int)groups_of(K), pitch = groups * kGroupCodes + 16, scale_pitch = groups * kGroupScales;
+    uint8_t *codes = lds, *scales = lds + M * pitch;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int64_t n0 = (int64_t)blockIdx.x * 16 * R;
+    int64_t row[R];
+#pragma unroll
+    for (int j = 0; j < R; j++) row[j] = min(n0 + j * 16 + r, N - 1);  // rows past the end repeat the last one
+    const int64_t scale_row = min(n0 + Scales<SIM_TYPE_MX4, R, U>::tile() * 16 + r, N - 1);
+    u32x4 w[U][R];
+    Scales<SIM_TYPE_MX4, R, U> sc[2];
+    f32x4 acc[R][MT];
+#pragma unroll
+    for (int j = 0; j < R; j++)
+#pragma unroll
+        for (int m = 0; m < MT; m++) acc[j][m] = f32x4{0};
+    const int steps = groups * 2;
+    bool ready = false;
+    const auto prepare = [&] {  // A to LDS, while the first rows of B are on their way
+        for (int i = threadIdx.x; i < M * groups * 32; i += 64 * W) {
+            const int m = i / (groups * 32), at = i % (groups * 32);  // eight columns each
+            if (XT == SIM_TYPE_MX4) {
+                if ((at & 3) == 0) {
+                    const int64_t g = (int64_t)m * groups * 32 + at;
+                    *(u32x4 *)(codes + m * pitch + at * 4) = *(const u32x4 *)((const uint8_t *)x + g * 4);
+                    scales[m * scale_pitch + at / 4] = xs[g / 4];
+                }
+            } else {
+                float v[8];
+                load8<XT == SIM_TYPE_MX4 ? SIM_TYPE_F32 : XT>((const typename Elem<XT == SIM_TYPE_MX4 ? SIM_TYPE_F32 : XT>::type *)x + m * x_stride + at * 8, K - at * 8, v);
+                uint32_t sb;
+                *(uint32_t *)(codes + m * pitch + at * 4) = quantize8(v, sb);
+                if ((at & 3) == 0) scales[m * scale_pitch + at / 4] = (uint8_t)sb;
+            }
+        }
+        __syncthreads();
+    };
+    // every wave prepares: a wave without a run would otherwise miss the barrier
+    const int runs = (steps + U - 1) / U;
+    if (wave >= runs) prepare();
+    ring<U, W>(
+        runs, wave, [&](int p, int run) { sc[p].load(bs, scale_row, K, run); },
+        [&](int i, int run) {
+            const int step = min(run * U + i, steps - 1);
+#pragma unroll
+            for (int j = 0; j < R; j++)
+                w[i][j] = *(const u32x4 *)(bc + row[j] * groups * kGroupCodes + step * (kStep / 2) + q * 16);
+        },
+        [&](int i, int p, int run) {
+            if (!ready) {
+                ready = true;
+                prepare();
+            }
+            const int step = run * U + i;
+            if (step < steps) {
+                i32x8 a[MT];
+                int sa[MT];
+#pragma unroll
+                for (int m = 0; m < MT; m++) {
+                    const int at = m * 16 + r < M ? m * 16 + r : 0;
+                    a[m] = i32x8{0};
+                    *(u32x4 *)&a[m] = *(const u32x4 *)(codes + at * pitch + step * (kStep / 2) + q * 16);
+                    sa[m] = scales[at * scale_pitch + step * 4 + q];
+                }
+#pragma unroll
+                for (int j = 0; j < R; j++) {
+                    i32x8 b = {0};
+                    *(u32x4 *)&b = w[i][j];
+                    const int sb = sc[p].get_byte(i, j, r, q);
+#pragma unroll
+                    for (int m = 0; m < MT; m++)
+                        acc[j][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a[m], acc[j][m], 4, 4, 0, sb, 0, sa[m]);
+                }
+            }
+        });
+    __syncthreads();  // A is no longer needed: the parts of the sum take its place
+    f32x4 *part = (f32x4 *)lds;
+#pragma unroll
+    for (int j = 0; j < R; j++)
+#pragma unroll
+        for (int m = 0; m < MT; m++) part[((wave * R + j) * MT + m) * 64 + lane] = acc[j][m];
+    __syncthreads();
+    if (wave < R * MT) {
+        const int j = wave / MT, m = wave % MT;
+        f32x4 v = {0};
+#pragma unroll
+        for (int p = 0; p < W; p++) v += part[((p * R + j) * MT + m) * 64 + lane];
+        const int64_t n = n0 + j * 16 + 4 * q;
+        if (m * 16 + r < M)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (n + i < N) out[(int64_t)(m * 16 + r) * stride + n + i] = Elem<T>::put(v[i]);
+    }
+}
+
+inline size_t skinny_lds(int64_t M, int64_t K) { return (size_t)(M * (groups_of(K) * (kGroupCodes + kGroupScales) + 16)); }
+inline bool skinny(int64_t M, int64_t K) { return M <= kSkinnyRows && K > 0 && K < (1 << 20) && skinny_lds(M, K) <= kSkinnyLds; }
+
+template <int T, int XT, int R, int MT>
+void launch_skinny(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride, const uint8_t *bc, const uint8_t *bs,
+                   int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
+    const size_t lds = std::max(skinny_lds(M, K), (size_t)kSkinnyWaves * R * MT * 1024);
+    matmul_skinny<T, XT, R, MT><<<(uint32_t)((N + 16 * R - 1) / (16 * R)), 64 * kSkinnyWaves, lds, st>>>(
+        x, xs, x_stride, bc, bs, (int)M, N, (int)K, (typename Elem<T>::type *)out, stride);
+}
+template <int T, int XT>
+void skinny_t(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride, const uint8_t *bc, const uint8_t *bs,
+              int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
+    if (M <= 16) launch_skinny<T, XT, 2, 1>(st, x, xs, x_stride, bc, bs, M, N, K, out, stride);
+    else launch_skinny<T, XT, 2, 2>(st, x, xs, x_stride, bc, bs, M, N, K, out, stride);
+}
+
 template <int T>
 sim_status matmul_t(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs, int64_t M,
                     int64_t N, int64_t K, void *out, int64_t stride) {
-    if (M >= 128 && N >= 128 && K > 0 && K < (1 << 23)) {  // offsets within a tile fit in 32 bits
-        if (((M + 255) / 256) * ((N + 255) / 256) >= 200) launch_tile<T, 2, 2, 4, 4>(st, ac, as, bc, bs, M, N, K, out, stride);
-        else launch_tile<T, 2, 2, 2, 2>(st, ac, as, bc, bs, M, N, K, out, stride);
+    if (skinny(M, K)) {
+        skinny_t<T, SIM_TYPE_MX4>(st, ac, as, 0, bc, bs, M, N, K, out, stride);
+        return SIM_OPS_LAUNCH_OK();
+    }
+    if (K > 0 && K < (1 << 23)) {  // offsets within a tile fit in 32 bits
+        // The tile by what 256 of it at a time cost, in microseconds for 4096
+        // columns (measured, beside some 4 for each launch: 64 tiles or 256 of
+        // a kind take the same time; 4096 x 4096 in 256 tiles of 256 x 256
+        // 43 us, in 1024 of 128 x 128 54; 333 x 5001 x 2056 9.1, 11.1 and 11.3
+        // us in tiles of 64 x 128, 64 x 64 and 128 x 128).
+        const auto cost = [&](int64_t bm, int64_t bn, double each) {
+            return (double)((((M + bm - 1) / bm) * ((N + bn - 1) / bn) + 255) / 256) * each;
+        };
+        const double c[4] = {cost(256, 256, 38.), cost(128, 128, 12.5), cost(64, 128, 9.2), cost(64, 64, 6.6)};
+        switch (std::min_element(c, c + 4) - c) {
+            case 0: launch_tile<T, 2, 2, 4, 4>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+            case 1: launch_tile<T, 2, 2, 2, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+            case 2: launch_tile<T, 2, 2, 1, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+            default: launch_tile<T, 2, 2, 1, 1>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+        }
         return SIM_OPS_LAUNCH_OK();
     }
     const uint32_t grid = (uint32_t)(((M + 63) / 64) * ((N + 63) / 64));
@@ -274,7 +428,26 @@ sim_status matmul_t(hipStream_t st, const uint8_t *ac, const uint8_t *as, const 
     return SIM_OPS_LAUNCH_OK();
 }
 
+template <int T>
+sim_status linear_t(hipStream_t st, const void *x, int x_type, int64_t x_stride, const uint8_t *wc, const uint8_t *ws,
+                    int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
+    if (x_type == SIM_TYPE_F32) skinny_t<T, SIM_TYPE_F32>(st, x, nullptr, x_stride, wc, ws, M, N, K, out, stride);
+    else if (x_type == SIM_TYPE_F16) skinny_t<T, SIM_TYPE_F16>(st, x, nullptr, x_stride, wc, ws, M, N, K, out, stride);
+    else skinny_t<T, SIM_TYPE_BF16>(st, x, nullptr, x_stride, wc, ws, M, N, K, out, stride);
+    return SIM_OPS_LAUNCH_OK();
+}
+
 }  // namespace
+
+// A launch less where every workgroup can put the few rows into 4 bits itself.
+bool linear_in_one(int64_t M, int64_t K) { return skinny(M, K) && M * K <= kOwnQuantize; }
+
+sim_status launch_linear(hipStream_t st, const void *x, int x_type, int64_t x_stride, const uint8_t *wc, const uint8_t *ws,
+                         int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride) {
+    if (type == SIM_TYPE_F32) return linear_t<SIM_TYPE_F32>(st, x, x_type, x_stride, wc, ws, M, N, K, out, stride);
+    if (type == SIM_TYPE_F16) return linear_t<SIM_TYPE_F16>(st, x, x_type, x_stride, wc, ws, M, N, K, out, stride);
+    return linear_t<SIM_TYPE_BF16>(st, x, x_type, x_stride, wc, ws, M, N, K, out, stride);
+}
 
 sim_status launch_matmul(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs,
                          int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride) {

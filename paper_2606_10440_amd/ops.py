@@ -13,7 +13,8 @@ arguments raise ``SimError`` before anything is enqueued.
 from __future__ import annotations
 
 import ctypes as C
-from typing import NamedTuple, Optional
+import math
+from typing import NamedTuple
 
 import torch
 
@@ -63,13 +64,17 @@ def lib():
     return _lib
 
 
-def _call(device, fn, *args):
-    """fn(current stream of device, *args) with that device current."""
-    if device.index == torch.cuda.current_device():
-        st = fn(torch.cuda.current_stream().cuda_stream, *args)
+_raw_stream = torch._C._cuda_getCurrentRawStream   # what current_stream(i).cuda_stream is, without the object
+_device_now = torch._C._cuda_getDevice
+
+
+def _call(dev, fn, *args):
+    """fn(current stream of GPU dev, *args) with that GPU current."""
+    if dev == _device_now():
+        st = fn(_raw_stream(dev), *args)
     else:
-        with torch.cuda.device(device):
-            st = fn(torch.cuda.current_stream().cuda_stream, *args)
+        with torch.cuda.device(dev):
+            st = fn(_raw_stream(dev), *args)
     if st != SIM_OK:
         raise SimError(st, lib().sim_ops_last_error().decode())
 
@@ -80,25 +85,17 @@ def _need(ok, why):
 
 
 def _rows(x, what):
-    """A matrix whose rows are contiguous; (pointer, row stride)."""
-    _need(x.dim() == 2, f"{what} must have two dimensions")
-    _need(x.dtype in _TYPE, f"{what} must be float32, float16 or bfloat16")
-    _need(x.is_cuda, f"{what} must be on the GPU")
-    _need(x.shape[1] <= 1 or x.stride(1) == 1, f"{what} must have contiguous rows")
-    _need(x.shape[0] <= 1 or x.stride(0) >= x.shape[1], f"the rows of {what} must not overlap")
-    return x.data_ptr(), max(x.stride(0), x.shape[1])
-
-
-def _same_device(device, *tensors):
-    _need(all(t is None or t.device == device for t in tensors), "tensors are on different devices")
-
-
-def _space(n, device):
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
-
-
-def _p(t):
-    return None if t is None else t.data_ptr()
+    """(type, rows, columns, row stride, GPU) of a matrix whose rows are contiguous."""
+    t, dev = _TYPE.get(x.dtype), x.get_device()
+    if t is None or dev < 0 or x.dim() != 2:
+        _need(x.dim() == 2, f"{what} must have two dimensions")
+        _need(t is not None, f"{what} must be float32, float16 or bfloat16")
+        _need(False, f"{what} must be on the GPU")
+    rows, cols = x.shape
+    stride, step = x.stride()
+    if (step != 1 and cols > 1) or (stride < cols and rows > 1):
+        _need(False, f"the rows of {what} must be contiguous and must not overlap")
+    return t, rows, cols, stride if stride > cols else cols, dev
 
 
 # ------------------------------------------------------------------ 4-bit tensors
@@ -116,44 +113,45 @@ class Mx4(NamedTuple):
         return self.codes.numel() + self.scales.numel()
 
 
-def _check_mx4(q, what):
-    K = q.shape[-1]
-    rows = 1
-    for n in q.shape[:-1]:
-        rows *= n
-    groups = -(-K // 256)
-    for t, pitch, name in ((q.codes, groups * 128, "codes"), (q.scales, groups * 8, "scales")):
-        _need(t.dtype == torch.uint8 and t.is_cuda and t.is_contiguous() and t.shape == (rows, pitch),
-              f"the {name} of {what} must be a contiguous uint8 [{rows}, {pitch}] on the GPU")
-    return rows, K
+def _stored(q, what):
+    """(rows, columns, GPU) of a 4-bit tensor whose arrays are as they must be."""
+    codes, scales, shape = q
+    K = shape[-1]
+    rows = shape[0] if len(shape) == 2 else math.prod(shape[:-1])
+    groups, dev = (K + 255) // 256, codes.get_device()
+    if not (codes.shape == (rows, groups * 128) and scales.shape == (rows, groups * 8) and codes.dtype is torch.uint8
+            and scales.dtype is torch.uint8 and codes.is_contiguous() and scales.is_contiguous() and dev >= 0
+            and scales.get_device() == dev):
+        _need(False, f"codes and scales of {what} must be contiguous uint8 [{rows}, {groups * 128}] and "
+                     f"[{rows}, {groups * 8}] on one GPU")
+    return rows, K, dev
 
 
 def mx4_quantize(x, transpose=False) -> Mx4:
     """``x`` [..., K] in 4 bits, a scale for 32 elements along its last axis.
     With ``transpose`` (two dimensions) the result is that of ``x.t()``."""
-    _need(x.dim() >= 1, "x needs a dimension")
-    if transpose:
-        _need(x.dim() == 2, "only a matrix can be transposed")
-    flat = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
-    ptr, stride = _rows(flat, "x")
-    rows, cols = flat.shape
+    shape = tuple(x.shape)
+    if len(shape) != 2:
+        _need(len(shape) > 0 and not transpose, "x needs a dimension, and two to be transposed")
+        x = x.reshape(-1, shape[-1])
+    t, rows, cols, stride, dev = _rows(x, "x")
     R, K = (cols, rows) if transpose else (rows, cols)
-    groups = -(-K // 256)
-    codes = torch.empty((R, groups * 128), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((R, groups * 8), dtype=torch.uint8, device=x.device)
-    _call(x.device, lib().sim_mx4_quantize, ptr, _TYPE[x.dtype], rows, cols, stride, int(transpose), codes.data_ptr(),
+    groups = (K + 255) // 256
+    codes = x.new_empty((R, groups * 128), dtype=torch.uint8)
+    scales = x.new_empty((R, groups * 8), dtype=torch.uint8)
+    _call(dev, lib().sim_mx4_quantize, x.data_ptr(), t, rows, cols, stride, 1 if transpose else 0, codes.data_ptr(),
           scales.data_ptr())
-    return Mx4(codes, scales, (R, K) if transpose else tuple(x.shape))
+    return Mx4(codes, scales, (R, K) if transpose else shape)
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.bfloat16):
     """The values that ``q`` stands for."""
-    rows, K = _check_mx4(q, "q")
-    _need(dtype in _TYPE, "dtype must be float32, float16 or bfloat16")
-    out = torch.empty((rows, K), dtype=dtype, device=q.codes.device)
-    _call(out.device, lib().sim_mx4_dequantize, q.codes.data_ptr(), q.scales.data_ptr(), rows, K, out.data_ptr(),
-          _TYPE[dtype], K)
-    return out if len(q.shape) == 2 else out.view(q.shape)
+    rows, K, dev = _stored(q, "q")
+    t = _TYPE.get(dtype)
+    _need(t is not None, "dtype must be float32, float16 or bfloat16")
+    out = q.codes.new_empty(q.shape, dtype=dtype)
+    _call(dev, lib().sim_mx4_dequantize, q.codes.data_ptr(), q.scales.data_ptr(), rows, K, out.data_ptr(), t, K)
+    return out
 
 
 def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
@@ -162,33 +160,27 @@ def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
     bits on the way; ``b`` [N, K]; the result is [M, N] of ``dtype`` (or of
     ``out``, which may have strided rows)."""
     _need(isinstance(b, Mx4) and len(b.shape) == 2, "b must be a 4-bit matrix")
-    N, K = _check_mx4(b, "b")
+    N, K, dev = _stored(b, "b")
+    L = lib()
     plain = not isinstance(a, Mx4)
     if plain:
-        ptr, stride = _rows(a, "a")
-        M, device = a.shape[0], a.device
+        at, M, Ka, stride, adev = _rows(a, "a")
+        first, n, fn = (a.data_ptr(), at, stride), L.sim_mx4_linear_workspace(M, N, K), L.sim_mx4_linear
     else:
         _need(len(a.shape) == 2, "a must be a matrix")
-        M, device = _check_mx4(a, "a")[0], a.codes.device
-        _same_device(device, a.scales)
-    _need(a.shape[1] == K, "a and b differ in their last axis")
+        M, Ka, adev = _stored(a, "a")
+        first, n, fn = (a.codes.data_ptr(), a.scales.data_ptr()), L.sim_mx4_matmul_workspace(M, N, K), L.sim_mx4_matmul
+    _need(Ka == K and adev == dev, "a and b differ in their last axis or their GPU")
     if out is None:
-        _need(dtype in _TYPE, "dtype must be float32, float16 or bfloat16")
-        out = torch.empty((M, N), dtype=dtype, device=device)
-    _need(tuple(out.shape) == (M, N), "out has the wrong shape")
-    optr, ostride = _rows(out, "out")
-    _same_device(device, b.codes, b.scales, out)
-    L = lib()
-    if plain:
-        n = L.sim_mx4_linear_workspace(M, N, K)
-        ws = _space(n, device)
-        _call(device, L.sim_mx4_linear, ptr, _TYPE[a.dtype], stride, b.codes.data_ptr(), b.scales.data_ptr(), M, N, K, optr,
-              _TYPE[out.dtype], ostride, _p(ws), n)
+        t = _TYPE.get(dtype)
+        _need(t is not None, "dtype must be float32, float16 or bfloat16")
+        out, ostride = b.codes.new_empty((M, N), dtype=dtype), N
     else:
-        n = L.sim_mx4_matmul_workspace(M, N, K)
-        ws = _space(n, device)
-        _call(device, L.sim_mx4_matmul, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), M,
-              N, K, optr, _TYPE[out.dtype], ostride, _p(ws), n)
+        t, m, cols, ostride, odev = _rows(out, "out")
+        _need(m == M and cols == N and odev == dev, "out must be [M, N] on the same GPU")
+    ws = b.codes.new_empty(n) if n else None
+    _call(dev, fn, *first, b.codes.data_ptr(), b.scales.data_ptr(), M, N, K, out.data_ptr(), t, ostride,
+          ws.data_ptr() if n else None, n)
     return out
 
 
@@ -196,10 +188,8 @@ def mx4_linear_grad(dy, x, w):
     """Gradients ``(dx, dw)`` of ``y = x @ w.T`` computed in 4 bits, where
     rounding to 4 bits passes gradients through: ``dx = dy @ w`` and ``dw =
     dy.T @ x``, each operand quantised along the axis that is summed over."""
-    for t, n in ((dy, "dy"), (x, "x"), (w, "w")):
-        _rows(t, n)
-    _need(dy.shape == (x.shape[0], w.shape[0]) and x.shape[1] == w.shape[1], "dy, x and w do not fit together")
-    _same_device(dy.device, x, w)
+    (_, M, N, _, d0), (_, xm, K, _, d1), (_, wn, wk, _, d2) = _rows(dy, "dy"), _rows(x, "x"), _rows(w, "w")
+    _need(M == xm and N == wn and K == wk and d0 == d1 == d2, "dy, x and w do not fit together")
     dx = mx4_matmul(dy, mx4_quantize(w, transpose=True), dtype=x.dtype)
     dw = mx4_matmul(mx4_quantize(dy, transpose=True), mx4_quantize(x, transpose=True), dtype=w.dtype)
     return dx, dw
@@ -236,20 +226,19 @@ class Routes(NamedTuple):
 
 
 def _route_args(logits, k, mask):
-    _need(logits.dim() == 2 and 1 <= k <= min(logits.shape[1], MAX_TOPK), "k out of range")
-    ptr, stride = _rows(logits, "logits")
-    T, E = logits.shape
+    """(pointer, type, T, E, row stride, mask pointer, mask stride, k), GPU"""
+    t, T, E, stride, dev = _rows(logits, "logits")
+    _need(1 <= k <= E and k <= MAX_TOPK, "k out of range")
     mptr, mstride = None, 0
     if mask is not None:
-        _need(mask.dtype in (torch.bool, torch.uint8), "mask must be bool or uint8")
+        _need(mask.dtype in (torch.bool, torch.uint8) and mask.get_device() == dev, "mask must be bool or uint8 on the same GPU")
         _need(tuple(mask.shape) in ((E,), (T, E)), "mask must be [E] or [T, E]")
         _need(E == 1 or mask.stride(-1) == 1, "mask must have contiguous rows")
-        _same_device(logits.device, mask)
         if mask.dim() == 2:
             mstride = mask.stride(0)  # 0 where one row is expanded over the tokens
             _need(T <= 1 or mstride == 0 or mstride >= E, "the rows of mask must not overlap")
         mptr = mask.data_ptr()
-    return ptr, _TYPE[logits.dtype], T, E, stride, mptr, mstride, int(k)
+    return (logits.data_ptr(), t, T, E, stride, mptr, mstride, k), dev
 
 
 def moe_route(logits, k, mask=None, renormalize=True) -> Routes:
@@ -257,17 +246,18 @@ def moe_route(logits, k, mask=None, renormalize=True) -> Routes:
     softmax weights, and the experts' lists of slots.  ``mask`` ([E] or [T,
     E], true = allowed) takes experts out; ``renormalize`` divides a token's
     weights by their sum."""
-    args = _route_args(logits, k, mask)
-    T, E = logits.shape
-    dev = logits.device
-    i = torch.empty(2 * T * k + E + 1, dtype=torch.int32, device=dev)
-    experts, order, offsets = i[:T * k].view(T, k), i[T * k:2 * T * k], i[2 * T * k:]
-    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    args, dev = _route_args(logits, k, mask)
+    T, E = args[2], args[3]
+    slots = T * k
+    experts = logits.new_empty((T, k), dtype=torch.int32)
+    weights = logits.new_empty((T, k), dtype=torch.float32)
+    offsets = logits.new_empty(E + 1, dtype=torch.int32)
+    order = logits.new_empty(slots, dtype=torch.int32)
     L = lib()
     n = L.sim_moe_route_workspace(T, E, k)
-    ws = _space(n, dev)
-    _call(dev, L.sim_moe_route, *args, int(renormalize), experts.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
-          order.data_ptr(), _p(ws), n)
+    ws = logits.new_empty(n, dtype=torch.uint8) if n else None
+    _call(dev, L.sim_moe_route, *args, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(), offsets.data_ptr(),
+          order.data_ptr() if slots else None, ws.data_ptr() if n else None, n)
     return Routes(experts, weights, offsets, order)
 
 
@@ -276,13 +266,13 @@ def moe_route_grad(logits, experts, d_weights, mask=None, renormalize=True):
     the gradient [T, k] of the weights."""
     _need(experts.dim() == 2, "experts must be [T, k]")
     T, k = experts.shape
-    args = _route_args(logits, k, mask)
-    _need(logits.shape[0] == T and tuple(d_weights.shape) == (T, k), "experts and d_weights must be [T, k]")
-    _need(experts.dtype == torch.int32 and d_weights.dtype == torch.float32, "experts must be int32, d_weights float32")
+    args, dev = _route_args(logits, k, mask)
+    _need(args[2] == T and d_weights.shape == experts.shape, "experts and d_weights must be [T, k]")
+    _need(experts.dtype is torch.int32 and d_weights.dtype is torch.float32, "experts must be int32, d_weights float32")
     _need(experts.is_contiguous() and d_weights.is_contiguous(), "experts and d_weights must be contiguous")
-    _same_device(logits.device, experts, d_weights)
-    dz = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _call(logits.device, lib().sim_moe_route_grad, *args, int(renormalize), experts.data_ptr(), d_weights.data_ptr(),
+    _need(experts.get_device() == dev and d_weights.get_device() == dev, "tensors are on different GPUs")
+    dz = logits.new_empty((T, args[3]))
+    _call(dev, lib().sim_moe_route_grad, *args, 1 if renormalize else 0, experts.data_ptr(), d_weights.data_ptr(),
           dz.data_ptr())
     return dz
 
@@ -313,35 +303,32 @@ def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):
     ``w2[e] @ (silu(g) * u)`` with ``g, u = w13[e] @ x`` (w13 [E, 2F, D]: F
     gate rows, then F up rows; w2 [E, D, F]), and gets their weighted sum.  x
     is float16 or bfloat16; the weights have its type, or are ``Mx4``."""
-    xptr, xstride = _rows(x, "x")
-    _need(x.dtype != torch.float32, "x must be float16 or bfloat16")
-    args = _route_args(logits, k, mask)
-    T, D = x.shape
-    E = logits.shape[1]
-    _need(logits.shape[0] == T, "x and logits differ in their tokens")
+    t, T, D, xstride, dev = _rows(x, "x")
+    _need(t != 0, "x must be float16 or bfloat16")
+    (lptr, lt, lT, E, lstride, mptr, mstride, k), ldev = _route_args(logits, k, mask)
+    _need(lT == T and ldev == dev, "x and logits differ in their tokens or their GPU")
     mx4 = isinstance(w13, Mx4)
-    _need(mx4 == isinstance(w2, Mx4), "w13 and w2 must be of one kind")
-    _need(len(w13.shape) == 3 and len(w2.shape) == 3, "w13 must be [E, 2F, D], w2 [E, D, F]")
-    F = w2.shape[2]
-    _need(tuple(w13.shape) == (E, 2 * F, D) and tuple(w2.shape) == (E, D, F), "w13 must be [E, 2F, D], w2 [E, D, F]")
+    s13, s2 = tuple(w13.shape), tuple(w2.shape)
+    _need(mx4 == isinstance(w2, Mx4) and len(s2) == 3, "w13 must be [E, 2F, D], w2 [E, D, F], of one kind")
+    F = s2[2]
+    _need(s13 == (E, 2 * F, D) and s2 == (E, D, F), "w13 must be [E, 2F, D], w2 [E, D, F]")
     if mx4:
-        _check_mx4(w13, "w13")
-        _check_mx4(w2, "w2")
+        same = _stored(w13, "w13")[2] == _stored(w2, "w2")[2] == dev
         wargs = (w13.codes.data_ptr(), w13.scales.data_ptr(), w2.codes.data_ptr(), w2.scales.data_ptr(), _MX4)
-        _same_device(x.device, logits, w13.codes, w13.scales, w2.codes, w2.scales)
     else:
-        _need(w13.dtype == x.dtype and w2.dtype == x.dtype, "the weights must have the type of x or be in 4 bits")
+        _need(w13.dtype is x.dtype and w2.dtype is x.dtype, "the weights must have the type of x or be in 4 bits")
         _need(w13.is_contiguous() and w2.is_contiguous(), "the weights must be contiguous")
-        wargs = (w13.data_ptr(), None, w2.data_ptr(), None, _TYPE[x.dtype])
-        _same_device(x.device, logits, w13, w2)
+        same = w13.get_device() == w2.get_device() == dev
+        wargs = (w13.data_ptr(), None, w2.data_ptr(), None, t)
+    _need(same, "tensors are on different GPUs")
     if out is None:
-        out = torch.empty((T, D), dtype=x.dtype, device=x.device)
-    _need(tuple(out.shape) == (T, D) and out.dtype == x.dtype, "out must be like x")
-    optr, ostride = _rows(out, "out")
-    _same_device(x.device, out)
+        out, ostride = x.new_empty((T, D)), D
+    else:
+        ot, m, cols, ostride, odev = _rows(out, "out")
+        _need(ot == t and m == T and cols == D and odev == dev, "out must be like x")
     L = lib()
     n = L.sim_moe_layer_workspace(T, D, E, k, F)
-    ws = _space(n, x.device)
-    _call(x.device, L.sim_moe_layer, xptr, _TYPE[x.dtype], T, D, xstride, *args[:2], args[3], args[4], *args[5:],
-          int(renormalize), *wargs, F, optr, ostride, _p(ws), n)
+    ws = x.new_empty(n, dtype=torch.uint8) if n else None
+    _call(dev, L.sim_moe_layer, x.data_ptr(), t, T, D, xstride, lptr, lt, E, lstride, mptr, mstride, k,
+          1 if renormalize else 0, *wargs, F, out.data_ptr(), ostride, ws.data_ptr() if n else None, n)
     return out

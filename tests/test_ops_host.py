@@ -72,7 +72,8 @@ def test_dequantize_refusals(lib, change, want):
 
 MATMUL = [("ac", P), ("as", P), ("bc", P), ("bs", P), ("M", 4), ("N", 8), ("K", 64), ("out", P), ("type", 2), ("stride", 8),
           ("ws", P), ("ws_bytes", 1 << 30)]
-LINEAR = [("x", P), ("x_type", 2), ("x_stride", 64), ("wc", P), ("ws_", P), ("M", 4), ("N", 8), ("K", 64), ("out", P),
+# so many rows that they are put into 4 bits in a workspace
+LINEAR = [("x", P), ("x_type", 2), ("x_stride", 64), ("wc", P), ("ws_", P), ("M", 40), ("N", 8), ("K", 64), ("out", P),
           ("type", 2), ("stride", 8), ("ws", P), ("ws_bytes", 1 << 30)]
 
 
