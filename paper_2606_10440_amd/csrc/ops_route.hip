@@ -14,23 +14,105 @@ constexpr int kChunk = 64;           // tokens of one workgroup
 constexpr int kThreads = 16 * kChunk;
 constexpr int kScanChunks = 512;     // above it, counts are scanned by a kernel of their own
 
-// A token's keys: lane l of 16 holds experts 16 i + l.
-template <int T, int NV>
-__device__ inline void load_keys(const typename Elem<T>::type *__restrict__ z, const uint8_t *__restrict__ mask, int E,
-                                 bool live, uint32_t key[NV]) {
-    const int l = threadIdx.x & 15;
-    typename Elem<T>::type v[NV];
-    uint8_t ok[NV];
+typedef uint32_t u32_any __attribute__((aligned(1)));
+
+// N consecutive elements, at any alignment that their type has.
+template <int N, typename E> __device__ inline void load_some(const E *p, E v[N]) {
+    if (sizeof(E) * N >= 4) {
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const int e = i * 16 + l;
-        const bool in = live && e < E;
-        v[i] = in ? z[e] : Elem<T>::put(0.f);
-        ok[i] = in ? (mask ? mask[e] : 1) : 0;
+        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((uint32_t *)v)[i] = ((const u32_any *)p)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) v[i] = p[i];
     }
-#pragma unroll
-    for (int i = 0; i < NV; i++) key[i] = ok[i] ? order_key(Elem<T>::get(v[i])) : 0;
 }
+template <int N, typename E> __device__ inline void store_some(E *p, const E v[N]) {
+    if (sizeof(E) * N >= 4) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((u32_any *)p)[i] = ((const uint32_t *)v)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) p[i] = v[i];
+    }
+}
+
+// A token's logits: lane l of 16 holds experts NV l .. NV l + NV - 1, and ok
+// has a bit for each that may be used.
+template <int T, int NV>
+__device__ inline uint64_t load_logits(const typename Elem<T>::type *__restrict__ z, const uint8_t *__restrict__ mask, int E,
+                                       bool live, typename Elem<T>::type v[NV]) {
+    const int e0 = (threadIdx.x & 15) * NV;
+    uint64_t ok = 0;
+    if (live && e0 + NV <= E) {
+        uint8_t m[NV];
+        load_some<NV>(z + e0, v);
+        if (mask) {
+            load_some<NV>(mask + e0, m);
+#pragma unroll
+            for (int i = 0; i < NV; i++) ok |= (uint64_t)(m[i] != 0) << i;
+        } else {
+            ok = ~0ull;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const bool in = live && e0 + i < E;
+            v[i] = in ? z[e0 + i] : Elem<T>::put(0.f);
+            ok |= (uint64_t)(in && (!mask || mask[e0 + i])) << i;
+        }
+    }
+    return ok;
+}
+
+// The keys of a lane's experts and the search for the best of all.  16-bit
+// logits fit with their index in one word, the lower index higher: a search
+// is maxima and nothing else.  32-bit ones are searched as pairs.
+template <int T, int NV> struct Keys {
+    uint32_t k[NV];
+    static __device__ uint32_t of(typename Elem<T>::type v, uint32_t e) {
+        const uint16_t b = __builtin_bit_cast(uint16_t, v);
+        const uint16_t inf = T == SIM_TYPE_BF16 ? 0x7f80 : 0x7c00;
+        const uint16_t key = (b & 0x7fff) > inf ? 0xffff : (b & 0x7fff) == 0 ? 0x8000 : b == (inf | 0x8000) ? 0 : b & 0x8000 ? ~b : b | 0x8000;
+        return key ? (uint32_t)key << 16 | (0xffff - e) : 0;
+    }
+    static __device__ float value(uint32_t k) {
+        const uint16_t key = k >> 16;
+        return Elem<T>::get(__builtin_bit_cast(typename Elem<T>::type,
+                                               (uint16_t)(key == 0xffff ? 0x7fff : key & 0x8000 ? key & 0x7fff : ~key)));
+    }
+    // the best of 16 lanes and its expert; 0 where nothing is left.  It is
+    // taken out.
+    __device__ uint32_t take(uint32_t &e) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) m = max(m, k[i]);
+        m = max16(m);
+#pragma unroll
+        for (int i = 0; i < NV; i++) k[i] = k[i] == m ? 0 : k[i];
+        e = 0xffff - (m & 0xffff);
+        return m;
+    }
+};
+template <int NV> struct Keys<SIM_TYPE_F32, NV> {
+    uint32_t k[NV];
+    static __device__ uint32_t of(float v, uint32_t) { return order_key(v); }
+    static __device__ float value(uint32_t k) { return key_value(k); }
+    __device__ uint32_t take(uint32_t &e) {
+        const uint32_t e0 = (threadIdx.x & 15) * NV;
+        uint32_t m = 0;
+        e = 0xffffu;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const bool better = k[i] > m;  // the first of equal ones has the lowest index
+            m = better ? k[i] : m;
+            e = better ? e0 + i : e;
+        }
+        best16(m, e);
+#pragma unroll
+        for (int i = 0; i < NV; i++) k[i] = e0 + i == e ? 0 : k[i];
+        return m;
+    }
+};
 
 // Exclusive prefix sums over kThreads values (one a thread) and their total.
 __device__ inline int block_scan(int v, int *wave_sum, int &total) {
@@ -51,23 +133,13 @@ __device__ inline int block_scan(int v, int *wave_sum, int &total) {
     return before + s - v;
 }
 
-// Slots of one chunk to their places: base[e] = place of its first slot of
-// expert e.  A wave takes one expert after another and looks 64 slots over at
-// a time, so that equal experts stay in slot order.
-__device__ inline void place_slots(const int16_t *slot_expert, int n, int first_slot, const int *count, const int *base,
-                                   int E, int32_t *__restrict__ order) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int e = wave; e < E; e += kThreads / 64) {
-        if (!count[e]) continue;
-        int at = base[e];
-        for (int s = 0; s < n; s += 64) {
-            const bool mine = s + lane < n && slot_expert[s + lane] == e;
-            const uint64_t all = __ballot(mine);
-            if (mine) order[at + __popcll(all & ((1ull << lane) - 1))] = first_slot + s + lane;
-            at += __popcll(all);
-        }
-    }
-}
+__host__ __device__ inline int hist_pitch(int E) { return (E + 3) / 4 * 4; }
+
+// The tokens of a chunk that chose an expert, a bit for each.  A token has an
+// expert once at most, so the place of its slot in the expert's list is the
+// number of lower bits.
+__device__ inline void mark(uint64_t *chose, int e, int tok) { atomicOr((unsigned long long *)&chose[e], 1ull << tok); }
+__device__ inline int before_in(uint64_t chose, int tok) { return __popcll(chose & ((1ull << tok) - 1)); }
 
 // Choice and weights; counts of the chunk, or (one chunk only) the lists.
 template <int T, int NV>
@@ -75,86 +147,85 @@ __global__ __launch_bounds__(kThreads) void route_choose(const typename Elem<T>:
                                                          int E, int64_t stride, const uint8_t *__restrict__ mask,
                                                          int64_t mask_stride, int k, int renorm,
                                                          int32_t *__restrict__ experts, float *__restrict__ weights,
-                                                         int32_t *__restrict__ hist, int32_t *__restrict__ offsets,
+                                                         uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,
                                                          int32_t *__restrict__ order) {
-    __shared__ int count[SIM_MOE_MAX_EXPERTS];
+    __shared__ uint64_t chose[SIM_MOE_MAX_EXPERTS];
     __shared__ int base[SIM_MOE_MAX_EXPERTS];
     __shared__ int wave_sum[kThreads / 64];
-    __shared__ int16_t slot_expert[kChunk * SIM_MOE_MAX_TOPK];
     const int l = threadIdx.x & 15, tok = threadIdx.x >> 4;
     const int64_t t0 = (int64_t)blockIdx.x * kChunk, t = t0 + tok;
     const bool live = t < n_tok;
-    count[threadIdx.x] = 0;
-    uint32_t key[NV];
-    load_keys<T, NV>(logits + (live ? t : 0) * stride, mask ? mask + (live ? t : 0) * mask_stride : nullptr, E, live, key);
+    chose[threadIdx.x] = 0;
+    Keys<T, NV> key;
+    float z = 0.f, top = 0.f;
+    {
+        typename Elem<T>::type v[NV];
+        const uint64_t ok = load_logits<T, NV>(logits + (live ? t : 0) * stride, mask ? mask + (live ? t : 0) * mask_stride : nullptr, E, live, v);
+#pragma unroll
+        for (int i = 0; i < NV; i++) key.k[i] = (ok >> i) & 1 ? Keys<T, NV>::of(v[i], l * NV + i) : 0;
+    }
+    if (!renorm) {  // the sum over all that are allowed
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) m = max(m, key.k[i]);
+        top = Keys<T, NV>::value(max16(m));
+#pragma unroll
+        for (int i = 0; i < NV; i++) z += key.k[i] ? fast_exp(Keys<T, NV>::value(key.k[i]) - top) : 0.f;
+        z = sum16(z);
+    }
     __syncthreads();
 
     uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};  // the choices l and l + 16
-    float top = 0.f, z = 0.f;
     for (int j = 0; j < k; j++) {
-        uint32_t bk = 0, bi = 0xffffu;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const bool take = key[i] > bk;  // the first of equal ones has the lowest index
-            bk = take ? key[i] : bk;
-            bi = take ? (uint32_t)(i * 16 + l) : bi;
-        }
-        best16(bk, bi);
-        if (j == 0) {
-            top = key_value(bk);
-#pragma unroll
-            for (int i = 0; i < NV; i++) z += key[i] ? expf(key_value(key[i]) - top) : 0.f;
-            z = sum16(z);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; i++)
-            if ((uint32_t)(i * 16 + l) == bi) key[i] = 0;
+        uint32_t e;
+        const uint32_t m = key.take(e);
+        if (j == 0) top = Keys<T, NV>::value(m);
         if (l == (j & 15)) {
-            mine[j >> 4] = bk;
-            mine_e[j >> 4] = bi;
+            mine[j >> 4] = m;
+            mine_e[j >> 4] = e;
         }
     }
     float w[2];
 #pragma unroll
-    for (int q = 0; q < 2; q++) w[q] = mine[q] ? expf(key_value(mine[q]) - top) : 0.f;
-    const float chosen = sum16(w[0] + w[1]);
+    for (int q = 0; q < 2; q++) w[q] = mine[q] ? fast_exp(Keys<T, NV>::value(mine[q]) - top) : 0.f;
+    if (renorm) z = sum16(w[0] + w[1]);
 #pragma unroll
     for (int q = 0; q < 2; q++) {
         const int j = q * 16 + l;
         if (live && j < k) {
-            const int e = mine[q] ? (int)mine_e[q] : -1;
-            experts[t * k + j] = e;
-            weights[t * k + j] = mine[q] ? w[q] / (renorm ? chosen : z) : 0.f;
-            slot_expert[tok * k + j] = (int16_t)e;
-            if (e >= 0) atomicAdd(&count[e], 1);
+            experts[t * k + j] = mine[q] ? (int)mine_e[q] : -1;
+            weights[t * k + j] = mine[q] ? w[q] / z : 0.f;
+            if (mine[q] && order) mark(chose, mine_e[q], tok);
         }
     }
     if (!order) return;
     __syncthreads();
+    const int count = __popcll(chose[threadIdx.x]);
     if (gridDim.x > 1) {
-        if ((int)threadIdx.x < E) hist[(int64_t)blockIdx.x * E + threadIdx.x] = count[threadIdx.x];
+        // at most kChunk: a byte
+        if ((int)threadIdx.x < hist_pitch(E)) hist[(int64_t)blockIdx.x * hist_pitch(E) + threadIdx.x] = (uint8_t)count;
         return;
     }
     int total;
-    const int mine_base = block_scan(count[threadIdx.x], wave_sum, total);
-    base[threadIdx.x] = mine_base;
-    if ((int)threadIdx.x < E) offsets[threadIdx.x] = mine_base;
+    base[threadIdx.x] = block_scan(count, wave_sum, total);
+    if ((int)threadIdx.x < E) offsets[threadIdx.x] = base[threadIdx.x];
     if (threadIdx.x == 0) offsets[E] = total;
     __syncthreads();
-    const int n = (int)n_tok * k;
-    place_slots(slot_expert, n, 0, count, base, E, order);
-    for (int s = total + threadIdx.x; s < n; s += kThreads) order[s] = -1;
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+        if (live && mine[q]) order[base[mine_e[q]] + before_in(chose[mine_e[q]], tok)] = tok * k + q * 16 + l;
+    for (int s = total + threadIdx.x; s < (int)n_tok * k; s += kThreads) order[s] = -1;
 }
 
-// Counts of each chunk to the sums over the chunks before it; the row past
-// the last gets the totals.
-__global__ __launch_bounds__(kThreads) void route_scan(int32_t *__restrict__ hist, int chunks, int E) {
+// The sums over the chunks before each; the row past the last gets the totals.
+__global__ __launch_bounds__(kThreads) void route_scan(const uint8_t *__restrict__ hist, int32_t *__restrict__ sums, int chunks,
+                                                       int E) {
     __shared__ int part_sum[64][16];
-    const int e = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
+    const int e = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4, pitch = hist_pitch(E);
     const int per = (chunks + 63) / 64, c0 = part * per, c1 = min(chunks, c0 + per);
     int s = 0;
     if (e < E)
-        for (int c = c0; c < c1; c++) s += hist[(int64_t)c * E + e];
+        for (int c = c0; c < c1; c++) s += hist[(int64_t)c * pitch + e];
     part_sum[part][threadIdx.x & 15] = s;
     __syncthreads();
     if (e >= E) return;
@@ -165,119 +236,156 @@ __global__ __launch_bounds__(kThreads) void route_scan(int32_t *__restrict__ his
         total += v;
     }
     for (int c = c0; c < c1; c++) {
-        const int v = hist[(int64_t)c * E + e];
-        hist[(int64_t)c * E + e] = before;
-        before += v;
+        sums[(int64_t)c * E + e] = before;
+        before += hist[(int64_t)c * pitch + e];
     }
-    if (part == 0) hist[(int64_t)chunks * E + e] = total;
+    if (part == 0) sums[(int64_t)chunks * E + e] = total;
 }
 
 // Lists of one chunk, from the counts of all (each workgroup adds them up
 // itself) or from the scanned ones.
 __global__ __launch_bounds__(kThreads) void route_place(const int32_t *__restrict__ experts, int64_t n_tok, int E, int k,
-                                                        const int32_t *__restrict__ hist, int scanned,
+                                                        const uint8_t *__restrict__ hist, const int32_t *__restrict__ sums,
                                                         int32_t *__restrict__ offsets, int32_t *__restrict__ order) {
-    __shared__ int count[SIM_MOE_MAX_EXPERTS];   // of this chunk
-    __shared__ int before[SIM_MOE_MAX_EXPERTS];  // of the chunks before
+    __shared__ uint64_t chose[SIM_MOE_MAX_EXPERTS];  // in this chunk
+    __shared__ int before[SIM_MOE_MAX_EXPERTS];      // slots of the chunks before
     __shared__ int all[SIM_MOE_MAX_EXPERTS];
     __shared__ int wave_sum[kThreads / 64];
-    __shared__ int16_t slot_expert[kChunk * SIM_MOE_MAX_TOPK];
     const int chunk = blockIdx.x, chunks = gridDim.x, t = threadIdx.x;
     const int first = chunk * kChunk * k;
     const int n = (int)min((int64_t)kChunk * k, n_tok * k - first);
-    count[t] = before[t] = all[t] = 0;
+    chose[t] = 0;
+    before[t] = all[t] = 0;
+    int mine[2];  // the experts of this thread's slots
+#pragma unroll
+    for (int q = 0; q < 2; q++) mine[q] = t + q * kThreads < n ? experts[(int64_t)first + t + q * kThreads] : -1;
     __syncthreads();
-    for (int s = t; s < n; s += kThreads) {
-        const int e = experts[(int64_t)first + s];
-        slot_expert[s] = (int16_t)e;
-        if (e >= 0) atomicAdd(&count[e], 1);
-    }
-    if (scanned) {
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+        if (mine[q] >= 0) mark(chose, mine[q], (t + q * kThreads) / k);
+    if (sums) {
         if (t < E) {
-            before[t] = hist[(int64_t)chunk * E + t];
-            all[t] = hist[(int64_t)chunks * E + t];
+            before[t] = sums[(int64_t)chunk * E + t];
+            all[t] = sums[(int64_t)chunks * E + t];
         }
     } else {
-        int width = 16;  // lanes over the experts, the rest over the chunks
-        while (width < E) width <<= 1;
-        const int e = t & (width - 1), step = kThreads / width;
-        if (e < E) {
-            int b = 0, a = 0;
-            for (int c = t / width; c < chunks; c += step) {
-                const int v = hist[(int64_t)c * E + e];
-                a += v;
-                b += c < chunk ? v : 0;
+        // a thread adds up four experts' bytes over every step-th chunk
+        const int pitch = hist_pitch(E);
+        int width = 4;
+        while (width * 4 < pitch) width <<= 1;
+        const int e = (t & (width - 1)) * 4, step = kThreads / width;
+        if (e < pitch) {
+            int a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
+            for (int c = t / width; c < chunks; c += 8 * step) {  // eight loads under way
+                uint32_t v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    v[i] = c + i * step < chunks ? *(const uint32_t *)(hist + (int64_t)(c + i * step) * pitch + e) : 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+#pragma unroll
+                    for (int x = 0; x < 4; x++) {
+                        const int n = (v[i] >> (8 * x)) & 255;
+                        a[x] += n;
+                        b[x] += c + i * step < chunk ? n : 0;
+                    }
             }
-            atomicAdd(&all[e], a);
-            atomicAdd(&before[e], b);
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+                atomicAdd(&all[e + x], a[x]);
+                atomicAdd(&before[e + x], b[x]);
+            }
         }
     }
     __syncthreads();
     int total;
-    const int mine = block_scan(all[t], wave_sum, total);
-    before[t] += mine;
+    const int base = block_scan(all[t], wave_sum, total);
+    before[t] += base;
     if (chunk == 0) {
-        if (t < E) offsets[t] = mine;
+        if (t < E) offsets[t] = base;
         if (t == 0) offsets[E] = total;
     }
     __syncthreads();
-    place_slots(slot_expert, n, first, count, before, E, order);
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int s = t + q * kThreads;
+        if (mine[q] >= 0) order[before[mine[q]] + before_in(chose[mine[q]], s / k)] = first + s;
+    }
     for (int64_t s = max((int64_t)total, (int64_t)first) + t; s < (int64_t)first + n; s += kThreads) order[s] = -1;
 }
 
-// Gradient: sixteen lanes a token again; each chosen expert's w g is taken up
-// by the lane that holds that expert.
+// Gradient: sixteen lanes a token again.  Lane l has the choices l and l +
+// 16; a row in LDS brings their part to the lanes that hold the experts.
 template <int T, int NV>
 __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *__restrict__ logits, int64_t n_tok, int E,
                                                   int64_t stride, const uint8_t *__restrict__ mask, int64_t mask_stride,
                                                   int k, int renorm, const int32_t *__restrict__ experts,
                                                   const float *__restrict__ dw, typename Elem<T>::type *__restrict__ dz) {
+    typedef typename Elem<T>::type El;
+    __shared__ __align__(16) float rows[16][NV * 16];
     const int l = threadIdx.x & 15;
     const int64_t t = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const bool live = t < n_tok;
-    const int64_t tt = live ? t : 0;
-    uint32_t key[NV];
-    load_keys<T, NV>(logits + tt * stride, mask ? mask + tt * mask_stride : nullptr, E, live, key);
-    uint32_t m = 0;
+    if (t >= n_tok) return;  // sixteen lanes at a time: they share no barrier
+    float *row = rows[threadIdx.x >> 4];
+    const El *zt = logits + t * stride;
+    const uint8_t *mt = mask ? mask + t * mask_stride : nullptr;
+    int e[2];
+    float g[2], v[2];
 #pragma unroll
-    for (int i = 0; i < NV; i++) m = max(m, key[i]);
-    const float top = key_value(max16(m));
-    // g and whether it was chosen, of the experts held here
-    float g[NV];
-    uint64_t chosen = 0;
-#pragma unroll
-    for (int i = 0; i < NV; i++) g[i] = 0.f;
-    for (int j = 0; j < k; j++) {
-        const int e = live ? experts[t * k + j] : -1;
-        const float gj = live ? dw[t * k + j] : 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; i++)
-            if (e == i * 16 + l && key[i]) {
-                g[i] = gj;
-                chosen |= 1ull << i;
-            }
+    for (int q = 0; q < 2; q++) {
+        const int j = q * 16 + l;
+        e[q] = j < k ? experts[t * k + j] : -1;
+        if (e[q] < 0 || e[q] >= E || (mt && !mt[e[q]])) e[q] = -1;
+        g[q] = e[q] >= 0 ? dw[t * k + j] : 0.f;
+        v[q] = e[q] >= 0 ? Elem<T>::get(zt[e[q]]) : -INFINITY;
     }
-    float p[NV], z = 0.f, dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const bool counts = renorm ? (chosen >> i) & 1 : key[i] != 0;
-        p[i] = counts ? expf(key_value(key[i]) - top) : 0.f;
-        z += p[i];
+    for (int i = 0; i < NV; i++) row[i * 16 + l] = 0.f;
+    float top, p[NV];
+    uint64_t ok = 0;
+    if (renorm) {
+        uint32_t m = max(order_key(v[0]), order_key(v[1]));
+        top = key_value(max16(m));
+    } else {
+        El all[NV];
+        ok = load_logits<T, NV>(zt, mt, E, true, all);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) m = max(m, (ok >> i) & 1 ? order_key(Elem<T>::get(all[i])) : 0u);
+        top = key_value(max16(m));
+#pragma unroll
+        for (int i = 0; i < NV; i++) p[i] = (ok >> i) & 1 ? fast_exp(Elem<T>::get(all[i]) - top) : 0.f;
     }
+    float w[2], z = 0.f;
+#pragma unroll
+    for (int q = 0; q < 2; q++) w[q] = e[q] >= 0 ? fast_exp(v[q] - top) : 0.f;
+    if (renorm) z = w[0] + w[1];
+    else
+#pragma unroll
+        for (int i = 0; i < NV; i++) z += p[i];
     const float inv = 1.f / sum16(z);
+    float dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        p[i] *= inv;
-        dot += (chosen >> i) & 1 ? g[i] * p[i] : 0.f;
+    for (int q = 0; q < 2; q++) {
+        w[q] *= inv;
+        dot += e[q] >= 0 ? g[q] * w[q] : 0.f;
     }
     dot = sum16(dot);
 #pragma unroll
+    for (int q = 0; q < 2; q++)
+        if (e[q] >= 0) row[e[q]] = renorm ? w[q] * (g[q] - dot) : g[q];
+    El out[NV];
+#pragma unroll
     for (int i = 0; i < NV; i++) {
-        const int e = i * 16 + l;
-        const bool sel = (chosen >> i) & 1;
-        const float d = key[i] && (sel || !renorm) ? p[i] * ((sel ? g[i] : 0.f) - dot) : 0.f;
-        if (live && e < E) dz[t * E + e] = Elem<T>::put(d);
+        const float r = row[l * NV + i];
+        out[i] = Elem<T>::put(renorm ? r : (ok >> i) & 1 ? p[i] * inv * (r - dot) : 0.f);
     }
+    El *o = dz + t * E + l * NV;
+    if (l * NV + NV <= E) store_some<NV>(o, out);
+    else
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+            if (l * NV + i < E) o[i] = out[i];
 }
 
 // Calls f with the smallest register count that holds E experts in 16 lanes.
@@ -291,20 +399,22 @@ template <typename F> void with_nv(int E, F &&f) {
     else f(std::integral_constant<int, 64>());
 }
 
+inline size_t hist_bytes(size_t chunks, int E) { return (chunks * hist_pitch(E) + 15) / 16 * 16; }
+
 template <int T>
 sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets, int32_t *order,
                    void *ws) {
     const uint32_t chunks = (uint32_t)((a.T + kChunk - 1) / kChunk);
-    int32_t *hist = (int32_t *)ws;
+    uint8_t *hist = (uint8_t *)ws;
+    int32_t *sums = chunks > kScanChunks ? (int32_t *)(hist + hist_bytes(chunks, a.E)) : nullptr;
     with_nv(a.E, [&](auto nv) {
         route_choose<T, decltype(nv)::value><<<chunks, kThreads, 0, st>>>(
             (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts,
             weights, hist, offsets, order);
     });
     if (order && chunks > 1) {
-        const int scanned = chunks > kScanChunks;
-        if (scanned) route_scan<<<(a.E + 15) / 16, kThreads, 0, st>>>(hist, (int)chunks, a.E);
-        route_place<<<chunks, kThreads, 0, st>>>(experts, a.T, a.E, a.k, hist, scanned, offsets, order);
+        if (sums) route_scan<<<(a.E + 15) / 16, kThreads, 0, st>>>(hist, sums, (int)chunks, a.E);
+        route_place<<<chunks, kThreads, 0, st>>>(experts, a.T, a.E, a.k, hist, sums, offsets, order);
     }
     return SIM_OPS_LAUNCH_OK();
 }
@@ -327,7 +437,8 @@ __global__ void no_tokens(int32_t *offsets, int E) {
 
 size_t route_workspace(int64_t T, int E, int) {
     const size_t chunks = (size_t)((T + kChunk - 1) / kChunk);
-    return chunks > 1 ? (chunks + 1) * (size_t)E * sizeof(int32_t) : 0;
+    if (chunks <= 1) return 0;
+    return hist_bytes(chunks, E) + (chunks > kScanChunks ? (chunks + 1) * (size_t)E * sizeof(int32_t) : 0);
 }
 
 sim_status launch_route(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets,

@@ -17,6 +17,9 @@ __device__ inline float key_value(uint32_t k) {
     return __uint_as_float(k == 0xffffffffu ? 0x7fc00000u : k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
+// e^x for x <= 0: 2^(x log2 e), whose argument's rounding is the error
+__device__ inline float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
 // (key, index) of the higher key, the lower index where they tie
 __device__ inline void keep_better(uint32_t &k, uint32_t &i, uint32_t k2, uint32_t i2) {
     const bool take = k2 > k || (k2 == k && i2 < i);
