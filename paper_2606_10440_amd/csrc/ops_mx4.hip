@@ -36,39 +36,37 @@ __global__ __launch_bounds__(256) void quantize_rows(const typename Elem<T>::typ
 }
 
 // Blocks along the rows of x: the result's row c is column c of x.  A
-// workgroup takes 256 rows and 64 columns; a lane holds 32 rows of two
-// columns (two whole blocks), and the codes go through LDS so that a result
-// row is written 128 bytes at a time.
-template <int T, bool WIDE>
+// workgroup takes 256 rows and, of each, 256 bytes; a lane holds 32 rows (one
+// block) of eight bytes, all of them loaded before the first is used, and
+// the codes go through LDS so that a result row is written 128 bytes at a
+// time.
+template <int T>
 __global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::type *__restrict__ x, int64_t rows,
                                                      int64_t cols, int64_t stride, int64_t row_groups,
-                                                     uint32_t col_tiles, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+                                                     uint32_t col_tiles, uint8_t *__restrict__ codes,
+                                                     uint8_t *__restrict__ scales) {
     typedef typename Elem<T>::type E;
-    __shared__ __align__(16) uint8_t tile[64 * (kGroupCodes + 16)];
-    __shared__ __align__(8) uint8_t stile[64 * kGroupScales];
-    const int cp = threadIdx.x & 31, blk = threadIdx.x >> 5;  // column pair, block of 32 rows
-    const int64_t g = blockIdx.x / col_tiles;  // group of 256 rows
-    const int64_t c0 = (int64_t)(blockIdx.x % col_tiles) * 64, c = c0 + cp * 2;
+    typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+    constexpr int VC = 8 / sizeof(E), COLS = 32 * VC, PITCH = kGroupCodes + 16;
+    __shared__ __align__(16) uint8_t tile[COLS * PITCH];
+    __shared__ __align__(8) uint8_t stile[COLS * kGroupScales];
+    const int part = threadIdx.x & 31, blk = threadIdx.x >> 5;  // columns part VC .., rows blk 32 ..
+    const int64_t g = blockIdx.x / col_tiles;                   // group of 256 rows
+    const int64_t c0 = (int64_t)(blockIdx.x % col_tiles) * COLS, c = c0 + part * VC;
     const int64_t r0 = g * 256 + blk * 32;
-    E v[32][2];
+    E v[32][VC];
+    const E *p = x + r0 * stride + c;
+    if (r0 + 32 <= rows && c + VC <= cols) {
 #pragma unroll
-    for (int i = 0; i < 32; i++) {
-        v[i][0] = v[i][1] = Elem<T>::put(0.f);
-        const E *p = x + (r0 + i) * stride + c;
-        if (r0 + i < rows) {
-            if (WIDE) {  // even row length, both columns aligned to their size together
-                if (c < cols) {
-                    if (sizeof(E) == 2) *(uint32_t *)v[i] = *(const uint32_t *)p;
-                    else *(u32x2 *)v[i] = *(const u32x2 *)p;
-                }
-            } else {
-                if (c < cols) v[i][0] = p[0];
-                if (c + 1 < cols) v[i][1] = p[1];
-            }
-        }
+        for (int i = 0; i < 32; i++) *(u32x2 *)v[i] = *(const u32x2_any *)(p + i * stride);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; i++)
+#pragma unroll
+            for (int j = 0; j < VC; j++) v[i][j] = r0 + i < rows && c + j < cols ? p[i * stride + j] : Elem<T>::put(0.f);
     }
 #pragma unroll
-    for (int j = 0; j < 2; j++) {
+    for (int j = 0; j < VC; j++) {
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < 32; i++) m = max(m, mag(Elem<T>::get(v[i][j])));
@@ -82,19 +80,19 @@ __global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::typ
             for (int i = 0; i < 8; i++) f[i] = Elem<T>::get(v[q * 8 + i][j]);
             out[q] = sb == 255 ? 0u : pack8(f, s);
         }
-        const int col = cp * 2 + j;
-        *(u32x4 *)(tile + col * (kGroupCodes + 16) + blk * 16) = out;
+        const int col = part * VC + j;
+        *(u32x4 *)(tile + col * PITCH + blk * 16) = out;
         stile[col * kGroupScales + blk] = (uint8_t)sb;
     }
     __syncthreads();
 #pragma unroll
-    for (int n = threadIdx.x; n < 64 * 8; n += 256) {  // 16 bytes each
-        const int col = n >> 3, part = n & 7;
+    for (int n = threadIdx.x; n < COLS * 8; n += 256) {  // 16 bytes each
+        const int col = n >> 3, piece = n & 7;
         if (c0 + col < cols)
-            *(u32x4 *)(codes + ((c0 + col) * row_groups + g) * kGroupCodes + part * 16) =
-                *(const u32x4 *)(tile + col * (kGroupCodes + 16) + part * 16);
+            *(u32x4 *)(codes + ((c0 + col) * row_groups + g) * kGroupCodes + piece * 16) =
+                *(const u32x4 *)(tile + col * PITCH + piece * 16);
     }
-    if (threadIdx.x < 64 && c0 + threadIdx.x < cols)
+    if (threadIdx.x < COLS && c0 + threadIdx.x < cols)
         *(u32x2 *)(scales + ((c0 + threadIdx.x) * row_groups + g) * kGroupScales) =
             *(const u32x2 *)(stile + threadIdx.x * kGroupScales);
 }
@@ -152,10 +150,9 @@ sim_status quantize_t(hipStream_t st, const void *xv, int64_t rows, int64_t cols
     const E *x = (const E *)xv;
     if (transpose) {
         const int64_t rg = groups_of(rows);
-        const uint32_t ct = (uint32_t)((cols + 63) / 64), grid = (uint32_t)(ct * rg);
-        const bool wide = (uintptr_t)x % (2 * sizeof(E)) == 0 && stride % 2 == 0 && cols % 2 == 0;
-        if (wide) quantize_cols<T, true><<<grid, 256, 0, st>>>(x, rows, cols, stride, rg, ct, codes, scales);
-        else quantize_cols<T, false><<<grid, 256, 0, st>>>(x, rows, cols, stride, rg, ct, codes, scales);
+        constexpr int COLS = 256 / sizeof(E);
+        const uint32_t ct = (uint32_t)((cols + COLS - 1) / COLS);
+        quantize_cols<T><<<(uint32_t)(ct * rg), 256, 0, st>>>(x, rows, cols, stride, rg, ct, codes, scales);
         return SIM_OPS_LAUNCH_OK();
     }
     const int64_t per = groups_of(cols), n = rows * per;

@@ -64,10 +64,10 @@ __global__ __launch_bounds__(256) void matmul_simple(const uint8_t *__restrict__
 // its own barrier: that barrier says that the NEXT stage's codes are there.
 //
 // Of a stage's four blocks half h of the lanes takes blocks 2 h and 2 h + 1.
-// In LDS a row's four 16-byte pieces are permuted by bits 1 and 2 of the row
-// number, so that eight rows that are read together fill all banks once; the
-// copy writes LDS in lane order, so the permutation is applied to the
-// addresses that it reads.
+// In LDS a row's four 16-byte pieces are permuted by bits 2 and 3 of the row
+// number, so that the sixteen rows that are read together fill all banks
+// once; the copy writes LDS in lane order, so the permutation is applied to
+// the addresses that it reads.
 //
 // The operands change places in the instruction (B first), so that a lane
 // ends up with one row of the result and four columns in sequence; the
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
     for (int i = 0; i < COPIES; i++) {
         const bool in_a = i < A_COPIES;
         const int row = (in_a ? wave * A_COPIES + i : wave * (COPIES - A_COPIES) + i - A_COPIES) * 16 + (lane >> 2);
-        src[i] = (uint32_t)(min(row, in_a ? a_last : b_last) * (uint32_t)code_pitch) + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
+        src[i] = (uint32_t)(min(row, in_a ? a_last : b_last) * (uint32_t)code_pitch) + ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte *)&codes[0][0];
     const uint32_t dst_a = lds0 + wave * A_COPIES * 1024, dst_b = lds0 + BM * kStageCodes + wave * (COPIES - A_COPIES) * 1024;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
     // in the order of first use: a row block, the column blocks, the other row blocks
     const auto nth_op = [&](int n) { return n == 0 ? 0 : n <= TN ? TM + n - 1 : n - TN; };
     const auto read_op = [&](int i, int stage, int s) {
-        const int piece = (h * 2 + s) ^ ((lane >> 1) & 3);
+        const int piece = (h * 2 + s) ^ ((lane >> 2) & 3);
         op[s][i] = *(const u32x4 *)(codes[(uint32_t)stage % kBuffers] + row_of(i) * kStageCodes + piece * 16);
     };
     const auto read_scale = [&](int i, int stage, int q) {
