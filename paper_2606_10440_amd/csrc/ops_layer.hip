@@ -54,19 +54,20 @@ __device__ inline bf16x8 widen8(uint32_t codes, float scale) {
     return r;
 }
 
-// A step's elements of lane l (q = l / 16) in instruction s: 16-bit weights
-// take 32 s + 8 q .. + 7, so that an instruction's load covers 64 contiguous
-// bytes of each row; 4-bit ones 32 q + 8 s, whose 32 codes are one load.
+// A step is 64 columns of 16-bit weights (two loads, whole cache lines, for
+// two instructions) or 128 of 4-bit ones (one load for four).  Elements of
+// lane l (q = l / 16) in instruction s: 32 s + 8 q .. + 7, or 32 q + 8 s .. + 7.
+template <int WT> constexpr int kCols = WT == SIM_TYPE_MX4 ? 128 : 64;
+template <int WT> constexpr int kIns = WT == SIM_TYPE_MX4 ? 4 : 2;
 template <int WT> __device__ inline int step_at(int q, int s) { return WT == SIM_TYPE_MX4 ? 32 * q + 8 * s : 32 * s + 8 * q; }
 
 // A step of one tile of sixteen weight rows; lane l holds row l % 16.
 template <int WT, bool EDGE> struct Weights {
-    u32x4 raw[4];
+    u32x4 raw[2];
     // base: the weights; row: this lane's; k0: the step's first column
     __device__ void load(const void *base, int64_t row, int K, int k0, int q) {
-        const uint16_t *p = (const uint16_t *)base + row * K;
 #pragma unroll
-        for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(p, k0 + step_at<WT>(q, s), K);
+        for (int s = 0; s < 2; s++) raw[s] = load_row8<EDGE>((const uint16_t *)base + row * K, k0 + step_at<WT>(q, s), K);
     }
     struct Operand {
         bf16x8 hi, lo;
@@ -96,10 +97,10 @@ template <bool EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
 
 // A step of sixteen inputs; lane l holds token l % 16.
 template <int T, int WT, bool EDGE> struct Inputs {
-    u32x4 raw[4];
+    u32x4 raw[kIns<WT>];
     __device__ void load(const uint16_t *row, int K, int k0, int q) {
 #pragma unroll
-        for (int s = 0; s < 4; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
+        for (int s = 0; s < kIns<WT>; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
     }
     template <typename W> static __device__ f32x4 mul(u32x4 v, const typename W::Operand &w, f32x4 c) {
         if (T == SIM_TYPE_BF16) return W::mul(w, __builtin_bit_cast(bf16x8, v), c);
@@ -112,10 +113,10 @@ template <int T, int WT, bool EDGE> struct Inputs {
 // A step of sixteen rows of hidden values in their two parts (rows of a whole
 // number of steps), zeros where the lane has none.
 template <int WT> struct Hidden {
-    u32x4 hi[4], lo[4];
+    u32x4 hi[kIns<WT>], lo[kIns<WT>];
     __device__ void load(const __bf16 *h_hi, const __bf16 *h_lo, int64_t at, bool some, int k0, int q) {
 #pragma unroll
-        for (int s = 0; s < 4; s++) {
+        for (int s = 0; s < kIns<WT>; s++) {
             hi[s] = lo[s] = u32x4{0, 0, 0, 0};
             if (some) {
                 hi[s] = *(const u32x4 *)(h_hi + at + k0 + step_at<WT>(q, s));
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
             if (t == 0) plan.expert[i >> 4] = (int16_t)e;
         }
     }
-    const int steps = (D + kStep - 1) / kStep, items = used * tiles;
+    const int steps = (D + kCols<WT> - 1) / kCols<WT>, items = used * tiles;
     int turn = 0, held = -1;
     bool in_lds = false;
     // neighbours take neighbouring rows at the same time (measured: 109 us;
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
         typedef Inputs<T, WT, EDGE> In;
         f32x4 g = {0}, u = {0};
         if (in_lds) {
-            constexpr int U = WT == SIM_TYPE_MX4 ? 4 : 2;
+            constexpr int U = 4;
             typedef Weights<WT, EDGE> Wt;
             Wt wg[U], wu[U];
             Scales<WT, 2, U> sc[2];
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                 (steps + U - 1) / U, wave,
                 [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
                 [&](int i, int run) {  // a step past the last loads that again and is not used
-                    const int k0 = min(run * U + i, steps - 1) * kStep;
+                    const int k0 = min(run * U + i, steps - 1) * kCols<WT>;
                     wg[i].load(w13, row, D, k0, q);
                     wu[i].load(w13, row + F, D, k0, q);
                 },
@@ -316,15 +317,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                     if (run * U + i < steps) {
                         const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
-                        for (int s = 0; s < 4; s++) {
-                            const u32x4 v = *(const u32x4 *)(xr + ((run * U + i) * kStep + step_at<WT>(q, s)) * 2);
+                        for (int s = 0; s < kIns<WT>; s++) {
+                            const u32x4 v = *(const u32x4 *)(xr + ((run * U + i) * kCols<WT> + step_at<WT>(q, s)) * 2);
                             g = In::template mul<Wt>(v, wg[i].operand(s, cg), g);
                             u = In::template mul<Wt>(v, wu[i].operand(s, cu), u);
                         }
                     }
                 });
         } else {
-            constexpr int U = 2;
+            constexpr int U = WT == SIM_TYPE_MX4 ? 2 : 4;
             typedef Weights<WT, EDGE> Wt;
             Wt wg[U], wu[U];
             Scales<WT, 2, U> sc[2];
@@ -334,7 +335,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                 (steps + U - 1) / U, wave,
                 [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
                 [&](int i, int run) {
-                    const int k0 = min(run * U + i, steps - 1) * kStep;
+                    const int k0 = min(run * U + i, steps - 1) * kCols<WT>;
                     wg[i].load(w13, row, D, k0, q);
                     wu[i].load(w13, row + F, D, k0, q);
                     xi[i].load(xr, D, k0, q);
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                     if (run * U + i < steps) {
                         const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
-                        for (int s = 0; s < 4; s++) {
+                        for (int s = 0; s < kIns<WT>; s++) {
                             g = In::template mul<Wt>(xi[i].raw[s], wg[i].operand(s, cg), g);
                             u = In::template mul<Wt>(xi[i].raw[s], wu[i].operand(s, cu), u);
                         }
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
                                                               int max_lists, int splits, float *__restrict__ parts,
                                                               typename Elem<T>::type *__restrict__ y, int64_t y_stride) {
     static_assert(R <= kFewWaves, "a wave for each row tile");
-    constexpr int U = 2;
+    constexpr int U = WT == SIM_TYPE_MX4 ? 2 : 4;
     __shared__ f32x4 part[kFewWaves][R][64];
     __shared__ int16_t s_slot[kFewExperts * 16], s_expert[kFewExperts];
     __shared__ int last;
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
         s_slot[i] = plan.slot[i];
         if (i < max_lists) s_expert[i] = plan.expert[i];
     }
-    const int steps = h_pitch / kStep, per = (steps + U - 1) / U, total = *plan.n_used * per;  // runs
+    const int steps = h_pitch / kCols<WT>, per = (steps + U - 1) / U, total = *plan.n_used * per;  // runs
     const int begin = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
     typedef Weights<WT, EDGE> Wt;
     Wt w[U][R];
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
             sc[p].load(s2, first + min(d0 + sc[p].tile() * 16 + r, D - 1), F, k0);
         },
         [&](int i, int) {
-            const int at = min(k0 * U + i, steps - 1) * kStep;
+            const int at = min(k0 * U + i, steps - 1) * kCols<WT>;
             h[i].load(h_hi, h_lo, hidden, some, at, q);
 #pragma unroll
             for (int j = 0; j < R; j++) w[i][j].load(w2, row[j], F, at, q);
@@ -434,7 +435,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
                 for (int j = 0; j < R; j++) {
                     const float c = sc[p].get(i, j, r, q);
 #pragma unroll
-                    for (int s = 0; s < 4; s++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s, c), acc[j]);
+                    for (int s = 0; s < kIns<WT>; s++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s, c), acc[j]);
                 }
         });
 #pragma unroll
@@ -500,83 +501,88 @@ __device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int
     return -1;
 }
 
-template <int T, int WT, int CT, bool EDGE>
+// 16 RP hidden units of one expert.
+template <int T, int WT, int RP, int CT, int U, bool EDGE>
 __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
-                                                        const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
-                                                        int E, int k, const int32_t *__restrict__ offsets,
-                                                        const int32_t *__restrict__ order, const float *__restrict__ weights,
-                                                        uint32_t tiles, __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo,
-                                                        int h_pitch) {
-    __shared__ f32x4 part[kWaves][2][CT][64];
+                                                           const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
+                                                           int E, int k, const int32_t *__restrict__ offsets,
+                                                           const int32_t *__restrict__ order,
+                                                           const float *__restrict__ weights, uint32_t tiles,
+                                                           __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo, int h_pitch) {
+    __shared__ f32x4 part[kWaves][2 * RP][CT][64];
+    typedef Weights<WT, EDGE> Wt;
+    typedef Inputs<T, WT, EDGE> In;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const int e = nth_expert(offsets, E, blockIdx.x / tiles);
     if (e < 0) return;
-    const int f0 = (int)(blockIdx.x % tiles) * 16;
+    const int f0 = (int)(blockIdx.x % tiles) * 16 * RP;
     const int first = offsets[e], n = offsets[e + 1] - first;
-    const int64_t row = (int64_t)e * 2 * F + min(f0 + r, F - 1);
-    constexpr int U = 2;
-    const int steps = (D + kStep - 1) / kStep;
+    // tiles 2 j are gates, 2 j + 1 ups
+    const auto row_of = [&](int j) { return (int64_t)e * 2 * F + min(f0 + (j >> 1) * 16 + r, F - 1) + (int64_t)(j & 1) * F; };
+    int64_t row[2 * RP];
+#pragma unroll
+    for (int j = 0; j < 2 * RP; j++) row[j] = row_of(j);
+    const int steps = (D + kCols<WT> - 1) / kCols<WT>;
     for (int c0 = 0; c0 < n; c0 += 16 * CT) {
         const uint16_t *xr[CT];
 #pragma unroll
         for (int c = 0; c < CT; c++) xr[c] = x + (int64_t)(order[first + min(c0 + c * 16 + r, n - 1)] / k) * x_stride;
-        typedef Weights<WT, EDGE> Wt;
-        typedef Inputs<T, WT, EDGE> In;
-        Wt wg[U], wu[U];
-        Scales<WT, 2, U> sc[2];
+        Wt w[U][2 * RP];
+        Scales<WT, 2 * RP, U> sc[2];
+        const int64_t scale_row = row_of(sc[0].tile());
         In xi[U][CT];
-        f32x4 g[CT], u[CT];
+        f32x4 acc[2 * RP][CT];
 #pragma unroll
-        for (int c = 0; c < CT; c++) g[c] = u[c] = f32x4{0};
+        for (int j = 0; j < 2 * RP; j++)
+#pragma unroll
+            for (int c = 0; c < CT; c++) acc[j][c] = f32x4{0};
         ring<U, kWaves>(
-            (steps + U - 1) / U, wave,
-            [&](int p, int run) { sc[p].load(s13, row + (int64_t)sc[p].tile() * F, D, run); },
+            (steps + U - 1) / U, wave, [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
             [&](int i, int run) {
-                const int k0 = min(run * U + i, steps - 1) * kStep;
-                wg[i].load(w13, row, D, k0, q);
-                wu[i].load(w13, row + F, D, k0, q);
+                const int k0 = min(run * U + i, steps - 1) * kCols<WT>;
+#pragma unroll
+                for (int j = 0; j < 2 * RP; j++) w[i][j].load(w13, row[j], D, k0, q);
 #pragma unroll
                 for (int c = 0; c < CT; c++) xi[i][c].load(xr[c], D, k0, q);
             },
             [&](int i, int p, int run) {
-                if (run * U + i < steps) {
-                    const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
+                if (run * U + i < steps)
 #pragma unroll
-                    for (int s = 0; s < 4; s++) {
-                        const typename Wt::Operand og = wg[i].operand(s, cg), ou = wu[i].operand(s, cu);
+                    for (int j = 0; j < 2 * RP; j++) {
+                        const float scale = sc[p].get(i, j, r, q);
 #pragma unroll
-                        for (int c = 0; c < CT; c++) {
-                            g[c] = In::template mul<Wt>(xi[i][c].raw[s], og, g[c]);
-                            u[c] = In::template mul<Wt>(xi[i][c].raw[s], ou, u[c]);
+                        for (int s = 0; s < kIns<WT>; s++) {
+                            const typename Wt::Operand o = w[i][j].operand(s, scale);
+#pragma unroll
+                            for (int c = 0; c < CT; c++) acc[j][c] = In::template mul<Wt>(xi[i][c].raw[s], o, acc[j][c]);
                         }
                     }
-                }
             });
 #pragma unroll
-        for (int c = 0; c < CT; c++) {
-            part[wave][0][c][lane] = g[c];
-            part[wave][1][c][lane] = u[c];
-        }
+        for (int j = 0; j < 2 * RP; j++)
+#pragma unroll
+            for (int c = 0; c < CT; c++) part[wave][j][c][lane] = acc[j][c];
         __syncthreads();
-        for (int c = wave; c < CT; c += kWaves) {
-            if (c0 + c * 16 + r < n) {
+        for (int p = wave; p < RP * CT; p += kWaves) {
+            const int j = p / CT, c = p % CT, f = f0 + j * 16;
+            if (c0 + c * 16 + r < n && f < F) {
                 f32x4 sg = {0}, su = {0};
 #pragma unroll
                 for (int w = 0; w < kWaves; w++) {
-                    sg += part[w][0][c][lane];
-                    su += part[w][1][c][lane];
+                    sg += part[w][2 * j][c][lane];
+                    su += part[w][2 * j + 1][c][lane];
                 }
                 const int slot = order[first + c0 + c * 16 + r];
                 const float weight = weights[slot];
                 float v[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = f0 + 4 * q + i < F ? gated(sg[i], su[i], weight) : 0.f;
-                const int64_t at = (int64_t)slot * h_pitch + f0 + 4 * q;
+                for (int i = 0; i < 4; i++) v[i] = f + 4 * q + i < F ? gated(sg[i], su[i], weight) : 0.f;
+                const int64_t at = (int64_t)slot * h_pitch + f + 4 * q;
                 store_hidden(h_hi, h_lo, at, v);
-                if (blockIdx.x % tiles == tiles - 1)
-                    for (int f = f0 + 16; f < h_pitch; f += 16) {
+                if (f + 16 >= F)  // the rest of the last step
+                    for (int o = 16; f + o < h_pitch; o += 16) {
                         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-                        store_hidden(h_hi, h_lo, at + f - f0, zero);
+                        store_hidden(h_hi, h_lo, at + o, zero);
                     }
             }
         }
@@ -584,7 +590,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__res
     }
 }
 
-template <int WT, int R, int CT, bool EDGE>
+template <int WT, int R, int CT, int U, bool EDGE>
 __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
                                                           int h_pitch, int F, const void *__restrict__ w2,
                                                           const uint8_t *__restrict__ s2, int D, int E,
@@ -597,12 +603,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
     if (e < 0) return;
     const int d0 = (int)(blockIdx.x % tiles) * 16 * R;
     const int first = offsets[e], n = offsets[e + 1] - first;
-    const int steps = h_pitch / kStep;
+    const int steps = h_pitch / kCols<WT>;
     for (int c0 = 0; c0 < n; c0 += 16 * CT) {
         int64_t at[CT];
 #pragma unroll
         for (int c = 0; c < CT; c++) at[c] = (int64_t)order[first + min(c0 + c * 16 + r, n - 1)] * h_pitch;
-        constexpr int U = CT == 1 || WT == SIM_TYPE_MX4 ? 2 : 1;
         typedef Weights<WT, EDGE> Wt;
         Wt w[U][R];
         Scales<WT, R, U> sc[2];
@@ -621,7 +626,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
                 sc[p].load(s2, (int64_t)e * D + min(d0 + sc[p].tile() * 16 + r, D - 1), F, run);
             },
             [&](int i, int run) {
-                const int k0 = min(run * U + i, steps - 1) * kStep;
+                const int k0 = min(run * U + i, steps - 1) * kCols<WT>;
 #pragma unroll
                 for (int j = 0; j < R; j++) w[i][j].load(w2, row[j], F, k0, q);
 #pragma unroll
@@ -633,7 +638,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
                     for (int j = 0; j < R; j++) {
                         const float scale = sc[p].get(i, j, r, q);
 #pragma unroll
-                        for (int s = 0; s < 4; s++) {
+                        for (int s = 0; s < kIns<WT>; s++) {
                             const typename Wt::Operand o = w[i][j].operand(s, scale);
 #pragma unroll
                             for (int c = 0; c < CT; c++) acc[j][c] = h[i][c].template mul<Wt>(s, o, acc[j][c]);
@@ -735,14 +740,16 @@ template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, c
     __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
     const sim_status s = launch_route(st, r, experts, weights, offsets, order, ws + at.route);
     if (s != SIM_OK) return s;
-    constexpr int R = 2;
+    constexpr bool M = WT == SIM_TYPE_MX4;
+    // rows that share the activations' loads, and how far ahead they are loaded
+    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : CT == 1 ? 4 : 2, R = 4, UD = 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
-    const uint32_t tf = (uint32_t)((a.F + 15) / 16), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
-    group_up<T, WT, CT, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
+    const uint32_t tf = (uint32_t)((a.F + 16 * RP - 1) / (16 * RP)), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
+    group_up<T, WT, RP, CT, UU, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
         (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
         at.pitch);
-    group_down<WT, R, CT, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2,
-                                                                                  (int)a.D, r.E, offsets, order, td, part);
+    group_down<WT, R, CT, UD, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, r.E,
+                                                                      offsets, order, td, part);
     layer_join<T><<<(uint32_t)(r.T * tj), 256, 0, st>>>(part, experts, r.k, a.D, (typename Elem<T>::type *)a.y, a.y_stride, tj);
     return SIM_OPS_LAUNCH_OK();
 }
