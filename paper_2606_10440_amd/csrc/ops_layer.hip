@@ -157,6 +157,7 @@ constexpr int kFewExperts = 256;
 constexpr int kFewWaves = 4;
 constexpr int kFewGroups = 768;  // workgroups: three on each of 256 compute units
 constexpr int kMaxSplits = 32;
+constexpr int kJoin = 12;     // parts of a split sum that are loaded together
 
 // What the first kernel leaves for the second.
 struct FewPlan {
@@ -465,9 +466,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
         if (!last) return;
         v = f32x4{0};
         if (mine)
-            for (int p = 0; p < splits; p++)
+            for (int p0 = 0; p0 < splits; p0 += kJoin) {  // so many under way at once
+                float part[kJoin][4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[i] += __hip_atomic_load(at(p, i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                for (int p = 0; p < kJoin; p++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        part[p][i] = __hip_atomic_load(at(min(p0 + p, splits - 1), i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int p = 0; p < kJoin; p++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) v[i] += p0 + p < splits ? part[p][i] : 0.f;
+            }
     }
     if (mine)
 #pragma unroll
