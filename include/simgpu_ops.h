@@ -81,6 +81,18 @@ sim_status sim_mx4_linear(void *hip_stream, const void *x, int32_t x_type, int64
                           const uint8_t *w_scales, int64_t M, int64_t N, int64_t K, void *out, int32_t type,
                           int64_t row_stride, void *workspace, size_t workspace_bytes);
 
+/*
+ * Gradients of that layer, Y = X W^T, where rounding to 4 bits passes
+ * gradients through: dX = dY W and dW = dY^T X, each of the four operands put
+ * into 4 bits along the axis that is summed over.  dY [M, N], X [M, K], W
+ * [N, K], dX and dW of one type, with row strides; dX or dW may be NULL (not
+ * wanted).  workspace: sim_mx4_linear_grad_workspace bytes, 16-byte aligned.
+ */
+size_t sim_mx4_linear_grad_workspace(int64_t M, int64_t N, int64_t K);
+sim_status sim_mx4_linear_grad(void *hip_stream, int32_t type, const void *dy, int64_t dy_stride, const void *x,
+                               int64_t x_stride, const void *w, int64_t w_stride, int64_t M, int64_t N, int64_t K, void *dx,
+                               int64_t dx_stride, void *dw, int64_t dw_stride, void *workspace, size_t workspace_bytes);
+
 #define SIM_MOE_MAX_EXPERTS 1024
 #define SIM_MOE_MAX_TOPK 32
 #define SIM_MOE_LAYER_MAX_TOKENS 1024

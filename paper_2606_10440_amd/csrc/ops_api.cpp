@@ -144,6 +144,56 @@ sim_status sim_mx4_linear(void *stream, const void *x, int32_t x_type, int64_t x
     return done(launch_matmul((hipStream_t)stream, codes, scales, w_codes, w_scales, M, N, K, out, type, row_stride), __func__);
 }
 
+// Codes and scales of an R x C operand, one after the other.
+static size_t operand_bytes(int64_t R, int64_t C) {
+    return (size_t)(R * sim_mx4_code_pitch(C) + (R * sim_mx4_scale_pitch(C) + 15) / 16 * 16);
+}
+
+size_t sim_mx4_linear_grad_workspace(int64_t M, int64_t N, int64_t K) {
+    if (M <= 0 || N <= 0 || K <= 0 || M >= kMaxDim || N >= kMaxDim || K >= kMaxDim) return 0;
+    return operand_bytes(M, N) + operand_bytes(K, N) + operand_bytes(N, M) + operand_bytes(K, M);
+}
+
+sim_status sim_mx4_linear_grad(void *stream, int32_t type, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                               const void *w, int64_t w_stride, int64_t M, int64_t N, int64_t K, void *dx, int64_t dx_stride,
+                               void *dw, int64_t dw_stride, void *workspace, size_t workspace_bytes) {
+    NEED(is_float(type), "dy, x and w must be f32, f16 or bf16");
+    NEED(M >= 0 && N >= 0 && K >= 0, "negative size");
+    FITS(dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(K, M) && dims_ok(N, K) && dims_ok(K, N), "matrix too large");
+    const bool want_x = dx && M > 0 && K > 0, want_w = dw && N > 0 && K > 0;
+    if (!want_x && !want_w) return done(SIM_OK, __func__);
+    const size_t s = size_of(type);
+    const bool sum_n = N > 0, sum_m = M > 0;  // an empty sum gives zeros
+    NEED((!sum_n || !sum_m || dy) && (!(want_x && sum_n) || w) && (!(want_w && sum_m) || x), "null array");
+    NEED((M <= 1 || dy_stride >= N) && (M <= 1 || x_stride >= K) && (N <= 1 || w_stride >= K), "row stride below the row length");
+    NEED((!want_x || M == 1 || dx_stride >= K) && (!want_w || N == 1 || dw_stride >= K), "row stride below the row length");
+    NEED(aligned_to(dy, s) && aligned_to(x, s) && aligned_to(w, s) && aligned_to(dx, s) && aligned_to(dw, s),
+         "array not aligned to its type");
+    const size_t need = sim_mx4_linear_grad_workspace(M, N, K);
+    NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
+    uint8_t *at = (uint8_t *)workspace;
+    QuantizeJob job[kMaxJobs];
+    int n = 0;
+    // the operand of R rows whose blocks lie along C; x is C x R where it is transposed
+    const auto operand = [&](const void *from, int64_t R, int64_t C, int64_t stride, bool transpose) {
+        QuantizeJob &j = job[n++];
+        j = QuantizeJob{from, transpose ? C : R, transpose ? R : C, stride, transpose, at, at + R * sim_mx4_code_pitch(C)};
+        at += operand_bytes(R, C);
+        return &j;
+    };
+    const QuantizeJob *dy_n = nullptr, *w_n = nullptr, *dy_m = nullptr, *x_m = nullptr;
+    if (want_x && sum_n) dy_n = operand(dy, M, N, dy_stride, false), w_n = operand(w, K, N, w_stride, true);
+    if (want_w && sum_m) dy_m = operand(dy, N, M, dy_stride, true), x_m = operand(x, K, M, x_stride, true);
+    sim_status st = n ? launch_quantize_jobs((hipStream_t)stream, type, job, n) : SIM_OK;
+    if (st == SIM_OK && want_x)
+        st = dy_n ? launch_matmul((hipStream_t)stream, dy_n->codes, dy_n->scales, w_n->codes, w_n->scales, M, K, N, dx, type, dx_stride)
+                  : launch_matmul((hipStream_t)stream, nullptr, nullptr, nullptr, nullptr, M, K, 0, dx, type, dx_stride);
+    if (st == SIM_OK && want_w)
+        st = dy_m ? launch_matmul((hipStream_t)stream, dy_m->codes, dy_m->scales, x_m->codes, x_m->scales, N, K, M, dw, type, dw_stride)
+                  : launch_matmul((hipStream_t)stream, nullptr, nullptr, nullptr, nullptr, N, K, 0, dw, type, dw_stride);
+    return done(st, __func__);
+}
+
 size_t sim_moe_route_workspace(int64_t T, int32_t E, int32_t k) { return T > 0 && E > 0 ? route_workspace(T, E, k) : 0; }
 
 sim_status sim_moe_route(void *stream, const void *logits, int32_t type, int64_t T, int32_t E, int64_t logit_stride,

@@ -90,6 +90,14 @@ __device__ inline uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffff
 // ---- launchers (arguments already checked)
 sim_status launch_quantize(hipStream_t st, const void *x, int type, int64_t rows, int64_t cols, int64_t stride,
                            bool transpose, uint8_t *codes, uint8_t *scales);
+struct QuantizeJob {
+    const void *x;
+    int64_t rows, cols, stride;  // of x
+    bool transpose;
+    uint8_t *codes, *scales;
+};
+constexpr int kMaxJobs = 4;
+sim_status launch_quantize_jobs(hipStream_t st, int type, const QuantizeJob *job, int n);
 sim_status launch_dequantize(hipStream_t st, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols,
                              void *out, int type, int64_t stride);
 sim_status launch_matmul(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs,

@@ -10,11 +10,11 @@ namespace {
 // lanes a group of 256 columns; a half wave takes U groups at a time, so that
 // U loads are under way before the first is used.
 template <int T, bool WIDE, int U>
-__global__ __launch_bounds__(256) void quantize_rows(const typename Elem<T>::type *__restrict__ x, int64_t cols,
-                                                     int64_t stride, int64_t n_groups, uint32_t per_row,
-                                                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+__device__ inline void rows_block(uint32_t block, const typename Elem<T>::type *__restrict__ x, int64_t cols, int64_t stride,
+                                  int64_t n_groups, uint32_t per_row, uint8_t *__restrict__ codes,
+                                  uint8_t *__restrict__ scales) {
     const int lane = threadIdx.x & 31;
-    const int64_t g0 = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * U;
+    const int64_t g0 = ((int64_t)block * 8 + (threadIdx.x >> 5)) * U;
     float v[U][8];
 #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -35,24 +35,33 @@ __global__ __launch_bounds__(256) void quantize_rows(const typename Elem<T>::typ
     }
 }
 
+template <int T, bool WIDE, int U>
+__global__ __launch_bounds__(256) void quantize_rows(const typename Elem<T>::type *__restrict__ x, int64_t cols,
+                                                     int64_t stride, int64_t n_groups, uint32_t per_row,
+                                                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    rows_block<T, WIDE, U>(blockIdx.x, x, cols, stride, n_groups, per_row, codes, scales);
+}
+
 // Blocks along the rows of x: the result's row c is column c of x.  A
 // workgroup takes 256 rows and, of each, 256 bytes; a lane holds 32 rows (one
 // block) of eight bytes, all of them loaded before the first is used, and
 // the codes go through LDS so that a result row is written 128 bytes at a
 // time.
+// A type of two bytes for every T, so that code for those that have them compiles.
+template <int T> using E16 = std::conditional_t<T == SIM_TYPE_F32, _Float16, typename Elem<T>::type>;
+template <int T> constexpr int kTileCols = 256 / sizeof(typename Elem<T>::type);
 template <int T>
-__global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::type *__restrict__ x, int64_t rows,
-                                                     int64_t cols, int64_t stride, int64_t row_groups,
-                                                     uint32_t col_tiles, uint8_t *__restrict__ codes,
-                                                     uint8_t *__restrict__ scales) {
+__device__ inline void cols_block(uint32_t block, const typename Elem<T>::type *__restrict__ x, int64_t rows, int64_t cols,
+                                  int64_t stride, int64_t row_groups, uint32_t col_tiles, uint8_t *__restrict__ codes,
+                                  uint8_t *__restrict__ scales) {
     typedef typename Elem<T>::type E;
     typedef u32x2 __attribute__((aligned(2))) u32x2_any;
-    constexpr int VC = 8 / sizeof(E), COLS = 32 * VC, PITCH = kGroupCodes + 16;
+    constexpr int VC = 8 / sizeof(E), COLS = kTileCols<T>, PITCH = kGroupCodes + 16;
     __shared__ __align__(16) uint8_t tile[COLS * PITCH];
     __shared__ __align__(8) uint8_t stile[COLS * kGroupScales];
     const int part = threadIdx.x & 31, blk = threadIdx.x >> 5;  // columns part VC .., rows blk 32 ..
-    const int64_t g = blockIdx.x / col_tiles;                   // group of 256 rows
-    const int64_t c0 = (int64_t)(blockIdx.x % col_tiles) * COLS, c = c0 + part * VC;
+    const int64_t g = block / col_tiles;                       // group of 256 rows
+    const int64_t c0 = (int64_t)(block % col_tiles) * COLS, c = c0 + part * VC;
     const int64_t r0 = g * 256 + blk * 32;
     E v[32][VC];
     const E *p = x + r0 * stride + c;
@@ -65,11 +74,31 @@ __global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::typ
 #pragma unroll
             for (int j = 0; j < VC; j++) v[i][j] = r0 + i < rows && c + j < cols ? p[i * stride + j] : Elem<T>::put(0.f);
     }
+    // magnitudes of 16-bit values order as whole numbers too: two columns at once
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    uint32_t top[VC];
+    if (sizeof(E) == 2) {
+        u16x2 m[VC / 2];
+#pragma unroll
+        for (int j = 0; j < VC / 2; j++) {
+            m[j] = u16x2{0, 0};
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                m[j] = __builtin_elementwise_max(m[j], __builtin_bit_cast(u16x2, ((const uint32_t *)v[i])[j] & 0x7fff7fffu));
+            top[2 * j] = mag((float)__builtin_bit_cast(E16<T>, (uint16_t)m[j][0]));
+            top[2 * j + 1] = mag((float)__builtin_bit_cast(E16<T>, (uint16_t)m[j][1]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < VC; j++) {
+            top[j] = 0;
+#pragma unroll
+            for (int i = 0; i < 32; i++) top[j] = max(top[j], mag(Elem<T>::get(v[i][j])));
+        }
+    }
 #pragma unroll
     for (int j = 0; j < VC; j++) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 32; i++) m = max(m, mag(Elem<T>::get(v[i][j])));
+        const uint32_t m = top[j];
         const uint32_t sb = scale_byte(m);
         const float s = scale_value(sb);
         u32x4 out;
@@ -95,6 +124,52 @@ __global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::typ
     if (threadIdx.x < COLS && c0 + threadIdx.x < cols)
         *(u32x2 *)(scales + ((c0 + threadIdx.x) * row_groups + g) * kGroupScales) =
             *(const u32x2 *)(stile + threadIdx.x * kGroupScales);
+}
+
+template <int T>
+__global__ __launch_bounds__(256) void quantize_cols(const typename Elem<T>::type *__restrict__ x, int64_t rows, int64_t cols,
+                                                     int64_t stride, int64_t row_groups, uint32_t col_tiles,
+                                                     uint8_t *__restrict__ codes, uint8_t *__restrict__ scales) {
+    cols_block<T>(blockIdx.x, x, rows, cols, stride, row_groups, col_tiles, codes, scales);
+}
+
+// Several matrices of one type in one launch, each along its rows or its
+// columns: one that is wanted both ways is read from memory once.
+struct Jobs {
+    QuantizeJob job[kMaxJobs];
+    uint32_t end[kMaxJobs];  // blocks of the jobs up to this one
+};
+constexpr int kJobUnroll = 4;
+
+template <int T> __global__ __launch_bounds__(256) void quantize_jobs(Jobs jobs) {
+    int i = 0;
+    while (blockIdx.x >= jobs.end[i]) i++;
+    const QuantizeJob &j = jobs.job[i];
+    const uint32_t block = blockIdx.x - (i ? jobs.end[i - 1] : 0);
+    const typename Elem<T>::type *x = (const typename Elem<T>::type *)j.x;
+    if (j.transpose) {
+        cols_block<T>(block, x, j.rows, j.cols, j.stride, groups_of(j.rows), (uint32_t)((j.cols + kTileCols<T> - 1) / kTileCols<T>),
+                      j.codes, j.scales);
+    } else {
+        const int64_t per = groups_of(j.cols);
+        rows_block<T, false, kJobUnroll>(block, x, j.cols, j.stride, j.rows * per, (uint32_t)per, j.codes, j.scales);
+    }
+}
+
+template <int T> sim_status jobs_t(hipStream_t st, const QuantizeJob *job, int n) {
+    Jobs jobs = {};
+    uint32_t blocks = 0;
+    for (int i = 0; i < kMaxJobs; i++) {
+        if (i < n) {
+            const QuantizeJob &j = job[i];
+            jobs.job[i] = j;
+            blocks += j.transpose ? (uint32_t)(groups_of(j.rows) * ((j.cols + kTileCols<T> - 1) / kTileCols<T>))
+                                  : (uint32_t)((j.rows * groups_of(j.cols) + 8 * kJobUnroll - 1) / (8 * kJobUnroll));
+        }
+        jobs.end[i] = blocks;
+    }
+    quantize_jobs<T><<<blocks, 256, 0, st>>>(jobs);
+    return SIM_OPS_LAUNCH_OK();
 }
 
 // Back: a lane takes eight codes.  Their products with the scale are exact in
@@ -150,7 +225,7 @@ sim_status quantize_t(hipStream_t st, const void *xv, int64_t rows, int64_t cols
     const E *x = (const E *)xv;
     if (transpose) {
         const int64_t rg = groups_of(rows);
-        constexpr int COLS = 256 / sizeof(E);
+        constexpr int COLS = kTileCols<T>;
         const uint32_t ct = (uint32_t)((cols + COLS - 1) / COLS);
         quantize_cols<T><<<(uint32_t)(ct * rg), 256, 0, st>>>(x, rows, cols, stride, rg, ct, codes, scales);
         return SIM_OPS_LAUNCH_OK();
@@ -196,6 +271,12 @@ sim_status launch_quantize(hipStream_t st, const void *x, int type, int64_t rows
     if (type == SIM_TYPE_F32) return quantize_t<SIM_TYPE_F32>(st, x, rows, cols, stride, transpose, codes, scales);
     if (type == SIM_TYPE_F16) return quantize_t<SIM_TYPE_F16>(st, x, rows, cols, stride, transpose, codes, scales);
     return quantize_t<SIM_TYPE_BF16>(st, x, rows, cols, stride, transpose, codes, scales);
+}
+
+sim_status launch_quantize_jobs(hipStream_t st, int type, const QuantizeJob *job, int n) {
+    if (type == SIM_TYPE_F32) return jobs_t<SIM_TYPE_F32>(st, job, n);
+    if (type == SIM_TYPE_F16) return jobs_t<SIM_TYPE_F16>(st, job, n);
+    return jobs_t<SIM_TYPE_BF16>(st, job, n);
 }
 
 sim_status launch_dequantize(hipStream_t st, const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t cols,

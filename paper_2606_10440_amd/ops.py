@@ -23,7 +23,7 @@ from .sim import SIM_ERR_INVALID_ARG, SIM_OK, SimError
 
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
            "sim_mx4_matmul_workspace", "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
-           "sim_moe_route_workspace", "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer_workspace",
+           "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer_workspace",
            "sim_moe_layer", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
@@ -47,6 +47,9 @@ def lib():
         L.sim_mx4_matmul_workspace.restype = L.sim_mx4_linear_workspace.restype = sz
         L.sim_mx4_matmul.argtypes = [P, P, P, P, P, i64, i64, i64, P, i32, i64, P, sz]
         L.sim_mx4_linear.argtypes = [P, P, i32, i64, P, P, i64, i64, i64, P, i32, i64, P, sz]
+        L.sim_mx4_linear_grad_workspace.argtypes = [i64, i64, i64]
+        L.sim_mx4_linear_grad_workspace.restype = sz
+        L.sim_mx4_linear_grad.argtypes = [P, i32, P, i64, P, i64, P, i64, i64, i64, i64, P, i64, P, i64, P, sz]
         L.sim_moe_route_workspace.argtypes = [i64, i32, i32]
         L.sim_moe_route_workspace.restype = sz
         L.sim_moe_route.argtypes = [P, P, i32, i64, i32, i64, P, i64, i32, i32, P, P, P, P, P, sz]
@@ -55,8 +58,8 @@ def lib():
         L.sim_moe_layer_workspace.restype = sz
         L.sim_moe_layer.argtypes = [P, P, i32, i64, i64, i64, P, i32, i32, i64, P, i64, i32, i32, P, P, P, P, i32,
                                     i64, P, i64, P, sz]
-        for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_moe_route",
-                     "sim_moe_route_grad", "sim_moe_layer"):
+        for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_mx4_linear_grad",
+                     "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer"):
             getattr(L, name).restype = C.c_int
         L.sim_ops_last_error.argtypes = []
         L.sim_ops_last_error.restype = C.c_char_p
@@ -184,14 +187,21 @@ def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
     return out
 
 
-def mx4_linear_grad(dy, x, w):
+def mx4_linear_grad(dy, x, w, need=(True, True)):
     """Gradients ``(dx, dw)`` of ``y = x @ w.T`` computed in 4 bits, where
     rounding to 4 bits passes gradients through: ``dx = dy @ w`` and ``dw =
-    dy.T @ x``, each operand quantised along the axis that is summed over."""
-    (_, M, N, _, d0), (_, xm, K, _, d1), (_, wn, wk, _, d2) = _rows(dy, "dy"), _rows(x, "x"), _rows(w, "w")
-    _need(M == xm and N == wn and K == wk and d0 == d1 == d2, "dy, x and w do not fit together")
-    dx = mx4_matmul(dy, mx4_quantize(w, transpose=True), dtype=x.dtype)
-    dw = mx4_matmul(mx4_quantize(dy, transpose=True), mx4_quantize(x, transpose=True), dtype=w.dtype)
+    dy.T @ x``, each operand quantised along the axis that is summed over.
+    All of one type.  ``need``: which of the two to compute (None where not)."""
+    (t, M, N, ys, dev), (tx, xm, K, xs, d1), (tw, wn, wk, ws, d2) = _rows(dy, "dy"), _rows(x, "x"), _rows(w, "w")
+    _need(M == xm and N == wn and K == wk and dev == d1 == d2, "dy, x and w do not fit together")
+    _need(t == tx == tw, "dy, x and w must have one type")
+    dx = x.new_empty((M, K)) if need[0] else None
+    dw = x.new_empty((N, K)) if need[1] else None
+    L = lib()
+    n = L.sim_mx4_linear_grad_workspace(M, N, K)
+    space = x.new_empty(n, dtype=torch.uint8) if n else None
+    _call(dev, L.sim_mx4_linear_grad, t, dy.data_ptr(), ys, x.data_ptr(), xs, w.data_ptr(), ws, M, N, K,
+          dx.data_ptr() if need[0] else None, K, dw.data_ptr() if need[1] else None, K, space.data_ptr() if n else None, n)
     return dx, dw
 
 
@@ -203,7 +213,7 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        return mx4_linear_grad(dy.contiguous(), *ctx.saved_tensors)
+        return mx4_linear_grad(dy.contiguous(), *ctx.saved_tensors, need=ctx.needs_input_grad)
 
 
 def mx4_linear(x, w):

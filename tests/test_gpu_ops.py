@@ -201,6 +201,23 @@ def test_linear_gradient(ops, mnk, kind):
     assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw)
 
 
+def test_linear_gradient_one_of_two_and_strides(ops):
+    M, N, K = 70, 90, 130
+    x, vx = rand(13, (M, K), "bf16", pad=3)
+    w, vw = rand(14, (N, K), "bf16", scale=K ** -0.5, pad=6)
+    dy, vdy = rand(15, (M, N), "bf16", pad=1)
+    both = ops.mx4_linear_grad(dy, x, w)
+    check(both[0], *ref.product(ref.mx4_values(vdy), ref.mx4_values(vw.T), "bf16"))
+    check(both[1], *ref.product(ref.mx4_values(vdy.T), ref.mx4_values(vx.T), "bf16"))
+    dx, none = ops.mx4_linear_grad(dy, x, w, need=(True, False))
+    assert none is None and torch.equal(dx, both[0])
+    none, dw = ops.mx4_linear_grad(dy, x, w, need=(False, True))
+    assert none is None and torch.equal(dw, both[1])
+    e = torch.empty(0, N, dtype=torch.bfloat16, device="cuda")
+    dx, dw = ops.mx4_linear_grad(e, torch.empty(0, K, dtype=torch.bfloat16, device="cuda"), w)
+    assert dx.shape == (0, K) and (dw == 0).all() and dw.shape == (N, K)
+
+
 def test_linear_gradient_against_differences(ops):
     # values that 4 bits hold exactly along either axis: then the layer is bilinear and differences are its gradient
     rng = np.random.default_rng(16)

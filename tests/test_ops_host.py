@@ -93,6 +93,19 @@ def test_linear_refusals(lib, change, want):
     assert run(lib, "sim_mx4_linear", LINEAR, **change) == want
 
 
+LGRAD = [("type", 2), ("dy", P), ("dy_stride", 8), ("x", P), ("x_stride", 64), ("w", P), ("w_stride", 64), ("M", 4), ("N", 8),
+         ("K", 64), ("dx", P), ("dx_stride", 64), ("dw", P), ("dw_stride", 64), ("ws", P), ("ws_bytes", 1 << 30)]
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(type=3), INVALID), (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(M=-1), INVALID),
+    (dict(dy_stride=7), INVALID), (dict(x_stride=63), INVALID), (dict(w_stride=63), INVALID), (dict(dx_stride=63), INVALID),
+    (dict(dw_stride=63), INVALID), (dict(dx=P + 1), INVALID), (dict(ws=None), INVALID), (dict(ws_bytes=64), INVALID),
+    (dict(N=1 << 31, dy_stride=1 << 31), SIZE), (dict(dx=None, dw=None), 0), (dict(K=0), 0)])
+def test_linear_gradient_refusals(lib, change, want):
+    assert run(lib, "sim_mx4_linear_grad", LGRAD, **change) == want
+
+
 ROUTE = [("logits", P), ("type", 0), ("T", 100), ("E", 16), ("stride", 16), ("mask", None), ("mask_stride", 0), ("k", 2),
          ("renorm", 1), ("experts", P), ("weights", P), ("offsets", P), ("order", P), ("ws", P), ("ws_bytes", 1 << 20)]
 ROUTE_BAD = [(dict(logits=None), INVALID), (dict(type=3), INVALID), (dict(T=-1), INVALID), (dict(E=0), INVALID),
