@@ -9,9 +9,10 @@
 // A wave keeps a ring of U steps' operands in registers and refills a place
 // as soon as it has been multiplied, weights and activations alike, since
 // loads return in the order in which they were issued.  Activations and 4-bit
-// weights enter as bf16; values of more than 8 significant bits (fp16, the
-// hidden values between the products) enter as the sum of two bf16 parts,
-// which is free where the weights' bytes bound the time.
+// weights enter as bf16; the hidden values between the products, and fp16
+// where the other operand is bf16, enter as the sum of two bf16 parts: the
+// range of the hidden values needs that of bf16, and the second instruction
+// is free where the weights' bytes bound the time.
 #include "ops_route_keys.h"
 #include "ops_stream.h"
 
@@ -70,10 +71,12 @@ template <int WT, bool EDGE> struct Weights {
         for (int s = 0; s < 2; s++) raw[s] = load_row8<EDGE>((const uint16_t *)base + row * K, k0 + step_at<WT>(q, s), K);
     }
     struct Operand {
+        u32x4 raw;
         bf16x8 hi, lo;
     };
     __device__ Operand operand(int s, float) const {
         Operand o;
+        o.raw = raw[s];
         if (WT == SIM_TYPE_F16) split_f16(raw[s], o.hi, o.lo);
         else o.hi = __builtin_bit_cast(bf16x8, raw[s]);
         return o;
@@ -103,6 +106,8 @@ template <int T, int WT, bool EDGE> struct Inputs {
         for (int s = 0; s < kIns<WT>; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
     }
     template <typename W> static __device__ f32x4 mul(u32x4 v, const typename W::Operand &w, f32x4 c) {
+        if constexpr (T == SIM_TYPE_F16 && WT == SIM_TYPE_F16)  // as they are
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w.raw), __builtin_bit_cast(f16x8, v), c, 0, 0, 0);
         if (T == SIM_TYPE_BF16) return W::mul(w, __builtin_bit_cast(bf16x8, v), c);
         bf16x8 hi, lo;
         split_f16(v, hi, lo);
@@ -156,8 +161,8 @@ constexpr int kFewTokens = 16;
 constexpr int kFewExperts = 256;
 constexpr int kFewWaves = 4;
 constexpr int kFewGroups = 768;  // workgroups: three on each of 256 compute units
-constexpr int kMaxSplits = 32;
-constexpr int kJoin = 12;     // parts of a split sum that are loaded together
+constexpr int kMaxSplits = 16;
+constexpr int kJoin = 16;     // parts of a split sum that are loaded together
 
 // What the first kernel leaves for the second.
 struct FewPlan {
@@ -261,6 +266,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                                                             FewPlan plan, int down_tiles) {
     __shared__ __align__(16) FewRoute rt;
     __shared__ f32x4 part[2][kFewWaves][2][64];
+    __shared__ int s_token[16];  // of the inputs in LDS
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const int used = few_route(route, rt);
     if (blockIdx.x == 0) {
@@ -286,12 +292,21 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
             held = e;
             in_lds = !EDGE && __popc(tokens) * pitch <= kFewInputs;
             if (in_lds) {
+                if (wave == 0 && has && q == 0) s_token[__popc(tokens & ((1u << r) - 1))] = r;
                 __syncthreads();
-                uint32_t left = tokens;
-                for (int n = 0; left; n++, left &= left - 1) {
-                    const uint16_t *from = x + (int64_t)(__ffs(left) - 1) * x_stride;
-                    for (int c = threadIdx.x; c < D / 8; c += 64 * kFewWaves)
-                        *(u32x4 *)(rt.inputs + n * pitch + c * 16) = *(const u32x4_a2 *)(from + c * 8);
+                const int pieces = D / 8, all = __popc(tokens) * pieces;
+                for (int c0 = threadIdx.x; c0 < all; c0 += 4 * 64 * kFewWaves) {  // four loads under way
+                    u32x4 v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int c = min(c0 + i * 64 * kFewWaves, all - 1), n = c / pieces;
+                        v[i] = *(const u32x4_a2 *)(x + (int64_t)s_token[n] * x_stride + (c - n * pieces) * 8);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int c = c0 + i * 64 * kFewWaves, n = c / pieces;
+                        if (c < all) *(u32x4 *)(rt.inputs + n * pitch + (c - n * pieces) * 16) = v[i];
+                    }
                 }
                 __syncthreads();
             }
@@ -379,6 +394,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
     }
 }
 
+template <int WT> constexpr int few_down_run = WT == SIM_TYPE_MX4 ? 2 : 4;  // steps
+
 // 16 R output columns of all tokens; the steps of all used experts are one
 // list, dealt to the splits and their waves.
 template <int T, int WT, int R, bool EDGE>
@@ -388,7 +405,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
                                                               int max_lists, int splits, float *__restrict__ parts,
                                                               typename Elem<T>::type *__restrict__ y, int64_t y_stride) {
     static_assert(R <= kFewWaves, "a wave for each row tile");
-    constexpr int U = WT == SIM_TYPE_MX4 ? 2 : 4;
+    constexpr int U = few_down_run<WT>;
     __shared__ f32x4 part[kFewWaves][R][64];
     __shared__ int16_t s_slot[kFewExperts * 16], s_expert[kFewExperts];
     __shared__ int last;
@@ -735,7 +752,11 @@ template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const Layer
     const int tf = (int)((a.F + 15) / 16), td = (int)((a.D + 16 * R - 1) / (16 * R));
     few_up<T, WT, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
         r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
-    const int splits = std::max(1, std::min(kMaxSplits, kFewGroups / td));
+    // as many parts as workgroups fit, but a run for every wave: joining costs
+    // a part about half a microsecond (one token, 11 experts of 1024 x 2869:
+    // 25 us in 24 parts, 20 us in 15)
+    const int64_t runs = lists * ((at.pitch / kCols<WT> + few_down_run<WT> - 1) / few_down_run<WT>);
+    const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMaxSplits, kFewGroups / td), runs / kFewWaves));
     few_down<T, WT, R, EDGE><<<td * splits, 64 * kFewWaves, 0, st>>>(
         hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, (int)lists, splits, (float *)(ws + at.part),
         (typename Elem<T>::type *)a.y, a.y_stride);
@@ -751,8 +772,8 @@ template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, c
     const sim_status s = launch_route(st, r, experts, weights, offsets, order, ws + at.route);
     if (s != SIM_OK) return s;
     constexpr bool M = WT == SIM_TYPE_MX4;
-    // rows that share the activations' loads, and how far ahead they are loaded
-    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : CT == 1 ? 4 : 2, R = 4, UD = 2;
+    // rows that share the activations' loads, and how far ahead all are loaded
+    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : 4 / CT, R = 4, UD = 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
     const uint32_t tf = (uint32_t)((a.F + 16 * RP - 1) / (16 * RP)), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
     group_up<T, WT, RP, CT, UU, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
@@ -777,7 +798,8 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
     }
     const bool edge = a.D % kStep || a.F % kStep;
     if (few(r.T, r.E)) return edge ? few_t<T, WT, true>(st, a, ws) : few_t<T, WT, false>(st, a, ws);
-    // columns by the tokens of an average expert
+    // columns by the tokens of an average expert (sixteen lists of 19: 397 us
+    // with two column tiles, 482 with one; four are no faster than two at 80)
     const int64_t mean = r.T * r.k / r.E;
     if (mean <= 10) return edge ? group_t<T, WT, 1, true>(st, a, ws) : group_t<T, WT, 1, false>(st, a, ws);
     return edge ? group_t<T, WT, 2, true>(st, a, ws) : group_t<T, WT, 2, false>(st, a, ws);
