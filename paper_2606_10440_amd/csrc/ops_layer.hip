@@ -773,7 +773,7 @@ template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, c
     if (s != SIM_OK) return s;
     constexpr bool M = WT == SIM_TYPE_MX4;
     // rows that share the activations' loads, and how far ahead all are loaded
-    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : 4 / CT, R = 4, UD = 2;
+    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : 4 / CT, R = 4, UD = CT == 4 ? 1 : 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
     const uint32_t tf = (uint32_t)((a.F + 16 * RP - 1) / (16 * RP)), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
     group_up<T, WT, RP, CT, UU, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
@@ -798,10 +798,14 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
     }
     const bool edge = a.D % kStep || a.F % kStep;
     if (few(r.T, r.E)) return edge ? few_t<T, WT, true>(st, a, ws) : few_t<T, WT, false>(st, a, ws);
-    // columns by the tokens of an average expert (sixteen lists of 19: 397 us
-    // with two column tiles, 482 with one; four are no faster than two at 80)
+    // columns by the tokens of an average expert (lists of 19 of 150 tokens,
+    // 4096 x 4096 bf16: 397 us with two column tiles, 482 with one; lists of
+    // 98, 2048 x 2710: 137 us with four, 214 with two; 4-bit weights, whose
+    // activations take twice the registers, gain nothing from four)
     const int64_t mean = r.T * r.k / r.E;
     if (mean <= 10) return edge ? group_t<T, WT, 1, true>(st, a, ws) : group_t<T, WT, 1, false>(st, a, ws);
+    if constexpr (WT != SIM_TYPE_MX4)
+        if (mean > 24) return edge ? group_t<T, WT, 4, true>(st, a, ws) : group_t<T, WT, 4, false>(st, a, ws);
     return edge ? group_t<T, WT, 2, true>(st, a, ws) : group_t<T, WT, 2, false>(st, a, ws);
 }
 
