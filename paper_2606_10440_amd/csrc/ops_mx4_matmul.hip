@@ -276,17 +276,18 @@ void launch_tile(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uin
 // block l / 16 of 128 columns.  The rows of A lie in LDS, where they are put
 // into 4 bits first if they are not (XT).
 constexpr int kSkinnyRows = 32;
-constexpr int kSkinnyLds = 49152;  // bytes of A
+constexpr int kSkinnyLds[2] = {49152, 147456};  // bytes of A: three workgroups on a compute unit, or one
 constexpr int kSkinnyWaves = 8;
-constexpr int64_t kOwnQuantize = 32768;  // elements
+constexpr int64_t kOwnQuantize = 16384;  // elements
 
-template <int T, int XT, int R, int MT>
+template <int T, int XT, int R, int MT, int LDS>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *__restrict__ x, const uint8_t *__restrict__ xs,
                                                                    int64_t x_stride, const uint8_t *__restrict__ bc,
                                                                    const uint8_t *__restrict__ bs, int M, int64_t N, int K,
                                                                    typename Elem<T>::type *__restrict__ out, int64_t stride) {
     constexpr int U = 4, W = kSkinnyWaves;
-    extern __shared__ __align__(16) uint8_t lds[];
+    __shared__ __align__(16) uint8_t lds[LDS];
+    static_assert(W * R * MT * 1024 <= LDS, "the parts of the sum fit");
     const int groups = (int)groups_of(K), pitch = groups * kGroupCodes + 16, scale_pitch = groups * kGroupScales;
     uint8_t *codes = lds, *scales = lds + M * pitch;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
@@ -305,20 +306,47 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *_
     const int steps = groups * 2;
     bool ready = false;
     const auto prepare = [&] {  // A to LDS, while the first rows of B are on their way
-        for (int i = threadIdx.x; i < M * groups * 32; i += 64 * W) {
-            const int m = i / (groups * 32), at = i % (groups * 32);  // eight columns each
-            if (XT == SIM_TYPE_MX4) {
-                if ((at & 3) == 0) {
-                    const int64_t g = (int64_t)m * groups * 32 + at;
-                    *(u32x4 *)(codes + m * pitch + at * 4) = *(const u32x4 *)((const uint8_t *)x + g * 4);
-                    scales[m * scale_pitch + at / 4] = xs[g / 4];
+        constexpr int AHEAD = XT == SIM_TYPE_MX4 ? 4 : 2;  // loads under way
+        if (XT == SIM_TYPE_MX4) {
+            const int pieces = M * groups * 8;  // of sixteen bytes of codes, and as many bytes of scales
+            for (int i0 = threadIdx.x; i0 < pieces; i0 += AHEAD * 64 * W) {
+                u32x4 c[AHEAD];
+                uint8_t sb[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; u++) {
+                    const int i = min(i0 + u * 64 * W, pieces - 1);
+                    c[u] = ((const u32x4 *)x)[i];
+                    sb[u] = xs[i];
                 }
-            } else {
-                float v[8];
-                load8<XT == SIM_TYPE_MX4 ? SIM_TYPE_F32 : XT>((const typename Elem<XT == SIM_TYPE_MX4 ? SIM_TYPE_F32 : XT>::type *)x + m * x_stride + at * 8, K - at * 8, v);
-                uint32_t sb;
-                *(uint32_t *)(codes + m * pitch + at * 4) = quantize8(v, sb);
-                if ((at & 3) == 0) scales[m * scale_pitch + at / 4] = (uint8_t)sb;
+#pragma unroll
+                for (int u = 0; u < AHEAD; u++) {
+                    const int i = i0 + u * 64 * W, m = i / (groups * 8);
+                    if (i < pieces) {
+                        *(u32x4 *)(codes + m * pitch + (i - m * groups * 8) * 16) = c[u];
+                        scales[i] = sb[u];
+                    }
+                }
+            }
+        } else {
+            constexpr int FT = XT == SIM_TYPE_MX4 ? SIM_TYPE_F32 : XT;
+            const int pieces = M * groups * 32;  // of eight columns; whole waves take part to the end
+            for (int i0 = threadIdx.x; i0 < pieces; i0 += AHEAD * 64 * W) {
+                float v[AHEAD][8];
+#pragma unroll
+                for (int u = 0; u < AHEAD; u++) {
+                    const int i = i0 + u * 64 * W, m = i / (groups * 32), at = i - m * groups * 32;
+                    load8<FT>((const typename Elem<FT>::type *)x + (i < pieces ? m : 0) * x_stride + at * 8, i < pieces ? K - at * 8 : 0, v[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; u++) {
+                    const int i = i0 + u * 64 * W, m = i / (groups * 32), at = i - m * groups * 32;
+                    uint32_t sb;
+                    const uint32_t c = quantize8(v[u], sb);
+                    if (i < pieces) {
+                        *(uint32_t *)(codes + m * pitch + at * 4) = c;
+                        if ((at & 3) == 0) scales[m * scale_pitch + at / 4] = (uint8_t)sb;
+                    }
+                }
             }
         }
         __syncthreads();
@@ -382,20 +410,29 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *_
 }
 
 inline size_t skinny_lds(int64_t M, int64_t K) { return (size_t)(M * (groups_of(K) * (kGroupCodes + kGroupScales) + 16)); }
-inline bool skinny(int64_t M, int64_t K) { return M <= kSkinnyRows && K > 0 && K < (1 << 20) && skinny_lds(M, K) <= kSkinnyLds; }
+inline bool skinny(int64_t M, int64_t K) { return M <= kSkinnyRows && K > 0 && K < (1 << 20) && skinny_lds(M, K) <= kSkinnyLds[1]; }
 
-template <int T, int XT, int R, int MT>
-void launch_skinny(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride, const uint8_t *bc, const uint8_t *bs,
-                   int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
-    const size_t lds = std::max(skinny_lds(M, K), (size_t)kSkinnyWaves * R * MT * 1024);
-    matmul_skinny<T, XT, R, MT><<<(uint32_t)((N + 16 * R - 1) / (16 * R)), 64 * kSkinnyWaves, lds, st>>>(
-        x, xs, x_stride, bc, bs, (int)M, N, (int)K, (typename Elem<T>::type *)out, stride);
-}
 template <int T, int XT>
 void skinny_t(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride, const uint8_t *bc, const uint8_t *bs,
               int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
-    if (M <= 16) launch_skinny<T, XT, 2, 1>(st, x, xs, x_stride, bc, bs, M, N, K, out, stride);
-    else launch_skinny<T, XT, 2, 2>(st, x, xs, x_stride, bc, bs, M, N, K, out, stride);
+    typedef typename Elem<T>::type E;
+    constexpr int R = 2;
+    const uint32_t grid = (uint32_t)((N + 16 * R - 1) / (16 * R));
+    const auto launch = [&](auto mt, auto lds) {
+        matmul_skinny<T, XT, R, decltype(mt)::value, decltype(lds)::value><<<grid, 64 * kSkinnyWaves, 0, st>>>(
+            x, xs, x_stride, bc, bs, (int)M, N, (int)K, (E *)out, stride);
+    };
+    typedef std::integral_constant<int, kSkinnyLds[0]> Small;
+    typedef std::integral_constant<int, kSkinnyLds[1]> Large;
+    const bool small = skinny_lds(M, K) <= (size_t)kSkinnyLds[0];
+    if constexpr (XT == SIM_TYPE_MX4) {
+        if (M <= 16) small ? launch(std::integral_constant<int, 1>(), Small()) : launch(std::integral_constant<int, 1>(), Large());
+        else small ? launch(std::integral_constant<int, 2>(), Small()) : launch(std::integral_constant<int, 2>(), Large());
+    } else {  // at most kOwnQuantize elements, which always fit
+        static_assert(kOwnQuantize * 34 / 64 + kSkinnyRows * (kGroupCodes + kGroupScales + 16) <= kSkinnyLds[0], "they fit");
+        if (M <= 16) launch(std::integral_constant<int, 1>(), Small());
+        else launch(std::integral_constant<int, 2>(), Small());
+    }
 }
 
 template <int T>
