@@ -145,7 +145,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
         const int first = (wave * SCALE_COPIES + i) * 16, row = first + (lane >> 2);
         const bool in_a = first < BM;
         const int at = in_a ? min(row, a_last) : min(row - BM, b_last);
-        const uint32_t offset = (uint32_t)at * (uint32_t)scale_pitch + min(g + ((lane & 3) >> 1), groups - 1) * kGroupScales + (lane & 1) * 4;
+        // a row's four words are permuted by bits 3 and 4 of its number, against bank conflicts
+        const int word = (lane & 3) ^ (((first >> 3) & 2) | (lane >> 5));
+        const uint32_t offset = (uint32_t)at * (uint32_t)scale_pitch + min(g + (word >> 1), groups - 1) * kGroupScales + (word & 1) * 4;
         copy4_to_lds(sdst + (uint32_t)(g / kScaleGroups) % kScaleBuffers * (ROWS * SCALE_ROW) + i * 256, in_a ? as_base : bs_base, offset);
     };
 
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
         op[s][i] = *(const u32x4 *)(codes[(uint32_t)stage % kBuffers] + row_of(i) * kStageCodes + piece * 16);
     };
     const auto read_scale = [&](int i, int stage, int q) {
-        const uint8_t *p = scales[(uint32_t)stage / (2 * kScaleGroups) % kScaleBuffers] + stage % (2 * kScaleGroups) * 4 + h * 2;
+        const uint8_t *p = scales[(uint32_t)stage / (2 * kScaleGroups) % kScaleBuffers] + ((stage % (2 * kScaleGroups)) ^ ((lane >> 3) & 3)) * 4 + h * 2;
         sc[q][i] = *(const uint16_t *)(p + row_of(i) * SCALE_ROW);
     };
     const auto product = [&](auto sel, auto parity, int n) {
