@@ -43,7 +43,8 @@ typedef enum { SIM_TYPE_F32 = 0, SIM_TYPE_F16 = 1, SIM_TYPE_BF16 = 2, SIM_TYPE_M
  *   codes  [R, sim_mx4_code_pitch(K)]  = ceil(K / 256) * 128 bytes a row, the
  *          even element in the low four bits;
  *   scales [R, sim_mx4_scale_pitch(K)] = ceil(K / 256) * 8 bytes a row.
- * Codes and scales past column K are 0.  Both arrays are 16-byte aligned.
+ * Codes and scales past column K are 0.  Codes are 16-byte, scales 8-byte
+ * aligned, as any run of whole rows is.
  */
 int64_t sim_mx4_code_pitch(int64_t K);
 int64_t sim_mx4_scale_pitch(int64_t K);

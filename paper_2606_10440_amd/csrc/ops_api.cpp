@@ -78,7 +78,7 @@ sim_status sim_mx4_quantize(void *stream, const void *x, int32_t type, int64_t r
     NEED(x && codes && scales, "null array");
     NEED(rows == 1 || row_stride >= cols, "row stride below the row length");
     NEED(aligned_to(x, size_of(type)), "x not aligned to its type");
-    NEED(aligned_to(codes, 16) && aligned_to(scales, 16), "codes and scales must be 16-byte aligned");
+    NEED(aligned_to(codes, 16) && aligned_to(scales, 8), "codes must be 16-byte, scales 8-byte aligned");
     return done(launch_quantize((hipStream_t)stream, x, type, rows, cols, row_stride, transpose, codes, scales), __func__);
 }
 
@@ -91,7 +91,7 @@ sim_status sim_mx4_dequantize(void *stream, const uint8_t *codes, const uint8_t 
     NEED(codes && scales && out, "null array");
     NEED(rows == 1 || row_stride >= cols, "row stride below the row length");
     NEED(aligned_to(out, size_of(type)), "out not aligned to its type");
-    NEED(aligned_to(codes, 16) && aligned_to(scales, 16), "codes and scales must be 16-byte aligned");
+    NEED(aligned_to(codes, 16) && aligned_to(scales, 8), "codes must be 16-byte, scales 8-byte aligned");
     return done(launch_dequantize((hipStream_t)stream, codes, scales, rows, cols, out, type, row_stride), __func__);
 }
 
@@ -107,8 +107,8 @@ sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a
     NEED(out && (K == 0 || (a_codes && a_scales && b_codes && b_scales)), "null array");
     NEED(M == 1 || row_stride >= N, "row stride below the row length");
     NEED(aligned_to(out, size_of(type)), "out not aligned to its type");
-    NEED(aligned_to(a_codes, 16) && aligned_to(a_scales, 16) && aligned_to(b_codes, 16) && aligned_to(b_scales, 16),
-         "codes and scales must be 16-byte aligned");
+    NEED(aligned_to(a_codes, 16) && aligned_to(a_scales, 8) && aligned_to(b_codes, 16) && aligned_to(b_scales, 8),
+         "codes must be 16-byte, scales 8-byte aligned");
     const size_t need = sim_mx4_matmul_workspace(M, N, K);
     NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
     return done(launch_matmul((hipStream_t)stream, a_codes, a_scales, b_codes, b_scales, M, N, K, out, type, row_stride),
@@ -130,7 +130,7 @@ sim_status sim_mx4_linear(void *stream, const void *x, int32_t x_type, int64_t x
     NEED(out && (K == 0 || (x && w_codes && w_scales)), "null array");
     NEED(M == 1 || (x_stride >= K && row_stride >= N), "row stride below the row length");
     NEED(aligned_to(x, size_of(x_type)) && aligned_to(out, size_of(type)), "x or out not aligned to its type");
-    NEED(aligned_to(w_codes, 16) && aligned_to(w_scales, 16), "codes and scales must be 16-byte aligned");
+    NEED(aligned_to(w_codes, 16) && aligned_to(w_scales, 8), "codes must be 16-byte, scales 8-byte aligned");
     const size_t need = sim_mx4_linear_workspace(M, N, K);
     NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
     if (linear_in_one(M, K))
@@ -248,7 +248,7 @@ sim_status sim_moe_layer(void *stream, const void *x, int32_t type, int64_t T, i
     NEED(F == 0 || (mx4 ? s13 && s2 : !s13 && !s2), "scales go with 4-bit weights");
     NEED(T == 1 || (x_stride >= D && y_stride >= D), "row stride below the row length");
     NEED(aligned_to(x, 2) && aligned_to(y, 2) && aligned_to(w13, mx4 ? 16 : 2) && aligned_to(w2, mx4 ? 16 : 2) &&
-             aligned_to(s13, 16) && aligned_to(s2, 16),
+             aligned_to(s13, 8) && aligned_to(s2, 8),
          "array not aligned");
     const size_t need = sim_moe_layer_workspace(T, D, E, k, F);
     NEED(workspace && workspace_bytes >= need && aligned_to(workspace, 16), "workspace too small or not aligned");

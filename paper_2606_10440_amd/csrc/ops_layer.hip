@@ -156,6 +156,13 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 // the second, the columns of tokens that did not choose an expert are zero,
 // so all experts add into one accumulator and nothing has to be joined but
 // the parts of the split contraction.
+//
+// 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 106 us for 459 MB of
+// gates and ups (4.3 TB/s), 68 us for 230 MB of downs (3.4 TB/s, 57 us without
+// the hidden values' loads); one token, k = 6 of 64 bf16 experts of 2048 x
+// 1408: 24.5 us for 69 MB, 8.5 of which are the launch, the routing and the
+// epilogue, and 11 us for 35 MB.  The kernels for more tokens take 206, 39
+// and (both small) 20 us where these take 177, 35 and 14.
 
 constexpr int kFewTokens = 16;
 constexpr int kFewExperts = 256;
@@ -509,6 +516,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
 // The router's lists give each expert its tokens, CT tiles of sixteen at a
 // time as columns.  The second product leaves one row per slot, and a last
 // kernel adds a token's rows up.
+//
+// 150 tokens, k = 2 of 16 bf16 experts of 4096 x 4096: 210 us for 913 MB of
+// gates and ups, 121 us for 456 MB of downs (4.3 and 3.8 TB/s; a last round of
+// workgroups that is half full); 64 tokens, k = 4 of 32 of 4096 x 2048: 303 us
+// in all, 5.3 TB/s.  What bounds them beside memory are cache accesses, one
+// for every lane's sixteen bytes: so several rows of weights share a load of
+// activations, and a step is whole cache lines.
 
 constexpr int kWaves = 4;
 

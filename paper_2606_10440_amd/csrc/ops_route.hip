@@ -5,6 +5,11 @@
 // runs four tokens at once and every exchange stays within a row of 16 lanes.
 // A logit is compared as a whole number that orders as the value does, NaN
 // highest, 0 for what cannot be chosen (masked, -infinity, past E).
+//
+// 16385 tokens, 256 bf16 experts, a mask of its own for each token, k = 8:
+// choice 11 us (k searches of 16 registers a lane, 1.1 TB/s), lists 8.7 us (a
+// workgroup reads the 66 KB of all chunks' counts), gradient 8 us; 8 tokens,
+// 64 experts: 4.7 us in one launch.
 #include "ops_route_keys.h"
 
 namespace simops {

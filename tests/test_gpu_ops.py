@@ -92,6 +92,30 @@ def test_quantize_every_bf16(ops, transpose):
 
 
 @pytest.mark.parametrize("transpose", [False, True])
+def test_quantize_every_fp16(ops, transpose):
+    v = np.arange(1 << 16, dtype=np.uint16).view(np.float16)
+    v = v[np.isfinite(v)]
+    rng = np.random.default_rng(3)
+    x = np.zeros((len(v), 32), np.float16)
+    x[:, 0] = v
+    x[:, 1:] = (v[:, None].astype(np.float32) * rng.uniform(-1, 1, (len(v), 31))).astype(np.float16)
+    t = torch.from_numpy(x)
+    d = t.cuda().t().contiguous() if transpose else t.cuda()
+    same_codes(ops.mx4_quantize(d, transpose=transpose), x.astype(np.float64))
+
+
+def test_rows_of_a_stored_tensor(ops):
+    # any run of rows is a tensor of its own, its scales at a multiple of eight bytes
+    x, v = rand(17, (7, 200), "bf16")
+    w, vw = rand(18, (40, 200), "bf16")
+    q, qw = ops.mx4_quantize(x), ops.mx4_quantize(w)
+    part, pw = ops.Mx4(q.codes[1:4], q.scales[1:4], (3, 200)), ops.Mx4(qw.codes[3:38], qw.scales[3:38], (35, 200))
+    assert torch.equal(ops.mx4_dequantize(part, torch.float32), ops.mx4_dequantize(q, torch.float32)[1:4])
+    want = ops.mx4_matmul(q, qw, dtype=torch.float32)
+    assert torch.equal(ops.mx4_matmul(part, pw, dtype=torch.float32), want[1:4, 3:38])
+
+
+@pytest.mark.parametrize("transpose", [False, True])
 def test_quantize_ties_and_extremes(ops, transpose):
     rows = []
     for e in (-149, -130, -128, -127, -126, -100, 0, 60, 125):
