@@ -265,7 +265,7 @@ __device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
 }
 
 // Gate and up products, sixteen hidden units of one expert after another.
-template <int T, int WT, bool EDGE>
+template <int T, int WT, int U, bool EDGE>
 __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, const uint16_t *__restrict__ x, int64_t x_stride,
                                                             int D, const void *__restrict__ w13,
                                                             const uint8_t *__restrict__ s13, int F, int tiles,
@@ -322,7 +322,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
         typedef Inputs<T, WT, EDGE> In;
         f32x4 g = {0}, u = {0};
         if (in_lds) {
-            constexpr int U = 4;
             typedef Weights<WT, EDGE> Wt;
             Wt wg[U], wu[U];
             Scales<WT, 2, U> sc[2];
@@ -348,23 +347,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                     }
                 });
         } else {
-            constexpr int U = WT == SIM_TYPE_MX4 ? 2 : 4;
+            constexpr int V = WT == SIM_TYPE_MX4 ? 2 : U;  // (registers)
             typedef Weights<WT, EDGE> Wt;
-            Wt wg[U], wu[U];
-            Scales<WT, 2, U> sc[2];
+            Wt wg[V], wu[V];
+            Scales<WT, 2, V> sc[2];
             const uint16_t *xr = x + (int64_t)(has ? r : __ffs(tokens) - 1) * x_stride;
-            In xi[U];
-            ring<U, kFewWaves>(
-                (steps + U - 1) / U, wave,
+            In xi[V];
+            ring<V, kFewWaves>(
+                (steps + V - 1) / V, wave,
                 [&](int p, int run) { sc[p].load(s13, scale_row, D, run); },
                 [&](int i, int run) {
-                    const int k0 = min(run * U + i, steps - 1) * kCols<WT>;
+                    const int k0 = min(run * V + i, steps - 1) * kCols<WT>;
                     wg[i].load(w13, row, D, k0, q);
                     wu[i].load(w13, row + F, D, k0, q);
                     xi[i].load(xr, D, k0, q);
                 },
                 [&](int i, int p, int run) {
-                    if (run * U + i < steps) {
+                    if (run * V + i < steps) {
                         const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
                         for (int s = 0; s < kIns<WT>; s++) {
@@ -764,8 +763,14 @@ template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const Layer
     constexpr int R = WT == SIM_TYPE_MX4 ? 4 : 2;  // row tiles that share the hidden values
     const int64_t lists = std::min<int64_t>(r.E, r.T * r.k);
     const int tf = (int)((a.F + 15) / 16), td = (int)((a.D + 16 * R - 1) / (16 * R));
-    few_up<T, WT, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
-        r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
+    // runs of four steps where there is one for each wave, else of two (8
+    // tokens, k = 4 of 64 bf16 experts of 896 x 2048: 60 us, 74 with runs of four)
+    const auto up = [&](auto u) {
+        few_up<T, WT, decltype(u)::value, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
+            r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
+    };
+    if (a.D >= 4 * kFewWaves * kCols<WT>) up(std::integral_constant<int, 4>());
+    else up(std::integral_constant<int, 2>());
     // as many parts as workgroups fit, but a run for every wave: joining costs
     // a part about half a microsecond (one token, 11 experts of 1024 x 2869:
     // 25 us in 24 parts, 20 us in 15)
