@@ -66,16 +66,15 @@ sim_status sim_mx4_dequantize(void *hip_stream, const uint8_t *codes, const uint
 /*
  * out[m, n] = sum over k of A[m, k] B[n, k], A: M x K, B: N x K, both in 4
  * bits; summed in 32 bits and rounded once to type.  K = 0 gives zeros.
- * workspace: sim_mx4_matmul_workspace bytes, 16-byte aligned (NULL if 0).
  */
-size_t sim_mx4_matmul_workspace(int64_t M, int64_t N, int64_t K);
 sim_status sim_mx4_matmul(void *hip_stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                           const uint8_t *b_scales, int64_t M, int64_t N, int64_t K, void *out, int32_t type,
-                          int64_t row_stride, void *workspace, size_t workspace_bytes);
+                          int64_t row_stride);
 
 /*
  * The same product of x (M x K of x_type, put into 4 bits on the way exactly
  * as sim_mx4_quantize does) with a 4-bit W (N x K): a linear layer.
+ * workspace: sim_mx4_linear_workspace bytes, 16-byte aligned (NULL if 0).
  */
 size_t sim_mx4_linear_workspace(int64_t M, int64_t N, int64_t K);
 sim_status sim_mx4_linear(void *hip_stream, const void *x, int32_t x_type, int64_t x_stride, const uint8_t *w_codes,

@@ -95,11 +95,9 @@ sim_status sim_mx4_dequantize(void *stream, const uint8_t *codes, const uint8_t 
     return done(launch_dequantize((hipStream_t)stream, codes, scales, rows, cols, out, type, row_stride), __func__);
 }
 
-size_t sim_mx4_matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
-
 sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *b_codes,
                           const uint8_t *b_scales, int64_t M, int64_t N, int64_t K, void *out, int32_t type,
-                          int64_t row_stride, void *workspace, size_t workspace_bytes) {
+                          int64_t row_stride) {
     NEED(is_float(type), "out must be f32, f16 or bf16");
     NEED(M >= 0 && N >= 0 && K >= 0, "negative size");
     FITS(dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(N, K), "matrix too large");
@@ -109,15 +107,13 @@ sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a
     NEED(aligned_to(out, size_of(type)), "out not aligned to its type");
     NEED(aligned_to(a_codes, 16) && aligned_to(a_scales, 8) && aligned_to(b_codes, 16) && aligned_to(b_scales, 8),
          "codes must be 16-byte, scales 8-byte aligned");
-    const size_t need = sim_mx4_matmul_workspace(M, N, K);
-    NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
     return done(launch_matmul((hipStream_t)stream, a_codes, a_scales, b_codes, b_scales, M, N, K, out, type, row_stride),
                 __func__);
 }
 
 size_t sim_mx4_linear_workspace(int64_t M, int64_t N, int64_t K) {
     if (!dims_ok(M, K) || M == 0 || K == 0 || linear_in_one(M, K)) return 0;
-    return (size_t)((M * (sim_mx4_code_pitch(K) + sim_mx4_scale_pitch(K)) + 15) / 16 * 16) + sim_mx4_matmul_workspace(M, N, K);
+    return (size_t)((M * (sim_mx4_code_pitch(K) + sim_mx4_scale_pitch(K)) + 15) / 16 * 16);
 }
 
 sim_status sim_mx4_linear(void *stream, const void *x, int32_t x_type, int64_t x_stride, const uint8_t *w_codes,

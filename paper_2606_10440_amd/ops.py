@@ -22,7 +22,7 @@ from . import sim
 from .sim import SIM_ERR_INVALID_ARG, SIM_OK, SimError
 
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
-           "sim_mx4_matmul_workspace", "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
+           "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
            "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer_workspace",
            "sim_moe_layer", "sim_ops_last_error")
 
@@ -43,9 +43,9 @@ def lib():
         L.sim_mx4_code_pitch.restype = L.sim_mx4_scale_pitch.restype = i64
         L.sim_mx4_quantize.argtypes = [P, P, i32, i64, i64, i64, i32, P, P]
         L.sim_mx4_dequantize.argtypes = [P, P, P, i64, i64, P, i32, i64]
-        L.sim_mx4_matmul_workspace.argtypes = L.sim_mx4_linear_workspace.argtypes = [i64, i64, i64]
-        L.sim_mx4_matmul_workspace.restype = L.sim_mx4_linear_workspace.restype = sz
-        L.sim_mx4_matmul.argtypes = [P, P, P, P, P, i64, i64, i64, P, i32, i64, P, sz]
+        L.sim_mx4_linear_workspace.argtypes = [i64, i64, i64]
+        L.sim_mx4_linear_workspace.restype = sz
+        L.sim_mx4_matmul.argtypes = [P, P, P, P, P, i64, i64, i64, P, i32, i64]
         L.sim_mx4_linear.argtypes = [P, P, i32, i64, P, P, i64, i64, i64, P, i32, i64, P, sz]
         L.sim_mx4_linear_grad_workspace.argtypes = [i64, i64, i64]
         L.sim_mx4_linear_grad_workspace.restype = sz
@@ -136,7 +136,7 @@ def mx4_quantize(x, transpose=False) -> Mx4:
     shape = tuple(x.shape)
     if len(shape) != 2:
         _need(len(shape) > 0 and not transpose, "x needs a dimension, and two to be transposed")
-        x = x.reshape(-1, shape[-1])
+        x = x.reshape(math.prod(shape[:-1]), shape[-1])
     t, rows, cols, stride, dev = _rows(x, "x")
     R, K = (cols, rows) if transpose else (rows, cols)
     groups = (K + 255) // 256
@@ -168,11 +168,9 @@ def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
     plain = not isinstance(a, Mx4)
     if plain:
         at, M, Ka, stride, adev = _rows(a, "a")
-        first, n, fn = (a.data_ptr(), at, stride), L.sim_mx4_linear_workspace(M, N, K), L.sim_mx4_linear
     else:
         _need(len(a.shape) == 2, "a must be a matrix")
         M, Ka, adev = _stored(a, "a")
-        first, n, fn = (a.codes.data_ptr(), a.scales.data_ptr()), L.sim_mx4_matmul_workspace(M, N, K), L.sim_mx4_matmul
     _need(Ka == K and adev == dev, "a and b differ in their last axis or their GPU")
     if out is None:
         t = _TYPE.get(dtype)
@@ -181,9 +179,14 @@ def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
     else:
         t, m, cols, ostride, odev = _rows(out, "out")
         _need(m == M and cols == N and odev == dev, "out must be [M, N] on the same GPU")
-    ws = b.codes.new_empty(n) if n else None
-    _call(dev, fn, *first, b.codes.data_ptr(), b.scales.data_ptr(), M, N, K, out.data_ptr(), t, ostride,
-          ws.data_ptr() if n else None, n)
+    if plain:
+        n = L.sim_mx4_linear_workspace(M, N, K)
+        ws = b.codes.new_empty(n) if n else None
+        _call(dev, L.sim_mx4_linear, a.data_ptr(), at, stride, b.codes.data_ptr(), b.scales.data_ptr(), M, N, K, out.data_ptr(),
+              t, ostride, ws.data_ptr() if n else None, n)
+    else:
+        _call(dev, L.sim_mx4_matmul, a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), M, N, K,
+              out.data_ptr(), t, ostride)
     return out
 
 

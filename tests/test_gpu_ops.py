@@ -459,6 +459,7 @@ def test_nothing_to_do(ops):
     r = ops.moe_route(z, 2)
     assert r.experts.shape == (0, 2) and (r.offsets == 0).all() and r.offsets.numel() == 9 and r.order.numel() == 0
     assert ops.moe_route_grad(z, r.experts, torch.empty(0, 2, device="cuda")).shape == (0, 8)
+    assert ops.mx4_quantize(torch.empty(2, 3, 0, device="cuda")).codes.shape == (6, 0)
     q = ops.mx4_quantize(torch.empty(0, 64, device="cuda"))
     assert ops.mx4_dequantize(q).shape == (0, 64)
     w = ops.mx4_quantize(torch.randn(5, 64, device="cuda"))

@@ -70,8 +70,7 @@ def test_dequantize_refusals(lib, change, want):
     assert run(lib, "sim_mx4_dequantize", DEQUANT, **change) == want
 
 
-MATMUL = [("ac", P), ("as", P), ("bc", P), ("bs", P), ("M", 4), ("N", 8), ("K", 64), ("out", P), ("type", 2), ("stride", 8),
-          ("ws", P), ("ws_bytes", 1 << 30)]
+MATMUL = [("ac", P), ("as", P), ("bc", P), ("bs", P), ("M", 4), ("N", 8), ("K", 64), ("out", P), ("type", 2), ("stride", 8)]
 # so many rows that they are put into 4 bits in a workspace
 LINEAR = [("x", P), ("x_type", 2), ("x_stride", 64), ("wc", P), ("ws_", P), ("M", 40), ("N", 8), ("K", 64), ("out", P),
           ("type", 2), ("stride", 8), ("ws", P), ("ws_bytes", 1 << 30)]
