@@ -24,14 +24,32 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// 16-bit elements k .. k + 7 of a row of K as raw bits, zeros past its end.
-// EDGE: K need not be a whole number of steps.
-template <bool EDGE> __device__ inline u32x4 load_row8(const uint16_t *__restrict__ row, int k, int K) {
-    if (!EDGE || k + 8 <= K) return *(const u32x4_a2 *)(row + k);
-    uint16_t v[8];
+// A row of K 16-bit elements: a whole number of steps, at least one load
+// long, or shorter than that.
+enum Edge { kWhole, kTail, kTiny };
+
+// Elements k .. k + 7 of a row as raw bits.  Past the end of a kTail row the
+// row's last eight are loaded instead, and tail8 puts them in their place: no
+// branch stands around the load, so that loads under way are still counted
+// (100 tokens, k = 2 of 16 bf16 experts of 2080 x 2080: 127 us, 187 with branches).
+template <int EDGE> __device__ inline u32x4 load8(const uint16_t *__restrict__ row, int k, int K) {
+    if (EDGE == kTiny) {
+        uint16_t v[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = k + i < K ? row[k + i] : 0;
-    return *(u32x4 *)v;
+        for (int i = 0; i < 8; i++) v[i] = k + i < K ? row[k + i] : 0;
+        return *(u32x4 *)v;
+    }
+    return *(const u32x4_a2 *)(row + (EDGE == kTail ? min(k, K - 8) : k));
+}
+// What load8 gave, with zeros past the end of a kTail row.
+template <int EDGE> __device__ inline u32x4 tail8(u32x4 v, int k, int K) {
+    if (EDGE != kTail) return v;
+    const int n = min(k + 8 - K, 8);  // elements past the end
+    if (n <= 0) return v;
+    if (n & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    if (n & 2) v = u32x4{v[1], v[2], v[3], 0};
+    if (n & 4) v = u32x4{v[2], v[3], 0, 0};
+    return n & 8 ? u32x4{0, 0, 0, 0} : v;
 }
 
 // fp16 to the two bf16 values that add up to it
@@ -63,12 +81,16 @@ template <int WT> constexpr int kIns = WT == SIM_TYPE_MX4 ? 4 : 2;
 template <int WT> __device__ inline int step_at(int q, int s) { return WT == SIM_TYPE_MX4 ? 32 * q + 8 * s : 32 * s + 8 * q; }
 
 // A step of one tile of sixteen weight rows; lane l holds row l % 16.
-template <int WT, bool EDGE> struct Weights {
+template <int WT, int EDGE> struct Weights {
     u32x4 raw[2];
     // base: the weights; row: this lane's; k0: the step's first column
     __device__ void load(const void *base, int64_t row, int K, int k0, int q) {
 #pragma unroll
-        for (int s = 0; s < 2; s++) raw[s] = load_row8<EDGE>((const uint16_t *)base + row * K, k0 + step_at<WT>(q, s), K);
+        for (int s = 0; s < 2; s++) raw[s] = load8<EDGE>((const uint16_t *)base + row * K, k0 + step_at<WT>(q, s), K);
+    }
+    __device__ void tail(int K, int k0, int q) {
+#pragma unroll
+        for (int s = 0; s < 2; s++) raw[s] = tail8<EDGE>(raw[s], k0 + step_at<WT>(q, s), K);
     }
     struct Operand {
         u32x4 raw;
@@ -86,11 +108,12 @@ template <int WT, bool EDGE> struct Weights {
         return WT == SIM_TYPE_F16 ? mfma(w.lo, x, c) : c;
     }
 };
-template <bool EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
+template <int EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
     u32x4 raw;
     __device__ void load(const void *base, int64_t row, int K, int k0, int q) {
         raw = *(const u32x4 *)((const uint8_t *)base + row * groups_of(K) * kGroupCodes + k0 / 2 + q * 16);
     }
+    __device__ void tail(int, int, int) {}  // rows are padded
     struct Operand {
         bf16x8 hi;
     };
@@ -99,11 +122,15 @@ template <bool EDGE> struct Weights<SIM_TYPE_MX4, EDGE> {
 };
 
 // A step of sixteen inputs; lane l holds token l % 16.
-template <int T, int WT, bool EDGE> struct Inputs {
+template <int T, int WT, int EDGE> struct Inputs {
     u32x4 raw[kIns<WT>];
     __device__ void load(const uint16_t *row, int K, int k0, int q) {
 #pragma unroll
-        for (int s = 0; s < kIns<WT>; s++) raw[s] = load_row8<EDGE>(row, k0 + step_at<WT>(q, s), K);
+        for (int s = 0; s < kIns<WT>; s++) raw[s] = load8<EDGE>(row, k0 + step_at<WT>(q, s), K);
+    }
+    __device__ void tail(int K, int k0, int q) {
+#pragma unroll
+        for (int s = 0; s < kIns<WT>; s++) raw[s] = tail8<EDGE>(raw[s], k0 + step_at<WT>(q, s), K);
     }
     template <typename W> static __device__ f32x4 mul(u32x4 v, const typename W::Operand &w, f32x4 c) {
         if constexpr (T == SIM_TYPE_F16 && WT == SIM_TYPE_F16)  // as they are
@@ -141,7 +168,7 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         hi[i] = (__bf16)v[i];
-        lo[i] = (__bf16)(v[i] - (float)hi[i]);
+        lo[i] = (__bf16)(fabsf((float)hi[i]) < INFINITY ? v[i] - (float)hi[i] : 0.f);  // inf - inf is no part of inf
     }
     *(u32x2 *)(h_hi + at) = *(u32x2 *)hi;
     *(u32x2 *)(h_lo + at) = *(u32x2 *)lo;
@@ -153,9 +180,9 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 // themselves are the sixteen columns of every product.  The first kernel
 // routes, every workgroup for itself, which costs less than a launch, and
 // then takes tiles of sixteen hidden units of the used experts in turn.  In
-// the second, the columns of tokens that did not choose an expert are zero,
-// so all experts add into one accumulator and nothing has to be joined but
-// the parts of the split contraction.
+// the second, a step's sums are added to the columns of the tokens that chose
+// its expert, so all experts share one accumulator and nothing has to be
+// joined but the parts of the split contraction.
 //
 // 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 106 us for 459 MB of
 // gates and ups (4.3 TB/s), 68 us for 230 MB of downs (3.4 TB/s, 57 us without
@@ -265,7 +292,7 @@ __device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
 }
 
 // Gate and up products, sixteen hidden units of one expert after another.
-template <int T, int WT, int U, bool EDGE>
+template <int T, int WT, int U, int EDGE>
 __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, const uint16_t *__restrict__ x, int64_t x_stride,
                                                             int D, const void *__restrict__ w13,
                                                             const uint8_t *__restrict__ s13, int F, int tiles,
@@ -294,25 +321,26 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
         const int e = __builtin_amdgcn_readfirstlane(rt.list[item / tiles]), f0 = item % tiles * 16;
         const uint32_t tokens = rt.tokens[e];
         const bool has = (tokens >> r) & 1;
-        const int pitch = D * 2 + 16;  // so that sixteen rows start in different banks
+        const int pitch = steps * kCols<WT> * 2 + 16;  // so that sixteen rows start in different banks
         if (e != held) {  // the expert's inputs to LDS, where they fit
             held = e;
-            in_lds = !EDGE && __popc(tokens) * pitch <= kFewInputs;
+            in_lds = __popc(tokens) * pitch <= kFewInputs;
             if (in_lds) {
                 if (wave == 0 && has && q == 0) s_token[__popc(tokens & ((1u << r) - 1))] = r;
                 __syncthreads();
-                const int pieces = D / 8, all = __popc(tokens) * pieces;
+                const int pieces = steps * kCols<WT> / 8, all = __popc(tokens) * pieces;
                 for (int c0 = threadIdx.x; c0 < all; c0 += 4 * 64 * kFewWaves) {  // four loads under way
                     u32x4 v[4];
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         const int c = min(c0 + i * 64 * kFewWaves, all - 1), n = c / pieces;
-                        v[i] = *(const u32x4_a2 *)(x + (int64_t)s_token[n] * x_stride + (c - n * pieces) * 8);
+                        v[i] = load8<EDGE>(x + (int64_t)s_token[n] * x_stride, (c - n * pieces) * 8, D);
                     }
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
                         const int c = c0 + i * 64 * kFewWaves, n = c / pieces;
-                        if (c < all) *(u32x4 *)(rt.inputs + n * pitch + (c - n * pieces) * 16) = v[i];
+                        if (c < all)
+                            *(u32x4 *)(rt.inputs + n * pitch + (c - n * pieces) * 16) = tail8<EDGE>(v[i], (c - n * pieces) * 8, D);
                     }
                 }
                 __syncthreads();
@@ -337,6 +365,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                 },
                 [&](int i, int p, int run) {
                     if (run * U + i < steps) {
+                        if (EDGE && run * U + i == steps - 1) {
+                            wg[i].tail(D, (steps - 1) * kCols<WT>, q);
+                            wu[i].tail(D, (steps - 1) * kCols<WT>, q);
+                        }
                         const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
                         for (int s = 0; s < kIns<WT>; s++) {
@@ -364,6 +396,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
                 },
                 [&](int i, int p, int run) {
                     if (run * V + i < steps) {
+                        if (EDGE && run * V + i == steps - 1) {
+                            wg[i].tail(D, (steps - 1) * kCols<WT>, q);
+                            wu[i].tail(D, (steps - 1) * kCols<WT>, q);
+                            xi[i].tail(D, (steps - 1) * kCols<WT>, q);
+                        }
                         const float cg = sc[p].get(i, 0, r, q), cu = sc[p].get(i, 1, r, q);
 #pragma unroll
                         for (int s = 0; s < kIns<WT>; s++) {
@@ -404,7 +441,7 @@ template <int WT> constexpr int few_down_run = WT == SIM_TYPE_MX4 ? 2 : 4;  // s
 
 // 16 R output columns of all tokens; the steps of all used experts are one
 // list, dealt to the splits and their waves.
-template <int T, int WT, int R, bool EDGE>
+template <int T, int WT, int R, int EDGE>
 __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
                                                               int h_pitch, int F, const void *__restrict__ w2,
                                                               const uint8_t *__restrict__ s2, int D, int n_tok, FewPlan plan,
@@ -421,7 +458,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
         s_slot[i] = plan.slot[i];
         if (i < max_lists) s_expert[i] = plan.expert[i];
     }
-    const int steps = h_pitch / kCols<WT>, per = (steps + U - 1) / U, total = *plan.n_used * per;  // runs
+    const int steps = (F + kCols<WT> - 1) / kCols<WT>, per = (steps + U - 1) / U, total = *plan.n_used * per;  // runs
     const int begin = (int)((int64_t)total * split / splits), end = (int)((int64_t)total * (split + 1) / splits);
     typedef Weights<WT, EDGE> Wt;
     Wt w[U][R];
@@ -431,9 +468,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
     for (int i = 0; i < R; i++) acc[i] = f32x4{0};
     __syncthreads();
     Scales<WT, R, U> sc[2];
+    bool some[2] = {false, false};
     int64_t row[R], hidden = 0;  // of the run that is being loaded
-    int k0 = 0;
-    bool some = false;
+    int k0 = 0, loading = 0;
     ring<U, kFewWaves>(
         end - begin, wave,
         [&](int p, int run) {
@@ -441,7 +478,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
             const int64_t first = (int64_t)__builtin_amdgcn_readfirstlane(s_expert[a]) * D;
             const int slot = s_slot[a * 16 + r];
             k0 = begin + run - a * per;
-            some = slot >= 0;
+            some[loading = p] = slot >= 0;
             hidden = (int64_t)slot * h_pitch;
 #pragma unroll
             for (int j = 0; j < R; j++) row[j] = first + min(d0 + j * 16 + r, D - 1);
@@ -449,17 +486,21 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
         },
         [&](int i, int) {
             const int at = min(k0 * U + i, steps - 1) * kCols<WT>;
-            h[i].load(h_hi, h_lo, hidden, some, at, q);
+            h[i].load(h_hi, h_lo, hidden, some[loading], at, q);
 #pragma unroll
             for (int j = 0; j < R; j++) w[i][j].load(w2, row[j], F, at, q);
         },
         [&](int i, int p, int run) {
-            if ((begin + run) % per * U + i < steps)
+            const int step = (begin + run) % per * U + i;
+            if (step < steps)
 #pragma unroll
                 for (int j = 0; j < R; j++) {
+                    if (EDGE && step == steps - 1) w[i][j].tail(F, step * kCols<WT>, q);
                     const float c = sc[p].get(i, j, r, q);
+                    f32x4 sum = {0};
 #pragma unroll
-                    for (int s = 0; s < kIns<WT>; s++) acc[j] = h[i].template mul<Wt>(s, w[i][j].operand(s, c), acc[j]);
+                    for (int s = 0; s < kIns<WT>; s++) sum = h[i].template mul<Wt>(s, w[i][j].operand(s, c), sum);
+                    acc[j] += some[p] ? sum : f32x4{0};  // zeros times an infinite weight are no zeros
                 }
         });
 #pragma unroll
@@ -542,7 +583,7 @@ __device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int
 }
 
 // 16 RP hidden units of one expert.
-template <int T, int WT, int RP, int CT, int U, bool EDGE>
+template <int T, int WT, int RP, int CT, int U, int EDGE>
 __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
                                                            const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
                                                            int E, int k, const int32_t *__restrict__ offsets,
@@ -586,6 +627,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__res
                 for (int c = 0; c < CT; c++) xi[i][c].load(xr[c], D, k0, q);
             },
             [&](int i, int p, int run) {
+                if (EDGE && run * U + i == steps - 1) {
+#pragma unroll
+                    for (int j = 0; j < 2 * RP; j++) w[i][j].tail(D, (steps - 1) * kCols<WT>, q);
+#pragma unroll
+                    for (int c = 0; c < CT; c++) xi[i][c].tail(D, (steps - 1) * kCols<WT>, q);
+                }
                 if (run * U + i < steps)
 #pragma unroll
                     for (int j = 0; j < 2 * RP; j++) {
@@ -630,7 +677,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__res
     }
 }
 
-template <int WT, int R, int CT, int U, bool EDGE>
+template <int WT, int R, int CT, int U, int EDGE>
 __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
                                                           int h_pitch, int F, const void *__restrict__ w2,
                                                           const uint8_t *__restrict__ s2, int D, int E,
@@ -643,7 +690,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
     if (e < 0) return;
     const int d0 = (int)(blockIdx.x % tiles) * 16 * R;
     const int first = offsets[e], n = offsets[e + 1] - first;
-    const int steps = h_pitch / kCols<WT>;
+    const int steps = (F + kCols<WT> - 1) / kCols<WT>;
     for (int c0 = 0; c0 < n; c0 += 16 * CT) {
         int64_t at[CT];
 #pragma unroll
@@ -676,6 +723,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
                 if (run * U + i < steps)
 #pragma unroll
                     for (int j = 0; j < R; j++) {
+                        if (EDGE && run * U + i == steps - 1) w[i][j].tail(F, (steps - 1) * kCols<WT>, q);
                         const float scale = sc[p].get(i, j, r, q);
 #pragma unroll
                         for (int s = 0; s < kIns<WT>; s++) {
@@ -722,7 +770,15 @@ __global__ __launch_bounds__(256) void layer_join(const float *__restrict__ part
 }
 
 inline size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
-inline bool few(int64_t T, int E) { return T <= kFewTokens && E <= kFewExperts; }
+inline bool few(int64_t T, int E, int64_t D, int64_t F) { return T <= kFewTokens && E <= kFewExperts && D >= 8 && F >= 8; }
+
+// Calls f with the kind of rows of K elements as a constant.  Rows of less
+// than eight are left to the form of one column tile for more tokens.
+template <int WT, int CT, typename Fn> inline void by_edge(int64_t K, Fn &&f) {
+    if (K % kCols<WT> == 0) f(std::integral_constant<int, kWhole>());
+    else if (K >= 8) f(std::integral_constant<int, kTail>());
+    else if constexpr (CT == 1) f(std::integral_constant<int, kTiny>());
+}
 
 // The workspace in the order in which it is handed out.
 struct Layout {
@@ -736,7 +792,7 @@ struct Layout {
         const auto take = [&](size_t bytes) { const size_t p = at; at += aligned(bytes); return p; };
         hi = take(n * pitch * 2);
         lo = take(n * pitch * 2);
-        if (few(T, E)) {
+        if (few(T, E, D, F)) {
             n_used = take(4);
             expert = take(lists * 2);
             slot = take(lists * 16 * 2);
@@ -754,7 +810,7 @@ struct Layout {
     }
 };
 
-template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
+template <int T, int WT> sim_status few_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
     const RouteArgs &r = a.route;
     const Layout at(r.T, a.D, r.E, r.k, a.F);
     __bf16 *hi = (__bf16 *)(ws + at.hi), *lo = (__bf16 *)(ws + at.lo);
@@ -765,24 +821,30 @@ template <int T, int WT, bool EDGE> sim_status few_t(hipStream_t st, const Layer
     const int tf = (int)((a.F + 15) / 16), td = (int)((a.D + 16 * R - 1) / (16 * R));
     // runs of four steps where there is one for each wave, else of two (8
     // tokens, k = 4 of 64 bf16 experts of 896 x 2048: 60 us, 74 with runs of four)
-    const auto up = [&](auto u) {
-        few_up<T, WT, decltype(u)::value, EDGE><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
+    const auto up = [&](auto u, auto edge) {
+        few_up<T, WT, decltype(u)::value, decltype(edge)::value><<<(uint32_t)std::min<int64_t>(kFewGroups, lists * tf), 64 * kFewWaves, 0, st>>>(
             r, (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, tf, hi, lo, at.pitch, plan, td);
     };
-    if (a.D >= 4 * kFewWaves * kCols<WT>) up(std::integral_constant<int, 4>());
-    else up(std::integral_constant<int, 2>());
+    by_edge<WT, 0>(a.D, [&](auto edge) {
+        if (a.D >= 4 * kFewWaves * kCols<WT>) up(std::integral_constant<int, 4>(), edge);
+        else up(std::integral_constant<int, 2>(), edge);
+    });
     // as many parts as workgroups fit, but a run for every wave: joining costs
     // a part about half a microsecond (one token, 11 experts of 1024 x 2869:
     // 25 us in 24 parts, 20 us in 15)
-    const int64_t runs = lists * ((at.pitch / kCols<WT> + few_down_run<WT> - 1) / few_down_run<WT>);
+    const int64_t runs = lists * ((a.F + kCols<WT> * few_down_run<WT> - 1) / (kCols<WT> * few_down_run<WT>));
     const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(kMaxSplits, kFewGroups / td), runs / kFewWaves));
-    few_down<T, WT, R, EDGE><<<td * splits, 64 * kFewWaves, 0, st>>>(
-        hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, (int)lists, splits, (float *)(ws + at.part),
-        (typename Elem<T>::type *)a.y, a.y_stride);
+    const auto down = [&](auto edge) {
+        few_down<T, WT, R, decltype(edge)::value><<<td * splits, 64 * kFewWaves, 0, st>>>(
+            hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, (int)r.T, plan, (int)lists, splits, (float *)(ws + at.part),
+            (typename Elem<T>::type *)a.y, a.y_stride);
+    };
+    if constexpr (WT == SIM_TYPE_MX4) down(std::integral_constant<int, kWhole>());  // rows and hidden values are padded
+    else by_edge<WT, 0>(a.F, down);
     return SIM_OPS_LAUNCH_OK();
 }
 
-template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
+template <int T, int WT, int CT> sim_status group_t(hipStream_t st, const LayerArgs &a, uint8_t *ws) {
     const RouteArgs &r = a.route;
     const Layout at(r.T, a.D, r.E, r.k, a.F);
     int32_t *experts = (int32_t *)(ws + at.experts), *offsets = (int32_t *)(ws + at.offsets), *order = (int32_t *)(ws + at.order);
@@ -795,11 +857,17 @@ template <int T, int WT, int CT, bool EDGE> sim_status group_t(hipStream_t st, c
     constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : 4 / CT, R = 4, UD = CT == 4 ? 1 : 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
     const uint32_t tf = (uint32_t)((a.F + 16 * RP - 1) / (16 * RP)), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
-    group_up<T, WT, RP, CT, UU, EDGE><<<lists * tf, 64 * kWaves, 0, st>>>(
-        (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
-        at.pitch);
-    group_down<WT, R, CT, UD, EDGE><<<lists * td, 64 * kWaves, 0, st>>>(hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, r.E,
-                                                                      offsets, order, td, part);
+    by_edge<WT, CT>(a.D, [&](auto edge) {
+        group_up<T, WT, RP, CT, UU, decltype(edge)::value><<<lists * tf, 64 * kWaves, 0, st>>>(
+            (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
+            at.pitch);
+    });
+    const auto down = [&](auto edge) {
+        group_down<WT, R, CT, UD, decltype(edge)::value><<<lists * td, 64 * kWaves, 0, st>>>(
+            hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, r.E, offsets, order, td, part);
+    };
+    if constexpr (M) down(std::integral_constant<int, kWhole>());  // rows and hidden values are padded
+    else by_edge<WT, CT>(a.F, down);
     layer_join<T><<<(uint32_t)(r.T * tj), 256, 0, st>>>(part, experts, r.k, a.D, (typename Elem<T>::type *)a.y, a.y_stride, tj);
     return SIM_OPS_LAUNCH_OK();
 }
@@ -815,17 +883,16 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
         layer_zero<T><<<(uint32_t)r.T, 256, 0, st>>>((typename Elem<T>::type *)a.y, a.y_stride, a.D);
         return SIM_OPS_LAUNCH_OK();
     }
-    const bool edge = a.D % kStep || a.F % kStep;
-    if (few(r.T, r.E)) return edge ? few_t<T, WT, true>(st, a, ws) : few_t<T, WT, false>(st, a, ws);
+    if (few(r.T, r.E, a.D, a.F)) return few_t<T, WT>(st, a, ws);
     // columns by the tokens of an average expert (lists of 19 of 150 tokens,
     // 4096 x 4096 bf16: 397 us with two column tiles, 482 with one; lists of
     // 98, 2048 x 2710: 137 us with four, 214 with two; 4-bit weights, whose
     // activations take twice the registers, gain nothing from four)
     const int64_t mean = r.T * r.k / r.E;
-    if (mean <= 10) return edge ? group_t<T, WT, 1, true>(st, a, ws) : group_t<T, WT, 1, false>(st, a, ws);
+    if (mean <= 10 || a.D < 8 || a.F < 8) return group_t<T, WT, 1>(st, a, ws);
     if constexpr (WT != SIM_TYPE_MX4)
-        if (mean > 24) return edge ? group_t<T, WT, 4, true>(st, a, ws) : group_t<T, WT, 4, false>(st, a, ws);
-    return edge ? group_t<T, WT, 2, true>(st, a, ws) : group_t<T, WT, 2, false>(st, a, ws);
+        if (mean > 24) return group_t<T, WT, 4>(st, a, ws);
+    return group_t<T, WT, 2>(st, a, ws);
 }
 
 }  // namespace

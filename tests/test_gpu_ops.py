@@ -375,7 +375,10 @@ def test_route_gradient_against_differences(ops, renorm):
 # ------------------------------------------------------------------ experts' layer
 
 LAYERS = [(1, 4, 2, 64, 32), (1, 8, 8, 200, 70), (2, 5, 1, 33, 17), (7, 16, 3, 256, 128), (15, 3, 2, 130, 257), (16, 6, 4, 512, 96),
-          (17, 40, 2, 128, 64), (33, 2, 2, 96, 48), (65, 12, 3, 160, 100), (130, 3, 2, 72, 40)]
+          (17, 40, 2, 128, 64), (33, 2, 2, 96, 48), (65, 12, 3, 160, 100), (130, 3, 2, 72, 40),
+          # rows shorter than one load, ends of rows at every place in a load
+          (1, 2, 1, 1, 1), (3, 4, 2, 7, 9), (40, 3, 2, 9, 5), (5, 4, 2, 8, 8), (6, 4, 2, 579, 323), (20, 4, 2, 453, 197),
+          (90, 3, 2, 582, 199), (9, 5, 3, 1100, 716), (110, 2, 2, 77, 510)]
 
 
 def layer_case(ops, seed, T, E, D, F, kind, weights, pad=0):
@@ -423,6 +426,36 @@ def test_layer_unused_experts_and_other_tokens_have_no_effect(ops, weights, T, E
     assert torch.isnan(got[2]).all()
     keep = torch.arange(T, device="cuda") != 2
     assert torch.equal(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("T,E", [(1, 3), (5, 4), (16, 6), (40, 4)])
+@pytest.mark.parametrize("kind,weights", [("bf16", "same"), ("fp16", "same"), ("bf16", "mx4")])
+def test_layer_infinite_weights_reach_only_their_experts_tokens(ops, kind, weights, T, E):
+    (x, z, w13, w2), _ = layer_case(ops, 43, T, E, 64, 48, kind, weights)
+    at = torch.arange(T, device="cuda")
+    z.zero_()
+    z[at, (at + 1) % E], z[at, (at + 2) % E] = 2.0, 1.0  # all but expert 0 for the first, and so on
+    want = ops.moe_layer(x, z, w13, w2, 2)
+    hit = ((at + 1) % E == 0) | ((at + 2) % E == 0)
+    if weights == "mx4":
+        w2.scales[7, 0] = 255
+    else:
+        w2[0, 7, 3] = float("inf")
+    got = ops.moe_layer(x, z, w13, w2, 2)
+    assert not torch.isfinite(got[hit, 7]).any()
+    want[hit, 7] = got[hit, 7] = 0
+    assert torch.equal(got, want)
+
+
+def test_layer_infinite_hidden_value(ops):
+    # x large enough that silu(g) u passes the 32-bit range, to +inf: the result is the sign of each weight of w2 times inf
+    for T in (3, 40):
+        x = torch.full((T, 64), 2.0 ** 100, dtype=torch.bfloat16, device="cuda")
+        w13 = torch.ones(1, 64, 64, dtype=torch.bfloat16, device="cuda")
+        w2 = torch.ones(1, 64, 32, dtype=torch.bfloat16, device="cuda")
+        w2[0, ::2] = -1
+        got = ops.moe_layer(x, torch.zeros(T, 1, device="cuda"), w13, w2, 1)
+        assert (got[:, ::2] == -float("inf")).all() and (got[:, 1::2] == float("inf")).all()
 
 
 def test_layer_nan_scale_in_a_used_expert(ops):
