@@ -1,17 +1,21 @@
-"""Build libsimgpu.so (host builder + HIP engines) for gfx950 with hipcc.
+"""Build libsimgpu.so (host builder + HIP engines) for gfx950 with hipcc, and
+_ops_torch.so (the operators' binding to torch, no GPU code) with the host
+compiler.
 
-Each source is compiled to an object in parallel, then linked into the
-shared library next to this file."""
+Each source of the library is compiled to an object in parallel, then linked
+into the shared library next to this file."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libsimgpu.so")
+BINDING = os.path.join(HERE, "_ops_torch.so")
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.cpp", "engine_launch.cpp", "engine_wg.hip", "engine_lane.hip", "engine_b1.hip",
            "engine_wave.hip", "engine_wave_rr8.hip", "engine_grid.hip", "engine_res.hip", "engine_route.hip", "noalloc.hip",
@@ -58,17 +62,32 @@ EXTRA = {"engine_res.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=DPP"],
          "engine_lane.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]}
 
 
+def _binding() -> list:
+    """The command that builds the binding to torch."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    include = [os.path.join(at, "include"), sysconfig.get_paths()["include"], os.path.join(rocm, "include")]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+            "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            "-I", os.path.join(ROOT, "include"), *(x for d in include for x in ("-isystem", d)),
+            os.path.join(CSRC, "ops_torch.cpp"), "-o", BINDING + ".tmp",
+            "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+
+
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJDIR, exist_ok=True)
     srcs = [s for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
     objs = [os.path.join(OBJDIR, s + ".o") for s in srcs]
     jobs = [[hipcc, *FLAGS, *EXTRA.get(s, []), "-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(srcs, objs)]
+    jobs.append(_binding())
     with ThreadPoolExecutor(max_workers=min(len(jobs), 8)) as ex:
         list(ex.map(lambda c: _run(c, verbose), jobs))
     tmp = LIB + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB)
+    os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 

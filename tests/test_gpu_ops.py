@@ -537,3 +537,60 @@ def test_other_stream_and_graph(ops, T):
         torch.cuda.synchronize()
         eager = step(ops, *args)
         assert all(torch.equal(a, b) for a, b in zip(held, eager)), i
+
+
+def test_binding_refuses_tensors_that_do_not_fit(ops):
+    from paper_2606_10440_amd.sim import SimError
+    x = torch.randn(4, 64, device="cuda").bfloat16()
+    w, z = ops.mx4_quantize(torch.randn(8, 64, device="cuda")), torch.randn(4, 8, device="cuda")
+    r = ops.moe_route(z, 2)
+    dw, mask = torch.ones(4, 2, device="cuda"), torch.ones(4, 8, dtype=torch.bool, device="cuda")
+    w13, w2 = torch.zeros(8, 32, 64, device="cuda").bfloat16(), torch.zeros(8, 64, 16, device="cuda").bfloat16()
+    Mx4 = ops.Mx4
+    for i, call in enumerate([
+            lambda: ops.mx4_quantize(x.double()), lambda: ops.mx4_quantize(x[:, ::2]), lambda: ops.mx4_quantize(x.cpu()),
+            lambda: ops.mx4_quantize(x[:1].expand(4, 64)), lambda: ops.mx4_quantize(x[0, 0]), lambda: ops.mx4_quantize(None),
+            lambda: ops.mx4_quantize(x[0], transpose=True),
+            lambda: ops.mx4_dequantize(x), lambda: ops.mx4_dequantize(w, torch.float64), lambda: ops.mx4_dequantize(w, "bf16"),
+            lambda: ops.mx4_dequantize(Mx4(w.codes[:, :64], w.scales, w.shape)),
+            lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales, (8, 300))),
+            lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales, (-8, 64))),
+            lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales, (1 << 39, 1 << 39, 64))),
+            lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales, ())), lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales, 8)),
+            lambda: ops.mx4_dequantize(Mx4(w.codes, w.scales.cpu(), w.shape)),
+            lambda: ops.mx4_dequantize(Mx4(w.codes.view(torch.int8), w.scales, w.shape)),
+            lambda: ops.mx4_matmul(x[:, :32], w), lambda: ops.mx4_matmul(x, x), lambda: ops.mx4_matmul(x, w, dtype=torch.int32),
+            lambda: ops.mx4_matmul(x, Mx4(w.codes, w.scales, (2, 4, 64))),
+            lambda: ops.mx4_matmul(Mx4(w.codes, w.scales, (2, 4, 64)), w),
+            lambda: ops.mx4_matmul(x, w, out=torch.empty(4, 9, device="cuda")),
+            lambda: ops.mx4_matmul(w, w, out=torch.empty(8, 8)), lambda: ops.mx4_matmul(x, w, out=z.to(torch.int32)),
+            lambda: ops.mx4_linear_grad(z, x, w2[:, :, 0]), lambda: ops.mx4_linear_grad(z.bfloat16(), x, torch.zeros(8, 64, device="cuda")),
+            lambda: ops.moe_route(z, 0), lambda: ops.moe_route(z, 9), lambda: ops.moe_route(z, 2, mask=mask.float()),
+            lambda: ops.moe_route(z, 2, mask=mask[0, :7]), lambda: ops.moe_route(z, 2, mask=mask.cpu()),
+            lambda: ops.moe_route(z, 2, mask=mask.t().contiguous().t()), lambda: ops.moe_route(z, 2, mask=mask[:3]),
+            lambda: ops.moe_route(torch.zeros(2, 1025, device="cuda"), 2),
+            lambda: ops.moe_route_grad(z, r.experts.long(), dw), lambda: ops.moe_route_grad(z, r.experts, dw.half()),
+            lambda: ops.moe_route_grad(z, r.experts[:3], dw[:3]), lambda: ops.moe_route_grad(z, r.experts, dw.t().contiguous().t()),
+            lambda: ops.moe_route_grad(z, r.order, dw), lambda: ops.moe_route_grad(z, r.experts, dw.cpu()),
+            lambda: ops.moe_layer(x.float(), z, w13, w2, 2), lambda: ops.moe_layer(x[:3], z, w13, w2, 2),
+            lambda: ops.moe_layer(x, z, w13.half(), w2, 2), lambda: ops.moe_layer(x, z, w13, w, 2),
+            lambda: ops.moe_layer(x, z, w13[:, :30].contiguous(), w2, 2), lambda: ops.moe_layer(x, z, w13[:, :, ::2], w2, 2),
+            lambda: ops.moe_layer(x, z[:, :7].contiguous(), w13, w2, 2), lambda: ops.moe_layer(x, z, w13.cpu(), w2, 2),
+            lambda: ops.moe_layer(x, z, w13, w2, 2, out=torch.empty(4, 64, device="cuda")),
+            lambda: ops.moe_layer(x, z, w13, w2, 2, out=x[:, :63])]):
+        with pytest.raises(SimError):
+            call()
+            print("not refused:", i)
+    with pytest.raises(TypeError):
+        ops.moe_route(z, "2")
+    assert torch.equal(ops.mx4_dequantize(Mx4(w.codes, w.scales, torch.Size((2, 4, 64)))).view(8, 64), ops.mx4_dequantize(w))
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 70), (5,), (2, 2, 2, 300), (0, 4, 64)])
+def test_shapes_of_any_rank(ops, shape):
+    x = torch.randn(shape, device="cuda")
+    q = ops.mx4_quantize(x)
+    flat = ops.mx4_quantize(x.reshape(-1, shape[-1]) if x.numel() else x.new_empty(0, shape[-1]))
+    assert type(q) is ops.Mx4 and type(q.shape) is tuple and q.shape == shape
+    assert torch.equal(q.codes, flat.codes) and torch.equal(q.scales, flat.scales)
+    assert ops.mx4_dequantize(q).shape == shape
