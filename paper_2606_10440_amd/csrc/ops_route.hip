@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kChunk = 64;           // tokens of one workgroup
 constexpr int kThreads = 16 * kChunk;
+constexpr int kPart = 16;            // tokens of one where there are few
 constexpr int kScanChunks = 512;     // above it, counts are scanned by a kernel of their own
 
 typedef uint32_t u32_any __attribute__((aligned(1)));
@@ -146,9 +147,9 @@ __host__ __device__ inline int hist_pitch(int E) { return (E + 3) / 4 * 4; }
 __device__ inline void mark(uint64_t *chose, int e, int tok) { atomicOr((unsigned long long *)&chose[e], 1ull << tok); }
 __device__ inline int before_in(uint64_t chose, int tok) { return __popcll(chose & ((1ull << tok) - 1)); }
 
-// Choice and weights; counts of the chunk, or (one chunk only) the lists.
-template <int T, int NV>
-__global__ __launch_bounds__(kThreads) void route_choose(const typename Elem<T>::type *__restrict__ logits, int64_t n_tok,
+// Choice and weights of CH tokens; their counts, or (one chunk only) the lists.
+template <int T, int NV, int CH>
+__global__ __launch_bounds__(16 * CH) void route_choose(const typename Elem<T>::type *__restrict__ logits, int64_t n_tok,
                                                          int E, int64_t stride, const uint8_t *__restrict__ mask,
                                                          int64_t mask_stride, int k, int renorm,
                                                          int32_t *__restrict__ experts, float *__restrict__ weights,
@@ -158,9 +159,9 @@ __global__ __launch_bounds__(kThreads) void route_choose(const typename Elem<T>:
     __shared__ int base[SIM_MOE_MAX_EXPERTS];
     __shared__ int wave_sum[kThreads / 64];
     const int l = threadIdx.x & 15, tok = threadIdx.x >> 4;
-    const int64_t t0 = (int64_t)blockIdx.x * kChunk, t = t0 + tok;
+    const int64_t t = (int64_t)blockIdx.x * CH + tok;
     const bool live = t < n_tok;
-    chose[threadIdx.x] = 0;
+    for (int e = threadIdx.x; e < SIM_MOE_MAX_EXPERTS; e += 16 * CH) chose[e] = 0;
     Keys<T, NV> key;
     float z = 0.f, top = 0.f;
     {
@@ -205,14 +206,14 @@ __global__ __launch_bounds__(kThreads) void route_choose(const typename Elem<T>:
     }
     if (!order) return;
     __syncthreads();
-    const int count = __popcll(chose[threadIdx.x]);
-    if (gridDim.x > 1) {
+    if (CH < kChunk || gridDim.x > 1) {
         // at most kChunk: a byte
-        if ((int)threadIdx.x < hist_pitch(E)) hist[(int64_t)blockIdx.x * hist_pitch(E) + threadIdx.x] = (uint8_t)count;
+        for (int e = threadIdx.x; e < hist_pitch(E); e += 16 * CH)
+            hist[(int64_t)blockIdx.x * hist_pitch(E) + e] = (uint8_t)__popcll(chose[e]);
         return;
     }
     int total;
-    base[threadIdx.x] = block_scan(count, wave_sum, total);
+    base[threadIdx.x] = block_scan(__popcll(chose[threadIdx.x]), wave_sum, total);
     if ((int)threadIdx.x < E) offsets[threadIdx.x] = base[threadIdx.x];
     if (threadIdx.x == 0) offsets[E] = total;
     __syncthreads();
@@ -248,10 +249,11 @@ __global__ __launch_bounds__(kThreads) void route_scan(const uint8_t *__restrict
 }
 
 // Lists of one chunk, from the counts of all (each workgroup adds them up
-// itself) or from the scanned ones.
+// itself; of chunks, or of their parts) or from the scanned ones.
 __global__ __launch_bounds__(kThreads) void route_place(const int32_t *__restrict__ experts, int64_t n_tok, int E, int k,
-                                                        const uint8_t *__restrict__ hist, const int32_t *__restrict__ sums,
-                                                        int32_t *__restrict__ offsets, int32_t *__restrict__ order) {
+                                                        const uint8_t *__restrict__ hist, int parts, int rows,
+                                                        const int32_t *__restrict__ sums, int32_t *__restrict__ offsets,
+                                                        int32_t *__restrict__ order) {
     __shared__ uint64_t chose[SIM_MOE_MAX_EXPERTS];  // in this chunk
     __shared__ int before[SIM_MOE_MAX_EXPERTS];      // slots of the chunks before
     __shared__ int all[SIM_MOE_MAX_EXPERTS];
@@ -274,25 +276,25 @@ __global__ __launch_bounds__(kThreads) void route_place(const int32_t *__restric
             all[t] = sums[(int64_t)chunks * E + t];
         }
     } else {
-        // a thread adds up four experts' bytes over every step-th chunk
+        // a thread adds up four experts' bytes over every step-th row
         const int pitch = hist_pitch(E);
         int width = 4;
         while (width * 4 < pitch) width <<= 1;
         const int e = (t & (width - 1)) * 4, step = kThreads / width;
         if (e < pitch) {
             int a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
-            for (int c = t / width; c < chunks; c += 8 * step) {  // eight loads under way
+            for (int c = t / width; c < rows; c += 8 * step) {  // eight loads under way
                 uint32_t v[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++)
-                    v[i] = c + i * step < chunks ? *(const uint32_t *)(hist + (int64_t)(c + i * step) * pitch + e) : 0;
+                    v[i] = c + i * step < rows ? *(const uint32_t *)(hist + (int64_t)(c + i * step) * pitch + e) : 0;
 #pragma unroll
                 for (int i = 0; i < 8; i++)
 #pragma unroll
                     for (int x = 0; x < 4; x++) {
                         const int n = (v[i] >> (8 * x)) & 255;
                         a[x] += n;
-                        b[x] += c + i * step < chunk ? n : 0;
+                        b[x] += c + i * step < chunk * parts ? n : 0;
                     }
             }
 #pragma unroll
@@ -404,22 +406,40 @@ template <typename F> void with_nv(int E, F &&f) {
     else f(std::integral_constant<int, 64>());
 }
 
+// How many groups of tokens are counted by themselves: those of kPart tokens
+// while these do not yet fill the GPU (119 tokens, k = 8 of 457: 16 us, 24 in
+// groups of 64; 1000, k = 8 of 256: 10.1 and 12.0), but one of 64 where no
+// second launch is needed and the search (registers times k) is not long (64
+// tokens of 512 fp32 experts: 19 and 13.7 us with k = 8, 14 and 11 with k = 4;
+// bf16: 12.6 and 11.5, 10.2 and 10.3).
+inline uint32_t count_rows(int64_t T, int E, int k) {
+    const bool parts = T > kPart && T <= kPart * 256 && (T > kChunk || (E > 256 && k > 4));
+    const int64_t n = parts ? kPart : kChunk;
+    return (uint32_t)((T + n - 1) / n);
+}
+
 inline size_t hist_bytes(size_t chunks, int E) { return (chunks * hist_pitch(E) + 15) / 16 * 16; }
 
 template <int T>
 sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets, int32_t *order,
                    void *ws) {
-    const uint32_t chunks = (uint32_t)((a.T + kChunk - 1) / kChunk);
+    const uint32_t chunks = (uint32_t)((a.T + kChunk - 1) / kChunk), rows = count_rows(a.T, a.E, a.k);
     uint8_t *hist = (uint8_t *)ws;
-    int32_t *sums = chunks > kScanChunks ? (int32_t *)(hist + hist_bytes(chunks, a.E)) : nullptr;
-    with_nv(a.E, [&](auto nv) {
-        route_choose<T, decltype(nv)::value><<<chunks, kThreads, 0, st>>>(
+    int32_t *sums = chunks > kScanChunks ? (int32_t *)(hist + hist_bytes(rows, a.E)) : nullptr;
+    const auto choose = [&](auto nv, auto ch) {
+        constexpr int CH = decltype(ch)::value;
+        route_choose<T, decltype(nv)::value, CH><<<(uint32_t)((a.T + CH - 1) / CH), 16 * CH, 0, st>>>(
             (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts,
             weights, hist, offsets, order);
+    };
+    with_nv(a.E, [&](auto nv) {
+        if (rows > chunks) choose(nv, std::integral_constant<int, kPart>());
+        else choose(nv, std::integral_constant<int, kChunk>());
     });
-    if (order && chunks > 1) {
+    if (order && rows > 1) {
         if (sums) route_scan<<<(a.E + 15) / 16, kThreads, 0, st>>>(hist, sums, (int)chunks, a.E);
-        route_place<<<chunks, kThreads, 0, st>>>(experts, a.T, a.E, a.k, hist, sums, offsets, order);
+        route_place<<<chunks, kThreads, 0, st>>>(experts, a.T, a.E, a.k, hist, rows > chunks ? kChunk / kPart : 1, (int)rows, sums,
+                                                 offsets, order);
     }
     return SIM_OPS_LAUNCH_OK();
 }
@@ -440,10 +460,10 @@ __global__ void no_tokens(int32_t *offsets, int E) {
 
 }  // namespace
 
-size_t route_workspace(int64_t T, int E, int) {
-    const size_t chunks = (size_t)((T + kChunk - 1) / kChunk);
-    if (chunks <= 1) return 0;
-    return hist_bytes(chunks, E) + (chunks > kScanChunks ? (chunks + 1) * (size_t)E * sizeof(int32_t) : 0);
+size_t route_workspace(int64_t T, int E, int k) {
+    const size_t rows = count_rows(T, E, k), chunks = (size_t)((T + kChunk - 1) / kChunk);
+    if (rows <= 1) return 0;
+    return hist_bytes(rows, E) + (chunks > kScanChunks ? (chunks + 1) * (size_t)E * sizeof(int32_t) : 0);
 }
 
 sim_status launch_route(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets,

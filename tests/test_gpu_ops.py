@@ -296,7 +296,7 @@ def check_route(r, want):
 
 
 ROUTES = [(1, 1, 1), (1, 8, 2), (3, 16, 16), (5, 17, 3), (8, 64, 6), (16, 33, 32), (63, 100, 4), (64, 128, 8), (65, 256, 8),
-          (130, 40, 1), (200, 257, 5), (129, 1024, 10), (1000, 60, 4)]
+          (130, 40, 1), (200, 257, 5), (129, 1024, 10), (1000, 60, 4), (17, 300, 6), (64, 513, 32), (4096, 12, 2), (4097, 12, 2)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
