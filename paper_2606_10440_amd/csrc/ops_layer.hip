@@ -228,12 +228,12 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 // its expert, so all experts share one accumulator and nothing has to be
 // joined but the parts of the split contraction.
 //
-// 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 106 us for 459 MB of
-// gates and ups (4.3 TB/s), 68 us for 230 MB of downs (3.4 TB/s, 57 us without
+// 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 101 us for 459 MB of
+// gates and ups (4.5 TB/s), 68 us for 230 MB of downs (3.4 TB/s, 57 us without
 // the hidden values' loads); one token, k = 6 of 64 bf16 experts of 2048 x
-// 1408: 24.5 us for 69 MB, 8.5 of which are the launch, the routing and the
-// epilogue, and 11 us for 35 MB.  The kernels for more tokens take 206, 39
-// and (both small) 20 us where these take 177, 35 and 14.
+// 1408: 23 us for 69 MB, some 7 of which are the launch, the routing and the
+// epilogue, and 12 us for 35 MB.  The kernels for more tokens took 206, 39
+// and (both small) 20 us where these took 177, 35 and 14.
 
 constexpr int kFewTokens = 16;
 constexpr int kFewExperts = 256;
@@ -253,10 +253,7 @@ struct FewPlan {
 constexpr int kFewInputs = 24576;  // bytes of inputs that a workgroup of the first kernel keeps in LDS
 
 struct FewRoute {
-    union {
-        uint32_t key[kFewTokens * kFewExperts];
-        uint8_t inputs[kFewInputs];  // once the choices are made
-    };
+    uint8_t inputs[kFewInputs];
     float weight[kFewTokens * SIM_MOE_MAX_TOPK];
     uint8_t pos[kFewTokens][kFewExperts];  // which choice of the token the expert is
     uint32_t tokens[kFewExperts];          // bit t: token t chose the expert
@@ -264,10 +261,69 @@ struct FewRoute {
     int count[kFewWaves];
 };
 
-__device__ inline float load_logit(const void *p, int type, int64_t i) {
-    if (type == SIM_TYPE_F32) return ((const float *)p)[i];
-    if (type == SIM_TYPE_F16) return (float)((const _Float16 *)p)[i];
-    return (float)((const __bf16 *)p)[i];
+// A token's choices; lane l of its sixteen holds experts l, l + 16, ... in NV
+// registers (16 tokens, k = 8 of 128 bf16 experts of 2048 x 256: the kernel
+// takes 36 us, 40.4 with the keys in LDS).
+template <int NV> __device__ inline void few_choose(const RouteArgs &a, FewRoute &s, int t, int l) {
+    float v[NV];
+    const auto load = [&](const auto *z) {
+#pragma unroll
+        for (int i = 0; i < NV; i++) v[i] = (float)z[t * a.stride + min(l + 16 * i, a.E - 1)];
+    };
+    if (a.type == SIM_TYPE_F32) load((const float *)a.logits);
+    else if (a.type == SIM_TYPE_F16) load((const _Float16 *)a.logits);
+    else load((const __bf16 *)a.logits);
+    uint32_t ok = ~0u;
+    if (a.mask) {
+        uint8_t m[NV];
+#pragma unroll
+        for (int i = 0; i < NV; i++) m[i] = a.mask[t * a.mask_stride + min(l + 16 * i, a.E - 1)];
+        ok = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) ok |= (uint32_t)(m[i] != 0) << i;
+    }
+    uint32_t key[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) key[i] = l + 16 * i < a.E && (ok >> i) & 1 ? order_key(v[i]) : 0;
+
+    float top = 0.f, z = 0.f, w[2];
+    uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};
+    for (int j = 0; j < a.k; j++) {
+        uint32_t bk = 0, bi = 0xffffu;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const bool take = key[i] > bk;
+            bk = take ? key[i] : bk;
+            bi = take ? (uint32_t)(l + 16 * i) : bi;
+        }
+        best16(bk, bi);
+        if (j == 0) {
+            top = key_value(bk);
+            if (!a.renorm) {
+#pragma unroll
+                for (int i = 0; i < NV; i++) z += key[i] ? expf(key_value(key[i]) - top) : 0.f;
+                z = sum16(z);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NV; i++) key[i] = (uint32_t)(l + 16 * i) == bi ? 0 : key[i];
+        if (l == (j & 15)) {
+            if (j < 16) mine[0] = bk, mine_e[0] = bi;
+            else mine[1] = bk, mine_e[1] = bi;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < 2; q++) w[q] = mine[q] ? expf(key_value(mine[q]) - top) : 0.f;
+    if (a.renorm) z = sum16(w[0] + w[1]);
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int j = q * 16 + l;
+        if (j < a.k && mine[q]) {
+            s.weight[t * a.k + j] = w[q] / z;
+            s.pos[t][mine_e[q]] = (uint8_t)j;
+            atomicOr(&s.tokens[mine_e[q]], 1u << t);
+        }
+    }
 }
 
 // All tokens' choices, sixteen threads a token; returns the number of used
@@ -276,50 +332,11 @@ __device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
     const int l = threadIdx.x & 15, t = threadIdx.x >> 4, n_tok = (int)a.T, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     static_assert(64 * kFewWaves == kFewExperts && 4 * kFewWaves == kFewTokens, "a thread for each expert, sixteen for each token");
     s.tokens[threadIdx.x] = 0;
-    uint32_t *key = s.key + t * kFewExperts;
-    if (t < n_tok)
-        for (int e = l; e < a.E; e += 16) {
-            const bool ok = !a.mask || a.mask[t * a.mask_stride + e];
-            key[e] = ok ? order_key(load_logit(a.logits, a.type, t * a.stride + e)) : 0;
-        }
     __syncthreads();
     if (t < n_tok) {
-        float top = 0.f, z = 0.f, w[2] = {0.f, 0.f};
-        uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};
-        for (int j = 0; j < a.k; j++) {
-            uint32_t bk = 0, bi = 0xffffu;
-            for (int e = l; e < a.E; e += 16) {  // a lane's own keys only, its last choice already 0
-                const uint32_t v = key[e];
-                const bool take = v > bk;
-                bk = take ? v : bk;
-                bi = take ? (uint32_t)e : bi;
-            }
-            best16(bk, bi);
-            if (j == 0) {
-                top = key_value(bk);
-                if (!a.renorm) {
-                    for (int e = l; e < a.E; e += 16) z += key[e] ? expf(key_value(key[e]) - top) : 0.f;
-                    z = sum16(z);
-                }
-            }
-            if (bk && (bi & 15) == (uint32_t)l) key[bi] = 0;
-            if (l == (j & 15)) {
-                if (j < 16) mine[0] = bk, mine_e[0] = bi;
-                else mine[1] = bk, mine_e[1] = bi;
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < 2; q++) w[q] = mine[q] ? expf(key_value(mine[q]) - top) : 0.f;
-        if (a.renorm) z = sum16(w[0] + w[1]);
-#pragma unroll
-        for (int q = 0; q < 2; q++) {
-            const int j = q * 16 + l;
-            if (j < a.k && mine[q]) {
-                s.weight[t * a.k + j] = w[q] / z;
-                s.pos[t][mine_e[q]] = (uint8_t)j;
-                atomicOr(&s.tokens[mine_e[q]], 1u << t);
-            }
-        }
+        if (a.E <= 64) few_choose<4>(a, s, t, l);
+        else if (a.E <= 128) few_choose<8>(a, s, t, l);
+        else few_choose<kFewExperts / 16>(a, s, t, l);
     }
     __syncthreads();
     const uint64_t all = __ballot(s.tokens[threadIdx.x] != 0);

@@ -378,7 +378,9 @@ LAYERS = [(1, 4, 2, 64, 32), (1, 8, 8, 200, 70), (2, 5, 1, 33, 17), (7, 16, 3, 2
           (17, 40, 2, 128, 64), (33, 2, 2, 96, 48), (65, 12, 3, 160, 100), (130, 3, 2, 72, 40),
           # rows shorter than one load, ends of rows at every place in a load
           (1, 2, 1, 1, 1), (3, 4, 2, 7, 9), (40, 3, 2, 9, 5), (5, 4, 2, 8, 8), (6, 4, 2, 579, 323), (20, 4, 2, 453, 197),
-          (90, 3, 2, 582, 199), (9, 5, 3, 1100, 716), (110, 2, 2, 77, 510)]
+          (90, 3, 2, 582, 199), (9, 5, 3, 1100, 716), (110, 2, 2, 77, 510),
+          # many experts, many choices
+          (5, 100, 4, 64, 32), (16, 256, 8, 64, 32), (3, 257, 2, 64, 32), (4, 40, 32, 64, 40)]
 
 
 def layer_case(ops, seed, T, E, D, F, kind, weights, pad=0):
