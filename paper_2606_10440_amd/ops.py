@@ -17,14 +17,15 @@ import ctypes as C
 from typing import NamedTuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import sim
 from .sim import SimError
 
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
            "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
-           "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer_workspace",
-           "sim_moe_layer", "sim_ops_last_error")
+           "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route",
+           "sim_moe_route_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
 
@@ -127,17 +128,21 @@ def mx4_linear_grad(dy, x, w, need=(True, True)):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w):
+        if x.dtype != w.dtype:  # the gradient would be refused, a whole forward pass later
+            raise SimError(sim.SIM_ERR_INVALID_ARG, "mx4_linear: x and w must have one type")
         ctx.save_for_backward(x, w)
         return mx4_matmul(x, mx4_quantize(w), dtype=x.dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         return mx4_linear_grad(dy.contiguous(), *ctx.saved_tensors, need=ctx.needs_input_grad)
 
 
 def mx4_linear(x, w):
     """``x @ w.T`` with both put into 4 bits, for training: x [M, K] and w
-    [N, K] get the gradients of ``mx4_linear_grad``."""
+    [N, K], of one type, get the gradients of ``mx4_linear_grad`` (which have
+    none themselves)."""
     return _Linear.apply(x, w)
 
 
@@ -178,6 +183,7 @@ class _RouteWeights(torch.autograd.Function):
         return r.experts, r.weights, r.offsets, r.order
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, _e, dw, _o, _s):
         logits, experts, mask = ctx.saved_tensors
         return moe_route_grad(logits, experts, dw.contiguous(), mask, ctx.renormalize), None, None, None
@@ -193,5 +199,6 @@ def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):
     token x [T, D] goes through the k experts that ``moe_route`` gives it,
     ``w2[e] @ (silu(g) * u)`` with ``g, u = w13[e] @ x`` (w13 [E, 2F, D]: F
     gate rows, then F up rows; w2 [E, D, F]), and gets their weighted sum.  x
-    is float16 or bfloat16; the weights have its type, or are ``Mx4``."""
+    is float16 or bfloat16; the weights have its type, or are ``Mx4``.  For
+    inference: the result carries no gradients."""
     return _c().layer(x, logits, w13, w2, k, mask, renormalize, out)

@@ -158,3 +158,12 @@ def test_binding_refuses_host_tensors(lib):
                  lambda: ops.moe_layer(x, x, x, x, 2)):
         with pytest.raises(SimError):
             call()
+
+
+@pytest.mark.parametrize("x,w", [("bfloat16", "float32"), ("float32", "float16")])
+def test_linear_layer_refuses_types_that_its_gradient_refuses(x, w):
+    import torch
+    from paper_2606_10440_amd import ops
+    from paper_2606_10440_amd.sim import SimError
+    with pytest.raises(SimError, match="one type"):
+        ops.mx4_linear(torch.zeros(2, 32, dtype=getattr(torch, x), requires_grad=True), torch.zeros(4, 32, dtype=getattr(torch, w)))
