@@ -146,8 +146,10 @@ sim_status sim_moe_route_grad(void *hip_stream, const void *logits, int32_t type
  *   (codes in w13, w2 and scales in s13, s2, of E 2 F x D and E D x F);
  *   T <= SIM_MOE_LAYER_MAX_TOKENS.
  * Sums, softmax, silu and the weights are in 32 bits; what passes between
- * the two products is kept to 16 significant bits; y is rounded once.  A
- * token without experts gets zeros.  workspace: sim_moe_layer_workspace
+ * the two products is kept to 16 significant bits, in two parts; y is rounded
+ * once.  An infinity among a token's x or its experts' weights makes the
+ * results that it enters infinite or NaN, and no others.  A token without
+ * experts gets zeros.  workspace: sim_moe_layer_workspace
  * bytes, 16-byte aligned.
  */
 size_t sim_moe_layer_workspace(int64_t T, int64_t D, int32_t E, int32_t k, int64_t F);

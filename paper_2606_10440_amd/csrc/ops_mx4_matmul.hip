@@ -14,7 +14,6 @@
 namespace simops {
 namespace {
 
-//
 // This kernel takes what the others do not: an empty sum, and rows so long
 // that offsets within a tile pass 32 bits.
 template <int T>
@@ -62,9 +61,9 @@ __global__ __launch_bounds__(256) void matmul_simple(const uint8_t *__restrict__
 // scales likewise, for two groups of 256 columns at a time (16 bytes a row),
 // two such pairs ahead.  Past the end the copies repeat the last stage, so
 // that the loop has no branches: it is one run of matrix instructions with
-// everything else dealt out between them.  A stage is two rounds of matrix instructions, and the operands of each round
-// are read from LDS during the round before, the first ones of a stage before
-// its own barrier: that barrier says that the NEXT stage's codes are there.
+// everything else dealt out between them.  A stage is two rounds of matrix
+// instructions, and the operands of each round are read from LDS during the
+// round before, the first ones of a stage before its own barrier: that barrier says that the NEXT stage's codes are there.
 //
 // Of a stage's four blocks half h of the lanes takes blocks 2 h and 2 h + 1.
 // In LDS a row's four 16-byte pieces are permuted by bits 2 and 3 of the row
