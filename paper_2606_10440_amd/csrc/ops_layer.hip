@@ -1019,11 +1019,19 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
     // columns by the tokens of an average expert (lists of 19 of 150 tokens,
     // 4096 x 4096 bf16: 397 us with two column tiles, 482 with one; lists of
     // 98, 2048 x 2710: 137 us with four, 214 with two; 4-bit weights, whose
-    // activations take twice the registers, gain nothing from four)
-    const int64_t mean = r.T * r.k / r.E;
-    if (mean <= 10 || a.D < 8 || a.F < 8) return group_t<T, WT, 1>(st, a, ws);
+    // activations take twice the registers, gain nothing from four), but fewer
+    // where there are so few workgroups that sharing the lists among more of
+    // them gains more than the weights' loads cost: one tile (30 tokens, k = 2
+    // of 2 of 4096 x 512 bf16: 27 us, 33 with two; 60, k = 2 of 4 4-bit ones of
+    // 2048 x 512: 20.5 and 25), or two (160, k = 1 of 4 of 2048 x 2048 fp16:
+    // 50 us, 65 with four; 64, k = 2 of 4 of 1024 x 1024: 23.5 and 30), except
+    // for rows of an odd length, whose loads cost twice (120, k = 4 of 4 of
+    // 3520 x 545 fp16: 86 us, 62 with four)
+    const int64_t mean = r.T * r.k / r.E, tiles = std::min<int64_t>(r.E, r.T * r.k) * ((a.F + 31) / 32);
+    const bool odd = (a.D | a.F) & 1;
+    if (mean <= 10 || a.D < 8 || a.F < 8 || (tiles * ((mean + 31) / 32) <= kSlots / 8 && !odd)) return group_t<T, WT, 1>(st, a, ws);
     if constexpr (WT != SIM_TYPE_MX4)
-        if (mean > 24) return group_t<T, WT, 4>(st, a, ws);
+        if (mean > 24 && (tiles > kSlots / 2 || odd)) return group_t<T, WT, 4>(st, a, ws);
     return group_t<T, WT, 2>(st, a, ws);
 }
 
