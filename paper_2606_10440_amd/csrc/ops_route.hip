@@ -358,7 +358,11 @@ __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *
         ok = load_logits<T, NV>(zt, mt, E, true, all);
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < NV; i++) m = max(m, (ok >> i) & 1 ? order_key(Elem<T>::get(all[i])) : 0u);
+        for (int i = 0; i < NV; i++) {
+            const uint32_t key = (ok >> i) & 1 ? order_key(Elem<T>::get(all[i])) : 0u;
+            m = max(m, key);
+            if (!key) ok &= ~(1ull << i);  // -infinity takes no part, as in the choice: a row of nothing else has no sum
+        }
         top = key_value(max16(m));
 #pragma unroll
         for (int i = 0; i < NV; i++) p[i] = (ok >> i) & 1 ? fast_exp(Elem<T>::get(all[i]) - top) : 0.f;
