@@ -1,6 +1,6 @@
 """Build libsimgpu.so (host builder + HIP engines) for gfx950 with hipcc, and
 _ops_torch.so (the operators' binding to torch, no GPU code) with the host
-compiler.
+compiler, the latter where torch is there.
 
 Each source of the library is compiled to an object in parallel, then linked
 into the shared library next to this file."""
@@ -62,9 +62,13 @@ EXTRA = {"engine_res.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=DPP"],
          "engine_lane.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]}
 
 
-def _binding() -> list:
-    """The command that builds the binding to torch."""
-    import torch
+def _binding() -> list | None:
+    """The command that builds the binding to torch; None where there is no torch."""
+    try:
+        import torch
+    except ImportError:
+        print("no torch: the operators' binding is not built", file=sys.stderr, flush=True)
+        return None
     at = os.path.dirname(torch.__file__)
     rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
     include = [os.path.join(at, "include"), sysconfig.get_paths()["include"], os.path.join(rocm, "include")]
@@ -81,13 +85,16 @@ def build(verbose: bool = False) -> str:
     srcs = [s for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
     objs = [os.path.join(OBJDIR, s + ".o") for s in srcs]
     jobs = [[hipcc, *FLAGS, *EXTRA.get(s, []), "-c", "-o", o, os.path.join(CSRC, s)] for s, o in zip(srcs, objs)]
-    jobs.append(_binding())
+    binding = _binding()
+    if binding:
+        jobs.append(binding)
     with ThreadPoolExecutor(max_workers=min(len(jobs), 8)) as ex:
         list(ex.map(lambda c: _run(c, verbose), jobs))
     tmp = LIB + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB)
-    os.replace(BINDING + ".tmp", BINDING)
+    if binding:
+        os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 
