@@ -11,6 +11,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <c10/util/SmallVector.h>
 #include <torch/csrc/Dtype.h>
@@ -196,13 +197,21 @@ PyObject *dequantize(PyObject *const *a) {  // q, dtype
     return wrap(out);
 }
 
-// A result of type [M, N], given or new.
+// A result of type [M, N], given or new.  One that is given is written behind
+// autograd's back: it must not require a gradient, and written() counts the
+// write, so that a gradient that has saved it is refused.
 struct Result {
     Tensor t;
     Rows r;
+    bool given;
     Result(PyObject *out, int64_t M, int64_t N, at::ScalarType type, c10::Device dev)
-        : t(out == Py_None ? fresh({M, N}, type, dev) : tensor(out, "out")), r(rows_of(t, "out")) {
+        : t(out == Py_None ? fresh({M, N}, type, dev) : tensor(out, "out")), r(rows_of(t, "out")), given(out != Py_None) {
         need(r.rows == M && r.cols == N && r.dev == dev, "out must have the result's sizes and be on the same GPU");
+        need(!given || !t.requires_grad() || !c10::GradMode::is_enabled(), "out must not require a gradient: the result has none");
+    }
+    PyObject *written() const {
+        if (given && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        return wrap(t);
     }
 };
 
@@ -218,14 +227,14 @@ PyObject *matmul(PyObject *const *a) {  // a, b, dtype, out
         need(x.cols == K && x.dev == b.dev, misfit);
         const Result y(a[3], x.rows, N, type, b.dev);
         call(b.dev, g.sim_mx4_matmul, x.codes, x.scales, b.codes, b.scales, x.rows, N, K, y.r.p, y.r.type, y.r.stride);
-        return wrap(y.t);
+        return y.written();
     }
     const Rows x = rows_of(a[0], "a");
     need(x.cols == K && x.dev == b.dev, misfit);
     const Result y(a[3], x.rows, N, type, b.dev);
     const Space ws(g.sim_mx4_linear_workspace(x.rows, N, K), b.dev);
     call(b.dev, g.sim_mx4_linear, x.p, x.type, x.stride, b.codes, b.scales, x.rows, N, K, y.r.p, y.r.type, y.r.stride, ws.p, ws.n);
-    return wrap(y.t);
+    return y.written();
 }
 
 PyObject *linear_grad(PyObject *const *a) {  // dy, x, w, which are wanted: of x, of w
@@ -340,7 +349,7 @@ PyObject *layer(PyObject *const *a) {  // x, logits, w13, w2, k, mask, renormali
     const Space ws(g.sim_moe_layer_workspace(r.T, D, r.E, (int32_t)r.k, F), x.dev);
     call(x.dev, g.sim_moe_layer, x.p, x.type, r.T, D, x.stride, r.z.p, r.z.type, r.E, r.z.stride, r.mask, r.mask_stride,
          (int32_t)r.k, renorm, w13.p, w13.scales, w2.p, w2.scales, w2.type, F, y.r.p, y.r.stride, ws.p, ws.n);
-    return wrap(y.t);
+    return y.written();
 }
 
 // ------------------------------------------------------------------ the module

@@ -10,6 +10,9 @@ tensors' device; results and workspaces come from torch's allocator, so a call
 may be captured into a graph.  Every step runs in the library's HIP kernels;
 there is no host or torch fallback.  Refused arguments raise ``SimError``
 before anything is enqueued.
+
+Results carry no gradients, whatever the arguments require, but those of
+``mx4_linear`` and ``moe_route_train``.  ``out`` must not require one.
 """
 from __future__ import annotations
 
