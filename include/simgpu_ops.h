@@ -12,7 +12,8 @@
  * current device and the call returns.  Argument errors return synchronously
  * and enqueue nothing; sim_ops_last_error has their text.  Sizes of zero are
  * allowed unless a call says otherwise (nothing is enqueued where nothing is
- * to be written).  Strides count elements.  The results of a call depend on its
+ * to be written).  Strides count elements.  What a call writes must not overlap
+ * what it reads, unless it says otherwise.  The results of a call depend on its
  * arguments only: no atomic whose order changes a result is used.
  */
 #ifndef SIMGPU_OPS_H
@@ -149,8 +150,8 @@ sim_status sim_moe_route_grad(void *hip_stream, const void *logits, int32_t type
  * the two products is kept to 16 significant bits, in two parts; y is rounded
  * once.  An infinity among a token's x or its experts' weights makes the
  * results that it enters infinite or NaN, and no others.  A token without
- * experts gets zeros.  workspace: sim_moe_layer_workspace
- * bytes, 16-byte aligned.
+ * experts gets zeros.  y may be x: it is written once x has been read.
+ * workspace: sim_moe_layer_workspace bytes, 16-byte aligned.
  */
 size_t sim_moe_layer_workspace(int64_t T, int64_t D, int32_t E, int32_t k, int64_t F);
 sim_status sim_moe_layer(void *hip_stream, const void *x, int32_t type, int64_t T, int64_t D, int64_t x_stride,

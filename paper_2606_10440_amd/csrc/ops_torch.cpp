@@ -232,6 +232,15 @@ PyObject *matmul(PyObject *const *a) {  // a, b, dtype, out
     const Rows x = rows_of(a[0], "a");
     need(x.cols == K && x.dev == b.dev, misfit);
     const Result y(a[3], x.rows, N, type, b.dev);
+    if (y.given && y.t.is_alias_of(THPVariable_Unpack(a[0]))) {
+        // out may be a itself: then a is read whole before out is written
+        const int64_t groups = (K + 255) / 256;
+        const Tensor codes = fresh({x.rows, groups * 128}, at::kByte, b.dev), scales = fresh({x.rows, groups * 8}, at::kByte, b.dev);
+        uint8_t *const ac = (uint8_t *)codes.data_ptr(), *const as = (uint8_t *)scales.data_ptr();
+        call(b.dev, g.sim_mx4_quantize, x.p, x.type, x.rows, K, x.stride, 0, ac, as);
+        call(b.dev, g.sim_mx4_matmul, ac, as, b.codes, b.scales, x.rows, N, K, y.r.p, y.r.type, y.r.stride);
+        return y.written();
+    }
     const Space ws(g.sim_mx4_linear_workspace(x.rows, N, K), b.dev);
     call(b.dev, g.sim_mx4_linear, x.p, x.type, x.stride, b.codes, b.scales, x.rows, N, K, y.r.p, y.r.type, y.r.stride, ws.p, ws.n);
     return y.written();

@@ -116,7 +116,7 @@ def mx4_matmul(a, b: Mx4, dtype=torch.bfloat16, out=None):
     """``a @ b.T`` with both in 4 bits along their last axis, summed in 32
     bits.  ``a`` [M, K] is an ``Mx4``, or a plain tensor that is put into 4
     bits on the way; ``b`` [N, K]; the result is [M, N] of ``dtype`` (or of
-    ``out``, which may have strided rows)."""
+    ``out``, which may have strided rows, and may be a plain ``a``)."""
     return _c().matmul(a, b, dtype, out)
 
 
@@ -202,6 +202,6 @@ def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):
     token x [T, D] goes through the k experts that ``moe_route`` gives it,
     ``w2[e] @ (silu(g) * u)`` with ``g, u = w13[e] @ x`` (w13 [E, 2F, D]: F
     gate rows, then F up rows; w2 [E, D, F]), and gets their weighted sum.  x
-    is float16 or bfloat16; the weights have its type, or are ``Mx4``.  For
-    inference: the result carries no gradients."""
+    is float16 or bfloat16; the weights have its type, or are ``Mx4``; ``out``
+    may be x.  For inference: the result carries no gradients."""
     return _c().layer(x, logits, w13, w2, k, mask, renormalize, out)
