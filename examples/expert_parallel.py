@@ -61,7 +61,7 @@ def run_step(x, w_router, w13, w2, k, ranks, wire="mx4", lat=50, cap=64):
     routes = ops.moe_route(logits, k)
     if wire == "mx4":
         sent = ops.mx4_quantize(x)
-        lines = moe.lines_of(hidden // 2) + moe.lines_of(hidden // 32)
+        lines = moe.lines_of_token(sent)
         arrived = ops.mx4_dequantize(sent, x.dtype)
     else:
         lines, arrived = moe.lines_of(2 * hidden), x

@@ -19,6 +19,12 @@ def lines_of(n_bytes: int) -> int:
     return -(-n_bytes // LINE_BYTES)
 
 
+def lines_of_token(q) -> int:
+    """Lines that one row of a 4-bit tensor (``ops.Mx4``) takes: its codes,
+    then its scales, as they are stored."""
+    return lines_of(q.codes.shape[1]) + lines_of(q.scales.shape[1])
+
+
 def token_moves(experts, n_experts: int, n_ranks: int):
     """(home, away) endpoint pairs, one for each token and each other endpoint
     that has one of its experts; in token order.  ``experts`` is [T, k], -1
