@@ -81,6 +81,14 @@ constexpr int kDppXor2 = 0x4E;    // quad_perm 2,3,0,1
 constexpr int kDppHalfMirror = 0x141;  // lane i of 8 <-> 7 - i
 constexpr int kDppMirror = 0x140;      // lane i of 16 <-> 15 - i
 
+// Between the writes and the reads of LDS through which the lanes of a wave
+// exchange values: the wave's accesses are in order, and the compiler has to
+// keep them so.  It costs no instruction.
+__device__ inline void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Magnitude bits of 32-bit values order as whole numbers, NaN above infinity,
 // so a block's largest magnitude is a whole-number maximum.
 __device__ inline uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }

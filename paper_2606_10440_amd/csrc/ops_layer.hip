@@ -182,13 +182,10 @@ template <int WT, int CT, bool STAGED> struct Acts {
         const int lane = threadIdx.x & 63;
         return STAGED ? lane % kRowLanes * 8 : step_at<WT>(lane >> 4, s);
     }
-    // Between a step's reads and the next one's writes, and between its
-    // writes and reads: a wave's accesses of LDS are in order, and the
-    // compiler has to keep them so.
+    // between a step's reads and the next one's writes, and between its
+    // writes and reads
     static __device__ void fence() {
-        if (!STAGED) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        if (STAGED) wave_fence();
     }
     __device__ void put(uint8_t *lds) const {
         if (!STAGED) return;

@@ -382,9 +382,11 @@ __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *
         dot += e[q] >= 0 ? g[q] * w[q] : 0.f;
     }
     dot = sum16(dot);
+    wave_fence();  // the zeros are other lanes' than the values, and both than what is read
 #pragma unroll
     for (int q = 0; q < 2; q++)
         if (e[q] >= 0) row[e[q]] = renorm ? w[q] * (g[q] - dot) : g[q];
+    wave_fence();
     El out[NV];
 #pragma unroll
     for (int i = 0; i < NV; i++) {

@@ -66,3 +66,20 @@ def test_training_step_with_a_dropped_token(ops, renorm):  # noqa: F811
     (r.weights * torch.arange(1.0, 4.0, device="cuda")).sum().backward()
     assert (r.experts[4] == -1).all() and (z.grad[4] == 0).all()
     assert torch.isfinite(w.grad).all() and (w.grad != 0).any()
+
+
+@pytest.mark.parametrize("E,k", [(2, 1), (9, 1), (16, 1), (16, 2), (16, 15), (32, 1), (33, 16), (33, 17)])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_gradient_of_experts_held_by_other_lanes_than_the_choice(ops, E, k, renorm):  # noqa: F811
+    # token t's highest logit is expert t's: a choice is handed from the lane of its place to the lane of its expert
+    v = np.random.default_rng(E).permutation(E * E).reshape(E, E) / float(E * E)
+    v[np.arange(E), np.arange(E)] = 2.0
+    z = torch.from_numpy(v).float().cuda()
+    v = z.double().cpu().numpy()
+    want = ref.route(v, k, None, renorm)
+    r = ops.moe_route(z, k, renormalize=renorm)
+    check_route(r, want)
+    g = np.random.default_rng(3).standard_normal((E, k)).astype(np.float32)
+    dz = ops.moe_route_grad(z, r.experts, torch.from_numpy(g).cuda(), renormalize=renorm)
+    wz, bound = ref.route_grad(v, want[0], g.astype(np.float64), None, renorm)
+    check(dz, wz, bound + ref.UNIT["fp32"] * (np.abs(wz) + bound) + ref.TINY["fp32"])
