@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
                 if (sizeof(E) == 2) *(u32x2 *)p = *(u32x2 *)e;
                 else *(u32x4 *)p = *(u32x4 *)e;
             }
-        __builtin_amdgcn_wave_barrier();
+        wave_fence();
         const int64_t m_first = m0 + wave / WN * TM * 32 + i * 32, n = n_wave + lane % LANES * PER;
 #pragma unroll
         for (int k = 0; k < 32; k += 64 / LANES) {
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void matmul_tile(const uint8_t *__
                         if (n + c < N) o[c] = ((const E *)&v)[c];
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        wave_fence();
     }
 }
 
