@@ -90,12 +90,17 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 
 // Sixteen bytes per lane from base + offset to LDS at dst + 16 lane.  The
 // compiler does not count these copies: whoever reads dst waits for them.
+// They leave another value in m0, which it has to know for uses of its own
+// (it warns of m0 since it would not keep a value there for us: none is).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void copy_to_lds(uint32_t dst, const uint8_t *base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "m0");
 }
 __device__ inline void copy4_to_lds(uint32_t dst, const uint8_t *base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "m0");
 }
+#pragma clang diagnostic pop
 // All but the newest N copies (or loads) of this wave have arrived, its LDS
 // accesses are done, and so it is for the other waves.
 template <int N> __device__ inline void wait_and_meet() {
