@@ -80,6 +80,7 @@ __device__ inline void cols_block(uint32_t block, const typename Elem<T>::type *
     }
     // magnitudes of 16-bit values order as whole numbers too: two columns at once
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32_two __attribute__((may_alias));
     uint32_t top[VC];
     if (sizeof(E) == 2) {
         u16x2 m[VC / 2];
@@ -88,7 +89,7 @@ __device__ inline void cols_block(uint32_t block, const typename Elem<T>::type *
             m[j] = u16x2{0, 0};
 #pragma unroll
             for (int i = 0; i < 32; i++)
-                m[j] = __builtin_elementwise_max(m[j], __builtin_bit_cast(u16x2, ((const uint32_t *)v[i])[j] & 0x7fff7fffu));
+                m[j] = __builtin_elementwise_max(m[j], __builtin_bit_cast(u16x2, ((const u32_two *)v[i])[j] & 0x7fff7fffu));
             top[2 * j] = mag((float)__builtin_bit_cast(E16<T>, (uint16_t)m[j][0]));
             top[2 * j + 1] = mag((float)__builtin_bit_cast(E16<T>, (uint16_t)m[j][1]));
         }

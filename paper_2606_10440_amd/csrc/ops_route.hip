@@ -20,13 +20,13 @@ constexpr int kThreads = 16 * kChunk;
 constexpr int kPart = 16;            // tokens of one where there are few
 constexpr int kScanChunks = 512;     // above it, counts are scanned by a kernel of their own
 
-typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint32_t u32_any __attribute__((aligned(1), may_alias));  // words of elements of any type
 
 // N consecutive elements, at any alignment that their type has.
 template <int N, typename E> __device__ inline void load_some(const E *p, E v[N]) {
     if (sizeof(E) * N >= 4) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((uint32_t *)v)[i] = ((const u32_any *)p)[i];
+        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((u32_any *)v)[i] = ((const u32_any *)p)[i];
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++) v[i] = p[i];
@@ -35,7 +35,7 @@ template <int N, typename E> __device__ inline void load_some(const E *p, E v[N]
 template <int N, typename E> __device__ inline void store_some(E *p, const E v[N]) {
     if (sizeof(E) * N >= 4) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((u32_any *)p)[i] = ((const uint32_t *)v)[i];
+        for (int i = 0; i < (int)(sizeof(E) * N / 4); i++) ((u32_any *)p)[i] = ((const u32_any *)v)[i];
     } else {
 #pragma unroll
         for (int i = 0; i < N; i++) p[i] = v[i];
