@@ -36,6 +36,14 @@ bool dims_ok(int64_t rows, int64_t cols) {
     return rows >= 0 && cols >= 0 && rows < kMaxDim && cols < kMaxDim && (cols == 0 || rows <= kMaxElems / (groups_of(cols) * kGroup));
 }
 
+// What the calls take and their workspace queries, which give 0 for what is refused.
+bool linear_fits(int64_t M, int64_t N, int64_t K) { return dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(N, K); }
+bool linear_grad_fits(int64_t M, int64_t N, int64_t K) { return linear_fits(M, N, K) && dims_ok(K, M) && dims_ok(K, N); }
+bool layer_dims_fit(int64_t D, int64_t F) { return D < ((int64_t)1 << 20) && F < ((int64_t)1 << 20); }
+bool layer_tiles_fit(int64_t T, int64_t D, int32_t E, int32_t k, int64_t F) {
+    return std::min<int64_t>(E, T * k) * (std::max(D, F) / 16 + 1) <= kMaxLayerTiles;
+}
+
 #define NEED(cond, why) \
     do { \
         if (!(cond)) return refuse(SIM_ERR_INVALID_ARG, __func__, why); \
@@ -100,7 +108,7 @@ sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a
                           int64_t row_stride) {
     NEED(is_float(type), "out must be f32, f16 or bf16");
     NEED(M >= 0 && N >= 0 && K >= 0, "negative size");
-    FITS(dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(N, K), "matrix too large");
+    FITS(linear_fits(M, N, K), "matrix too large");
     if (M == 0 || N == 0) return done(SIM_OK, __func__);
     NEED(out && (K == 0 || (a_codes && a_scales && b_codes && b_scales)), "null array");
     NEED(M == 1 || row_stride >= N, "row stride below the row length");
@@ -112,7 +120,7 @@ sim_status sim_mx4_matmul(void *stream, const uint8_t *a_codes, const uint8_t *a
 }
 
 size_t sim_mx4_linear_workspace(int64_t M, int64_t N, int64_t K) {
-    if (!dims_ok(M, K) || M == 0 || K == 0 || linear_in_one(M, K)) return 0;
+    if (!linear_fits(M, N, K) || M == 0 || N == 0 || K == 0 || linear_in_one(M, K)) return 0;
     return (size_t)((M * (sim_mx4_code_pitch(K) + sim_mx4_scale_pitch(K)) + 15) / 16 * 16);
 }
 
@@ -121,7 +129,7 @@ sim_status sim_mx4_linear(void *stream, const void *x, int32_t x_type, int64_t x
                           int64_t row_stride, void *workspace, size_t workspace_bytes) {
     NEED(is_float(x_type) && is_float(type), "x and out must be f32, f16 or bf16");
     NEED(M >= 0 && N >= 0 && K >= 0, "negative size");
-    FITS(dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(N, K), "matrix too large");
+    FITS(linear_fits(M, N, K), "matrix too large");
     if (M == 0 || N == 0) return done(SIM_OK, __func__);
     NEED(out && (K == 0 || (x && w_codes && w_scales)), "null array");
     NEED(M == 1 || (x_stride >= K && row_stride >= N), "row stride below the row length");
@@ -146,7 +154,7 @@ static size_t operand_bytes(int64_t R, int64_t C) {
 }
 
 size_t sim_mx4_linear_grad_workspace(int64_t M, int64_t N, int64_t K) {
-    if (M <= 0 || N <= 0 || K <= 0 || M >= kMaxDim || N >= kMaxDim || K >= kMaxDim) return 0;
+    if (!linear_grad_fits(M, N, K) || M == 0 || N == 0 || K == 0) return 0;
     return operand_bytes(M, N) + operand_bytes(K, N) + operand_bytes(N, M) + operand_bytes(K, M);
 }
 
@@ -155,7 +163,7 @@ sim_status sim_mx4_linear_grad(void *stream, int32_t type, const void *dy, int64
                                void *dw, int64_t dw_stride, void *workspace, size_t workspace_bytes) {
     NEED(is_float(type), "dy, x and w must be f32, f16 or bf16");
     NEED(M >= 0 && N >= 0 && K >= 0, "negative size");
-    FITS(dims_ok(M, N) && dims_ok(N, M) && dims_ok(M, K) && dims_ok(K, M) && dims_ok(N, K) && dims_ok(K, N), "matrix too large");
+    FITS(linear_grad_fits(M, N, K), "matrix too large");
     const bool want_x = dx && M > 0 && K > 0, want_w = dw && N > 0 && K > 0;
     if (!want_x && !want_w) return done(SIM_OK, __func__);
     const size_t s = size_of(type);
@@ -221,7 +229,9 @@ sim_status sim_moe_route_grad(void *stream, const void *logits, int32_t type, in
 }
 
 size_t sim_moe_layer_workspace(int64_t T, int64_t D, int32_t E, int32_t k, int64_t F) {
-    if (T <= 0 || T > SIM_MOE_LAYER_MAX_TOKENS || D <= 0 || F < 0 || E < 1 || k < 1 || D >= kMaxDim || F >= kMaxDim) return 0;
+    if (T <= 0 || T > SIM_MOE_LAYER_MAX_TOKENS || D <= 0 || F < 0 || E < 1 || E > SIM_MOE_MAX_EXPERTS || k < 1 || k > E ||
+        k > SIM_MOE_MAX_TOPK || !layer_dims_fit(D, F) || !layer_tiles_fit(T, D, E, k, F))
+        return 0;
     return layer_workspace(T, D, E, k, F);
 }
 
@@ -236,8 +246,8 @@ sim_status sim_moe_layer(void *stream, const void *x, int32_t type, int64_t T, i
     NEED(weight_type == type || weight_type == SIM_TYPE_MX4, "weights must have the type of x or be in 4 bits");
     NEED(D >= 0 && F >= 0, "negative size");
     FITS(T <= SIM_MOE_LAYER_MAX_TOKENS, "too many tokens for one call");
-    FITS(D < ((int64_t)1 << 20) && F < ((int64_t)1 << 20), "matrix too large");
-    FITS(std::min<int64_t>(E, T * k) * (std::max(D, F) / 16 + 1) <= kMaxLayerTiles, "too many experts of that size");
+    FITS(layer_dims_fit(D, F), "matrix too large");
+    FITS(layer_tiles_fit(T, D, E, k, F), "too many experts of that size");
     if (T == 0 || D == 0) return done(SIM_OK, __func__);
     const bool mx4 = weight_type == SIM_TYPE_MX4;
     NEED(x && y && (F == 0 || (w13 && w2)), "null array");
