@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "../../include/simgpu_ops.h"
+#include "ops_forms.h"
 
 namespace simops {
 
@@ -19,12 +20,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-constexpr int kGroup = 256;       // columns to which a 4-bit row is padded
-constexpr int kGroupCodes = 128;  // its bytes of codes
-constexpr int kGroupScales = 8;   // and of scales
-
-__host__ __device__ inline int64_t groups_of(int64_t K) { return (K + kGroup - 1) / kGroup; }
 
 // ---- element types: the value of one element, and one value rounded to the type
 template <int T> struct Elem;
@@ -110,7 +105,7 @@ sim_status launch_dequantize(hipStream_t st, const uint8_t *codes, const uint8_t
                              void *out, int type, int64_t stride);
 sim_status launch_matmul(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs,
                          int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride);
-bool linear_in_one(int64_t M, int64_t K);  // whether launch_linear takes these sizes
+// for sizes that linear_in_one takes
 sim_status launch_linear(hipStream_t st, const void *x, int x_type, int64_t x_stride, const uint8_t *wc, const uint8_t *ws,
                          int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride);
 struct RouteArgs {

@@ -232,8 +232,6 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 // epilogue, and 12 us for 35 MB.  The kernels for more tokens took 206, 39
 // and (both small) 20 us where these took 177, 35 and 14.
 
-constexpr int kFewTokens = 16;
-constexpr int kFewExperts = 256;
 constexpr int kFewWaves = 4;
 constexpr int kFewGroups = 768;  // workgroups: three on each of 256 compute units
 constexpr int kMaxSplits = 16;
@@ -246,8 +244,6 @@ struct FewPlan {
     int16_t *slot;      // [n_used][16]: token's slot, -1
     uint32_t *arrived;  // [tiles of the second kernel]
 };
-
-constexpr int kFewInputs = 24576;  // bytes of inputs that a workgroup of the first kernel keeps in LDS
 
 struct FewRoute {
     uint8_t inputs[kFewInputs];
@@ -379,7 +375,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_up(RouteArgs route, con
         const int e = __builtin_amdgcn_readfirstlane(rt.list[item / tiles]), f0 = item % tiles * 16;
         const uint32_t tokens = rt.tokens[e];
         const bool has = (tokens >> r) & 1;
-        const int pitch = steps * kCols<WT> * 2 + 16;  // so that sixteen rows start in different banks
+        const int pitch = few_input_pitch(D, kCols<WT>);
         if (e != held) {  // the expert's inputs to LDS, where they fit
             held = e;
             in_lds = __popc(tokens) * pitch <= kFewInputs;
@@ -623,7 +619,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
 // activations, and a step is whole cache lines.
 
 constexpr int kWaves = 4;
-constexpr uint32_t kSlots = 512;  // workgroups that run at once: two on each of 256 compute units
 
 // Which expert the a-th non-empty list belongs to; -1 past the last.  The
 // same in every wave.
@@ -891,7 +886,6 @@ __global__ __launch_bounds__(256) void layer_join(const float *__restrict__ part
 }
 
 inline size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
-inline bool few(int64_t T, int E, int64_t D, int64_t F) { return T <= kFewTokens && E <= kFewExperts && D >= 8 && F >= 8; }
 
 // Calls f with the kind of rows of K elements as a constant.  Rows of less
 // than eight are left to the form of one column tile for more tokens.
@@ -1012,23 +1006,13 @@ template <int T, int WT> sim_status layer_t(hipStream_t st, const LayerArgs &a, 
         layer_zero<T><<<(uint32_t)r.T, 256, 0, st>>>((typename Elem<T>::type *)a.y, a.y_stride, a.D);
         return SIM_OPS_LAUNCH_OK();
     }
-    if (few(r.T, r.E, a.D, a.F)) return few_t<T, WT>(st, a, ws);
-    // columns by the tokens of an average expert (lists of 19 of 150 tokens,
-    // 4096 x 4096 bf16: 397 us with two column tiles, 482 with one; lists of
-    // 98, 2048 x 2710: 137 us with four, 214 with two; 4-bit weights, whose
-    // activations take twice the registers, gain nothing from four), but fewer
-    // where there are so few workgroups that sharing the lists among more of
-    // them gains more than the weights' loads cost: one tile (30 tokens, k = 2
-    // of 2 of 4096 x 512 bf16: 27 us, 33 with two; 60, k = 2 of 4 4-bit ones of
-    // 2048 x 512: 20.5 and 25), or two (160, k = 1 of 4 of 2048 x 2048 fp16:
-    // 50 us, 65 with four; 64, k = 2 of 4 of 1024 x 1024: 23.5 and 30), except
-    // for rows of an odd length, whose loads cost twice (120, k = 4 of 4 of
-    // 3520 x 545 fp16: 86 us, 62 with four)
-    const int64_t mean = r.T * r.k / r.E, tiles = std::min<int64_t>(r.E, r.T * r.k) * ((a.F + 31) / 32);
-    const bool odd = (a.D | a.F) & 1;
-    if (mean <= 10 || a.D < 8 || a.F < 8 || (tiles * ((mean + 31) / 32) <= kSlots / 8 && !odd)) return group_t<T, WT, 1>(st, a, ws);
-    if constexpr (WT != SIM_TYPE_MX4)
-        if (mean > 24 && (tiles > kSlots / 2 || odd)) return group_t<T, WT, 4>(st, a, ws);
+    switch (layer_form(r.T, r.E, r.k, a.D, a.F, a.mx4)) {
+        case kFew: return few_t<T, WT>(st, a, ws);
+        case kGroup1: return group_t<T, WT, 1>(st, a, ws);
+        case kGroup4:
+            if constexpr (WT != SIM_TYPE_MX4) return group_t<T, WT, 4>(st, a, ws);  // (4-bit weights never take it)
+        case kGroup2: break;
+    }
     return group_t<T, WT, 2>(st, a, ws);
 }
 

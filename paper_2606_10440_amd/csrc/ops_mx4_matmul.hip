@@ -306,10 +306,7 @@ void launch_tile(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uin
 // into 4 bits first if they are not (XT): a launch less, worth it for a few
 // (4 x 8192 x 4096: 8.2 us either way; 8 rows: 11.1 us against 8.5).
 // 1 x 8192 x 4096: 5.7 us, 3.1 TB/s, of which some 2.5 us are the launch.
-constexpr int kSkinnyRows = 32;
-constexpr int kSkinnyLds[2] = {49152, 147456};  // bytes of A: three workgroups on a compute unit, or one
 constexpr int kSkinnyWaves = 8;
-constexpr int64_t kOwnQuantize = 16384;  // elements
 
 template <int T, int XT, int R, int MT, int LDS>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *__restrict__ x, const uint8_t *__restrict__ xs,
@@ -440,9 +437,6 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void matmul_skinny(const void *_
     }
 }
 
-inline size_t skinny_lds(int64_t M, int64_t K) { return (size_t)(M * (groups_of(K) * (kGroupCodes + kGroupScales) + 16)); }
-inline bool skinny(int64_t M, int64_t K) { return M <= kSkinnyRows && K > 0 && K < (1 << 20) && skinny_lds(M, K) <= kSkinnyLds[1]; }
-
 template <int T, int XT>
 void skinny_t(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride, const uint8_t *bc, const uint8_t *bs,
               int64_t M, int64_t N, int64_t K, void *out, int64_t stride) {
@@ -469,30 +463,17 @@ void skinny_t(hipStream_t st, const void *x, const uint8_t *xs, int64_t x_stride
 template <int T>
 sim_status matmul_t(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uint8_t *bc, const uint8_t *bs, int64_t M,
                     int64_t N, int64_t K, void *out, int64_t stride) {
-    if (skinny(M, K)) {
-        skinny_t<T, SIM_TYPE_MX4>(st, ac, as, 0, bc, bs, M, N, K, out, stride);
-        return SIM_OPS_LAUNCH_OK();
+    switch (product_form(M, N, K)) {
+        case kSkinnySmall:
+        case kSkinnyLarge: skinny_t<T, SIM_TYPE_MX4>(st, ac, as, 0, bc, bs, M, N, K, out, stride); break;
+        case kTile256x256: launch_tile<T, 2, 2, 4, 4>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+        case kTile128x128: launch_tile<T, 2, 2, 2, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+        case kTile64x128: launch_tile<T, 2, 2, 1, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+        case kTile64x64: launch_tile<T, 2, 2, 1, 1>(st, ac, as, bc, bs, M, N, K, out, stride); break;
+        case kSimple:
+            matmul_simple<T><<<(uint32_t)(((M + 63) / 64) * ((N + 63) / 64)), 256, 0, st>>>(
+                ac, as, bc, bs, M, N, (int)groups_of(K), (typename Elem<T>::type *)out, stride);
     }
-    if (K > 0 && K < (1 << 23)) {  // offsets within a tile fit in 32 bits
-        // The tile by what 256 of it at a time cost, in microseconds for 4096
-        // columns (measured, beside some 4 for each launch: 64 tiles or 256 of
-        // a kind take the same time; 4096 x 4096 in 256 tiles of 256 x 256
-        // 43 us, in 1024 of 128 x 128 54; 333 x 5001 x 2056 9.1, 11.1 and 11.3
-        // us in tiles of 64 x 128, 64 x 64 and 128 x 128).
-        const auto cost = [&](int64_t bm, int64_t bn, double each) {
-            return (double)((((M + bm - 1) / bm) * ((N + bn - 1) / bn) + 255) / 256) * each;
-        };
-        const double c[4] = {cost(256, 256, 38.), cost(128, 128, 12.5), cost(64, 128, 9.2), cost(64, 64, 6.6)};
-        switch (std::min_element(c, c + 4) - c) {
-            case 0: launch_tile<T, 2, 2, 4, 4>(st, ac, as, bc, bs, M, N, K, out, stride); break;
-            case 1: launch_tile<T, 2, 2, 2, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
-            case 2: launch_tile<T, 2, 2, 1, 2>(st, ac, as, bc, bs, M, N, K, out, stride); break;
-            default: launch_tile<T, 2, 2, 1, 1>(st, ac, as, bc, bs, M, N, K, out, stride); break;
-        }
-        return SIM_OPS_LAUNCH_OK();
-    }
-    const uint32_t grid = (uint32_t)(((M + 63) / 64) * ((N + 63) / 64));
-    matmul_simple<T><<<grid, 256, 0, st>>>(ac, as, bc, bs, M, N, (int)groups_of(K), (typename Elem<T>::type *)out, stride);
     return SIM_OPS_LAUNCH_OK();
 }
 
@@ -506,9 +487,6 @@ sim_status linear_t(hipStream_t st, const void *x, int x_type, int64_t x_stride,
 }
 
 }  // namespace
-
-// A launch less where every workgroup can put the few rows into 4 bits itself.
-bool linear_in_one(int64_t M, int64_t K) { return skinny(M, K) && M * K <= kOwnQuantize; }
 
 sim_status launch_linear(hipStream_t st, const void *x, int x_type, int64_t x_stride, const uint8_t *wc, const uint8_t *ws,
                          int64_t M, int64_t N, int64_t K, void *out, int type, int64_t stride) {
