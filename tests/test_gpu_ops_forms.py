@@ -1,13 +1,14 @@
 """Each form of the operators' kernels, at sizes that run it (which size runs
 which form is checked on the CPU, ``test_ops_forms``): products by whole
 numbers, whose every partial sum is exact, so that each element, scale and
-stage shows."""
+stage shows; the few tokens' layer with its inputs in LDS and past it."""
 from __future__ import annotations
 
 import numpy as np
 import pytest
 
-from tests.test_gpu_ops import TYPES, ops  # noqa: F401 (ops: the fixture)
+from tests import ops_reference as ref
+from tests.test_gpu_ops import TYPES, check, layer_case, ops  # noqa: F401 (ops: the fixture)
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -82,3 +83,35 @@ def test_nan_stays_in_its_row_and_column(ops, form):  # noqa: F811
     bad = torch.zeros(M, N, dtype=torch.bool, device="cuda")
     bad[M - 2], bad[:, 37] = True, True
     assert torch.equal(torch.isnan(got), bad)
+
+
+# ------------------------------------------------------------------ the layer for few tokens
+
+# T, E, k, D, F: all tokens go to the first k - 1 experts, the last choice is spread over the others
+PAST_LDS = [(16, 3, 2, 2053, 70), (16, 2, 2, 1024, 96), (12, 5, 3, 1216, 41), (9, 4, 2, 4096, 33), (16, 16, 4, 1029, 900)]
+COLS = {"same": 64, "mx4": 128}  # columns of a step
+
+
+def spread(T, E, k, turned):
+    """Logits with that choice; turned: the common experts are the last ones, so that other workgroups meet them."""
+    z = np.random.default_rng(7).standard_normal((T, E)) * 0.1
+    z[:, :k - 1] += 4.0
+    z[np.arange(T), k - 1 + np.arange(T) % (E - k + 1)] += 2.0
+    return (z[:, ::-1] if turned else z).copy()
+
+
+def tokens_of_experts(z, k):
+    top = np.argsort(-z, axis=1, kind="stable")[:, :k]
+    return np.bincount(top.reshape(-1), minlength=z.shape[1])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+@pytest.mark.parametrize("weights", ["same", "mx4"])
+@pytest.mark.parametrize("case", PAST_LDS)
+@pytest.mark.parametrize("turned", [False, True])
+def test_layer_inputs_past_lds(ops, kind, weights, case, turned):  # noqa: F811
+    T, E, k, D, F = case
+    (x, _, w13, w2), (vx, _, v13, v2) = layer_case(ops, 90, T, E, D, F, kind, weights, pad=3)
+    z = torch.from_numpy(spread(T, E, k, turned)).float()
+    got = ops.moe_layer(x, z.cuda(), w13, w2, k)
+    check(got, *ref.layer(vx, z.double().numpy(), v13, v2, k, None, True, kind))

@@ -10,6 +10,7 @@ import subprocess
 import pytest
 
 from tests import test_gpu_ops_forms as forms
+from tests import test_gpu_ops_layer_tiles as layer_tiles
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -58,3 +59,22 @@ def test_products_run_the_form_they_are_for(ask):
 def test_linear_layers_of_one_launch(ask):
     assert set(ask("one", forms.IN_ONE)) == {"one"}
     assert ask("one", [(2, 70, 8193), (33, 70, 64), (1, 33, 16385)]) == ["two"] * 3
+
+
+@pytest.mark.parametrize("weights", ["same", "mx4"])
+def test_few_tokens_inputs_in_lds_and_past_it(ask, weights):
+    cols = forms.COLS[weights]
+    both = 0
+    for T, E, k, D, F in forms.PAST_LDS:
+        assert ask("layer", [(T, E, k, D, F, weights == "mx4")]) == ["0"]
+        n = [c for c in forms.tokens_of_experts(forms.spread(T, E, k, False), k) if c]
+        kinds = ask("inputs", [(c, D, cols) for c in n])
+        assert "past" in kinds
+        both += "lds" in kinds
+    assert both
+
+
+def test_layer_tilings(ask):
+    want = [2] * 4 + [4] * 4 + [1] * 3
+    assert [int(v) for v in ask("layer", [(*c, False) for c in layer_tiles.CASES])] == want
+    assert [int(v) for v in ask("layer", [(*c, True) for c in layer_tiles.CASES])] == [min(v, 2) for v in want]
