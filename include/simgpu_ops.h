@@ -2,7 +2,7 @@
  * simgpu operators -- what an expert-parallel step computes beside the
  * traffic that simgpu.h simulates: 4-bit microscaled tensors and their
  * product, the router with the experts' token lists, and the experts' layer
- * for few tokens.
+ * for few tokens, all experts on one GPU.
  *
  * C ABI of libsimgpu.so, in the manner of simgpu.h: every call returns a
  * sim_status, no C++ exception crosses the boundary, all array arguments are
@@ -140,7 +140,10 @@ sim_status sim_moe_route_grad(void *hip_stream, const void *logits, int32_t type
 /*
  * The experts' layer for few tokens, from the router's logits:
  *   y_t = sum over the chosen experts e of  w_te W2_e (silu(G_e x_t) * (U_e x_t))
- * with experts and weights chosen as by sim_moe_route.
+ * with experts chosen as by sim_moe_route, and its weights to within a few
+ * units in the last place (for few tokens a kernel of its own computes them,
+ * in another order).  The sum runs over all E experts that are routed to, so
+ * the call needs the weights of all of them.
  *   x [T, D], y [T, D] of type (F16 or BF16), row strides x_stride, y_stride;
  *   w13 [E, 2 F, D]: the F rows of G_e, then the F rows of U_e; w2 [E, D, F];
  *   weight_type: type (both contiguous, s13 = s2 = NULL), or SIM_TYPE_MX4

@@ -225,11 +225,12 @@ __device__ inline void store_hidden(__bf16 *h_hi, __bf16 *h_lo, int64_t at, cons
 // its expert, so all experts share one accumulator and nothing has to be
 // joined but the parts of the split contraction.
 //
-// 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 101 us for 459 MB of
-// gates and ups (4.5 TB/s), 68 us for 230 MB of downs (3.4 TB/s, 57 us without
-// the hidden values' loads); one token, k = 6 of 64 bf16 experts of 2048 x
-// 1408: 23 us for 69 MB, some 7 of which are the launch, the routing and the
-// epilogue, and 12 us for 35 MB.  The kernels for more tokens took 206, 39
+// 16 tokens, k = 8 of 128 4-bit experts of 4096 x 1280: 102 to 112 us for 459
+// MB of gates and ups (4.1 to 4.5 TB/s), 68 to 76 us for 230 MB of downs (3.0
+// to 3.4 TB/s, 57 us without the hidden values' loads); one token, k = 6 of 64
+// bf16 experts of 2048 x 1408: 22 us for 69 MB that the caches still hold, 25
+// from memory, some 7 of which are the launch, the routing and the epilogue,
+// and 12 to 13 us for 35 MB.  The kernels for more tokens took 206, 39
 // and (both small) 20 us where these took 177, 35 and 14.
 
 constexpr int kFewWaves = 4;
@@ -611,10 +612,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 3) void few_down(const __bf16 *__re
 // time as columns.  The second product leaves one row per slot, and a last
 // kernel adds a token's rows up.
 //
-// 150 tokens, k = 2 of 16 bf16 experts of 4096 x 4096: 210 us for 913 MB of
-// gates and ups, 121 us for 456 MB of downs (4.3 and 3.8 TB/s; a last round of
-// workgroups that is half full); 64 tokens, k = 4 of 32 of 4096 x 2048: 303 us
-// in all, 5.3 TB/s.  What bounds them beside memory are cache accesses, one
+// 150 tokens, k = 2 of 16 bf16 experts of 4096 x 4096, three of them masked: 179
+// us for 872 MB of gates and ups, 109 us for 436 MB of downs (4.9 and 4.0
+// TB/s; a last round of workgroups that is half full); 64 tokens, k = 4 of 32
+// of 4096 x 2048: 298 us in all, 5.4 TB/s.  A list that is longer than the
+// others runs on while these are done: all tokens' first choice one expert,
+// 426 us in place of 380 (150 tokens, no mask).  What bounds them beside memory are cache accesses, one
 // for every lane's sixteen bytes: so several rows of weights share a load of
 // activations, and a step is whole cache lines.
 

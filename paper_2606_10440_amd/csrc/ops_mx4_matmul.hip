@@ -76,8 +76,8 @@ __global__ __launch_bounds__(256) void matmul_simple(const uint8_t *__restrict__
 // results of 32 rows go through LDS once more to be stored sixteen bytes a
 // lane.
 //
-// 8192 x 8192 x 8192 to bf16: 278 to 295 us, 3.7 to 3.9 PFLOP/s; 4096 x 4096 x
-// 4096: 43 us, 3.2 PFLOP/s.  The matrix units are busy 53 % of the cycles, at
+// 8192 x 8192 x 8192 to bf16: 272 to 303 us, 3.6 to 4.0 PFLOP/s; 4096 x 4096 x
+// 4096: 44 to 46 us, 3.0 to 3.1 PFLOP/s.  The matrix units are busy 53 % of the cycles, at
 // a clock that their load has brought down to 1.77 GHz; the same loop without
 // its copies takes 215 us, without its operand reads 251.
 constexpr int kStageCodes = 64;  // bytes of a row
@@ -305,7 +305,8 @@ void launch_tile(hipStream_t st, const uint8_t *ac, const uint8_t *as, const uin
 // block l / 16 of 128 columns.  The rows of A lie in LDS, where they are put
 // into 4 bits first if they are not (XT): a launch less, worth it for a few
 // (4 x 8192 x 4096: 8.2 us either way; 8 rows: 11.1 us against 8.5).
-// 1 x 8192 x 4096: 5.7 us, 3.1 TB/s, of which some 2.5 us are the launch.
+// 1 x 8192 x 4096: 5.7 us where the caches hold B (3.1 TB/s), 7.4 us from
+// memory, of which some 2.5 us are the launch.
 constexpr int kSkinnyWaves = 8;
 
 template <int T, int XT, int R, int MT, int LDS>

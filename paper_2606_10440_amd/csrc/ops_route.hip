@@ -9,7 +9,7 @@
 // 16385 tokens, 256 bf16 experts, a mask of its own for each token, k = 8:
 // choice 11 us (k searches of 16 registers a lane, 1.1 TB/s), lists 8.7 us (a
 // workgroup reads the 66 KB of all chunks' counts), gradient 8 us; 8 tokens,
-// 64 experts: 4.7 us in one launch.
+// 64 experts: 4.5 us in one launch.
 #include "ops_route_keys.h"
 
 namespace simops {
