@@ -1,8 +1,9 @@
 /*
  * simgpu operators -- what an expert-parallel step computes beside the
- * traffic that simgpu.h simulates: 4-bit microscaled tensors and their
- * product, the router with the experts' token lists, and the experts' layer
- * for few tokens, all experts on one GPU.
+ * traffic that simgpu.h simulates: attention over a paged key-value cache,
+ * 4-bit microscaled tensors and their product, the router with the experts'
+ * token lists, the experts' layer for few tokens, all experts or a share of
+ * them on one GPU, and the choice of the next token.
  *
  * C ABI of libsimgpu.so, in the manner of simgpu.h: every call returns a
  * sim_status, no C++ exception crosses the boundary, all array arguments are
@@ -162,6 +163,55 @@ sim_status sim_moe_layer(void *hip_stream, const void *x, int32_t type, int64_t 
                          const uint8_t *mask, int64_t mask_stride, int32_t k, int32_t renormalize, const void *w13,
                          const uint8_t *s13, const void *w2, const uint8_t *s2, int32_t weight_type, int64_t F,
                          void *y, int64_t y_stride, void *workspace, size_t workspace_bytes);
+
+/*
+ * A paged key-value cache: keys and values are arrays of pages, page p of
+ * [kv_heads, page_size, D] elements, contiguous, at p * page_stride elements
+ * (the two may be parts of one buffer).  type is F16 or BF16; D a multiple of
+ * 8 up to SIM_CACHE_MAX_D; arrays 16-byte aligned, page strides multiples of 8.
+ *
+ * Write the rows k and v [T, kv_heads, D] of T tokens into it: token t goes to
+ * place slots[t] % page_size of page slots[t] / page_size.  A slot outside the
+ * cache is skipped, and so is its token.  Tokens must differ in their slots:
+ * where two have the same, each 16 bytes that it holds after the call are of
+ * one of them.  Strides between tokens and heads count elements; a row of D is
+ * contiguous and may lie anywhere its type may.
+ */
+#define SIM_CACHE_MAX_D 256
+sim_status sim_cache_append(void *hip_stream, int32_t type, const void *k, int64_t k_stride, int64_t k_head_stride,
+                            const void *v, int64_t v_stride, int64_t v_head_stride, int64_t T, int32_t kv_heads, int32_t D,
+                            const int64_t *slots, void *k_cache, int64_t k_page_stride, void *v_cache,
+                            int64_t v_page_stride, int64_t pages, int32_t page_size);
+
+/*
+ * Attention of one new token of each of B sequences over the cache:
+ *   out[b, h] = sum over j of p_j V_j,  p = softmax over j of (scale q[b, h] . K_j),
+ * K_j and V_j the rows of kv head h / (q_heads / kv_heads) of token j of the
+ * sequence: place j % page_size of page table[b, j / page_size], for
+ *   max(0, n - window) <= j < n = lengths[b]  (window 0: from 0 on).
+ * lengths count the new token where its row is in the cache; below 0 they
+ * count as 0, above table_pages * page_size (at most 2^30) as that.  Tokens on
+ * a page that is not one of the cache's (-1 say) are left out, and so is a
+ * score of -infinity; where nothing is left, out is 0.  What other places of
+ * the cache hold has no effect.  Scores, weights and sums are in 32 bits (the
+ * products' operands: q, K and V as they are, the weights in two parts of type).
+ * An infinity among the V makes the results that it enters infinite or NaN, and
+ * no others.
+ *   q, out [B, q_heads, D] of type, out's heads contiguous; kv_heads divides
+ *   q_heads; table [B, table_pages] i32; lengths [B] i32;
+ *   lse NULL or [B, q_heads] f32: log of the sum over j of e^(scale q . K_j),
+ *   -infinity where nothing is left; by it, parts of a sequence that different
+ *   calls attend to can be joined.
+ * workspace: sim_cache_attention_workspace bytes, 16-byte aligned (NULL if 0).
+ */
+size_t sim_cache_attention_workspace(int64_t B, int32_t q_heads, int32_t kv_heads, int32_t D, int32_t table_pages,
+                                     int32_t page_size, int32_t window);
+sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, int64_t q_stride, int64_t q_head_stride,
+                               int64_t B, int32_t q_heads, int32_t kv_heads, int32_t D, const void *k_cache,
+                               int64_t k_page_stride, const void *v_cache, int64_t v_page_stride, int64_t pages,
+                               int32_t page_size, const int32_t *table, int64_t table_stride, int32_t table_pages,
+                               const int32_t *lengths, float scale, int32_t window, void *out, int64_t out_stride,
+                               float *lse, void *workspace, size_t workspace_bytes);
 
 /* Text of this thread's last refused or failed operator call ("" if none). */
 const char *sim_ops_last_error(void);

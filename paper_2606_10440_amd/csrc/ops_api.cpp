@@ -1,6 +1,7 @@
 // C entry points of the operators: every argument is checked here, before
 // anything is enqueued; the launchers rely on what passed.
 #include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "ops_common.h"
@@ -264,6 +265,100 @@ sim_status sim_moe_layer(void *stream, const void *x, int32_t type, int64_t T, i
     a.w13 = w13, a.w2 = w2, a.s13 = s13, a.s2 = s2, a.mx4 = mx4, a.F = F;
     a.y = y, a.y_stride = y_stride;
     return done(launch_layer((hipStream_t)stream, a, workspace), __func__);
+}
+
+namespace {
+constexpr int64_t kMaxKeys = (int64_t)1 << 30;  // of one sequence
+constexpr int64_t kMaxGroups = (int64_t)1 << 31;  // workgroups of one launch
+
+// what the cache's users check alike
+const char *cache_bad(int32_t type, int32_t kv_heads, int32_t D, const void *k, int64_t k_page_stride, const void *v,
+                      int64_t v_page_stride, int64_t pages, int32_t page_size) {
+    if (type != SIM_TYPE_F16 && type != SIM_TYPE_BF16) return "the cache must be f16 or bf16";
+    if (kv_heads < 1) return "kv_heads must be positive";
+    if (D < 8 || D > SIM_CACHE_MAX_D || D % 8) return "D must be a multiple of 8 up to 256";
+    if (pages < 0 || page_size < 1) return "bad page count or size";
+    if (pages > 0 && (!k || !v)) return "null cache";
+    if (!aligned_to(k, 16) || !aligned_to(v, 16) || k_page_stride % 8 || v_page_stride % 8)
+        return "the cache must be 16-byte aligned, its page strides multiples of 8";
+    if (pages > 1 && (k_page_stride / D / kv_heads < page_size || v_page_stride / D / kv_heads < page_size))
+        return "page stride below the page";
+    return nullptr;
+}
+bool cache_fits(int32_t kv_heads, int64_t pages, int32_t page_size) {
+    return kv_heads <= 65536 && pages < kMaxDim && (int64_t)page_size * kv_heads < kMaxDim;
+}
+bool attention_fits(int64_t B, int32_t q_heads, int32_t kv_heads, int32_t D, int32_t table_pages, int32_t page_size, int32_t window) {
+    if (B < 1 || B >= kMaxDim || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || q_heads > 65536 || D < 8 ||
+        D > SIM_CACHE_MAX_D || D % 8 || table_pages < 0 || page_size < 1 || window < 0 ||
+        (int64_t)table_pages * page_size > kMaxKeys)
+        return false;
+    const int64_t tiles = attend_tiles(q_heads / kv_heads, D), units = attend_units(kv_heads * tiles);
+    return (attend_max_units(B, units, (int64_t)table_pages * page_size, window) * kv_heads + 8) * tiles < kMaxGroups / 256 &&
+           B * q_heads < kMaxGroups / 256;  // (a launch has 2^32 threads at most)
+}
+}  // namespace
+
+sim_status sim_cache_append(void *stream, int32_t type, const void *k, int64_t k_stride, int64_t k_head_stride, const void *v,
+                            int64_t v_stride, int64_t v_head_stride, int64_t T, int32_t kv_heads, int32_t D,
+                            const int64_t *slots, void *k_cache, int64_t k_page_stride, void *v_cache, int64_t v_page_stride,
+                            int64_t pages, int32_t page_size) {
+    if (const char *why = cache_bad(type, kv_heads, D, k_cache, k_page_stride, v_cache, v_page_stride, pages, page_size))
+        return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    NEED(T >= 0, "negative token count");
+    FITS(cache_fits(kv_heads, pages, page_size) && T < kMaxDim, "too large");
+    NEED(k_stride >= 0 && k_head_stride >= 0 && v_stride >= 0 && v_head_stride >= 0, "negative stride");
+    if (T == 0 || pages == 0) return done(SIM_OK, __func__);
+    NEED(k && v && slots, "null array");
+    NEED(aligned_to(k, 2) && aligned_to(v, 2) && aligned_to(slots, 8), "array not aligned to its type");
+    const AppendArgs a = {k, v, k_stride, k_head_stride, v_stride, v_head_stride, T, kv_heads, D, slots, k_cache, v_cache,
+                          k_page_stride, v_page_stride, pages, page_size};
+    return done(launch_append((hipStream_t)stream, a), __func__);
+}
+
+size_t sim_cache_attention_workspace(int64_t B, int32_t q_heads, int32_t kv_heads, int32_t D, int32_t table_pages,
+                                     int32_t page_size, int32_t window) {
+    if (!attention_fits(B, q_heads, kv_heads, D, table_pages, page_size, window)) return 0;
+    const int64_t capacity = (int64_t)table_pages * page_size;
+    if (!attend_splits(capacity, window)) return 0;
+    const int64_t units = attend_units((int64_t)kv_heads * attend_tiles(q_heads / kv_heads, D));
+    return (size_t)((attend_max_units(B, units, capacity, window) * q_heads * (D + 2) * 4 + 15) / 16 * 16);
+}
+
+sim_status sim_cache_attention(void *stream, int32_t type, const void *q, int64_t q_stride, int64_t q_head_stride, int64_t B,
+                               int32_t q_heads, int32_t kv_heads, int32_t D, const void *k_cache, int64_t k_page_stride,
+                               const void *v_cache, int64_t v_page_stride, int64_t pages, int32_t page_size,
+                               const int32_t *table, int64_t table_stride, int32_t table_pages, const int32_t *lengths,
+                               float scale, int32_t window, void *out, int64_t out_stride, float *lse, void *workspace,
+                               size_t workspace_bytes) {
+    if (const char *why = cache_bad(type, kv_heads, D, k_cache, k_page_stride, v_cache, v_page_stride, pages, page_size))
+        return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    NEED(B >= 0 && table_pages >= 0 && window >= 0, "negative size");
+    NEED(q_heads >= 1 && q_heads % kv_heads == 0, "kv_heads must divide q_heads");
+    NEED(std::isfinite(scale), "scale must be finite");
+    NEED(q_stride >= 0 && q_head_stride >= 0 && table_stride >= 0, "negative stride");
+    FITS((int64_t)table_pages * page_size <= kMaxKeys, "a row of the table has room for more than 2^30 tokens");
+    if (B == 0) return done(SIM_OK, __func__);
+    FITS(cache_fits(kv_heads, pages, page_size) && attention_fits(B, q_heads, kv_heads, D, table_pages, page_size, window), "too large");
+    NEED(q && out && lengths && (table_pages == 0 || table), "null array");
+    NEED(B == 1 || out_stride >= (int64_t)q_heads * D, "out's stride below its row");
+    NEED(aligned_to(q, 2) && aligned_to(out, 2) && aligned_to(table, 4) && aligned_to(lengths, 4) && aligned_to(lse, 4),
+         "array not aligned to its type");
+    const size_t need = sim_cache_attention_workspace(B, q_heads, kv_heads, D, table_pages, page_size, window);
+    NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
+    AttendArgs a;
+    a.q = q, a.q_stride = q_stride, a.q_head_stride = q_head_stride, a.B = B;
+    a.type = type, a.q_heads = q_heads, a.kv_heads = kv_heads, a.D = D;
+    a.k_cache = k_cache, a.v_cache = v_cache, a.k_page_stride = k_page_stride, a.v_page_stride = v_page_stride;
+    a.pages = pages, a.page_size = page_size;
+    a.table = table, a.table_stride = table_stride, a.capacity = (int64_t)table_pages * page_size, a.lengths = lengths;
+    a.scale_log2 = (float)(scale * 1.4426950408889634), a.window = window;
+    a.out = out, a.out_stride = out_stride, a.lse = lse, a.part = (float *)workspace;
+    a.tiles = attend_tiles(q_heads / kv_heads, D), a.units = attend_units((int64_t)kv_heads * a.tiles);
+    a.max_units = attend_max_units(B, a.units, a.capacity, window);
+    a.q_aligned = aligned_to(q, 16) && (B == 1 || q_stride % 8 == 0) && (q_heads == 1 || q_head_stride % 8 == 0);
+    a.out_aligned = aligned_to(out, 16) && (B == 1 || out_stride % 8 == 0);
+    return done(launch_attention((hipStream_t)stream, a), __func__);
 }
 
 }  // extern "C"

@@ -135,6 +135,36 @@ struct LayerArgs {
     void *y;
     int64_t y_stride;
 };
+struct AppendArgs {
+    const void *k, *v;
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride, T;
+    int heads, D;
+    const int64_t *slots;
+    void *k_cache, *v_cache;
+    int64_t k_page_stride, v_page_stride, pages;
+    int page_size;
+};
+sim_status launch_append(hipStream_t st, const AppendArgs &a);
+struct AttendArgs {
+    const void *q;
+    int64_t q_stride, q_head_stride, B;
+    int type, q_heads, kv_heads, D;
+    const void *k_cache, *v_cache;
+    int64_t k_page_stride, v_page_stride, pages;
+    int page_size;
+    const int32_t *table;
+    int64_t table_stride, capacity;  // tokens that a row of the table has room for
+    const int32_t *lengths;
+    float scale_log2;  // scale / ln 2
+    int window;
+    void *out;
+    int64_t out_stride;
+    float *lse, *part;
+    int64_t units, max_units;
+    int tiles;
+    bool q_aligned, out_aligned;
+};
+sim_status launch_attention(hipStream_t st, const AttendArgs &a);
 sim_status launch_layer(hipStream_t st, const LayerArgs &a, void *ws);
 size_t layer_workspace(int64_t T, int64_t D, int E, int k, int64_t F);
 

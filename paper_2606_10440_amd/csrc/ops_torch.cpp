@@ -19,6 +19,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 
 #include "simgpu_ops.h"
@@ -27,13 +28,14 @@ namespace {
 
 using at::Tensor;
 
-PyObject *g_error, *g_mx4, *g_routes;  // SimError, Mx4, Routes
+PyObject *g_error, *g_mx4, *g_routes, *g_cache;  // SimError, Mx4, Routes, PagedCache
 
 // The library's functions, as it was loaded for the rest of the package.
 #define SIM_OPS_CALLS(X)                                                                                            \
     X(sim_mx4_quantize) X(sim_mx4_dequantize) X(sim_mx4_matmul) X(sim_mx4_linear_workspace) X(sim_mx4_linear)       \
         X(sim_mx4_linear_grad_workspace) X(sim_mx4_linear_grad) X(sim_moe_route_workspace) X(sim_moe_route)         \
-            X(sim_moe_route_grad) X(sim_moe_layer_workspace) X(sim_moe_layer) X(sim_ops_last_error)
+            X(sim_moe_route_grad) X(sim_moe_layer_workspace) X(sim_moe_layer) X(sim_cache_append)          \
+                X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
 struct {
 #define X(name) decltype(&::name) name;
     SIM_OPS_CALLS(X)
@@ -361,6 +363,111 @@ PyObject *layer(PyObject *const *a) {  // x, logits, w13, w2, k, mask, renormali
     return y.written();
 }
 
+// ------------------------------------------------------------------ paged cache
+
+// A tensor [N, heads, D] whose rows of D are contiguous, for reading.
+struct Heads {
+    const void *p;
+    at::ScalarType type;
+    int64_t n, heads, D, stride, head_stride;
+    c10::Device dev;
+};
+Heads heads_of(const Tensor &x, const char *what) {
+    need(x.dim() == 3, what, " must have three dimensions");
+    need(x.scalar_type() == at::kHalf || x.scalar_type() == at::kBFloat16, what, " must be float16 or bfloat16");
+    need(x.is_cuda(), what, " must be on the GPU");
+    need(x.stride(2) == 1 || x.size(2) <= 1, what, "'s rows must be contiguous");
+    return {x.data_ptr(), x.scalar_type(), x.size(0), x.size(1), x.size(2), x.size(0) > 1 ? x.stride(0) : 0, x.size(1) > 1 ? x.stride(1) : 0, x.device()};
+}
+Heads heads_of(PyObject *o, const char *what) { return heads_of(tensor(o, what), what); }
+
+struct Paged {
+    void *k, *v;
+    at::ScalarType type;
+    int64_t pages, heads, size, D, k_stride, v_stride;
+    c10::Device dev;
+};
+Paged paged(PyObject *o) {
+    need(PyObject_TypeCheck(o, (PyTypeObject *)g_cache), "cache must be a PagedCache");
+    const Tensor &k = tensor(PyTuple_GET_ITEM(o, 0), "cache.k"), &v = tensor(PyTuple_GET_ITEM(o, 1), "cache.v");
+    need(k.dim() == 4 && v.dim() == 4 && k.sizes() == v.sizes(), "cache.k and cache.v must be [pages, kv heads, page size, D]");
+    need(k.scalar_type() == v.scalar_type() && (k.scalar_type() == at::kHalf || k.scalar_type() == at::kBFloat16),
+         "the cache must be float16 or bfloat16");
+    need(k.is_cuda() && v.device() == k.device(), "the cache must be on one GPU");
+    const int64_t pages = k.size(0), heads = k.size(1), size = k.size(2), D = k.size(3);
+    need(heads > 0 && heads < 1 << 20 && size > 0 && size < (int64_t)1 << 31, "bad sizes of the cache");
+    const auto whole_pages = [&](const Tensor &t) {
+        return (D <= 1 || t.stride(3) == 1) && (size == 1 || t.stride(2) == D) && (heads == 1 || t.stride(1) == size * D);
+    };
+    need(whole_pages(k) && whole_pages(v), "the cache's pages must be contiguous");
+    const int64_t page = heads * size * D;
+    return {k.data_ptr(), v.data_ptr(), k.scalar_type(), pages, heads, size, D, pages > 1 ? k.stride(0) : page, pages > 1 ? v.stride(0) : page, k.device()};
+}
+
+PyObject *append(PyObject *const *a) {  // cache, k, v, slots
+    const Paged c = paged(a[0]);
+    const Heads k = heads_of(a[1], "k"), v = heads_of(a[2], "v");
+    const Tensor &slots = tensor(a[3], "slots");
+    need(k.n == v.n && k.heads == c.heads && v.heads == c.heads && k.D == c.D && v.D == c.D, "k and v must be [T, kv heads, D]");
+    need(k.type == c.type && v.type == c.type, "k and v must have the cache's type");
+    need(slots.dim() == 1 && slots.size(0) == k.n && slots.scalar_type() == at::kLong && slots.is_contiguous(), "slots must be contiguous int64 [T]");
+    need(k.dev == c.dev && v.dev == c.dev && slots.device() == c.dev, "tensors are on different GPUs");
+    for (int i = 0; i < 2; i++)
+        need(!c10::GradMode::is_enabled() || !THPVariable_Unpack(PyTuple_GET_ITEM(a[0], i)).requires_grad(),
+             "the cache must not require a gradient: it is written in place");
+    call(c.dev, g.sim_cache_append, type_of(c.type), k.p, k.stride, k.head_stride, v.p, v.stride, v.head_stride, k.n, (int32_t)c.heads,
+         (int32_t)c.D, (const int64_t *)slots.data_ptr(), c.k, c.k_stride, c.v, c.v_stride, c.pages, (int32_t)c.size);
+    for (int i = 0; i < 2; i++) {
+        const Tensor &t = THPVariable_Unpack(PyTuple_GET_ITEM(a[0], i));
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
+    Py_RETURN_NONE;
+}
+
+PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, window, return_lse, out
+    const Heads q = heads_of(a[0], "q");
+    const Paged c = paged(a[1]);
+    const Tensor &table = tensor(a[2], "table"), &lengths = tensor(a[3], "lengths");
+    need(q.D == c.D, "q must be [B, q heads, D]");
+    need(q.heads > 0 && q.heads < 1 << 20 && q.heads % c.heads == 0, "the cache's heads must divide q's");
+    need(q.type == c.type, "q must have the cache's type");
+    need(table.dim() == 2 && table.size(0) == q.n && table.scalar_type() == at::kInt && (table.size(1) <= 1 || table.stride(1) == 1) && table.size(1) < (int64_t)1 << 31,
+         "table must be int32 [B, pages] with contiguous rows");
+    need(lengths.dim() == 1 && lengths.size(0) == q.n && lengths.scalar_type() == at::kInt && lengths.is_contiguous(), "lengths must be contiguous int32 [B]");
+    need(q.dev == c.dev && table.device() == c.dev && lengths.device() == c.dev, "tensors are on different GPUs");
+    const int64_t window = whole(a[5]);
+    need(window >= 0 && window < (int64_t)1 << 31, "window must not be negative");
+    const bool want_lse = truth(a[6]);
+    need(c.D > 0, "D must be a multiple of 8 up to 256");
+    const double scale = a[4] == Py_None ? 1 / std::sqrt((double)c.D) : PyFloat_AsDouble(a[4]);
+    if (scale == -1 && PyErr_Occurred()) throw Raised();
+    Tensor out, lse;
+    const bool given = a[7] != Py_None;
+    if (given) {
+        out = tensor(a[7], "out");
+        const Heads o = heads_of(out, "out");
+        need(o.n == q.n && o.heads == q.heads && o.D == q.D && o.type == q.type && o.dev == q.dev, "out must be as q");
+        need((o.heads == 1 || o.head_stride == o.D) && (o.n <= 1 || o.stride >= o.heads * o.D), "out's heads must be contiguous and must not overlap");
+        need(!out.requires_grad() || !c10::GradMode::is_enabled(), "out must not require a gradient: the result has none");
+        need(!out.is_alias_of(THPVariable_Unpack(a[0])), "out must not be q");
+    } else {
+        out = fresh({q.n, q.heads, q.D}, q.type, q.dev);
+    }
+    if (want_lse) lse = fresh({q.n, q.heads}, at::kFloat, q.dev);
+    const Space ws(g.sim_cache_attention_workspace(q.n, (int32_t)q.heads, (int32_t)c.heads, (int32_t)c.D, (int32_t)table.size(1), (int32_t)c.size, (int32_t)window), c.dev);
+    call(c.dev, g.sim_cache_attention, type_of(q.type), q.p, q.stride, q.head_stride, q.n, (int32_t)q.heads, (int32_t)c.heads, (int32_t)c.D, c.k,
+         c.k_stride, c.v, c.v_stride, c.pages, (int32_t)c.size, (const int32_t *)table.data_ptr(), table.size(0) > 1 ? table.stride(0) : 0,
+         (int32_t)table.size(1), (const int32_t *)lengths.data_ptr(), (float)scale, (int32_t)window, out.data_ptr(),
+         out.size(0) > 1 ? out.stride(0) : q.heads * q.D, want_lse ? (float *)lse.data_ptr() : nullptr, ws.p, ws.n);
+    if (given && !out.is_inference()) out.unsafeGetTensorImpl()->bump_version();
+    if (!want_lse) return wrap(out);
+    PyObject *po = wrap(out), *pl = wrap(lse);
+    PyObject *both = po && pl ? PyTuple_Pack(2, po, pl) : nullptr;
+    Py_XDECREF(po);
+    Py_XDECREF(pl);
+    return both;
+}
+
 // ------------------------------------------------------------------ the module
 
 template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -382,10 +489,11 @@ template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, 
     END_HANDLE_TH_ERRORS
 }
 
-// SimError, Mx4, Routes, {name: address} of the library's functions
+// SimError, Mx4, Routes, PagedCache, {name: address} of the library's functions
 PyObject *setup(PyObject *, PyObject *args) {
-    PyObject *error, *mx4, *routes, *at;
-    if (!PyArg_ParseTuple(args, "OO!O!O!", &error, &PyType_Type, &mx4, &PyType_Type, &routes, &PyDict_Type, &at)) return nullptr;
+    PyObject *error, *mx4, *routes, *cache, *at;
+    if (!PyArg_ParseTuple(args, "OO!O!O!O!", &error, &PyType_Type, &mx4, &PyType_Type, &routes, &PyType_Type, &cache, &PyDict_Type, &at))
+        return nullptr;
 #define X(name)                                                                        \
     {                                                                                  \
         PyObject *p = PyDict_GetItemString(at, #name);                                 \
@@ -394,8 +502,8 @@ PyObject *setup(PyObject *, PyObject *args) {
     }
     SIM_OPS_CALLS(X)
 #undef X
-    Py_INCREF(error), Py_INCREF(mx4), Py_INCREF(routes);
-    g_mx4 = mx4, g_routes = routes, g_error = error;
+    Py_INCREF(error), Py_INCREF(mx4), Py_INCREF(routes), Py_INCREF(cache);
+    g_mx4 = mx4, g_routes = routes, g_cache = cache, g_error = error;
     Py_RETURN_NONE;
 }
 
@@ -408,6 +516,8 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          ENTRY("route", route, 4),
                          ENTRY("route_grad", route_grad, 5),
                          ENTRY("layer", layer, 8),
+                         ENTRY("append", append, 4),
+                         ENTRY("attention", attention, 8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -28,7 +28,8 @@ from .sim import SimError
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
            "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
            "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route",
-           "sim_moe_route_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_ops_last_error")
+           "sim_moe_route_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_cache_append",
+           "sim_cache_attention_workspace", "sim_cache_attention", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
 
@@ -60,8 +61,13 @@ def lib():
         L.sim_moe_layer_workspace.restype = sz
         L.sim_moe_layer.argtypes = [P, P, i32, i64, i64, i64, P, i32, i32, i64, P, i64, i32, i32, P, P, P, P, i32,
                                     i64, P, i64, P, sz]
+        L.sim_cache_append.argtypes = [P, i32, P, i64, i64, P, i64, i64, i64, i32, i32, P, P, i64, P, i64, i64, i32]
+        L.sim_cache_attention_workspace.argtypes = [i64, i32, i32, i32, i32, i32, i32]
+        L.sim_cache_attention_workspace.restype = sz
+        L.sim_cache_attention.argtypes = [P, i32, P, i64, i64, i64, i32, i32, i32, P, i64, P, i64, i64, i32, P, i64, i32, P,
+                                          C.c_float, i32, P, i64, P, P, sz]
         for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_mx4_linear_grad",
-                     "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer"):
+                     "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer", "sim_cache_append", "sim_cache_attention"):
             getattr(L, name).restype = C.c_int
         L.sim_ops_last_error.argtypes = []
         L.sim_ops_last_error.restype = C.c_char_p
@@ -81,7 +87,7 @@ def _c():
             from . import _ops_torch
         except ImportError as e:
             raise RuntimeError("_ops_torch.so is missing or does not load: build it with paper_2606_10440_amd/build.py") from e
-        _ops_torch.setup(SimError, Mx4, Routes, {name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS})
+        _ops_torch.setup(SimError, Mx4, Routes, PagedCache, {name: C.cast(getattr(L, name), C.c_void_p).value for name in EXPORTS})
         _torch = _ops_torch
     return _torch
 
@@ -205,3 +211,33 @@ def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):
     is float16 or bfloat16; the weights have its type, or are ``Mx4``; ``out``
     may be x.  For inference: the result carries no gradients."""
     return _c().layer(x, logits, w13, w2, k, mask, renormalize, out)
+
+
+# ------------------------------------------------------------------ paged cache
+
+class PagedCache(NamedTuple):
+    """Keys and values of many sequences, ``k`` and ``v`` [pages, kv heads,
+    page size, D] (float16 or bfloat16; whole pages contiguous, so both may be
+    slices of one buffer [pages, 2, kv heads, page size, D]).  Which pages are
+    a sequence's is the caller's to say."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+
+def cache_append(cache: PagedCache, k, v, slots):
+    """Writes the rows k and v [T, kv heads, D] of T tokens into the cache, at
+    ``slots`` [T] (int64): page * page size + place in the page.  Tokens whose
+    slot is not in the cache (-1 say) are skipped; no two may have the same."""
+    _c().append(cache, k, v, slots)
+
+
+def cache_attention(q, cache: PagedCache, table, lengths, scale=None, window=0, return_lse=False, out=None):
+    """Attention of one new token of each sequence, q [B, q heads, D], over
+    its first ``lengths[b]`` tokens in the cache (or the last ``window`` of
+    these), on the pages ``table[b]`` (int32 [B, pages]; tokens on a page that
+    the cache does not have are left out).  Consecutive query heads share a
+    head of the cache.  ``scale`` is D ** -0.5 unless given.  Returns [B, q
+    heads, D], 0 where there is nothing to attend to; with ``return_lse`` also
+    the logarithm of each head's sum of weights, float32 [B, q heads].  ``out``
+    may have strided rows.  The result carries no gradients."""
+    return _c().attention(q, cache, table, lengths, scale, window, return_lse, out)
