@@ -139,6 +139,41 @@ sim_status sim_moe_route_grad(void *hip_stream, const void *logits, int32_t type
                               int32_t renormalize, const int32_t *experts, const float *d_weights, void *d_logits);
 
 /*
+ * The router with scores, a bias for the choice and groups.  As sim_moe_route,
+ * but
+ *   score: an expert's score s_e, the softmax over the token's allowed experts
+ *     or the sigmoid of its logit (0 where that is -infinity, which is never
+ *     chosen), in 32 bits, rounded from 64;
+ *   bias: NULL, or [E] f32: experts are chosen by s_e + bias_e, added in 32
+ *     bits (by their logits without one, which have the scores' order), ties to
+ *     the lowest expert; one whose sum is -infinity is never chosen;
+ *   groups: E / groups consecutive experts each (a whole number); of these the
+ *     top_groups highest take part (1 <= top_groups <= groups <= 64).  A group
+ *     is as high as the highest of its experts (group_best 1), or as the sum in
+ *     32 bits of s_e + bias_e of its two highest (2; of one where it has no
+ *     second that can be chosen); ties to the lowest group;
+ *   weights: the chosen scores, without bias, in 64 bits; with renormalize
+ *     divided by their sum; times scale (finite); rounded to 32 bits.
+ */
+enum { SIM_SCORE_SOFTMAX = 0, SIM_SCORE_SIGMOID = 1 };
+#define SIM_MOE_MAX_GROUPS 64
+sim_status sim_moe_route_scored(void *hip_stream, const void *logits, int32_t type, int64_t T, int32_t E,
+                                int64_t logit_stride, const uint8_t *mask, int64_t mask_stride, int32_t score,
+                                const float *bias, int32_t groups, int32_t top_groups, int32_t group_best, int32_t k,
+                                int32_t renormalize, float scale, int32_t *experts, float *weights, int32_t *offsets,
+                                int32_t *order, void *workspace, size_t workspace_bytes);
+
+/*
+ * Gradient of its weights with respect to the logits (the choice has none, nor
+ * has the bias), as sim_moe_route_grad; for sigmoid scores at the chosen e
+ *   renormalize: w_e (1 - s_e) (g_e - sum g w / scale);  else: w_e (1 - s_e) g_e.
+ */
+sim_status sim_moe_route_scored_grad(void *hip_stream, const void *logits, int32_t type, int64_t T, int32_t E,
+                                     int64_t logit_stride, const uint8_t *mask, int64_t mask_stride, int32_t score,
+                                     int32_t k, int32_t renormalize, float scale, const int32_t *experts,
+                                     const float *d_weights, void *d_logits);
+
+/*
  * The experts' layer for few tokens, from the router's logits:
  *   y_t = sum over the chosen experts e of  w_te W2_e (silu(G_e x_t) * (U_e x_t))
  * with experts chosen as by sim_moe_route, and its weights to within a few

@@ -229,6 +229,51 @@ sim_status sim_moe_route_grad(void *stream, const void *logits, int32_t type, in
     return done(launch_route_grad((hipStream_t)stream, a, experts, d_weights, d_logits), __func__);
 }
 
+static const char *scored_bad(int32_t score, float scale) {
+    if (score != SIM_SCORE_SOFTMAX && score != SIM_SCORE_SIGMOID) return "unknown score";
+    if (!std::isfinite(scale)) return "scale must be finite";
+    return nullptr;
+}
+
+sim_status sim_moe_route_scored(void *stream, const void *logits, int32_t type, int64_t T, int32_t E, int64_t logit_stride,
+                                const uint8_t *mask, int64_t mask_stride, int32_t score, const float *bias, int32_t groups,
+                                int32_t top_groups, int32_t group_best, int32_t k, int32_t renormalize, float scale,
+                                int32_t *experts, float *weights, int32_t *offsets, int32_t *order, void *workspace,
+                                size_t workspace_bytes) {
+    if (const char *why = route_bad(logits, type, T, E, logit_stride, mask, mask_stride, k))
+        return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    if (const char *why = scored_bad(score, scale)) return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    NEED(groups >= 1 && groups <= SIM_MOE_MAX_GROUPS && E % groups == 0, "groups must divide the experts, 64 at most");
+    NEED(top_groups >= 1 && top_groups <= groups, "top_groups out of range");
+    NEED(group_best == 1 || group_best == 2, "group_best must be 1 or 2");
+    NEED(aligned_to(bias, 4), "bias not aligned to its type");
+    FITS(T <= kMaxTokens && T < kMaxDim / k, "too many tokens");
+    NEED((offsets != nullptr) == (order != nullptr) || (T == 0 && offsets), "offsets and order go together");
+    NEED(T == 0 || (experts && weights), "null array");
+    NEED(aligned_to(experts, 4) && aligned_to(weights, 4) && aligned_to(offsets, 4) && aligned_to(order, 4), "output not aligned");
+    const size_t need = order ? sim_moe_route_workspace(T, E, k) : 0;
+    NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
+    RouteArgs a = {logits, type, T, E, logit_stride, mask, mask_stride, k, renormalize != 0};
+    a.scored = true, a.score = score, a.bias = bias;
+    a.groups = groups, a.top_groups = top_groups, a.group_best = group_best, a.scale = scale;
+    return done(launch_route((hipStream_t)stream, a, experts, weights, offsets, order, workspace), __func__);
+}
+
+sim_status sim_moe_route_scored_grad(void *stream, const void *logits, int32_t type, int64_t T, int32_t E, int64_t logit_stride,
+                                     const uint8_t *mask, int64_t mask_stride, int32_t score, int32_t k, int32_t renormalize,
+                                     float scale, const int32_t *experts, const float *d_weights, void *d_logits) {
+    if (const char *why = route_bad(logits, type, T, E, logit_stride, mask, mask_stride, k))
+        return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    if (const char *why = scored_bad(score, scale)) return refuse(SIM_ERR_INVALID_ARG, __func__, why);
+    FITS(T <= kMaxTokens && T < kMaxDim / k, "too many tokens");
+    if (T == 0) return done(SIM_OK, __func__);
+    NEED(experts && d_weights && d_logits, "null array");
+    NEED(aligned_to(experts, 4) && aligned_to(d_weights, 4) && aligned_to(d_logits, size_of(type)), "array not aligned");
+    RouteArgs a = {logits, type, T, E, logit_stride, mask, mask_stride, k, renormalize != 0};
+    a.score = score, a.scale = scale;
+    return done(launch_route_grad((hipStream_t)stream, a, experts, d_weights, d_logits), __func__);
+}
+
 size_t sim_moe_layer_workspace(int64_t T, int64_t D, int32_t E, int32_t k, int64_t F) {
     if (T <= 0 || T > SIM_MOE_LAYER_MAX_TOKENS || D <= 0 || F < 0 || E < 1 || E > SIM_MOE_MAX_EXPERTS || k < 1 || k > E ||
         k > SIM_MOE_MAX_TOPK || !layer_dims_fit(D, F) || !layer_tiles_fit(T, D, E, k, F))

@@ -118,6 +118,12 @@ struct RouteArgs {
     int64_t mask_stride;
     int k;
     bool renorm;
+    // the choice by scores (scored), and what its gradient needs of it
+    bool scored = false;
+    int score = SIM_SCORE_SOFTMAX;
+    const float *bias = nullptr;
+    int groups = 1, top_groups = 1, group_best = 1;
+    float scale = 1.f;
 };
 sim_status launch_route(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets,
                         int32_t *order, void *ws);

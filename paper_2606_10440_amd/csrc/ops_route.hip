@@ -147,6 +147,51 @@ __host__ __device__ inline int hist_pitch(int E) { return (E + 3) / 4 * 4; }
 __device__ inline void mark(uint64_t *chose, int e, int tok) { atomicOr((unsigned long long *)&chose[e], 1ull << tok); }
 __device__ inline int before_in(uint64_t chose, int tok) { return __popcll(chose & ((1ull << tok) - 1)); }
 
+// The choices of CH tokens, sixteen threads a token with the choices l and l +
+// 16 each (had: whether there is one), and what is made of them: their counts,
+// or (one chunk only) the lists.
+struct Lists {
+    uint64_t chose[SIM_MOE_MAX_EXPERTS];  // zeros, before
+    int base[SIM_MOE_MAX_EXPERTS];
+    int wave_sum[kThreads / 64];
+};
+template <int CH>
+__device__ inline void clear(Lists &s) {
+    for (int e = threadIdx.x; e < SIM_MOE_MAX_EXPERTS; e += 16 * CH) s.chose[e] = 0;
+}
+template <int CH>
+__device__ inline void finish(Lists &s, int64_t t, bool live, int k, int E, int n_tok, const uint32_t e[2], const uint32_t had[2],
+                              const float w[2], int32_t *__restrict__ experts, float *__restrict__ weights,
+                              uint8_t *__restrict__ hist, int32_t *__restrict__ offsets, int32_t *__restrict__ order) {
+    const int l = threadIdx.x & 15, tok = threadIdx.x >> 4;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int j = q * 16 + l;
+        if (live && j < k) {
+            experts[t * k + j] = had[q] ? (int)e[q] : -1;
+            weights[t * k + j] = had[q] ? w[q] : 0.f;
+            if (had[q] && order) mark(s.chose, e[q], tok);
+        }
+    }
+    if (!order) return;
+    __syncthreads();
+    if (CH < kChunk || gridDim.x > 1) {
+        // at most kChunk: a byte
+        for (int i = threadIdx.x; i < hist_pitch(E); i += 16 * CH)
+            hist[(int64_t)blockIdx.x * hist_pitch(E) + i] = (uint8_t)__popcll(s.chose[i]);
+        return;
+    }
+    int total;
+    s.base[threadIdx.x] = block_scan(__popcll(s.chose[threadIdx.x]), s.wave_sum, total);
+    if ((int)threadIdx.x < E) offsets[threadIdx.x] = s.base[threadIdx.x];
+    if (threadIdx.x == 0) offsets[E] = total;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+        if (live && had[q]) order[s.base[e[q]] + before_in(s.chose[e[q]], tok)] = tok * k + q * 16 + l;
+    for (int i = total + threadIdx.x; i < n_tok * k; i += kThreads) order[i] = -1;
+}
+
 // Choice and weights of CH tokens; their counts, or (one chunk only) the lists.
 template <int T, int NV, int CH>
 __global__ __launch_bounds__(16 * CH) void route_choose(const typename Elem<T>::type *__restrict__ logits, int64_t n_tok,
@@ -155,13 +200,11 @@ __global__ __launch_bounds__(16 * CH) void route_choose(const typename Elem<T>::
                                                          int32_t *__restrict__ experts, float *__restrict__ weights,
                                                          uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,
                                                          int32_t *__restrict__ order) {
-    __shared__ uint64_t chose[SIM_MOE_MAX_EXPERTS];
-    __shared__ int base[SIM_MOE_MAX_EXPERTS];
-    __shared__ int wave_sum[kThreads / 64];
+    __shared__ Lists lists;
     const int l = threadIdx.x & 15, tok = threadIdx.x >> 4;
     const int64_t t = (int64_t)blockIdx.x * CH + tok;
     const bool live = t < n_tok;
-    for (int e = threadIdx.x; e < SIM_MOE_MAX_EXPERTS; e += 16 * CH) chose[e] = 0;
+    clear<CH>(lists);
     Keys<T, NV> key;
     float z = 0.f, top = 0.f;
     {
@@ -196,31 +239,8 @@ __global__ __launch_bounds__(16 * CH) void route_choose(const typename Elem<T>::
     for (int q = 0; q < 2; q++) w[q] = mine[q] ? fast_exp(Keys<T, NV>::value(mine[q]) - top) : 0.f;
     if (renorm) z = sum16(w[0] + w[1]);
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        const int j = q * 16 + l;
-        if (live && j < k) {
-            experts[t * k + j] = mine[q] ? (int)mine_e[q] : -1;
-            weights[t * k + j] = mine[q] ? w[q] / z : 0.f;
-            if (mine[q] && order) mark(chose, mine_e[q], tok);
-        }
-    }
-    if (!order) return;
-    __syncthreads();
-    if (CH < kChunk || gridDim.x > 1) {
-        // at most kChunk: a byte
-        for (int e = threadIdx.x; e < hist_pitch(E); e += 16 * CH)
-            hist[(int64_t)blockIdx.x * hist_pitch(E) + e] = (uint8_t)__popcll(chose[e]);
-        return;
-    }
-    int total;
-    base[threadIdx.x] = block_scan(__popcll(chose[threadIdx.x]), wave_sum, total);
-    if ((int)threadIdx.x < E) offsets[threadIdx.x] = base[threadIdx.x];
-    if (threadIdx.x == 0) offsets[E] = total;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 2; q++)
-        if (live && mine[q]) order[base[mine_e[q]] + before_in(chose[mine_e[q]], tok)] = tok * k + q * 16 + l;
-    for (int s = total + threadIdx.x; s < (int)n_tok * k; s += kThreads) order[s] = -1;
+    for (int q = 0; q < 2; q++) w[q] = w[q] / z;
+    finish<CH>(lists, t, live, k, E, (int)min(n_tok, (int64_t)CH), mine_e, mine, w, experts, weights, hist, offsets, order);
 }
 
 // The sums over the chunks before each; the row past the last gets the totals.
@@ -326,7 +346,7 @@ __global__ __launch_bounds__(kThreads) void route_place(const int32_t *__restric
 template <int T, int NV>
 __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *__restrict__ logits, int64_t n_tok, int E,
                                                   int64_t stride, const uint8_t *__restrict__ mask, int64_t mask_stride,
-                                                  int k, int renorm, const int32_t *__restrict__ experts,
+                                                  int k, int renorm, float scale, const int32_t *__restrict__ experts,
                                                   const float *__restrict__ dw, typename Elem<T>::type *__restrict__ dz) {
     typedef typename Elem<T>::type El;
     __shared__ __align__(16) float rows[16][NV * 16];
@@ -343,7 +363,7 @@ __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *
         const int j = q * 16 + l;
         e[q] = j < k ? experts[t * k + j] : -1;
         if (e[q] < 0 || e[q] >= E || (mt && !mt[e[q]])) e[q] = -1;
-        g[q] = e[q] >= 0 ? dw[t * k + j] : 0.f;
+        g[q] = e[q] >= 0 ? dw[t * k + j] * scale : 0.f;
         v[q] = e[q] >= 0 ? Elem<T>::get(zt[e[q]]) : -INFINITY;
     }
 #pragma unroll
@@ -401,6 +421,279 @@ __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *
             if (l * NV + i < E) o[i] = out[i];
 }
 
+// ------------------------------------------------------------------ scores, bias, groups
+
+// e^x for x <= 0 in 64 bits: 2^n times the exponential's series at what is left,
+// at most ln 2 / 2 in magnitude, up to r^12 / 12! (the next term is below 2^-53).
+__device__ inline double exp64(double x) {
+    x = x < -800. ? -800. : x;  // (0 then; a NaN stays)
+    // the nearest whole number in the low bits of 1.5 2^52 and it
+    const double magic = 6755399441055744., t = __builtin_fma(x, 1.4426950408889634, magic), n = t - magic;
+    // ln 2 as 24 bits, by which n is multiplied exactly, and the rest
+    const double r = __builtin_fma(n, 1.904654299957768e-09, __builtin_fma(n, -0.693147182464599609375, x));
+    double p = 1. / 479001600.;
+    p = __builtin_fma(p, r, 1. / 39916800.);
+    p = __builtin_fma(p, r, 1. / 3628800.);
+    p = __builtin_fma(p, r, 1. / 362880.);
+    p = __builtin_fma(p, r, 1. / 40320.);
+    p = __builtin_fma(p, r, 1. / 5040.);
+    p = __builtin_fma(p, r, 1. / 720.);
+    p = __builtin_fma(p, r, 1. / 120.);
+    p = __builtin_fma(p, r, 1. / 24.);
+    p = __builtin_fma(p, r, 1. / 6.);
+    p = __builtin_fma(p, r, .5);
+    p = __builtin_fma(p, r, 1.);
+    p = __builtin_fma(p, r, 1.);
+    return __builtin_ldexp(p, (int)__builtin_bit_cast(uint64_t, t));
+}
+// 1 / x for 1 <= x <= 2^11, to the last place but one
+__device__ inline double reciprocal(double x) {
+    double y = __builtin_amdgcn_rcp(x);
+    y = __builtin_fma(__builtin_fma(-x, y, 1.), y, y);
+    return __builtin_fma(__builtin_fma(-x, y, 1.), y, y);
+}
+__device__ inline double sigmoid64(double z) {
+    const double e = exp64(-__builtin_fabs(z));
+    return (z < 0. ? e : 1.) * reciprocal(1. + e);
+}
+template <int CTRL> __device__ inline double dpp_f64(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, dpp_u32<CTRL>((uint32_t)b) | (uint64_t)dpp_u32<CTRL>((uint32_t)(b >> 32)) << 32);
+}
+__device__ inline double sum16(double v) {
+    v += dpp_f64<kDppXor1>(v);
+    v += dpp_f64<kDppXor2>(v);
+    v += dpp_f64<kDppHalfMirror>(v);
+    v += dpp_f64<kDppMirror>(v);
+    return v;
+}
+
+// The two highest keys of those seen.
+struct Two {
+    uint32_t a = 0, b = 0;
+    __device__ void add(uint32_t k) {
+        b = max(b, min(a, k));
+        a = max(a, k);
+    }
+    template <int CTRL> __device__ void merge() {
+        const uint32_t a2 = dpp_u32<CTRL>(a), b2 = dpp_u32<CTRL>(b);
+        b = max(min(a, a2), max(b, b2));
+        a = max(a, a2);
+    }
+    // of a group, as a key; 0 where nothing of it can be chosen
+    __device__ uint32_t value(int best) const { return best == 1 || !b ? a : order_key(key_value(a) + key_value(b)); }
+};
+
+// Which groups a token keeps, a bit for each, from its experts' keys.  Where a
+// group is a whole number of lanes, a power of two, each lane merges with those
+// of its own; else the groups are searched one after another.
+template <int NV> __device__ inline uint64_t top_groups(const uint32_t key[NV], int E, int groups, int top, int best) {
+    const int l = threadIdx.x & 15, size = E / groups, lanes = size / NV;
+    uint64_t keep = 0;
+    if (lanes * NV == size && (lanes & (lanes - 1)) == 0) {
+        Two two;
+#pragma unroll
+        for (int i = 0; i < NV; i++) two.add(key[i]);
+        if (lanes >= 2) two.merge<kDppXor1>();
+        if (lanes >= 4) two.merge<kDppXor2>();
+        if (lanes >= 8) two.merge<kDppHalfMirror>();
+        if (lanes >= 16) two.merge<kDppMirror>();
+        const uint32_t mine = l / lanes;
+        uint32_t v = two.value(best);
+        for (int j = 0; j < top; j++) {
+            uint32_t k = v, i = mine;
+            best16(k, i);
+            if (k) keep |= 1ull << i;
+            if (mine == i) v = 0;
+        }
+        return keep;
+    }
+    uint32_t v[SIM_MOE_MAX_GROUPS / 16] = {};  // of groups l, l + 16, ...
+    for (int g = 0; g < groups; g++) {
+        Two two;
+#pragma unroll
+        for (int i = 0; i < NV; i++) two.add((uint32_t)(l * NV + i - g * size) < (uint32_t)size ? key[i] : 0);
+        two.merge<kDppXor1>();
+        two.merge<kDppXor2>();
+        two.merge<kDppHalfMirror>();
+        two.merge<kDppMirror>();
+#pragma unroll
+        for (int q = 0; q < SIM_MOE_MAX_GROUPS / 16; q++)
+            if (g == q * 16 + l) v[q] = two.value(best);
+    }
+    for (int j = 0; j < top; j++) {
+        uint32_t k = 0, i = 0xffffu;
+#pragma unroll
+        for (int q = 0; q < SIM_MOE_MAX_GROUPS / 16; q++) keep_better(k, i, v[q], q * 16 + l);
+        best16(k, i);
+        if (k) keep |= 1ull << i;
+#pragma unroll
+        for (int q = 0; q < SIM_MOE_MAX_GROUPS / 16; q++)
+            if ((int)i == q * 16 + l) v[q] = 0;
+    }
+    return keep;
+}
+
+// The choice by scores.  Which of two experts is higher must not depend on how
+// a score was computed, so scores are in 64 bits and rounded to 32, in which
+// the bias and the groups' sums are added: what is compared is the definition's
+// but where a 64-bit value lies within its own error of the middle between two
+// 32-bit ones.  64-bit fused operations run at the rate of 32-bit ones here.
+template <int T, int NV, int CH>
+__global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__restrict__ experts, float *__restrict__ weights,
+                                                        uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,
+                                                        int32_t *__restrict__ order) {
+    typedef typename Elem<T>::type El;
+    __shared__ Lists lists;
+    const int l = threadIdx.x & 15, tok = threadIdx.x >> 4, E = a.E, k = a.k;
+    const int64_t t = (int64_t)blockIdx.x * CH + tok;
+    const bool live = t < a.T;
+    const El *const z = (const El *)a.logits + (live ? t : 0) * a.stride;
+    const uint8_t *const mask = a.mask ? a.mask + (live ? t : 0) * a.mask_stride : nullptr;
+    clear<CH>(lists);
+    Keys<SIM_TYPE_F32, NV> key;
+    El v[NV];
+    uint64_t ok = load_logits<T, NV>(z, mask, E, live, v);
+    uint32_t top = 0;  // the highest of the allowed logits
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+        const uint32_t by = (ok >> i) & 1 ? order_key(Elem<T>::get(v[i])) : 0;
+        if (!by) ok &= ~(1ull << i);
+        key.k[i] = by;
+        top = max(top, by);
+    }
+    double high = 0., inv = 0.;
+    if (a.score == SIM_SCORE_SOFTMAX) {
+        high = key_value(max16(top));
+        if (a.bias || !a.renorm || (a.groups > a.top_groups && a.group_best == 2)) {
+            double sum = 0.;
+#pragma unroll
+            for (int i = 0; i < NV; i++) sum += (ok >> i) & 1 ? exp64(Elem<T>::get(v[i]) - high) : 0.;
+            inv = 1. / sum16(sum);
+        }
+    }
+    const bool grouped = a.groups > a.top_groups, by_score = a.bias || (grouped && a.group_best == 2);
+    if (by_score) {
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const double x = Elem<T>::get(v[i]);
+            const float s = (float)(a.score == SIM_SCORE_SIGMOID ? sigmoid64(x) : exp64(x - high) * inv);
+            key.k[i] = (ok >> i) & 1 ? order_key(a.bias ? s + a.bias[min(l * NV + i, E - 1)] : s) : 0;
+        }
+    }
+    if (grouped) {
+        const uint64_t keep = top_groups<NV>(key.k, E, a.groups, a.top_groups, a.group_best);
+        const int size = E / a.groups;
+        int g = l * NV / size, in = l * NV - g * size;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            // without a bias the logits have the scores' order, and a finer one
+            if (by_score && !a.bias && key.k[i]) key.k[i] = order_key(Elem<T>::get(v[i]));
+            if (!((keep >> (g & 63)) & 1)) key.k[i] = 0;
+            if (++in == size) in = 0, g++;
+        }
+    }
+    __syncthreads();
+
+    uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};  // the choices l and l + 16
+    for (int j = 0; j < k; j++) {
+        uint32_t e;
+        const uint32_t m = key.take(e);
+        if (l == (j & 15)) {
+            mine[j >> 4] = m;
+            mine_e[j >> 4] = e;
+        }
+    }
+    // the weights from the chosen logits again, relative to the highest chosen
+    // one where they are divided by their sum
+    double x[2], w64[2];
+    uint32_t first = 0;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        x[q] = mine[q] ? (double)Elem<T>::get(z[mine_e[q]]) : 0.;
+        first = max(first, mine[q] ? order_key((float)x[q]) : 0u);
+    }
+    const bool sigmoid = a.score == SIM_SCORE_SIGMOID;
+    if (a.renorm) {
+        high = key_value(max16(first));
+        if (sigmoid && high > 0.) high = 0.;
+    }
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        if (!mine[q]) w64[q] = 0.;
+        else if (!sigmoid) w64[q] = exp64(x[q] - high);
+        else if (a.renorm) w64[q] = exp64((x[q] > 0. ? 0. : x[q]) - high) * reciprocal(1. + exp64(-__builtin_fabs(x[q])));
+        else w64[q] = sigmoid64(x[q]);
+    }
+    if (a.renorm) inv = 1. / sum16(w64[0] + w64[1]);
+    else if (sigmoid) inv = 1.;
+    float w[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) w[q] = (float)(w64[q] * inv * a.scale);
+    finish<CH>(lists, t, live, k, E, (int)min(a.T, (int64_t)CH), mine_e, mine, w, experts, weights, hist, offsets, order);
+}
+
+// Gradient of sigmoid weights: at the chosen experts only.  As in route_grad,
+// lane l has the choices l and l + 16.
+template <int T, int NV>
+__global__ __launch_bounds__(256) void route_grad_sigmoid(RouteArgs a, const int32_t *__restrict__ experts,
+                                                          const float *__restrict__ dw, typename Elem<T>::type *__restrict__ dz) {
+    typedef typename Elem<T>::type El;
+    __shared__ __align__(16) float rows[16][NV * 16];
+    const int l = threadIdx.x & 15, E = a.E, k = a.k;
+    const int64_t t = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (t >= a.T) return;  // sixteen lanes at a time: they share no barrier
+    float *row = rows[threadIdx.x >> 4];
+    const El *zt = (const El *)a.logits + t * a.stride;
+    const uint8_t *mt = a.mask ? a.mask + t * a.mask_stride : nullptr;
+    int e[2];
+    float g[2], z[2], w[2];
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const int j = q * 16 + l;
+        e[q] = j < k ? experts[t * k + j] : -1;
+        if (e[q] < 0 || e[q] >= E || (mt && !mt[e[q]])) e[q] = -1;
+        z[q] = e[q] >= 0 ? Elem<T>::get(zt[e[q]]) : 0.f;
+        if (z[q] == -INFINITY) e[q] = -1;
+        g[q] = e[q] >= 0 ? dw[t * k + j] * a.scale : 0.f;
+        top = max(top, e[q] >= 0 ? order_key(z[q]) : 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i++) row[i * 16 + l] = 0.f;
+    float high = 0.f, dot = 0.f, inv = 1.f;
+    if (a.renorm) {
+        high = key_value(max16(top));
+        high = high > 0.f ? 0.f : high;
+    }
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const float s = fast_exp((z[q] > 0.f ? 0.f : z[q]) - high) / (1.f + fast_exp(-fabsf(z[q])));  // times e^-high
+        w[q] = e[q] >= 0 ? s : 0.f;
+    }
+    if (a.renorm) {
+        inv = 1.f / sum16(w[0] + w[1]);
+        dot = sum16((e[0] >= 0 ? g[0] * w[0] : 0.f) + (e[1] >= 0 ? g[1] * w[1] : 0.f)) * inv;
+    }
+    wave_fence();  // the zeros are other lanes' than the values, and both than what is read
+#pragma unroll
+    for (int q = 0; q < 2; q++)
+        if (e[q] >= 0) {
+            const float far = fast_exp(-fabsf(z[q])), rest = (z[q] < 0.f ? 1.f : far) / (1.f + far);  // 1 - s
+            row[e[q]] = w[q] * inv * (g[q] - dot) * rest;
+        }
+    wave_fence();
+    El out[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) out[i] = Elem<T>::put(row[l * NV + i]);
+    El *o = dz + t * E + l * NV;
+    if (l * NV + NV <= E) store_some<NV>(o, out);
+    else
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+            if (l * NV + i < E) o[i] = out[i];
+}
+
 // Calls f with the smallest register count that holds E experts in 16 lanes.
 template <typename F> void with_nv(int E, F &&f) {
     if (E <= 16) f(std::integral_constant<int, 1>());
@@ -434,6 +727,10 @@ sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *
     int32_t *sums = chunks > kScanChunks ? (int32_t *)(hist + hist_bytes(rows, a.E)) : nullptr;
     const auto choose = [&](auto nv, auto ch) {
         constexpr int CH = decltype(ch)::value;
+        if (a.scored) {
+            route_scored<T, decltype(nv)::value, CH><<<(uint32_t)((a.T + CH - 1) / CH), 16 * CH, 0, st>>>(a, experts, weights, hist, offsets, order);
+            return;
+        }
         route_choose<T, decltype(nv)::value, CH><<<(uint32_t)((a.T + CH - 1) / CH), 16 * CH, 0, st>>>(
             (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts,
             weights, hist, offsets, order);
@@ -453,9 +750,13 @@ sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *
 template <int T>
 sim_status route_grad_t(hipStream_t st, const RouteArgs &a, const int32_t *experts, const float *dw, void *dz) {
     with_nv(a.E, [&](auto nv) {
-        route_grad<T, decltype(nv)::value><<<(uint32_t)((a.T + 15) / 16), 256, 0, st>>>(
-            (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts, dw,
-            (typename Elem<T>::type *)dz);
+        const uint32_t grid = (uint32_t)((a.T + 15) / 16);
+        if (a.score == SIM_SCORE_SIGMOID)
+            route_grad_sigmoid<T, decltype(nv)::value><<<grid, 256, 0, st>>>(a, experts, dw, (typename Elem<T>::type *)dz);
+        else
+            route_grad<T, decltype(nv)::value><<<grid, 256, 0, st>>>(
+                (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, a.scale, experts,
+                dw, (typename Elem<T>::type *)dz);
     });
     return SIM_OPS_LAUNCH_OK();
 }

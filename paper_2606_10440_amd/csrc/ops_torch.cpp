@@ -34,8 +34,8 @@ PyObject *g_error, *g_mx4, *g_routes, *g_cache;  // SimError, Mx4, Routes, Paged
 #define SIM_OPS_CALLS(X)                                                                                            \
     X(sim_mx4_quantize) X(sim_mx4_dequantize) X(sim_mx4_matmul) X(sim_mx4_linear_workspace) X(sim_mx4_linear)       \
         X(sim_mx4_linear_grad_workspace) X(sim_mx4_linear_grad) X(sim_moe_route_workspace) X(sim_moe_route)         \
-            X(sim_moe_route_grad) X(sim_moe_layer_workspace) X(sim_moe_layer) X(sim_cache_append)          \
-                X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
+            X(sim_moe_route_grad) X(sim_moe_route_scored) X(sim_moe_route_scored_grad) X(sim_moe_layer_workspace)       \
+                X(sim_moe_layer) X(sim_cache_append) X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
 struct {
 #define X(name) decltype(&::name) name;
     SIM_OPS_CALLS(X)
@@ -294,19 +294,51 @@ struct Router {
     }
 };
 
-PyObject *route(PyObject *const *a) {  // logits, k, mask, renormalize
+int score_of(PyObject *o) {
+    const char *s = PyUnicode_Check(o) ? PyUnicode_AsUTF8(o) : nullptr;
+    const std::string name = s ? s : "";
+    need(name == "softmax" || name == "sigmoid", "score must be \"softmax\" or \"sigmoid\"");
+    return name == "softmax" ? SIM_SCORE_SOFTMAX : SIM_SCORE_SIGMOID;
+}
+double number(PyObject *o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised();
+    return v;
+}
+int32_t small(PyObject *o, const char *what) {
+    const int64_t v = whole(o);
+    need(v > INT32_MIN && v < INT32_MAX, what, " out of range");
+    return (int32_t)v;
+}
+
+PyObject *route(PyObject *const *a) {  // logits, k, mask, renormalize, score, bias, groups, top_groups, group_best, scale
     const Router r(a[0], whole(a[1]), a[2]);
     const bool renorm = truth(a[3]);
+    const int score = score_of(a[4]);
+    const float *bias = nullptr;
+    if (a[5] != Py_None) {
+        const Tensor &t = tensor(a[5], "bias");
+        need(t.dim() == 1 && t.size(0) == r.E && t.scalar_type() == at::kFloat && t.is_contiguous() && t.device() == r.z.dev,
+             "bias must be contiguous float32 [E] on the same GPU");
+        bias = (const float *)t.data_ptr();
+    }
+    const int32_t groups = small(a[6], "groups"), top_groups = a[7] == Py_None ? groups : small(a[7], "top_groups"), best = small(a[8], "group_best");
+    const float scale = (float)number(a[9]);
+    const bool plain = score == SIM_SCORE_SOFTMAX && !bias && groups == 1 && top_groups == 1 && (best == 1 || best == 2) && scale == 1.f;
     const Tensor experts = fresh({r.T, r.k}, at::kInt, r.z.dev), weights = fresh({r.T, r.k}, at::kFloat, r.z.dev);
     const Tensor offsets = fresh({r.E + 1}, at::kInt, r.z.dev), order = fresh({r.T * r.k}, at::kInt, r.z.dev);
     const Space ws(g.sim_moe_route_workspace(r.T, r.E, (int32_t)r.k), r.z.dev);
-    call(r.z.dev, g.sim_moe_route, r.z.p, r.z.type, r.T, r.E, r.z.stride, r.mask, r.mask_stride, (int32_t)r.k, renorm,
-         (int32_t *)experts.data_ptr(), (float *)weights.data_ptr(), (int32_t *)offsets.data_ptr(),
-         r.T ? (int32_t *)order.data_ptr() : nullptr, ws.p, ws.n);
+    int32_t *const e = (int32_t *)experts.data_ptr(), *const o = (int32_t *)offsets.data_ptr(), *const s = r.T ? (int32_t *)order.data_ptr() : nullptr;
+    float *const w = (float *)weights.data_ptr();
+    if (plain)
+        call(r.z.dev, g.sim_moe_route, r.z.p, r.z.type, r.T, r.E, r.z.stride, r.mask, r.mask_stride, (int32_t)r.k, renorm, e, w, o, s, ws.p, ws.n);
+    else
+        call(r.z.dev, g.sim_moe_route_scored, r.z.p, r.z.type, r.T, r.E, r.z.stride, r.mask, r.mask_stride, score, bias, groups, top_groups,
+             best, (int32_t)r.k, renorm, scale, e, w, o, s, ws.p, ws.n);
     return named(g_routes, {wrap(experts), wrap(weights), wrap(offsets), wrap(order)});
 }
 
-PyObject *route_grad(PyObject *const *a) {  // logits, experts, d_weights, mask, renormalize
+PyObject *route_grad(PyObject *const *a) {  // logits, experts, d_weights, mask, renormalize, score, scale
     const Tensor &e = tensor(a[1], "experts"), &dw = tensor(a[2], "d_weights");
     need(e.dim() == 2, "experts must be [T, k]");
     const Router r(a[0], e.size(1), a[3]);
@@ -316,8 +348,8 @@ PyObject *route_grad(PyObject *const *a) {  // logits, experts, d_weights, mask,
     need(e.is_contiguous() && dw.is_contiguous(), "experts and d_weights must be contiguous");
     need(e.device() == r.z.dev && dw.device() == r.z.dev, "tensors are on different GPUs");
     const Tensor dz = fresh({r.T, r.E}, THPVariable_Unpack(a[0]).scalar_type(), r.z.dev);
-    call(r.z.dev, g.sim_moe_route_grad, r.z.p, r.z.type, r.T, r.E, r.z.stride, r.mask, r.mask_stride, (int32_t)r.k, renorm,
-         (const int32_t *)e.data_ptr(), (const float *)dw.data_ptr(), dz.data_ptr());
+    call(r.z.dev, g.sim_moe_route_scored_grad, r.z.p, r.z.type, r.T, r.E, r.z.stride, r.mask, r.mask_stride, score_of(a[5]), (int32_t)r.k,
+         renorm, (float)number(a[6]), (const int32_t *)e.data_ptr(), (const float *)dw.data_ptr(), dz.data_ptr());
     return wrap(dz);
 }
 
@@ -439,8 +471,7 @@ PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, w
     need(window >= 0 && window < (int64_t)1 << 31, "window must not be negative");
     const bool want_lse = truth(a[6]);
     need(c.D > 0, "D must be a multiple of 8 up to 256");
-    const double scale = a[4] == Py_None ? 1 / std::sqrt((double)c.D) : PyFloat_AsDouble(a[4]);
-    if (scale == -1 && PyErr_Occurred()) throw Raised();
+    const double scale = a[4] == Py_None ? 1 / std::sqrt((double)c.D) : number(a[4]);
     Tensor out, lse;
     const bool given = a[7] != Py_None;
     if (given) {
@@ -513,8 +544,8 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          ENTRY("dequantize", dequantize, 2),
                          ENTRY("matmul", matmul, 4),
                          ENTRY("linear_grad", linear_grad, 5),
-                         ENTRY("route", route, 4),
-                         ENTRY("route_grad", route_grad, 5),
+                         ENTRY("route", route, 10),
+                         ENTRY("route_grad", route_grad, 7),
                          ENTRY("layer", layer, 8),
                          ENTRY("append", append, 4),
                          ENTRY("attention", attention, 8),

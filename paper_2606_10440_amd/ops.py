@@ -28,7 +28,7 @@ from .sim import SimError
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
            "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
            "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route",
-           "sim_moe_route_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_cache_append",
+           "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_cache_append",
            "sim_cache_attention_workspace", "sim_cache_attention", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
@@ -57,6 +57,9 @@ def lib():
         L.sim_moe_route_workspace.restype = sz
         L.sim_moe_route.argtypes = [P, P, i32, i64, i32, i64, P, i64, i32, i32, P, P, P, P, P, sz]
         L.sim_moe_route_grad.argtypes = [P, P, i32, i64, i32, i64, P, i64, i32, i32, P, P, P]
+        L.sim_moe_route_scored.argtypes = [P, P, i32, i64, i32, i64, P, i64, i32, P, i32, i32, i32, i32, i32, C.c_float, P, P, P, P,
+                                           P, sz]
+        L.sim_moe_route_scored_grad.argtypes = [P, P, i32, i64, i32, i64, P, i64, i32, i32, i32, C.c_float, P, P, P]
         L.sim_moe_layer_workspace.argtypes = [i64, i64, i32, i32, i64]
         L.sim_moe_layer_workspace.restype = sz
         L.sim_moe_layer.argtypes = [P, P, i32, i64, i64, i64, P, i32, i32, i64, P, i64, i32, i32, P, P, P, P, i32,
@@ -67,7 +70,8 @@ def lib():
         L.sim_cache_attention.argtypes = [P, i32, P, i64, i64, i64, i32, i32, i32, P, i64, P, i64, i64, i32, P, i64, i32, P,
                                           C.c_float, i32, P, i64, P, P, sz]
         for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_mx4_linear_grad",
-                     "sim_moe_route", "sim_moe_route_grad", "sim_moe_layer", "sim_cache_append", "sim_cache_attention"):
+                     "sim_moe_route", "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer",
+                     "sim_cache_append", "sim_cache_attention"):
             getattr(L, name).restype = C.c_int
         L.sim_ops_last_error.argtypes = []
         L.sim_ops_last_error.restype = C.c_char_p
@@ -168,26 +172,34 @@ class Routes(NamedTuple):
     order: torch.Tensor
 
 
-def moe_route(logits, k, mask=None, renormalize=True) -> Routes:
+def moe_route(logits, k, mask=None, renormalize=True, score="softmax", bias=None, groups=1, top_groups=None, group_best=1,
+              scale=1.0) -> Routes:
     """The k experts of each token with the highest logits [T, E], their
     softmax weights, and the experts' lists of slots.  ``mask`` ([E] or [T,
     E], true = allowed) takes experts out; ``renormalize`` divides a token's
-    weights by their sum."""
-    return _c().route(logits, k, mask, renormalize)
+    weights by their sum; ``scale`` multiplies them.
+
+    ``score`` "sigmoid" takes each logit's sigmoid for its softmax.  ``bias``
+    (float32 [E]) is added to the scores for the choice, not for the weights:
+    by it a caller balances the experts' load.  With ``groups`` of consecutive
+    experts only those of the ``top_groups`` highest take part, a group being
+    as high as its highest expert or the sum of its two highest
+    (``group_best``)."""
+    return _c().route(logits, k, mask, renormalize, score, bias, groups, top_groups, group_best, scale)
 
 
-def moe_route_grad(logits, experts, d_weights, mask=None, renormalize=True):
+def moe_route_grad(logits, experts, d_weights, mask=None, renormalize=True, score="softmax", scale=1.0):
     """Gradient of ``moe_route``'s weights with respect to the logits, from
     the gradient [T, k] of the weights."""
-    return _c().route_grad(logits, experts, d_weights, mask, renormalize)
+    return _c().route_grad(logits, experts, d_weights, mask, renormalize, score, scale)
 
 
 class _RouteWeights(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, logits, k, mask, renormalize):
-        r = moe_route(logits, k, mask, renormalize)
+    def forward(ctx, logits, k, mask, renormalize, score, bias, groups, top_groups, group_best, scale):
+        r = moe_route(logits, k, mask, renormalize, score, bias, groups, top_groups, group_best, scale)
         ctx.save_for_backward(logits, r.experts, mask)
-        ctx.renormalize = renormalize
+        ctx.how = renormalize, score, scale
         ctx.mark_non_differentiable(r.experts, r.offsets, r.order)
         return r.experts, r.weights, r.offsets, r.order
 
@@ -195,12 +207,14 @@ class _RouteWeights(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, _e, dw, _o, _s):
         logits, experts, mask = ctx.saved_tensors
-        return moe_route_grad(logits, experts, dw.contiguous(), mask, ctx.renormalize), None, None, None
+        return (moe_route_grad(logits, experts, dw.contiguous(), mask, *ctx.how),) + (None,) * 9
 
 
-def moe_route_train(logits, k, mask=None, renormalize=True) -> Routes:
-    """``moe_route`` whose weights carry gradients to the logits."""
-    return Routes(*_RouteWeights.apply(logits, k, mask, renormalize))
+def moe_route_train(logits, k, mask=None, renormalize=True, score="softmax", bias=None, groups=1, top_groups=None, group_best=1,
+                    scale=1.0) -> Routes:
+    """``moe_route`` whose weights carry gradients to the logits (the bias has
+    none: the choice is not differentiable)."""
+    return Routes(*_RouteWeights.apply(logits, k, mask, renormalize, score, bias, groups, top_groups, group_best, scale))
 
 
 def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):

@@ -1,0 +1,258 @@
+"""The router with scores, a bias and groups on the GPU against its 64-bit definition: choices and lists exactly, weights
+and gradients to their bounds."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from tests import route_reference as ref
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"fp32": 2.0 ** -24, "fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"fp32": 2.0 ** -126, "fp16": 2.0 ** -24, "bf16": 2.0 ** -126}  # (32-bit values below 2^-126 count as 0)
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2606_10440_amd import ops as o
+    return o
+
+
+def logits(seed, T, E, kind, spread=1.5, pad=0):
+    x = torch.from_numpy(np.random.default_rng(seed).standard_normal((T, E)) * spread).to(TYPES[kind])
+    d = torch.full((T, E + pad), float("nan"), dtype=x.dtype, device="cuda")[:, :E]
+    d.copy_(x)
+    return d, x.double().numpy()
+
+
+def masks(seed, T, E, how):
+    if not how:
+        return None, None
+    g = np.random.default_rng(seed)
+    m = g.random(E) < 0.7 if how == "expert" else (g.random((T, E)) < 0.4) & (g.random((T, 1)) > 0.2)
+    return torch.from_numpy(m).cuda(), m
+
+
+def check(r, want, rel=2.0 ** -24 + 2.0 ** -45):
+    # weights computed in 64 bits and rounded once
+    experts, weights, offsets, order = want
+    assert np.array_equal(r.experts.cpu().numpy(), experts)
+    assert np.array_equal(r.offsets.cpu().numpy(), offsets) and np.array_equal(r.order.cpu().numpy(), order)
+    w = r.weights.double().cpu().numpy()
+    assert np.array_equal(np.isnan(w), np.isnan(weights))
+    assert (np.abs(w - weights) <= rel * np.abs(weights) + 2.0 ** -150)[~np.isnan(weights)].all()
+
+
+SHAPES = [  # T, E, groups, top_groups, best, k
+    (1, 1, 1, 1, 1, 1), (3, 8, 4, 2, 2, 3), (16, 16, 16, 5, 2, 5), (17, 64, 8, 3, 2, 6), (5, 64, 8, 3, 1, 6), (65, 60, 5, 2, 2, 4),
+    (40, 256, 8, 4, 2, 8), (130, 256, 8, 4, 1, 8), (70, 160, 8, 3, 1, 6), (33, 160, 8, 3, 2, 6), (20, 96, 3, 2, 2, 7), (9, 1024, 64, 10, 2, 32),
+    (9, 1024, 16, 3, 2, 32), (18, 512, 1, 1, 1, 10), (1100, 32, 4, 2, 2, 4), (6, 30, 30, 4, 2, 4), (6, 700, 7, 7, 2, 17), (7, 640, 64, 6, 1, 9),
+    (4, 36, 2, 1, 2, 20)]
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_choices(ops, kind, score, shape):
+    T, E, groups, top_groups, best, k = shape
+    z, v = logits(E + k, T, E, kind, pad=3)
+    for n, (biased, how, renorm, scale) in enumerate([(True, "", True, 2.5), (False, "", False, 1.0), (True, "token", False, -0.5),
+                                                      (False, "token", True, 1.0), (True, "expert", True, 0.0)]):
+        mask, m = masks(n, T, E, how)
+        bias = np.random.default_rng(n).standard_normal(E).astype(np.float32) * 0.1 if biased else None
+        r = ops.moe_route(z, k, mask, renorm, score=score, bias=None if bias is None else torch.from_numpy(bias).cuda(),
+                          groups=groups, top_groups=top_groups, group_best=best, scale=scale)
+        want = ref.route(v, k, m, renorm, score, bias, groups, top_groups, best, scale)
+        if score == "softmax" and not biased and groups == 1 and scale == 1.0:
+            # the plain router, which computes in 32 bits: an exponential of an argument up to far, sums over 16 lanes, a division
+            check(r, want, (E / 16 + 16 + np.ptp(v, 1).max()) * ref.U32)
+        else:
+            check(r, want)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_many_tokens(ops, kind, score):
+    # so many that their counts are scanned by a kernel of their own; ties in 16 bits
+    z, v = logits(1, 33000, 8, kind)
+    b = np.array([0, 0.1, 0, 0.1, -0.1, 0.3, 0, 0], np.float32)
+    r = ops.moe_route(z, 2, score=score, bias=torch.from_numpy(b).cuda(), groups=4, top_groups=2, group_best=2)
+    check(r, ref.route(v, 2, None, True, score, b, 4, 2, 2))
+
+
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+def test_ties_go_to_the_lowest(ops, best, biased, score):
+    z = torch.zeros(3, 48, device="cuda")
+    z[1, 10:] = 1.0
+    z[2, ::7] = 200.0  # saturated scores
+    z[2, 1::7] = 100.0
+    b = np.zeros(48, np.float32) if biased else None
+    r = ops.moe_route(z, 6, score=score, bias=None if b is None else torch.from_numpy(b).cuda(), groups=6, top_groups=3, group_best=best)
+    check(r, ref.route(z.double().cpu().numpy(), 6, None, True, score, b, 6, 3, best))
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("biased", [False, True])
+def test_infinities_and_nan(ops, score, biased):
+    g = np.random.default_rng(4)
+    v = g.standard_normal((12, 32)).astype(np.float32)
+    v[0] = -np.inf
+    v[1, 3:] = -np.inf
+    v[2, 5] = np.inf if score == "sigmoid" else 3.0
+    v[3, 5] = np.nan
+    v[4] = -1000.0
+    v[4, 7] = -900.0
+    v[5] = 3e38
+    v[6] = -3e38
+    v[7, :] = -0.0
+    v[7, 4] = 0.0
+    b = np.zeros(32, np.float32)
+    b[9], b[10], b[11], b[12] = -np.inf, np.inf, 5.0, 3e38
+    if not biased:
+        b = None
+    for renorm in (True, False):
+        for groups, top, best in ((1, 1, 1), (4, 2, 2), (4, 2, 1)):
+            if best == 2 and not biased and score == "softmax":
+                continue
+            z = torch.from_numpy(v).cuda()
+            want = ref.route(v.astype(np.float64), 5, None, renorm, score, b, groups, top, best)
+            r = ops.moe_route(z, 5, None, renorm, score=score, bias=None if b is None else torch.from_numpy(b).cuda(), groups=groups,
+                              top_groups=top, group_best=best)
+            rows = [t for t in range(12) if not (score == "softmax" and t == 3)]  # a NaN makes all of that row's scores NaN
+            assert np.array_equal(r.experts.cpu().numpy()[rows], want[0][rows])
+            w = r.weights.double().cpu().numpy()[rows]
+            assert np.array_equal(np.isnan(w), np.isnan(want[1][rows]))
+            fin = ~np.isnan(w)
+            # 2^-150: half a step of the smallest 32-bit values; the plain router's 32-bit exponential is 0 below 2^-126
+            plain = score == "softmax" and not biased and groups == 1
+            rel, least = (60 * 2.0 ** -23, 2.0 ** -126) if plain else (2.0 ** -23, 2.0 ** -150)
+            assert (np.abs(w - want[1][rows])[fin] <= rel * np.abs(want[1][rows][fin]) + least).all()
+
+
+def test_every_bf16_logit_has_its_score(ops):
+    bits = (np.arange(1 << 16, dtype=np.uint32) << 16).view(np.float32)
+    v = bits[np.isfinite(bits)].astype(np.float64)
+    z = torch.from_numpy(v).to(torch.bfloat16).cuda().reshape(-1, 1)
+    r = ops.moe_route(z, 1, renormalize=False, score="sigmoid")
+    with np.errstate(over="ignore"):
+        e = np.exp(-np.abs(v))
+        want = np.where(v < 0, e, 1.0) / (1 + e)
+    w = r.weights.double().cpu().numpy()[:, 0]
+    assert (np.abs(w - want) <= (2.0 ** -24 + 2.0 ** -45) * want + 2.0 ** -150).all()
+
+
+def test_defaults_are_the_plain_router(ops):
+    z, v = logits(2, 50, 40, "bf16")
+    a = ops.moe_route(z, 4)
+    b = ops.moe_route(z, 4, score="softmax", bias=None, groups=1, top_groups=1, group_best=1, scale=1.0)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    c = ops.moe_route(z, 4, groups=8)  # all groups take part
+    assert torch.equal(a.experts, c.experts) and torch.allclose(a.weights, c.weights, rtol=2e-6)
+
+
+# ------------------------------------------------------------------ gradient
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("T,E,k,how", [(1, 1, 1, ""), (50, 60, 4, "token"), (33, 256, 8, "expert"), (20, 1024, 32, ""), (17, 100, 17, "")])
+def test_gradient(ops, kind, score, renorm, T, E, k, how):
+    z, v = logits(E, T, E, kind, pad=5)
+    mask, m = masks(7, T, E, how)
+    b = torch.from_numpy(np.random.default_rng(1).standard_normal(E).astype(np.float32) * 0.1).cuda()
+    r = ops.moe_route(z, k, mask, renorm, score=score, bias=b, scale=2.5)
+    g = np.random.default_rng(5).standard_normal((T, k)).astype(np.float32)
+    got = ops.moe_route_grad(z, r.experts, torch.from_numpy(g).cuda(), mask, renorm, score=score, scale=2.5)
+    want, bound = ref.grad(v, r.experts.cpu().numpy(), g.astype(np.float64), m, renorm, score, 2.5)
+    assert got.dtype == z.dtype
+    off = np.abs(got.double().cpu().numpy() - want)
+    assert (off <= bound + UNIT[kind] * (np.abs(want) + bound) + TINY[kind]).all()
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_gradient_against_differences(ops, score, renorm):
+    # of the 64-bit weights with the experts held
+    T, E, k = 4, 24, 5
+    z, v = logits(3, T, E, "fp32")
+    b = np.random.default_rng(2).standard_normal(E).astype(np.float32) * 0.1
+    r = ops.moe_route(z, k, None, renorm, score=score, bias=torch.from_numpy(b).cuda(), scale=1.5)
+    e = r.experts.cpu().numpy()
+    g = np.random.default_rng(6).standard_normal((T, k))
+    got = ops.moe_route_grad(z, r.experts, torch.from_numpy(g.astype(np.float32)).cuda(), None, renorm, score=score, scale=1.5)
+    got = got.double().cpu().numpy()
+    g = g.astype(np.float32).astype(np.float64)
+
+    def loss(x, t):
+        s = ref.scores(x[None], np.ones((1, E), bool), score)[0, e[t]]
+        return 1.5 * (g[t] * (s / s.sum() if renorm else s)).sum()
+
+    h = 1e-5
+    for t in range(T):
+        for i in range(E):
+            up, down = v[t].copy(), v[t].copy()
+            up[i] += h
+            down[i] -= h
+            # the third derivative of these is below 10: h^2 10 / 6; rounding 1e-16 / h
+            assert abs(got[t, i] - (loss(up, t) - loss(down, t)) / (2 * h)) < 1e-9 + 40 * 2.0 ** -23
+
+
+def test_train_carries_the_gradient(ops):
+    z, v = logits(9, 30, 64, "bf16")
+    z.requires_grad_()
+    b = torch.zeros(64, device="cuda", requires_grad=True)
+    r = ops.moe_route_train(z, 6, score="sigmoid", bias=b, groups=8, top_groups=4, group_best=2, scale=2.5)
+    g = torch.randn(30, 6, device="cuda")
+    (r.weights * g).sum().backward()
+    assert b.grad is None and not r.experts.requires_grad
+    assert torch.equal(z.grad, ops.moe_route_grad(z.detach(), r.experts, g, score="sigmoid", scale=2.5))
+
+
+def test_graph_and_streams(ops):
+    z, _ = logits(1, 200, 128, "bf16")
+    b = torch.randn(128, device="cuda") * 0.1
+    how = dict(score="sigmoid", bias=b, groups=8, top_groups=3, group_best=2)
+
+    def both(x):
+        r = ops.moe_route(x, 6, **how)
+        return r + (ops.moe_route_grad(x, r.experts, r.weights, score="sigmoid"),)
+
+    want = both(z)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = both(z)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    held = z.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(held)
+    for i in range(4):
+        x = logits(i, 200, 128, "bf16")[0]
+        held.copy_(x)
+        graph.replay()
+        want = both(x)
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+def test_refusals(ops):
+    from paper_2606_10440_amd import SimError
+    z = torch.zeros(4, 16, device="cuda")
+    for bad in [dict(score="tanh"), dict(score=None), dict(groups=3), dict(groups=0), dict(groups=17), dict(groups=-1), dict(top_groups=2),
+                dict(groups=4, top_groups=5), dict(groups=4, top_groups=0), dict(group_best=0), dict(group_best=3), dict(scale=float("inf")),
+                dict(scale=float("nan")), dict(bias=torch.zeros(15, device="cuda")), dict(bias=torch.zeros(16)),
+                dict(bias=torch.zeros(16, device="cuda").half()), dict(bias=torch.zeros(32, device="cuda")[::2]), dict(bias=[0.0] * 16)]:
+        with pytest.raises(SimError):
+            ops.moe_route(z, 2, **bad)
+    r = ops.moe_route(z, 2)
+    for bad in [dict(score="tanh"), dict(scale=float("inf"))]:
+        with pytest.raises(SimError):
+            ops.moe_route_grad(z, r.experts, r.weights, **bad)
