@@ -200,6 +200,22 @@ sim_status sim_moe_layer(void *hip_stream, const void *x, int32_t type, int64_t 
                          void *y, int64_t y_stride, void *workspace, size_t workspace_bytes);
 
 /*
+ * The same layer on choices that are given, for a share of the experts: those
+ * first .. first + n - 1, whose weights w13 [n, 2 F, D] and w2 [n, D, F] hold:
+ *   y_t = sum over the choices j with first <= e = experts[t, j] < first + n of
+ *         weights[t, j] W2_e (silu(G_e x_t) * (U_e x_t)).
+ *   experts [T, k] i32, any values (an expert twice counts twice); weights
+ *   [T, k] f32; 1 <= k <= SIM_MOE_MAX_TOPK, 1 <= n <= SIM_MOE_MAX_EXPERTS.
+ * The sum of y over the shares is the layer's result.
+ * workspace: sim_moe_experts_workspace bytes, 16-byte aligned.
+ */
+size_t sim_moe_experts_workspace(int64_t T, int64_t D, int32_t n, int32_t k, int64_t F);
+sim_status sim_moe_experts(void *hip_stream, const void *x, int32_t type, int64_t T, int64_t D, int64_t x_stride,
+                           const int32_t *experts, const float *weights, int32_t k, int32_t first, int32_t n,
+                           const void *w13, const uint8_t *s13, const void *w2, const uint8_t *s2, int32_t weight_type,
+                           int64_t F, void *y, int64_t y_stride, void *workspace, size_t workspace_bytes);
+
+/*
  * A paged key-value cache: keys and values are arrays of pages, page p of
  * [kv_heads, page_size, D] elements, contiguous, at p * page_stride elements
  * (the two may be parts of one buffer).  type is F16 or BF16; D a multiple of

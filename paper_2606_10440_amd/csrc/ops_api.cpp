@@ -312,6 +312,48 @@ sim_status sim_moe_layer(void *stream, const void *x, int32_t type, int64_t T, i
     return done(launch_layer((hipStream_t)stream, a, workspace), __func__);
 }
 
+static bool experts_fit(int64_t T, int64_t D, int32_t n, int32_t k, int64_t F) {
+    return layer_dims_fit(D, F) && layer_tiles_fit(T, D, n, k, F);
+}
+
+size_t sim_moe_experts_workspace(int64_t T, int64_t D, int32_t n, int32_t k, int64_t F) {
+    if (T <= 0 || T > SIM_MOE_LAYER_MAX_TOKENS || D <= 0 || F < 0 || n < 1 || n > SIM_MOE_MAX_EXPERTS || k < 1 ||
+        k > SIM_MOE_MAX_TOPK || !experts_fit(T, D, n, k, F))
+        return 0;
+    return layer_workspace(T, D, n, k, F);
+}
+
+sim_status sim_moe_experts(void *stream, const void *x, int32_t type, int64_t T, int64_t D, int64_t x_stride,
+                           const int32_t *experts, const float *weights, int32_t k, int32_t first, int32_t n, const void *w13,
+                           const uint8_t *s13, const void *w2, const uint8_t *s2, int32_t weight_type, int64_t F, void *y,
+                           int64_t y_stride, void *workspace, size_t workspace_bytes) {
+    NEED(type == SIM_TYPE_F16 || type == SIM_TYPE_BF16, "x must be f16 or bf16");
+    NEED(weight_type == type || weight_type == SIM_TYPE_MX4, "weights must have the type of x or be in 4 bits");
+    NEED(T >= 0 && D >= 0 && F >= 0, "negative size");
+    NEED(k >= 1 && k <= SIM_MOE_MAX_TOPK, "k out of range");
+    NEED(first >= 0 && n >= 1 && n <= SIM_MOE_MAX_EXPERTS && first <= INT32_MAX - n, "share of the experts out of range");
+    FITS(T <= SIM_MOE_LAYER_MAX_TOKENS, "too many tokens for one call");
+    FITS(layer_dims_fit(D, F), "matrix too large");
+    FITS(layer_tiles_fit(T, D, n, k, F), "too many experts of that size");
+    if (T == 0 || D == 0) return done(SIM_OK, __func__);
+    const bool mx4 = weight_type == SIM_TYPE_MX4;
+    NEED(x && y && experts && weights && (F == 0 || (w13 && w2)), "null array");
+    NEED(F == 0 || (mx4 ? s13 && s2 : !s13 && !s2), "scales go with 4-bit weights");
+    NEED(T == 1 || (x_stride >= D && y_stride >= D), "row stride below the row length");
+    NEED(aligned_to(x, 2) && aligned_to(y, 2) && aligned_to(w13, mx4 ? 16 : 2) && aligned_to(w2, mx4 ? 16 : 2) &&
+             aligned_to(s13, 8) && aligned_to(s2, 8) && aligned_to(experts, 4) && aligned_to(weights, 4),
+         "array not aligned");
+    const size_t need = sim_moe_experts_workspace(T, D, n, k, F);
+    NEED(workspace && workspace_bytes >= need && aligned_to(workspace, 16), "workspace too small or not aligned");
+    LayerArgs a;
+    a.route = RouteArgs{nullptr, SIM_TYPE_F32, T, n, 0, nullptr, 0, k, false};
+    a.route.given = experts, a.route.given_weights = weights, a.route.first = first;
+    a.x = x, a.type = type, a.D = D, a.x_stride = x_stride;
+    a.w13 = w13, a.w2 = w2, a.s13 = s13, a.s2 = s2, a.mx4 = mx4, a.F = F;
+    a.y = y, a.y_stride = y_stride;
+    return done(launch_layer((hipStream_t)stream, a, workspace), __func__);
+}
+
 namespace {
 constexpr int64_t kMaxKeys = (int64_t)1 << 30;  // of one sequence
 constexpr int64_t kMaxGroups = (int64_t)1 << 31;  // workgroups of one launch

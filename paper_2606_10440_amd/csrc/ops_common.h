@@ -124,6 +124,10 @@ struct RouteArgs {
     const float *bias = nullptr;
     int groups = 1, top_groups = 1, group_best = 1;
     float scale = 1.f;
+    // choices that are made already, of experts first .. first + E - 1 and others
+    const int32_t *given = nullptr;
+    const float *given_weights = nullptr;
+    int first = 0;
 };
 sim_status launch_route(hipStream_t st, const RouteArgs &a, int32_t *experts, float *weights, int32_t *offsets,
                         int32_t *order, void *ws);

@@ -327,7 +327,18 @@ __device__ inline int few_route(const RouteArgs &a, FewRoute &s) {
     static_assert(64 * kFewWaves == kFewExperts && 4 * kFewWaves == kFewTokens, "a thread for each expert, sixteen for each token");
     s.tokens[threadIdx.x] = 0;
     __syncthreads();
-    if (t < n_tok) {
+    if (a.given) {
+        uint32_t e[2], had[2];
+        float w[2];
+        given_choices(a, min(t, n_tok - 1), e, had, w);
+#pragma unroll
+        for (int q = 0; q < 2; q++)
+            if (t < n_tok && had[q]) {
+                s.weight[t * a.k + q * 16 + l] = w[q];
+                s.pos[t][e[q]] = (uint8_t)(q * 16 + l);
+                atomicOr(&s.tokens[e[q]], 1u << t);
+            }
+    } else if (t < n_tok) {
         if (a.E <= 64) few_choose<4>(a, s, t, l);
         else if (a.E <= 128) few_choose<8>(a, s, t, l);
         else few_choose<kFewExperts / 16>(a, s, t, l);

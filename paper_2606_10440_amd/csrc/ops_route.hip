@@ -421,6 +421,22 @@ __global__ __launch_bounds__(256) void route_grad(const typename Elem<T>::type *
             if (l * NV + i < E) o[i] = out[i];
 }
 
+// Lists of choices that are given.
+template <int CH>
+__global__ __launch_bounds__(16 * CH) void route_given(RouteArgs a, int32_t *__restrict__ experts, float *__restrict__ weights,
+                                                       uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,
+                                                       int32_t *__restrict__ order) {
+    __shared__ Lists lists;
+    const int64_t t = (int64_t)blockIdx.x * CH + (threadIdx.x >> 4);
+    const bool live = t < a.T;
+    clear<CH>(lists);
+    uint32_t e[2], had[2];
+    float w[2];
+    given_choices(a, live ? t : 0, e, had, w);
+    __syncthreads();
+    finish<CH>(lists, t, live, a.k, a.E, (int)min(a.T, (int64_t)CH), e, had, w, experts, weights, hist, offsets, order);
+}
+
 // ------------------------------------------------------------------ scores, bias, groups
 
 // e^x for x <= 0 in 64 bits: 2^n times the exponential's series at what is left,
@@ -735,10 +751,15 @@ sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *
             (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts,
             weights, hist, offsets, order);
     };
-    with_nv(a.E, [&](auto nv) {
-        if (rows > chunks) choose(nv, std::integral_constant<int, kPart>());
-        else choose(nv, std::integral_constant<int, kChunk>());
-    });
+    if (a.given) {
+        if (rows > chunks) route_given<kPart><<<rows, 16 * kPart, 0, st>>>(a, experts, weights, hist, offsets, order);
+        else route_given<kChunk><<<chunks, kThreads, 0, st>>>(a, experts, weights, hist, offsets, order);
+    } else {
+        with_nv(a.E, [&](auto nv) {
+            if (rows > chunks) choose(nv, std::integral_constant<int, kPart>());
+            else choose(nv, std::integral_constant<int, kChunk>());
+        });
+    }
     if (order && rows > 1) {
         if (sums) route_scan<<<(a.E + 15) / 16, kThreads, 0, st>>>(hist, sums, (int)chunks, a.E);
         route_place<<<chunks, kThreads, 0, st>>>(experts, a.T, a.E, a.k, hist, rows > chunks ? kChunk / kPart : 1, (int)rows, sums,

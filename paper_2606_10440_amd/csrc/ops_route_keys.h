@@ -51,4 +51,32 @@ __device__ inline uint32_t max16(uint32_t v) {
     return v;
 }
 
+// A token's given choices l and l + 16, in sixteen lanes: the expert's place in
+// the share (had: whether it is in it) and its weight.  An expert that a token
+// names more than once is its first choice, with the sum of the weights.
+__device__ inline void given_choices(const RouteArgs &a, int64_t t, uint32_t e[2], uint32_t had[2], float w[2]) {
+    const int l = threadIdx.x & 15;
+    int all[2];
+    float weight[2];
+#pragma unroll
+    for (int q = 0; q < 2; q++) {
+        const bool in = q * 16 + l < a.k;
+        all[q] = in ? a.given[t * a.k + q * 16 + l] : -1;
+        weight[q] = in ? a.given_weights[t * a.k + q * 16 + l] : 0.f;
+        had[q] = in && all[q] >= a.first && (int64_t)all[q] - a.first < a.E;
+        e[q] = had[q] ? (uint32_t)(all[q] - a.first) : 0;
+        w[q] = 0.f;
+    }
+    for (int j = 0; j < a.k; j++) {
+        const int from = (threadIdx.x & 48) | (j & 15), other = __shfl(j < 16 ? all[0] : all[1], from);
+        const float its = __shfl(j < 16 ? weight[0] : weight[1], from);
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+            if (other != all[q]) continue;
+            w[q] += its;
+            if (j < q * 16 + l) had[q] = 0;
+        }
+    }
+}
+
 }  // namespace simops

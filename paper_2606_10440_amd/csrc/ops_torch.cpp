@@ -35,7 +35,7 @@ PyObject *g_error, *g_mx4, *g_routes, *g_cache;  // SimError, Mx4, Routes, Paged
     X(sim_mx4_quantize) X(sim_mx4_dequantize) X(sim_mx4_matmul) X(sim_mx4_linear_workspace) X(sim_mx4_linear)       \
         X(sim_mx4_linear_grad_workspace) X(sim_mx4_linear_grad) X(sim_moe_route_workspace) X(sim_moe_route)         \
             X(sim_moe_route_grad) X(sim_moe_route_scored) X(sim_moe_route_scored_grad) X(sim_moe_layer_workspace)       \
-                X(sim_moe_layer) X(sim_cache_append) X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
+                X(sim_moe_layer) X(sim_moe_experts_workspace) X(sim_moe_experts) X(sim_cache_append) X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
 struct {
 #define X(name) decltype(&::name) name;
     SIM_OPS_CALLS(X)
@@ -395,6 +395,32 @@ PyObject *layer(PyObject *const *a) {  // x, logits, w13, w2, k, mask, renormali
     return y.written();
 }
 
+PyObject *experts(PyObject *const *a) {  // x, experts, weights, w13, w2, first, out
+    const Rows x = rows_of(a[0], "x");
+    need(x.type != SIM_TYPE_F32, "x must be float16 or bfloat16");
+    const at::ScalarType type = THPVariable_Unpack(a[0]).scalar_type();
+    const Tensor &e = tensor(a[1], "experts"), &w = tensor(a[2], "weights");
+    need(e.dim() == 2 && e.size(0) == x.rows && w.sizes() == e.sizes(), "experts and weights must be [T, k]");
+    need(e.scalar_type() == at::kInt && w.scalar_type() == at::kFloat, "experts must be int32, weights float32");
+    need(e.is_contiguous() && w.is_contiguous(), "experts and weights must be contiguous");
+    need(e.device() == x.dev && w.device() == x.dev, "tensors are on different GPUs");
+    const int64_t k = e.size(1), D = x.cols;
+    need(k >= 1 && k <= SIM_MOE_MAX_TOPK, "k out of range");
+    const Weights w13(a[3], type, x.dev, "w13"), w2(a[4], type, x.dev, "w2");
+    need(w13.type == w2.type && w13.shape.size() == 3 && w2.shape.size() == 3 && w2.shape[1] == D && w13.shape[0] == w2.shape[0] &&
+             w13.shape[1] == 2 * w2.shape[2] && w13.shape[2] == D,
+         "w13 must be [n, 2F, D], w2 [n, D, F], of one kind");
+    const int64_t n = w2.shape[0], F = w2.shape[2];
+    need(n >= 1 && n <= SIM_MOE_MAX_EXPERTS, "expert count out of range");
+    const int32_t first = small(a[5], "first");
+    const Result y(a[6], x.rows, D, type, x.dev);
+    need(y.r.type == x.type, "out must have the type of x");
+    const Space ws(g.sim_moe_experts_workspace(x.rows, D, (int32_t)n, (int32_t)k, F), x.dev);
+    call(x.dev, g.sim_moe_experts, x.p, x.type, x.rows, D, x.stride, (const int32_t *)e.data_ptr(), (const float *)w.data_ptr(), (int32_t)k,
+         first, (int32_t)n, w13.p, w13.scales, w2.p, w2.scales, w2.type, F, y.r.p, y.r.stride, ws.p, ws.n);
+    return y.written();
+}
+
 // ------------------------------------------------------------------ paged cache
 
 // A tensor [N, heads, D] whose rows of D are contiguous, for reading.
@@ -547,6 +573,7 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          ENTRY("route", route, 10),
                          ENTRY("route_grad", route_grad, 7),
                          ENTRY("layer", layer, 8),
+                         ENTRY("experts", experts, 7),
                          ENTRY("append", append, 4),
                          ENTRY("attention", attention, 8),
                          {nullptr, nullptr, 0, nullptr}};

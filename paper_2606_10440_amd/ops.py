@@ -28,7 +28,8 @@ from .sim import SimError
 EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim_mx4_dequantize",
            "sim_mx4_matmul", "sim_mx4_linear_workspace", "sim_mx4_linear",
            "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route",
-           "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer_workspace", "sim_moe_layer", "sim_cache_append",
+           "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer_workspace", "sim_moe_layer",
+           "sim_moe_experts_workspace", "sim_moe_experts", "sim_cache_append",
            "sim_cache_attention_workspace", "sim_cache_attention", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
@@ -64,6 +65,9 @@ def lib():
         L.sim_moe_layer_workspace.restype = sz
         L.sim_moe_layer.argtypes = [P, P, i32, i64, i64, i64, P, i32, i32, i64, P, i64, i32, i32, P, P, P, P, i32,
                                     i64, P, i64, P, sz]
+        L.sim_moe_experts_workspace.argtypes = [i64, i64, i32, i32, i64]
+        L.sim_moe_experts_workspace.restype = sz
+        L.sim_moe_experts.argtypes = [P, P, i32, i64, i64, i64, P, P, i32, i32, i32, P, P, P, P, i32, i64, P, i64, P, sz]
         L.sim_cache_append.argtypes = [P, i32, P, i64, i64, P, i64, i64, i64, i32, i32, P, P, i64, P, i64, i64, i32]
         L.sim_cache_attention_workspace.argtypes = [i64, i32, i32, i32, i32, i32, i32]
         L.sim_cache_attention_workspace.restype = sz
@@ -71,7 +75,7 @@ def lib():
                                           C.c_float, i32, P, i64, P, P, sz]
         for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_mx4_linear_grad",
                      "sim_moe_route", "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer",
-                     "sim_cache_append", "sim_cache_attention"):
+                     "sim_moe_experts", "sim_cache_append", "sim_cache_attention"):
             getattr(L, name).restype = C.c_int
         L.sim_ops_last_error.argtypes = []
         L.sim_ops_last_error.restype = C.c_char_p
@@ -225,6 +229,16 @@ def moe_layer(x, logits, w13, w2, k, mask=None, renormalize=True, out=None):
     is float16 or bfloat16; the weights have its type, or are ``Mx4``; ``out``
     may be x.  For inference: the result carries no gradients."""
     return _c().layer(x, logits, w13, w2, k, mask, renormalize, out)
+
+
+def moe_experts(x, experts, weights, w13, w2, first=0, out=None):
+    """The experts' layer for few tokens on choices that are given (``experts``
+    [T, k] int32 and ``weights`` [T, k] float32, as ``moe_route`` returns
+    them), for a share of the experts: w13 [n, 2F, D] and w2 [n, D, F] are
+    those of experts ``first`` .. ``first + n - 1``, as ``moe_layer`` takes
+    them, and choices of others add nothing.  The results of the shares add up
+    to the layer's.  ``out`` may be x.  The result carries no gradients."""
+    return _c().experts(x, experts, weights, w13, w2, first, out)
 
 
 # ------------------------------------------------------------------ paged cache
