@@ -264,6 +264,35 @@ sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, in
                                const int32_t *lengths, float scale, int32_t window, void *out, int64_t out_stride,
                                float *lse, void *workspace, size_t workspace_bytes);
 
+/*
+ * The next token of each of B rows of logits [B, V] (F32, F16 or BF16, V <=
+ * SIM_SAMPLE_MAX_V), from uniform random numbers u [B] that are given:
+ *   w_i = e^((z_i - max z) / temperature); logits in falling order, ties to the
+ *     lowest index, i's place in it being its rank;
+ *   kept are those with rank < top_k, of these the ones before which the
+ *     order's weights sum up to less than top_p times the first top_k's sum,
+ *     and of these the ones with w_i >= min_p; the highest always is;
+ *   the token is the first kept i, in the order of the indices, up to and with
+ *     which the kept weights' sum is above u times the sum of all of them.
+ * Weights and sums are in 64 bits, so that only values that close to a border
+ * depend on the order of summation.  A temperature that is not above 0 means
+ * the highest logit's first index; top_k below 1 or above V, a top_p of 1 or
+ * more or NaN, and a min_p that is not above 0 keep all; a top_p of 0 or less
+ * and a min_p above 1 keep the highest.  u below 0 or NaN counts as 0, above 1
+ * - 2^-24 as that.  -infinity is never chosen; a row whose highest logit is
+ * -infinity, +infinity or NaN gets -1.
+ *   temperature, top_k, top_p, min_p: [B] (f32; top_k i32), or NULL for the
+ *   same value in all rows, which is given beside it (temperature >= 0, finite;
+ *   0 <= top_p <= 1; 0 <= min_p <= 1; not read where there is an array).
+ * workspace: sim_sample_workspace bytes, 16-byte aligned (NULL if 0).
+ */
+#define SIM_SAMPLE_MAX_V (1 << 20)
+size_t sim_sample_workspace(int64_t B, int32_t V);
+sim_status sim_sample(void *hip_stream, const void *logits, int32_t type, int64_t B, int32_t V, int64_t logit_stride,
+                      const float *u, const float *temperature, float all_temperature, const int32_t *top_k, int32_t all_k,
+                      const float *top_p, float all_p, const float *min_p, float all_min, int32_t *tokens, void *workspace,
+                      size_t workspace_bytes);
+
 /* Text of this thread's last refused or failed operator call ("" if none). */
 const char *sim_ops_last_error(void);
 

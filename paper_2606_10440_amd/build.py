@@ -19,7 +19,8 @@ BINDING = os.path.join(HERE, "_ops_torch.so")
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.cpp", "engine_launch.cpp", "engine_wg.hip", "engine_lane.hip", "engine_b1.hip",
            "engine_wave.hip", "engine_wave_rr8.hip", "engine_grid.hip", "engine_res.hip", "engine_route.hip", "noalloc.hip",
-           "ops_api.cpp", "ops_mx4.hip", "ops_mx4_matmul.hip", "ops_route.hip", "ops_layer.hip", "ops_cache.hip"]
+           "ops_api.cpp", "ops_mx4.hip", "ops_mx4_matmul.hip", "ops_route.hip", "ops_layer.hip", "ops_cache.hip",
+           "ops_sample.hip"]
 ARCH = os.environ.get("SIMGPU_ARCH", "gfx950")
 OBJDIR = os.path.join(ROOT, "_build", "simgpu")
 

@@ -448,4 +448,30 @@ sim_status sim_cache_attention(void *stream, int32_t type, const void *q, int64_
     return done(launch_attention((hipStream_t)stream, a), __func__);
 }
 
+static bool sample_fits(int64_t B, int32_t V) { return B >= 0 && B < kMaxDim / 1024 && V <= SIM_SAMPLE_MAX_V; }
+
+size_t sim_sample_workspace(int64_t B, int32_t V) { return B > 0 && V > 0 && sample_fits(B, V) ? sample_workspace(B, V) : 0; }
+
+sim_status sim_sample(void *stream, const void *logits, int32_t type, int64_t B, int32_t V, int64_t logit_stride, const float *u,
+                      const float *temperature, float all_temperature, const int32_t *top_k, int32_t all_k, const float *top_p,
+                      float all_p, const float *min_p, float all_min, int32_t *tokens, void *workspace, size_t workspace_bytes) {
+    NEED(is_float(type), "logits must be f32, f16 or bf16");
+    NEED(B >= 0 && V >= 1, "there must be a logit to choose");
+    FITS(sample_fits(B, V), "too many logits");
+    NEED(temperature || (all_temperature >= 0 && std::isfinite(all_temperature)), "temperature must be finite and not negative");
+    NEED(top_p || (all_p >= 0 && all_p <= 1), "top_p must be from 0 to 1");
+    NEED(min_p || (all_min >= 0 && all_min <= 1), "min_p must be from 0 to 1");
+    NEED(top_k || all_k >= 0, "top_k must not be negative");
+    if (B == 0) return done(SIM_OK, __func__);
+    NEED(logits && u && tokens, "null array");
+    NEED(B == 1 || logit_stride >= V, "logit stride below the row length");
+    NEED(aligned_to(logits, size_of(type)) && aligned_to(u, 4) && aligned_to(temperature, 4) && aligned_to(top_k, 4) &&
+             aligned_to(top_p, 4) && aligned_to(min_p, 4) && aligned_to(tokens, 4),
+         "array not aligned to its type");
+    const size_t need = sim_sample_workspace(B, V);
+    NEED(need == 0 || (workspace && workspace_bytes >= need && aligned_to(workspace, 16)), "workspace too small or not aligned");
+    const SampleArgs a = {logits, type, B, logit_stride, V, u, temperature, top_p, min_p, top_k, all_temperature, all_p, all_min, all_k, tokens};
+    return done(launch_sample((hipStream_t)stream, a, workspace), __func__);
+}
+
 }  // extern "C"

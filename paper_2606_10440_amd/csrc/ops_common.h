@@ -175,6 +175,19 @@ struct AttendArgs {
     bool q_aligned, out_aligned;
 };
 sim_status launch_attention(hipStream_t st, const AttendArgs &a);
+struct SampleArgs {
+    const void *logits;
+    int type;
+    int64_t B, stride;
+    int V;
+    const float *u, *temperature, *top_p, *min_p;  // NULL: the values below, for all rows
+    const int32_t *top_k;
+    float all_temperature, all_p, all_min;
+    int all_k;
+    int32_t *tokens;
+};
+sim_status launch_sample(hipStream_t st, const SampleArgs &a, void *ws);
+size_t sample_workspace(int64_t B, int V);
 sim_status launch_layer(hipStream_t st, const LayerArgs &a, void *ws);
 size_t layer_workspace(int64_t T, int64_t D, int E, int k, int64_t F);
 

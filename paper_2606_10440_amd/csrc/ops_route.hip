@@ -10,6 +10,7 @@
 // choice 11 us (k searches of 16 registers a lane, 1.1 TB/s), lists 8.7 us (a
 // workgroup reads the 66 KB of all chunks' counts), gradient 8 us; 8 tokens,
 // 64 experts: 4.5 us in one launch.
+#include "ops_exp64.h"
 #include "ops_route_keys.h"
 
 namespace simops {
@@ -439,29 +440,6 @@ __global__ __launch_bounds__(16 * CH) void route_given(RouteArgs a, int32_t *__r
 
 // ------------------------------------------------------------------ scores, bias, groups
 
-// e^x for x <= 0 in 64 bits: 2^n times the exponential's series at what is left,
-// at most ln 2 / 2 in magnitude, up to r^12 / 12! (the next term is below 2^-53).
-__device__ inline double exp64(double x) {
-    x = x < -800. ? -800. : x;  // (0 then; a NaN stays)
-    // the nearest whole number in the low bits of 1.5 2^52 and it
-    const double magic = 6755399441055744., t = __builtin_fma(x, 1.4426950408889634, magic), n = t - magic;
-    // ln 2 as 24 bits, by which n is multiplied exactly, and the rest
-    const double r = __builtin_fma(n, 1.904654299957768e-09, __builtin_fma(n, -0.693147182464599609375, x));
-    double p = 1. / 479001600.;
-    p = __builtin_fma(p, r, 1. / 39916800.);
-    p = __builtin_fma(p, r, 1. / 3628800.);
-    p = __builtin_fma(p, r, 1. / 362880.);
-    p = __builtin_fma(p, r, 1. / 40320.);
-    p = __builtin_fma(p, r, 1. / 5040.);
-    p = __builtin_fma(p, r, 1. / 720.);
-    p = __builtin_fma(p, r, 1. / 120.);
-    p = __builtin_fma(p, r, 1. / 24.);
-    p = __builtin_fma(p, r, 1. / 6.);
-    p = __builtin_fma(p, r, .5);
-    p = __builtin_fma(p, r, 1.);
-    p = __builtin_fma(p, r, 1.);
-    return __builtin_ldexp(p, (int)__builtin_bit_cast(uint64_t, t));
-}
 // 1 / x for 1 <= x <= 2^11, to the last place but one
 __device__ inline double reciprocal(double x) {
     double y = __builtin_amdgcn_rcp(x);
@@ -554,7 +532,7 @@ template <int NV> __device__ inline uint64_t top_groups(const uint32_t key[NV], 
 // a score was computed, so scores are in 64 bits and rounded to 32, in which
 // the bias and the groups' sums are added: what is compared is the definition's
 // but where a 64-bit value lies within its own error of the middle between two
-// 32-bit ones.  64-bit fused operations run at the rate of 32-bit ones here.
+// 32-bit ones.
 template <int T, int NV, int CH>
 __global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__restrict__ experts, float *__restrict__ weights,
                                                         uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,

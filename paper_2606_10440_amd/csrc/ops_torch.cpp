@@ -35,7 +35,7 @@ PyObject *g_error, *g_mx4, *g_routes, *g_cache;  // SimError, Mx4, Routes, Paged
     X(sim_mx4_quantize) X(sim_mx4_dequantize) X(sim_mx4_matmul) X(sim_mx4_linear_workspace) X(sim_mx4_linear)       \
         X(sim_mx4_linear_grad_workspace) X(sim_mx4_linear_grad) X(sim_moe_route_workspace) X(sim_moe_route)         \
             X(sim_moe_route_grad) X(sim_moe_route_scored) X(sim_moe_route_scored_grad) X(sim_moe_layer_workspace)       \
-                X(sim_moe_layer) X(sim_moe_experts_workspace) X(sim_moe_experts) X(sim_cache_append) X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_ops_last_error)
+                X(sim_moe_layer) X(sim_moe_experts_workspace) X(sim_moe_experts) X(sim_cache_append) X(sim_cache_attention_workspace) X(sim_cache_attention) X(sim_sample_workspace) X(sim_sample) X(sim_ops_last_error)
 struct {
 #define X(name) decltype(&::name) name;
     SIM_OPS_CALLS(X)
@@ -525,6 +525,41 @@ PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, w
     return both;
 }
 
+// ------------------------------------------------------------------ the next token
+
+// A parameter of every row, or one number for all.
+template <typename V> struct Setting {
+    const V *p = nullptr;
+    V all = 0;
+    Setting(PyObject *o, int64_t B, c10::Device dev, const char *what) {
+        constexpr bool whole_number = std::is_integral<V>::value;
+        if (THPVariable_Check(o)) {
+            const Tensor &t = THPVariable_Unpack(o);
+            need(t.dim() == 1 && t.size(0) == B && t.scalar_type() == (whole_number ? at::kInt : at::kFloat) && t.is_contiguous() && t.device() == dev,
+                 what, whole_number ? " must be a number or contiguous int32 [B] on the same GPU" : " must be a number or contiguous float32 [B] on the same GPU");
+            if (B) p = (const V *)t.data_ptr();
+        } else {
+            if constexpr (whole_number) all = small(o, what);
+            else all = (V)number(o);
+        }
+    }
+};
+
+PyObject *sample(PyObject *const *a) {  // logits, u, temperature, top_k, top_p, min_p
+    const Rows z = rows_of(a[0], "logits");
+    need(z.cols >= 1 && z.cols < (int64_t)1 << 31, "there must be a logit to choose");
+    const Tensor &u = tensor(a[1], "u");
+    need(u.dim() == 1 && u.size(0) == z.rows && u.scalar_type() == at::kFloat && u.is_contiguous() && u.device() == z.dev,
+         "u must be contiguous float32 [B] on the same GPU");
+    const Setting<float> t(a[2], z.rows, z.dev, "temperature"), p(a[4], z.rows, z.dev, "top_p"), m(a[5], z.rows, z.dev, "min_p");
+    const Setting<int32_t> k(a[3], z.rows, z.dev, "top_k");
+    const Tensor tokens = fresh({z.rows}, at::kInt, z.dev);
+    const Space ws(g.sim_sample_workspace(z.rows, (int32_t)z.cols), z.dev);
+    call(z.dev, g.sim_sample, z.p, z.type, z.rows, (int32_t)z.cols, z.stride, (const float *)u.data_ptr(), t.p, t.all, k.p, k.all, p.p, p.all, m.p,
+         m.all, (int32_t *)tokens.data_ptr(), ws.p, ws.n);
+    return wrap(tokens);
+}
+
 // ------------------------------------------------------------------ the module
 
 template <PyObject *(*F)(PyObject *const *), int N> PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -574,6 +609,7 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          ENTRY("route_grad", route_grad, 7),
                          ENTRY("layer", layer, 8),
                          ENTRY("experts", experts, 7),
+                         ENTRY("sample", sample, 6),
                          ENTRY("append", append, 4),
                          ENTRY("attention", attention, 8),
                          {nullptr, nullptr, 0, nullptr}};

@@ -30,7 +30,7 @@ EXPORTS = ("sim_mx4_code_pitch", "sim_mx4_scale_pitch", "sim_mx4_quantize", "sim
            "sim_mx4_linear_grad_workspace", "sim_mx4_linear_grad", "sim_moe_route_workspace", "sim_moe_route",
            "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer_workspace", "sim_moe_layer",
            "sim_moe_experts_workspace", "sim_moe_experts", "sim_cache_append",
-           "sim_cache_attention_workspace", "sim_cache_attention", "sim_ops_last_error")
+           "sim_cache_attention_workspace", "sim_cache_attention", "sim_sample_workspace", "sim_sample", "sim_ops_last_error")
 
 MAX_EXPERTS, MAX_TOPK, MAX_LAYER_TOKENS = 1024, 32, 1024
 
@@ -73,9 +73,13 @@ def lib():
         L.sim_cache_attention_workspace.restype = sz
         L.sim_cache_attention.argtypes = [P, i32, P, i64, i64, i64, i32, i32, i32, P, i64, P, i64, i64, i32, P, i64, i32, P,
                                           C.c_float, i32, P, i64, P, P, sz]
+        L.sim_sample_workspace.argtypes = [i64, i32]
+        L.sim_sample_workspace.restype = sz
+        f32 = C.c_float
+        L.sim_sample.argtypes = [P, P, i32, i64, i32, i64, P, P, f32, P, i32, P, f32, P, f32, P, P, sz]
         for name in ("sim_mx4_quantize", "sim_mx4_dequantize", "sim_mx4_matmul", "sim_mx4_linear", "sim_mx4_linear_grad",
                      "sim_moe_route", "sim_moe_route_grad", "sim_moe_route_scored", "sim_moe_route_scored_grad", "sim_moe_layer",
-                     "sim_moe_experts", "sim_cache_append", "sim_cache_attention"):
+                     "sim_moe_experts", "sim_cache_append", "sim_cache_attention", "sim_sample"):
             getattr(L, name).restype = C.c_int
         L.sim_ops_last_error.argtypes = []
         L.sim_ops_last_error.restype = C.c_char_p
@@ -269,3 +273,18 @@ def cache_attention(q, cache: PagedCache, table, lengths, scale=None, window=0, 
     the logarithm of each head's sum of weights, float32 [B, q heads].  ``out``
     may have strided rows.  The result carries no gradients."""
     return _c().attention(q, cache, table, lengths, scale, window, return_lse, out)
+
+
+# ------------------------------------------------------------------ the next token
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The next token of each row of logits [B, V], int32 [B], from uniform
+    random numbers ``u`` [B] (float32 in [0, 1)).  Of the weights e^(logit /
+    temperature) the ``top_k`` highest are kept (0: all), of these the highest
+    ones that together have ``top_p`` of their sum, and of these the ones of at
+    least ``min_p`` times the highest; the token is where the kept weights'
+    running sum, in the order of the indices, passes u times the whole.
+    Temperature 0 takes the highest logit.  Each setting is a number or a
+    tensor [B] (float32; ``top_k`` int32).  A row without a finite highest
+    logit gets -1."""
+    return _c().sample(logits, u, temperature, top_k, top_p, min_p)
