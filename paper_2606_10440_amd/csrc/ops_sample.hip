@@ -3,15 +3,25 @@
 //
 // What is kept is a run of the logits' falling order, so it is known by the
 // lowest kept logit and how many of the logits that tie with it are kept, in
-// the order of their indices.  That logit is searched digit by digit of a key
-// that orders as the logits do, by the number of logits to a digit (top-k) or
-// by the sum of their weights (top-p).
+// the order of their indices.  A row is read by several workgroups, a slice
+// each, in up to four launches:
+//   tops    the highest logit of each slice;
+//   bins    the numbers of logits, or the sums of their weights, by how far
+//           they are below the highest, in steps of 1/128 of that distance;
+//   border  the logits of the bin in which the border lies (with a small
+//           top-k: of all above it too), which the row's last workgroup sorts:
+//           a small top-k's row is done with that;
+//   pick    the sums of the kept weights of 512 logits each; the row's last
+//           workgroup finds the 512 that the token is in, and the token.
+// A row whose border bin holds more than can be sorted (logits that are nearly
+// all the same, say) is searched by one workgroup alone, digit by digit of a
+// key that orders as the logits do.
 #include "ops_exp64.h"
 
 namespace simops {
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kDigit = 11;
 constexpr int kBins = 1 << kDigit;
@@ -46,10 +56,8 @@ struct Shared {
     uint64_t bin[kBins];
     uint64_t wave64[kWaves];
     double wave_d[kWaves];
-    uint32_t wave_key[kWaves], wave_at[kWaves];
     uint32_t digit;
     uint64_t above;
-    int found;
 };
 
 template <int T> struct Row {
@@ -60,6 +68,36 @@ template <int T> struct Row {
     __device__ double weight(uint32_t key) const { return exp64(((double)value_of<T>(key) - top) * per); }
     __device__ uint32_t key(int i) const { return key_of<T>(z[i]); }
 };
+
+// The first of kBins values at which their running sum reaches target, in all
+// threads, and the sum before it; -1 where all together do not.  The caller
+// keeps to barriers around it.
+template <typename Bin> __device__ inline int crossing(Bin &&bin, uint64_t target, uint64_t *wave_sums, uint64_t &before) {
+    constexpr int kEach = kBins / kThreads;
+    __shared__ int s_at;
+    __shared__ uint64_t s_before;
+    uint64_t v[kEach], own = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; i++) own += v[i] = bin(threadIdx.x * kEach + i);
+    uint64_t sum = own;
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t o = __shfl_up((unsigned long long)sum, d);
+        if ((int)(threadIdx.x & 63) >= d) sum += o;
+    }
+    if ((threadIdx.x & 63) == 63) wave_sums[threadIdx.x >> 6] = sum;
+    if (threadIdx.x == 0) s_at = -1;
+    __syncthreads();
+    uint64_t run = sum - own;
+    for (int w = 0; w < (int)(threadIdx.x >> 6); w++) run += wave_sums[w];
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+        if (run < target && run + v[i] >= target) s_at = threadIdx.x * kEach + i, s_before = run;
+        run += v[i];
+    }
+    __syncthreads();
+    before = s_before;
+    return s_at;
+}
 
 // Sum over the workgroup, in an order of its own.
 __device__ inline double block_sum(double v, Shared &s) {
@@ -84,7 +122,6 @@ __device__ inline bool search(const Row<T> &row, Shared &s, uint64_t target, uin
         const int bits = min(left, kDigit), shift = left - bits;
         __syncthreads();
         for (int i = threadIdx.x; i < kBins; i += kThreads) s.bin[i] = 0;
-        if (threadIdx.x == 0) s.found = 0;
         __syncthreads();
         for (int i = threadIdx.x; i < row.V; i += kThreads) {
             const uint32_t k = row.key(i);
@@ -95,22 +132,13 @@ __device__ inline bool search(const Row<T> &row, Shared &s, uint64_t target, uin
         if (threadIdx.x == 0 && extra && (left == 32 || (extra_key >> left) == prefix))
             atomicAdd((unsigned long long *)&s.bin[(extra_key >> shift) & ((1u << bits) - 1)], (unsigned long long)extra);
         __syncthreads();
-        // two bins a thread, from the highest down
-        const int hi = kBins - 1 - 2 * threadIdx.x;
-        const uint64_t a = s.bin[hi], b = s.bin[hi - 1];
-        uint64_t sum = a + b;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t o = __shfl_up((unsigned long long)sum, d);
-            if ((int)(threadIdx.x & 63) >= d) sum += o;
-        }
-        if ((threadIdx.x & 63) == 63) s.wave64[threadIdx.x >> 6] = sum;
+        // from the highest bin down
+        const auto bin = [&](int i) { return s.bin[kBins - 1 - i]; };
+        uint64_t before;
+        const int at = crossing(bin, target - above, s.wave64, before);
+        if (at < 0) return false;
+        s.digit = kBins - 1 - at, s.above = above + before;
         __syncthreads();
-        uint64_t before = above + sum - a - b;
-        for (int w = 0; w < (int)(threadIdx.x >> 6); w++) before += s.wave64[w];
-        if (before < target && before + a >= target) s.digit = hi, s.above = before, s.found = 1;
-        else if (before + a < target && before + a + b >= target) s.digit = hi - 1, s.above = before + a, s.found = 1;
-        __syncthreads();
-        if (!s.found) return false;
         prefix = (left < 32 ? prefix << bits : 0) | s.digit;
         above = s.above;
         left = shift;
@@ -163,42 +191,12 @@ __device__ inline int locate(Shared &s, int V, Weight &&weight, Target &&target_
     return lo + (past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : 0);
 }
 
-template <int T> __global__ __launch_bounds__(kThreads) void sample_rows(SampleArgs a) {
-    typedef typename Elem<T>::type El;
-    __shared__ Shared s;
-    const int64_t b = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Row<T> row;
-    row.z = (const El *)a.logits + b * a.stride;
-    row.V = a.V;
-
-    // the highest and its first index
-    uint32_t best = 0, at = 0;
-    for (int i = threadIdx.x; i < a.V; i += kThreads) {
-        const uint32_t k = row.key(i);
-        if (k > best) best = k, at = i;
-    }
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t k = __shfl_xor(best, d), i = __shfl_xor(at, d);
-        if (k > best || (k == best && i < at)) best = k, at = i;
-    }
-    if (lane == 0) s.wave_key[wave] = best, s.wave_at[wave] = at;
-    __syncthreads();
-    for (int w = 0; w < kWaves; w++)
-        if (s.wave_key[w] > best || (s.wave_key[w] == best && s.wave_at[w] < at)) best = s.wave_key[w], at = s.wave_at[w];
-    const float temperature = a.temperature ? a.temperature[b] : a.all_temperature, min_p = a.min_p ? a.min_p[b] : a.all_min;
-    const float top_p = a.top_p ? a.top_p[b] : a.all_p;
-    const int top_k = a.top_k ? a.top_k[b] : a.all_k;
-    if (best == 0 || best >= kInfinite<T> || !(temperature > 0.f) || top_k == 1 || top_p <= 0.f || min_p > 1.f) {
-        if (threadIdx.x == 0) a.tokens[b] = best == 0 || best >= kInfinite<T> ? -1 : (int)at;
-        return;
-    }
-    row.top = value_of<T>(best);
-    row.per = 1. / temperature;
-
+// A row by one workgroup alone.
+template <int T>
+__device__ inline int search_row(const Row<T> &row, Shared &s, int top_k, float top_p, float min_p, double u) {
     uint32_t lowest = 0;     // the lowest kept key
     uint64_t ties = ~0ull;   // how many of it are kept
-    if (top_k >= 1 && top_k < a.V) {
+    if (top_k >= 1 && top_k < row.V) {
         uint64_t above;
         if (search(row, s, (uint64_t)top_k, 0, 0, [](uint32_t k) { return (uint64_t)(k != 0); }, lowest, above)) ties = top_k - above;
         else lowest = 0;  // so many are not there
@@ -207,7 +205,7 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_rows(SampleA
         const uint32_t low_k = lowest;
         const double w_k = low_k ? row.weight(low_k) : 0.;
         double sum = 0.;
-        for (int i = threadIdx.x; i < a.V; i += kThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kThreads) {
             const uint32_t k = row.key(i);
             if (k > low_k) sum += row.weight(k);
         }
@@ -218,7 +216,7 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_rows(SampleA
         if (search(row, s, max((uint64_t)1, (uint64_t)__builtin_ceil(most * kUnit)), low_k, low_k ? ties * fixed(w_k) : 0,
                    [&](uint32_t k) { return k > low_k ? fixed(row.weight(k)) : 0; }, low_p, above)) {
             double over = 0., same = 0.;
-            for (int i = threadIdx.x; i < a.V; i += kThreads) {
+            for (int i = threadIdx.x; i < row.V; i += kThreads) {
                 const uint32_t k = row.key(i);
                 if (k > low_p) over += row.weight(k);
                 same += k == low_p;
@@ -231,12 +229,11 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_rows(SampleA
         }
     }
     // the last kept one of those that tie
-    int cut = a.V;
-    if (lowest && ties < (uint64_t)a.V)
-        cut = locate(s, a.V, [&](int i) { return row.key(i) == lowest ? 1. : 0.; }, [&](double all) { return (double)ties < all ? (double)ties - .5 : all; });
-    const double u = a.u[b] > 0.f ? (double)min(a.u[b], 1.f - 5.9604644775390625e-8f) : 0.;
-    const int token = locate(
-        s, a.V,
+    int cut = row.V;
+    if (lowest && ties < (uint64_t)row.V)
+        cut = locate(s, row.V, [&](int i) { return row.key(i) == lowest ? 1. : 0.; }, [&](double all) { return (double)ties < all ? (double)ties - .5 : all; });
+    return locate(
+        s, row.V,
         [&](int i) {
             const uint32_t k = row.key(i);
             if (k == 0 || k < lowest || (k == lowest && i > cut)) return 0.;
@@ -244,18 +241,483 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_rows(SampleA
             return w >= (double)min_p || !(min_p > 0.f) ? w : 0.;
         },
         [&](double all) { return u * all; });
-    if (threadIdx.x == 0) a.tokens[b] = token;
+}
+
+// ------------------------------------------------------------------ rows in slices
+
+constexpr int kChunk = 512;       // logits of one step of a wave, eight a lane
+constexpr int kMaxSlices = 64;    // of a row
+constexpr int kMaxChunks = SIM_SAMPLE_MAX_V / kChunk;
+constexpr int kList = 4096;       // logits that a workgroup sorts
+constexpr int kMaxSorted = 2048;  // up to this top-k all that are above the border are sorted too
+constexpr int kSliceGroups = 2048;  // workgroups of a launch
+constexpr int kRows = 1024;       // of one set of launches, and of the workspace
+
+// Where the rows' parts of the workspace are, and how a row is cut.
+struct Plan {
+    uint64_t *tops;    // [row][slice]: key and, complemented, index of the highest
+    uint64_t *bins;    // [row][kBins]
+    uint64_t *list;    // [row][kList]
+    double *sums;      // [row][chunks]
+    uint32_t *state;   // [row][8], see below
+    int64_t row0;
+    int chunks, slices, chunks_of_slice;
+};
+enum { kListed, kArrived, kPicked, kLowest, kCut, kMode, kState = 8 };  // in state
+enum { kOpen, kBordered, kDone };                                      // in state[kMode]
+
+enum Kind {
+    kToken,   // the highest, or -1
+    kSorted,  // a small top-k: all that is above its border is sorted
+    kNumber,  // a large top-k
+    kWeight,  // top-p
+    kAll,     // every logit, or what min-p leaves
+    kAlone,   // a large top-k with top-p: one workgroup searches
+};
+template <int T> struct Task {
+    Row<T> row;
+    Kind kind;
+    uint32_t best;
+    int first;  // index of the highest
+    float top, min_p, top_p;
+    int top_k;
+    __device__ int token() const { return best == 0 || best >= kInfinite<T> ? -1 : first; }
+};
+
+// What is to be done with a row, from its slices' tops; the same in every wave.
+template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Plan &p, int64_t b) {
+    typedef typename Elem<T>::type El;
+    const int lane = threadIdx.x & 63;
+    uint64_t top = lane < p.slices ? p.tops[(b - p.row0) * p.slices + lane] : 0;
+    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
+    Task<T> t;
+    t.row.z = (const El *)a.logits + b * a.stride;
+    t.row.V = a.V;
+    t.best = __builtin_amdgcn_readfirstlane((uint32_t)(top >> 32));
+    t.first = (int)~__builtin_amdgcn_readfirstlane((uint32_t)top);
+    t.top = value_of<T>(t.best);
+    const float temperature = a.temperature ? a.temperature[b] : a.all_temperature;
+    t.min_p = a.min_p ? a.min_p[b] : a.all_min;
+    t.top_p = a.top_p ? a.top_p[b] : a.all_p;
+    t.top_k = a.top_k ? a.top_k[b] : a.all_k;
+    t.row.top = t.top;
+    t.row.per = 1. / temperature;
+    if (t.best == 0 || t.best >= kInfinite<T> || !(temperature > 0.f) || t.top_k == 1 || t.top_p <= 0.f || t.min_p > 1.f) t.kind = kToken;
+    else if (t.top_k < 1 || t.top_k >= a.V) t.kind = t.top_p < 1.f ? kWeight : kAll;
+    else t.kind = t.top_k <= kMaxSorted ? kSorted : t.top_p < 1.f ? kAlone : kNumber;
+    return t;
+}
+__device__ inline double number_of(const SampleArgs &a, int64_t b) {
+    return a.u[b] > 0.f ? (double)min(a.u[b], 1.f - 5.9604644775390625e-8f) : 0.;
+}
+
+// Eight consecutive logits from i on; -infinity past the row.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+template <int T> __device__ inline void load8(const Row<T> &row, int i, typename Elem<T>::type v[8]) {
+    if (i + 8 <= row.V) {
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(v[0]) / 2; j++) ((u32x4_any *)v)[j] = ((const u32x4_any *)(row.z + i))[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = i + j < row.V ? row.z[i + j] : Elem<T>::put(-INFINITY);
+    }
+}
+// Calls f(first index, eight logits) for this wave's part of a slice.
+template <int T, typename F> __device__ inline void each_chunk(const Row<T> &row, const Plan &p, int slice, F &&f) {
+    const int end = min(p.chunks, (slice + 1) * p.chunks_of_slice);
+    for (int c = slice * p.chunks_of_slice + (int)(threadIdx.x >> 6); c < end; c += kWaves) {
+        typename Elem<T>::type v[8];
+        const int i = c * kChunk + (threadIdx.x & 63) * 8;
+        load8(row, i, v);
+        f(i, v, c);
+    }
+}
+
+// How far a logit is below the highest, as one of kBins: 128 to each doubling
+// of the distance plus 1/32, from 1/32 to 2048.
+__device__ inline int bin_of(float top, float z) {
+    return min((int)(__float_as_uint(top - z + 0.03125f) >> 16) - 0x3d00, kBins - 1);
+}
+// A weight as a whole multiple of 1 / kUnit: it lands in the low bits of 2^52 + w kUnit
+__device__ inline uint64_t fixed(double w) {
+    return __builtin_bit_cast(uint64_t, __builtin_fma(w, kUnit, 4503599627370496.)) & 0xfffffffffffffull;
+}
+
+template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleArgs a, Plan p) {
+    typedef typename Elem<T>::type El;
+    __shared__ uint64_t s_top[kWaves];
+    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
+    const int slice = (int)(blockIdx.x % p.slices);
+    Row<T> row;
+    row.z = (const El *)a.logits + b * a.stride;
+    row.V = a.V;
+    uint32_t best = 0, at = 0;
+    each_chunk<T>(row, p, slice, [&](int i, const El v[8], int) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const uint32_t k = key_of<T>(v[j]);
+            at = k > best ? i + j : at;
+            best = max(best, k);
+        }
+    });
+    uint64_t top = (uint64_t)best << 32 | (uint32_t)~at;
+    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
+    if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
+    // what the launches after this one count up from
+    for (int i = slice * kThreads + threadIdx.x; i < kBins; i += p.slices * kThreads) p.bins[r * kBins + i] = 0;
+    if (slice == 0 && threadIdx.x < kState) p.state[r * kState + threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x == 0) p.tops[r * p.slices + slice] = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
+}
+
+template <int T> __global__ __launch_bounds__(kThreads) void sample_bins(SampleArgs a, Plan p) {
+    typedef typename Elem<T>::type El;
+    __shared__ uint64_t s_bin[kBins];
+    const int64_t r = blockIdx.x / p.slices;
+    const int slice = (int)(blockIdx.x % p.slices);
+    const Task<T> t = task_of<T>(a, p, p.row0 + r);
+    if (t.kind != kSorted && t.kind != kNumber && t.kind != kWeight) return;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s_bin[i] = 0;
+    __syncthreads();
+    each_chunk<T>(t.row, p, slice, [&](int, const El v[8], int) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float z = Elem<T>::get(v[j]);
+            if (z == -INFINITY) continue;
+            const uint64_t n = t.kind == kWeight ? fixed(exp64(((double)z - t.row.top) * t.row.per)) : 1;
+            atomicAdd((unsigned long long *)&s_bin[bin_of(t.top, z)], (unsigned long long)n);
+        }
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kThreads)
+        if (s_bin[i]) atomicAdd((unsigned long long *)&p.bins[r * kBins + i], (unsigned long long)s_bin[i]);
+}
+
+// Sorts n of kList values, the highest first; what is past them is overwritten.
+__device__ inline void sort(uint64_t *v, int n) {
+    int all = 2;
+    while (all < n) all <<= 1;
+    for (int i = n + threadIdx.x; i < all; i += kThreads) v[i] = 0;
+    for (int run = 2; run <= all; run <<= 1)
+        for (int d = run >> 1; d; d >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < all / 2; i += kThreads) {
+                const int x = (i & (d - 1)) + ((i & ~(d - 1)) << 1), y = x + d;
+                const uint64_t p = v[x], q = v[y];
+                if ((p < q) == ((x & run) == 0)) v[x] = q, v[y] = p;
+            }
+        }
+    __syncthreads();
+}
+
+// Running sums over n values, a run of them to each thread: before(i) of each is
+// passed to f(i, before, value); returns the sum of all.
+template <typename Value, typename F> __device__ inline double scan(int n, double *wave_d, Value &&value, F &&f) {
+    const int each = (n + kThreads - 1) / kThreads, i0 = threadIdx.x * each, i1 = min(n, i0 + each), lane = threadIdx.x & 63;
+    double own = 0.;
+    for (int i = i0; i < i1; i++) own += value(i);
+    double sum = own;
+    for (int d = 1; d < 64; d <<= 1) {
+        const double o = __shfl_up(sum, d);
+        if (lane >= d) sum += o;
+    }
+    __syncthreads();
+    if (lane == 63) wave_d[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    double run = __shfl_up(sum, 1), all = 0.;
+    if (lane == 0) run = 0.;
+    for (int w = 0; w < kWaves; w++) {
+        if (w < (int)(threadIdx.x >> 6)) run += wave_d[w];
+        all += wave_d[w];
+    }
+    for (int i = i0; i < i1; i++) {
+        const double v = value(i);
+        f(i, run, v);
+        run += v;
+    }
+    return all;
+}
+__device__ inline int count(int n, int *wave_n) {
+    for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < kWaves; w++) n += wave_n[w];
+    return n;
+}
+
+template <typename V> __device__ inline V at_device(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Whether this workgroup is the last of a row's: what the others have written at
+// device scope before is there then.
+__device__ inline bool last_of(uint32_t *arrived, int of, int *s_last) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) *s_last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)of - 1;
+    __syncthreads();
+    return *s_last;
+}
+
+struct Sorting {
+    uint64_t list[kList];
+    double w[kMaxSorted];
+};
+
+// The token of a small top-k, from the n sorted logits down to its border.
+template <int T>
+__device__ inline int pick_sorted(const Task<T> &t, Sorting &s, int n, double u, double *wave_d, int *wave_n) {
+    const int k = min(n, t.top_k);
+    for (int i = threadIdx.x; i < k; i += kThreads) s.w[i] = t.row.weight((uint32_t)(s.list[i] >> 32));
+    __syncthreads();
+    const auto w = [&](int i) { return s.w[i]; };
+    int kept = 0;
+    const double all = scan(k, wave_d, w, [](int, double, double) {});
+    const double most = all * (double)t.top_p;
+    scan(k, wave_d, w, [&](int i, double before, double v) {
+        kept += i == 0 || ((t.top_p >= 1.f || before < most || t.top_p != t.top_p) && (!(t.min_p > 0.f) || v >= (double)t.min_p));
+    });
+    kept = count(kept, wave_n);
+    // in the order of the indices: their complements, the highest first, with the places of the weights
+    for (int i = threadIdx.x; i < kept; i += kThreads) s.list[i] = s.list[i] << 32 | (uint32_t)i;
+    sort(s.list, kept);
+    const auto in_order = [&](int i) { return s.w[(uint32_t)s.list[i]]; };
+    const double target = u * scan(kept, wave_d, in_order, [](int, double, double) {});
+    int first = kept, some = 0;  // the first that is above it; the last that has a weight, and one
+    scan(kept, wave_d, in_order, [&](int i, double run, double v) {
+        if (v > 0.) some = i + 1;
+        if (v > 0. && run + v > target) first = min(first, i);
+    });
+    for (int d = 1; d < 64; d <<= 1) first = min(first, __shfl_xor(first, d)), some = max(some, __shfl_xor(some, d));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = first, wave_n[kWaves + (threadIdx.x >> 6)] = some;
+    __syncthreads();
+    for (int w = 0; w < kWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kWaves + w]);
+    return (int)~(uint32_t)(s.list[first < kept ? first : some - 1] >> 32);
+}
+
+template <int T> __global__ __launch_bounds__(kThreads) void sample_border(SampleArgs a, Plan p) {
+    typedef typename Elem<T>::type El;
+    __shared__ union {
+        Sorting sorting;
+        Shared alone;
+    } s;
+    __shared__ uint64_t wave64[kWaves];
+    __shared__ double wave_d[kWaves];
+    __shared__ int wave_n[2 * kWaves], s_n, s_base, s_last;
+    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
+    const int slice = (int)(blockIdx.x % p.slices);
+    const Task<T> t = task_of<T>(a, p, b);
+    uint32_t *const state = p.state + r * kState;
+    const auto token = [&](int i) {
+        if (threadIdx.x == 0) a.tokens[b] = i, state[kMode] = kDone;
+    };
+    if (t.kind == kAll) return;
+    if (t.kind == kToken) {
+        if (slice == 0) token(t.token());
+        return;
+    }
+    if (t.kind == kAlone) {
+        if (slice == 0) token(search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, number_of(a, b)));
+        return;
+    }
+    const uint64_t *const bins = p.bins + r * kBins;
+    uint64_t target = (uint64_t)t.top_k, above = 0, all = 0;
+    if (t.kind == kWeight) {
+        for (int i = threadIdx.x; i < kBins; i += kThreads) all += bins[i];
+        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor((unsigned long long)all, d);
+        if ((threadIdx.x & 63) == 0) wave64[threadIdx.x >> 6] = all;
+        __syncthreads();
+        all = wave64[0] + wave64[1] + wave64[2] + wave64[3];
+        __syncthreads();
+        target = max((uint64_t)1, (uint64_t)__builtin_ceil((double)all * (double)t.top_p));
+    }
+    if (threadIdx.x == 0) s_n = 0;
+    int border = crossing([&](int i) { return bins[i]; }, target, wave64, above);
+    const bool whole = t.kind == kSorted;
+    if (border < 0) {  // a top-k beyond the logits that there are: all of them
+        if (!whole) {
+            if (slice == 0 && threadIdx.x == 0) state[kLowest] = 1, state[kCut] = (uint32_t)a.V, state[kMode] = kBordered;
+            return;
+        }
+        border = kBins - 1;
+    }
+    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8], int) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float z = Elem<T>::get(v[j]);
+            if (z == -INFINITY) continue;
+            const int bin = bin_of(t.top, z);
+            if (bin == border || (whole && bin < border)) {
+                const int n = atomicAdd(&s_n, 1);
+                if (n < kList) s.sorting.list[n] = (uint64_t)key_of<T>(v[j]) << 32 | (uint32_t)~(i + j);
+            }
+        }
+    });
+    __syncthreads();
+    const int mine = s_n;
+    uint64_t *const list = p.list + r * kList;
+    if (threadIdx.x == 0 && mine) s_base = (int)__hip_atomic_fetch_add(&state[kListed], (uint32_t)mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    for (int i = threadIdx.x; i < min(mine, kList); i += kThreads)
+        if (s_base + i < kList) __hip_atomic_store(&list[s_base + i], s.sorting.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!last_of(&state[kArrived], p.slices, &s_last)) return;
+
+    const int n = (int)at_device(&state[kListed]);
+    const double u = number_of(a, b);
+    if (n > kList) {
+        token(search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u));
+        return;
+    }
+    for (int i = threadIdx.x; i < n; i += kThreads) s.sorting.list[i] = at_device(&list[i]);
+    __syncthreads();
+    sort(s.sorting.list, n);
+    if (whole) {
+        token(pick_sorted<T>(t, s.sorting, n, u, wave_d, wave_n));
+        return;
+    }
+    int kept = 0;
+    if (t.kind == kNumber) {
+        kept = (int)((uint64_t)t.top_k - above);
+    } else {
+        const double most = (double)all * (double)t.top_p / kUnit, over = (double)above / kUnit;
+        scan(n, wave_d, [&](int i) { return t.row.weight((uint32_t)(s.sorting.list[i] >> 32)); },
+             [&](int, double before, double) { kept += over + before < most; });
+        kept = count(kept, wave_n);
+    }
+    if (threadIdx.x == 0) {
+        const uint64_t lowest = s.sorting.list[min(max(kept, 1), n) - 1];
+        state[kLowest] = (uint32_t)(lowest >> 32);
+        state[kCut] = ~(uint32_t)lowest;
+        state[kMode] = kBordered;
+    }
+}
+
+template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleArgs a, Plan p) {
+    typedef typename Elem<T>::type El;
+    __shared__ double wave_d[kWaves];
+    __shared__ int wave_n[2 * kWaves], s_last;
+    __shared__ double s_before, s_sum[kMaxChunks];
+    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
+    const int slice = (int)(blockIdx.x % p.slices), lane = threadIdx.x & 63;
+    const Task<T> t = task_of<T>(a, p, b);
+    uint32_t *const state = p.state + r * kState;
+    if (t.kind == kToken) {
+        if (slice == 0 && threadIdx.x == 0) a.tokens[b] = t.token();
+        return;
+    }
+    const bool all = t.kind == kAll;
+    if (!all && state[kMode] != kBordered) return;
+    const uint32_t lowest = all ? 1 : state[kLowest];
+    const int cut = all ? a.V : (int)state[kCut];
+    // further below the highest than this nothing is left by min-p, whatever the rounding
+    const float far = t.min_p > 0.f ? (float)(-log((double)t.min_p) / t.row.per * 1.0001 + 1e-30) : INFINITY;
+    const auto weight = [&](El v, int i) {
+        const uint32_t k = key_of<T>(v);
+        const bool in = (k > lowest || (k == lowest && i <= cut)) && !(t.top - Elem<T>::get(v) > far);
+        if (!in) return 0.;
+        const double w = exp64(((double)Elem<T>::get(v) - t.row.top) * t.row.per);
+        return !(t.min_p > 0.f) || w >= (double)t.min_p ? w : 0.;
+    };
+    double *const sums = p.sums + r * p.chunks;
+    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8], int c) {
+        double sum = 0.;
+#pragma unroll
+        for (int j = 0; j < 8; j++) sum += weight(v[j], i + j);
+        sum = wave_sum(sum);
+        if (lane == 0) __hip_atomic_store(&sums[c], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+    if (!last_of(&state[kPicked], p.slices, &s_last)) return;
+
+    for (int i = threadIdx.x; i < p.chunks; i += kThreads) s_sum[i] = at_device(&sums[i]);
+    __syncthreads();
+    const auto value = [&](int i) { return s_sum[i]; };
+    const double target = number_of(a, b) * scan(p.chunks, wave_d, value, [](int, double, double) {});
+    int first = p.chunks, some = 0;
+    scan(p.chunks, wave_d, value, [&](int i, double run, double v) {
+        if (v > 0.) some = i;
+        if (v > 0. && run + v > target) first = min(first, i);
+    });
+    for (int d = 1; d < 64; d <<= 1) first = min(first, __shfl_xor(first, d)), some = max(some, __shfl_xor(some, d));
+    __syncthreads();
+    if (lane == 0) wave_n[threadIdx.x >> 6] = first, wave_n[kWaves + (threadIdx.x >> 6)] = some;
+    __syncthreads();
+    for (int w = 0; w < kWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kWaves + w]);
+    const int chunk = first < p.chunks ? first : some;
+    scan(p.chunks, wave_d, value, [&](int i, double run, double) {
+        if (i == chunk) s_before = run;
+    });
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    El v[8];
+    double w[8], own = 0.;
+    load8(t.row, chunk * kChunk + lane * 8, v);
+#pragma unroll
+    for (int j = 0; j < 8; j++) own += w[j] = weight(v[j], chunk * kChunk + lane * 8 + j);
+    double sum = own;
+    for (int d = 1; d < 64; d <<= 1) {
+        const double o = __shfl_up(sum, d);
+        if (lane >= d) sum += o;
+    }
+    double run = __shfl_up(sum, 1);
+    run = s_before + (lane ? run : 0.);
+    int past = 8, last = -1;
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        run += w[j];
+        if (w[j] > 0.) {
+            last = j;
+            if (past == 8 && run > target) past = j;
+        }
+    }
+    const uint64_t is_past = __ballot(past < 8), is_some = __ballot(last >= 0);
+    const int l = is_past ? __ffsll((unsigned long long)is_past) - 1 : is_some ? 63 - __clzll((long long)is_some) : 0;
+    if (lane == l) a.tokens[b] = chunk * kChunk + lane * 8 + (is_past ? past : max(last, 0));
+}
+
+// How rows are cut: into slices that together fill the GPU several times.
+Plan plan_of(int64_t rows, int V, uint8_t *ws) {
+    Plan p = {};
+    p.chunks = (V + kChunk - 1) / kChunk;
+    const int most = (int)std::min<int64_t>({(int64_t)kMaxSlices, std::max<int64_t>(1, kSliceGroups / rows), (int64_t)(p.chunks + kWaves - 1) / kWaves});
+    p.chunks_of_slice = (p.chunks + most - 1) / most;
+    p.slices = (p.chunks + p.chunks_of_slice - 1) / p.chunks_of_slice;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t n = at; at += (bytes + 255) / 256 * 256; return ws + n; };
+    p.tops = (uint64_t *)take((size_t)rows * p.slices * 8);
+    p.bins = (uint64_t *)take((size_t)rows * kBins * 8);
+    p.list = (uint64_t *)take((size_t)rows * kList * 8);
+    p.sums = (double *)take((size_t)rows * p.chunks * 8);
+    p.state = (uint32_t *)take((size_t)rows * kState * 4);
+    p.row0 = (int64_t)at;  // the size, for the query
+    return p;
+}
+
+template <int T> sim_status sample_t(hipStream_t st, const SampleArgs &a, uint8_t *ws) {
+    const bool some_k = a.top_k || (a.all_k > 1 && a.all_k < a.V), some_p = a.top_p || a.all_p < 1.f;
+    const bool sorted = !a.top_k && some_k && a.all_k <= kMaxSorted;  // every row
+    for (int64_t row0 = 0; row0 < a.B; row0 += kRows) {
+        const int64_t rows = std::min<int64_t>(kRows, a.B - row0);
+        Plan p = plan_of(rows, a.V, ws);
+        p.row0 = row0;
+        const uint32_t grid = (uint32_t)(rows * p.slices);
+        sample_tops<T><<<grid, kThreads, 0, st>>>(a, p);
+        if (some_k || some_p) {
+            sample_bins<T><<<grid, kThreads, 0, st>>>(a, p);
+            sample_border<T><<<grid, kThreads, 0, st>>>(a, p);
+        }
+        if (!sorted) sample_pick<T><<<grid, kThreads, 0, st>>>(a, p);
+    }
+    return SIM_OPS_LAUNCH_OK();
 }
 
 }  // namespace
 
-size_t sample_workspace(int64_t, int) { return 0; }
+size_t sample_workspace(int64_t B, int V) { return (size_t)plan_of(std::min<int64_t>(B, kRows), V, nullptr).row0; }
 
-sim_status launch_sample(hipStream_t st, const SampleArgs &a, void *) {
-    if (a.type == SIM_TYPE_F32) sample_rows<SIM_TYPE_F32><<<(uint32_t)a.B, kThreads, 0, st>>>(a);
-    else if (a.type == SIM_TYPE_F16) sample_rows<SIM_TYPE_F16><<<(uint32_t)a.B, kThreads, 0, st>>>(a);
-    else sample_rows<SIM_TYPE_BF16><<<(uint32_t)a.B, kThreads, 0, st>>>(a);
-    return SIM_OPS_LAUNCH_OK();
+sim_status launch_sample(hipStream_t st, const SampleArgs &a, void *ws) {
+    if (a.type == SIM_TYPE_F32) return sample_t<SIM_TYPE_F32>(st, a, (uint8_t *)ws);
+    if (a.type == SIM_TYPE_F16) return sample_t<SIM_TYPE_F16>(st, a, (uint8_t *)ws);
+    return sample_t<SIM_TYPE_BF16>(st, a, (uint8_t *)ws);
 }
 
 }  // namespace simops
