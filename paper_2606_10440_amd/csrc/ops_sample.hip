@@ -4,13 +4,13 @@
 // What is kept is a run of the logits' falling order, so it is known by the
 // lowest kept logit and how many of the logits that tie with it are kept, in
 // the order of their indices.  A row is read by several workgroups, a slice
-// each, in up to four launches:
+// each, in up to five launches:
 //   tops    the highest logit of each slice;
 //   bins    the numbers of logits, or the sums of their weights, by how far
 //           they are below the highest, in steps of 1/128 of that distance;
 //   border  the logits of the bin in which the border lies (with a small
-//           top-k: of all above it too), which the row's last workgroup sorts:
-//           a small top-k's row is done with that;
+//           top-k: of all above it too) as a list;
+//   sorted  one workgroup sorts it: a small top-k's row is done with that;
 //   pick    the sums of the kept weights of 512 logits each; the row's last
 //           workgroup finds the 512 that the token is in, and the token.
 // A row whose border bin holds more than can be sorted (logits that are nearly
@@ -21,8 +21,10 @@
 namespace simops {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // of a workgroup that has a slice
 constexpr int kWaves = kThreads / 64;
+constexpr int kAll = 1024;     // of one that has what is left of a row, or all of it
+constexpr int kAllWaves = kAll / 64;
 constexpr int kDigit = 11;
 constexpr int kBins = 1 << kDigit;
 // Weights are at most 1: as whole multiples of 2^-44, of 2^20 of them, their
@@ -54,8 +56,8 @@ __device__ inline double wave_sum(double v) {
 
 struct Shared {
     uint64_t bin[kBins];
-    uint64_t wave64[kWaves];
-    double wave_d[kWaves];
+    uint64_t wave64[kAllWaves];
+    double wave_d[kAllWaves];
     uint32_t digit;
     uint64_t above;
 };
@@ -72,8 +74,8 @@ template <int T> struct Row {
 // The first of kBins values at which their running sum reaches target, in all
 // threads, and the sum before it; -1 where all together do not.  The caller
 // keeps to barriers around it.
-template <typename Bin> __device__ inline int crossing(Bin &&bin, uint64_t target, uint64_t *wave_sums, uint64_t &before) {
-    constexpr int kEach = kBins / kThreads;
+template <int NT, typename Bin> __device__ inline int crossing(Bin &&bin, uint64_t target, uint64_t *wave_sums, uint64_t &before) {
+    constexpr int kEach = kBins / NT;
     __shared__ int s_at;
     __shared__ uint64_t s_before;
     uint64_t v[kEach], own = 0;
@@ -106,7 +108,7 @@ __device__ inline double block_sum(double v, Shared &s) {
     if ((threadIdx.x & 63) == 0) s.wave_d[threadIdx.x >> 6] = v;
     __syncthreads();
     double sum = 0.;
-    for (int w = 0; w < kWaves; w++) sum += s.wave_d[w];
+    for (int w = 0; w < kAllWaves; w++) sum += s.wave_d[w];
     return sum;
 }
 
@@ -121,9 +123,9 @@ __device__ inline bool search(const Row<T> &row, Shared &s, uint64_t target, uin
     for (int left = kKeyBits<T>; left > 0;) {
         const int bits = min(left, kDigit), shift = left - bits;
         __syncthreads();
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.bin[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kAll) s.bin[i] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < row.V; i += kThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kAll) {
             const uint32_t k = row.key(i);
             if (left < 32 && (k >> left) != prefix) continue;
             const uint64_t n = add(k);
@@ -135,7 +137,7 @@ __device__ inline bool search(const Row<T> &row, Shared &s, uint64_t target, uin
         // from the highest bin down
         const auto bin = [&](int i) { return s.bin[kBins - 1 - i]; };
         uint64_t before;
-        const int at = crossing(bin, target - above, s.wave64, before);
+        const int at = crossing<kAll>(bin, target - above, s.wave64, before);
         if (at < 0) return false;
         s.digit = kBins - 1 - at, s.above = above + before;
         __syncthreads();
@@ -156,7 +158,7 @@ __device__ inline int locate(Shared &s, int V, Weight &&weight, Target &&target_
     double before = 0., target = 0.;
     bool first = true;
     do {
-        const int seg = (hi - lo + kWaves - 1) / kWaves, a = min(hi, lo + wave * seg), b = min(hi, a + seg);
+        const int seg = (hi - lo + kAllWaves - 1) / kAllWaves, a = min(hi, lo + wave * seg), b = min(hi, a + seg);
         double sum = 0.;
         for (int i = a + lane; i < b; i += 64) sum += weight(i);
         sum = wave_sum(sum);
@@ -165,13 +167,13 @@ __device__ inline int locate(Shared &s, int V, Weight &&weight, Target &&target_
         __syncthreads();
         if (first) {
             double all = 0.;
-            for (int w = 0; w < kWaves; w++) all += s.wave_d[w];
+            for (int w = 0; w < kAllWaves; w++) all += s.wave_d[w];
             target = target_of(all);
             first = false;
         }
         int at = 0;
         double run = before, start = before;
-        for (int w = 0; w < kWaves; w++) {
+        for (int w = 0; w < kAllWaves; w++) {
             const double v = s.wave_d[w];
             if (v > 0.) at = w, start = run;
             run += v;
@@ -205,7 +207,7 @@ __device__ inline int search_row(const Row<T> &row, Shared &s, int top_k, float 
         const uint32_t low_k = lowest;
         const double w_k = low_k ? row.weight(low_k) : 0.;
         double sum = 0.;
-        for (int i = threadIdx.x; i < row.V; i += kThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kAll) {
             const uint32_t k = row.key(i);
             if (k > low_k) sum += row.weight(k);
         }
@@ -216,7 +218,7 @@ __device__ inline int search_row(const Row<T> &row, Shared &s, int top_k, float 
         if (search(row, s, max((uint64_t)1, (uint64_t)__builtin_ceil(most * kUnit)), low_k, low_k ? ties * fixed(w_k) : 0,
                    [&](uint32_t k) { return k > low_k ? fixed(row.weight(k)) : 0; }, low_p, above)) {
             double over = 0., same = 0.;
-            for (int i = threadIdx.x; i < row.V; i += kThreads) {
+            for (int i = threadIdx.x; i < row.V; i += kAll) {
                 const uint32_t k = row.key(i);
                 if (k > low_p) over += row.weight(k);
                 same += k == low_p;
@@ -247,11 +249,23 @@ __device__ inline int search_row(const Row<T> &row, Shared &s, int top_k, float 
 
 constexpr int kChunk = 512;       // logits of one step of a wave, eight a lane
 constexpr int kMaxSlices = 64;    // of a row
-constexpr int kMaxChunks = SIM_SAMPLE_MAX_V / kChunk;
+constexpr int kMaxChunks = (SIM_SAMPLE_MAX_V + 7 + kChunk - 1) / kChunk;
 constexpr int kList = 4096;       // logits that a workgroup sorts
+constexpr int kStage = 512;       // logits that a slice's workgroup collects before it adds them to the list
 constexpr int kMaxSorted = 2048;  // up to this top-k all that are above the border are sorted too
 constexpr int kSliceGroups = 2048;  // workgroups of a launch
 constexpr int kRows = 1024;       // of one set of launches, and of the workspace
+
+enum Mode : uint32_t { kOpen, kBordered, kDone };
+
+// What the launches find out about a row.
+struct RowState {
+    uint32_t binned, listed, picked;  // workgroups that have come, and logits in the list
+    int border;                                // the bin of the border; -1: there are fewer logits than top-k
+    Mode mode;
+    uint32_t lowest, cut;                      // kBordered: the lowest kept key and the last kept index that has it
+    uint64_t above, all;                       // the bins' sums above the border, and all of them
+};
 
 // Where the rows' parts of the workspace are, and how a row is cut.
 struct Plan {
@@ -259,19 +273,17 @@ struct Plan {
     uint64_t *bins;    // [row][kBins]
     uint64_t *list;    // [row][kList]
     double *sums;      // [row][chunks]
-    uint32_t *state;   // [row][8], see below
+    RowState *state;
     int64_t row0;
     int chunks, slices, chunks_of_slice;
 };
-enum { kListed, kArrived, kPicked, kLowest, kCut, kMode, kState = 8 };  // in state
-enum { kOpen, kBordered, kDone };                                      // in state[kMode]
 
 enum Kind {
     kToken,   // the highest, or -1
     kSorted,  // a small top-k: all that is above its border is sorted
     kNumber,  // a large top-k
     kWeight,  // top-p
-    kAll,     // every logit, or what min-p leaves
+    kEvery,   // every logit, or what min-p leaves
     kAlone,   // a large top-k with top-p: one workgroup searches
 };
 template <int T> struct Task {
@@ -303,7 +315,7 @@ template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Pl
     t.row.top = t.top;
     t.row.per = 1. / temperature;
     if (t.best == 0 || t.best >= kInfinite<T> || !(temperature > 0.f) || t.top_k == 1 || t.top_p <= 0.f || t.min_p > 1.f) t.kind = kToken;
-    else if (t.top_k < 1 || t.top_k >= a.V) t.kind = t.top_p < 1.f ? kWeight : kAll;
+    else if (t.top_k < 1 || t.top_k >= a.V) t.kind = t.top_p < 1.f ? kWeight : kEvery;
     else t.kind = t.top_k <= kMaxSorted ? kSorted : t.top_p < 1.f ? kAlone : kNumber;
     return t;
 }
@@ -311,26 +323,41 @@ __device__ inline double number_of(const SampleArgs &a, int64_t b) {
     return a.u[b] > 0.f ? (double)min(a.u[b], 1.f - 5.9604644775390625e-8f) : 0.;
 }
 
-// Eight consecutive logits from i on; -infinity past the row.
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2), may_alias));
+// Rows are cut where memory is aligned, so that their first logits have
+// indices below 0 before them.  The index of a lane's first logit of a chunk:
+template <int T> __device__ inline int index_of(const Row<T> &row, int chunk) {
+    return chunk * kChunk + (int)(threadIdx.x & 63) * 8 - (int)((uintptr_t)row.z / sizeof(*row.z) % 8);
+}
+// Eight consecutive logits from i on; -infinity outside the row.
+typedef u32x4 u32x4_alias __attribute__((may_alias));
 template <int T> __device__ inline void load8(const Row<T> &row, int i, typename Elem<T>::type v[8]) {
-    if (i + 8 <= row.V) {
+    if (i >= 0 && i + 8 <= row.V) {
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(v[0]) / 2; j++) ((u32x4_any *)v)[j] = ((const u32x4_any *)(row.z + i))[j];
+        for (int j = 0; j < (int)sizeof(v[0]) / 2; j++) ((u32x4_alias *)v)[j] = ((const u32x4_alias *)(row.z + i))[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; j++) v[j] = i + j < row.V ? row.z[i + j] : Elem<T>::put(-INFINITY);
+        for (int j = 0; j < 8; j++) v[j] = i + j >= 0 && i + j < row.V ? row.z[i + j] : Elem<T>::put(-INFINITY);
     }
 }
-// Calls f(first index, eight logits) for this wave's part of a slice.
-template <int T, typename F> __device__ inline void each_chunk(const Row<T> &row, const Plan &p, int slice, F &&f) {
+constexpr int kAhead = 4;  // chunks that are loaded together
+// Calls f(first chunk, end of the slice, logits) for this wave's part of a
+// slice, every kWaves-th chunk.
+template <int T, typename F> __device__ inline void each_group(const Row<T> &row, const Plan &p, int slice, F &&f) {
     const int end = min(p.chunks, (slice + 1) * p.chunks_of_slice);
-    for (int c = slice * p.chunks_of_slice + (int)(threadIdx.x >> 6); c < end; c += kWaves) {
-        typename Elem<T>::type v[8];
-        const int i = c * kChunk + (threadIdx.x & 63) * 8;
-        load8(row, i, v);
-        f(i, v, c);
+    for (int c0 = slice * p.chunks_of_slice + (int)(threadIdx.x >> 6); c0 < end; c0 += kAhead * kWaves) {
+        typename Elem<T>::type v[kAhead][8];
+#pragma unroll
+        for (int n = 0; n < kAhead; n++) load8(row, index_of(row, min(c0 + n * kWaves, end - 1)), v[n]);
+        f(c0, end, v);
     }
+}
+// Calls f(index, eight logits) for each of them.
+template <int T, typename F> __device__ inline void each_chunk(const Row<T> &row, const Plan &p, int slice, F &&f) {
+    each_group<T>(row, p, slice, [&](int c0, int end, const typename Elem<T>::type v[kAhead][8]) {
+#pragma unroll
+        for (int n = 0; n < kAhead; n++)
+            if (c0 + n * kWaves < end) f(index_of(row, c0 + n * kWaves), v[n]);
+    });
 }
 
 // How far a logit is below the highest, as one of kBins: 128 to each doubling
@@ -351,35 +378,61 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleA
     Row<T> row;
     row.z = (const El *)a.logits + b * a.stride;
     row.V = a.V;
-    uint32_t best = 0, at = 0;
-    each_chunk<T>(row, p, slice, [&](int i, const El v[8], int) {
+    // the highest of eight at a time; which of them it is, only where they hold
+    // a lane's highest
+    float best = -INFINITY;
+    int at = 0;
+    each_chunk<T>(row, p, slice, [&](int i, const El v[8]) {
+        float m = Elem<T>::get(v[0]);
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const uint32_t k = key_of<T>(v[j]);
-            at = k > best ? i + j : at;
-            best = max(best, k);
-        }
+        for (int j = 1; j < 8; j++) m = __builtin_elementwise_maximum(m, Elem<T>::get(v[j]));
+        if (!(m <= best) && best == best) at = i, best = __builtin_elementwise_maximum(best, m);
     });
-    uint64_t top = (uint64_t)best << 32 | (uint32_t)~at;
+    uint32_t key = 0;
+    if (best != -INFINITY) {
+        El v[8];
+        load8(row, at, v);
+        int first = 0;
+#pragma unroll
+        for (int j = 7; j >= 0; j--) {
+            const uint32_t k = key_of<T>(v[j]);
+            first = k >= key ? j : first;
+            key = max(key, k);
+        }
+        at += first;
+    }
+    uint64_t top = (uint64_t)key << 32 | (uint32_t)~at;
     for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
     if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
     // what the launches after this one count up from
     for (int i = slice * kThreads + threadIdx.x; i < kBins; i += p.slices * kThreads) p.bins[r * kBins + i] = 0;
-    if (slice == 0 && threadIdx.x < kState) p.state[r * kState + threadIdx.x] = 0;
+    if (slice == 0 && threadIdx.x == 0) p.state[r] = RowState{};
     __syncthreads();
     if (threadIdx.x == 0) p.tops[r * p.slices + slice] = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
 }
 
+template <typename V> __device__ inline V at_device(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Whether this workgroup is the last of a row's: what the others have written at
+// device scope before is there then.
+__device__ inline bool last_of(uint32_t *arrived, int of, int *s_last) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) *s_last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)of - 1;
+    __syncthreads();
+    return *s_last;
+}
+
 template <int T> __global__ __launch_bounds__(kThreads) void sample_bins(SampleArgs a, Plan p) {
     typedef typename Elem<T>::type El;
-    __shared__ uint64_t s_bin[kBins];
+    __shared__ uint64_t s_bin[kBins], wave64[kWaves];
+    __shared__ int s_last;
     const int64_t r = blockIdx.x / p.slices;
     const int slice = (int)(blockIdx.x % p.slices);
     const Task<T> t = task_of<T>(a, p, p.row0 + r);
     if (t.kind != kSorted && t.kind != kNumber && t.kind != kWeight) return;
     for (int i = threadIdx.x; i < kBins; i += kThreads) s_bin[i] = 0;
     __syncthreads();
-    each_chunk<T>(t.row, p, slice, [&](int, const El v[8], int) {
+    each_chunk<T>(t.row, p, slice, [&](int, const El v[8]) {
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const float z = Elem<T>::get(v[j]);
@@ -390,30 +443,90 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_bins(SampleA
     });
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += kThreads)
-        if (s_bin[i]) atomicAdd((unsigned long long *)&p.bins[r * kBins + i], (unsigned long long)s_bin[i]);
+        if (s_bin[i]) __hip_atomic_fetch_add(&p.bins[r * kBins + i], s_bin[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    RowState &state = p.state[r];
+    if (!last_of(&state.binned, p.slices, &s_last)) return;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s_bin[i] = at_device(&p.bins[r * kBins + i]);
+    __syncthreads();
+    uint64_t target = (uint64_t)t.top_k, above = 0, all = 0;
+    if (t.kind == kWeight) {
+        for (int i = threadIdx.x; i < kBins; i += kThreads) all += s_bin[i];
+        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor((unsigned long long)all, d);
+        if ((threadIdx.x & 63) == 0) wave64[threadIdx.x >> 6] = all;
+        __syncthreads();
+        all = wave64[0] + wave64[1] + wave64[2] + wave64[3];
+        __syncthreads();
+        target = max((uint64_t)1, (uint64_t)__builtin_ceil((double)all * (double)t.top_p));
+    }
+    const int border = crossing<kThreads>([&](int i) { return s_bin[i]; }, target, wave64, above);
+    if (threadIdx.x == 0) state.border = border, state.above = above, state.all = all;
 }
 
-// Sorts n of kList values, the highest first; what is past them is overwritten.
-__device__ inline void sort(uint64_t *v, int n) {
-    int all = 2;
-    while (all < n) all <<= 1;
-    for (int i = n + threadIdx.x; i < all; i += kThreads) v[i] = 0;
-    for (int run = 2; run <= all; run <<= 1)
-        for (int d = run >> 1; d; d >>= 1) {
+// Sorts 1024 E values in registers, the highest first, by exchanges between
+// values that are further and further apart: value 1024 e + t is thread t's
+// e-th, so only those 64 to 512 apart go through LDS.
+template <int E> __device__ inline void sort_registers(uint64_t *lds, int n) {
+    const int t = threadIdx.x;
+    uint64_t v[E];
+#pragma unroll
+    for (int e = 0; e < E; e++) v[e] = e * kAll + t < n ? lds[e * kAll + t] : 0;
+    const auto across = [&](int run, int d) {
+        if (d >= 64) {
             __syncthreads();
-            for (int i = threadIdx.x; i < all / 2; i += kThreads) {
-                const int x = (i & (d - 1)) + ((i & ~(d - 1)) << 1), y = x + d;
-                const uint64_t p = v[x], q = v[y];
-                if ((p < q) == ((x & run) == 0)) v[x] = q, v[y] = p;
-            }
+#pragma unroll
+            for (int e = 0; e < E; e++) lds[e * kAll + t] = v[e];
+            __syncthreads();
         }
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            const uint64_t o = d >= 64 ? lds[e * kAll + (t ^ d)] : (uint64_t)__shfl_xor((unsigned long long)v[e], d);
+            const bool high = ((t & d) == 0) == (((e * kAll + t) & run) == 0);
+            v[e] = high ? max(v[e], o) : min(v[e], o);
+        }
+    };
+    for (int run = 2; run <= kAll; run <<= 1)
+        for (int d = run >> 1; d; d >>= 1) across(run, d);
+#pragma unroll
+    for (int r = 2; r <= E; r *= 2) {
+#pragma unroll
+        for (int d = r / 2; d; d /= 2)
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (!(e & d)) {
+                    const uint64_t x = max(v[e], v[e | d]), y = min(v[e], v[e | d]);
+                    v[e] = e & r ? y : x, v[e | d] = e & r ? x : y;
+                }
+        for (int d = kAll / 2; d; d >>= 1) across(r * kAll, d);
+    }
     __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; e++) lds[e * kAll + t] = v[e];
+    __syncthreads();
+}
+
+// Sorts n of kList (4 kAll) different values; what is past them may be overwritten.  Few
+// are put where the number of higher ones says.
+__device__ inline void sort(uint64_t *v, int n) {
+    if (n <= 128) {
+        const uint64_t own = (int)threadIdx.x < n ? v[threadIdx.x] : 0;
+        int place = 0;
+        for (int i = 0; i < n; i++) place += v[i] > own;
+        __syncthreads();
+        if ((int)threadIdx.x < n) v[place] = own;
+        __syncthreads();
+    } else if (n <= kAll) {
+        sort_registers<1>(v, n);
+    } else if (n <= 2 * kAll) {
+        sort_registers<2>(v, n);
+    } else {
+        sort_registers<4>(v, n);
+    }
 }
 
 // Running sums over n values, a run of them to each thread: before(i) of each is
 // passed to f(i, before, value); returns the sum of all.
-template <typename Value, typename F> __device__ inline double scan(int n, double *wave_d, Value &&value, F &&f) {
-    const int each = (n + kThreads - 1) / kThreads, i0 = threadIdx.x * each, i1 = min(n, i0 + each), lane = threadIdx.x & 63;
+template <int NT, typename Value, typename F> __device__ inline double scan(int n, double *wave_d, Value &&value, F &&f) {
+    const int each = (n + NT - 1) / NT, i0 = threadIdx.x * each, i1 = min(n, i0 + each), lane = threadIdx.x & 63;
     double own = 0.;
     for (int i = i0; i < i1; i++) own += value(i);
     double sum = own;
@@ -426,7 +539,7 @@ template <typename Value, typename F> __device__ inline double scan(int n, doubl
     __syncthreads();
     double run = __shfl_up(sum, 1), all = 0.;
     if (lane == 0) run = 0.;
-    for (int w = 0; w < kWaves; w++) {
+    for (int w = 0; w < NT / 64; w++) {
         if (w < (int)(threadIdx.x >> 6)) run += wave_d[w];
         all += wave_d[w];
     }
@@ -443,153 +556,203 @@ __device__ inline int count(int n, int *wave_n) {
     if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = n;
     __syncthreads();
     n = 0;
-    for (int w = 0; w < kWaves; w++) n += wave_n[w];
+    for (int w = 0; w < kAllWaves; w++) n += wave_n[w];
     return n;
 }
 
-template <typename V> __device__ inline V at_device(const V *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-// Whether this workgroup is the last of a row's: what the others have written at
-// device scope before is there then.
-__device__ inline bool last_of(uint32_t *arrived, int of, int *s_last) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) *s_last = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)of - 1;
-    __syncthreads();
-    return *s_last;
-}
-
+// The weights of the highest kMaxSorted, once these are sorted, take the place
+// of the rest of the list.
 struct Sorting {
-    uint64_t list[kList];
-    double w[kMaxSorted];
+    union {
+        uint64_t list[kList];
+        struct {
+            uint64_t highest[kMaxSorted];
+            double w[kMaxSorted];
+        };
+    };
 };
 
 // The token of a small top-k, from the n sorted logits down to its border.
 template <int T>
 __device__ inline int pick_sorted(const Task<T> &t, Sorting &s, int n, double u, double *wave_d, int *wave_n) {
     const int k = min(n, t.top_k);
-    for (int i = threadIdx.x; i < k; i += kThreads) s.w[i] = t.row.weight((uint32_t)(s.list[i] >> 32));
+    for (int i = threadIdx.x; i < k; i += kAll) s.w[i] = t.row.weight((uint32_t)(s.list[i] >> 32));
     __syncthreads();
     const auto w = [&](int i) { return s.w[i]; };
     int kept = 0;
-    const double all = scan(k, wave_d, w, [](int, double, double) {});
+    const double all = scan<kAll>(k, wave_d, w, [](int, double, double) {});
     const double most = all * (double)t.top_p;
-    scan(k, wave_d, w, [&](int i, double before, double v) {
+    scan<kAll>(k, wave_d, w, [&](int i, double before, double v) {
         kept += i == 0 || ((t.top_p >= 1.f || before < most || t.top_p != t.top_p) && (!(t.min_p > 0.f) || v >= (double)t.min_p));
     });
     kept = count(kept, wave_n);
     // in the order of the indices: their complements, the highest first, with the places of the weights
-    for (int i = threadIdx.x; i < kept; i += kThreads) s.list[i] = s.list[i] << 32 | (uint32_t)i;
+    for (int i = threadIdx.x; i < kept; i += kAll) s.list[i] = s.list[i] << 32 | (uint32_t)i;
+    __syncthreads();
     sort(s.list, kept);
     const auto in_order = [&](int i) { return s.w[(uint32_t)s.list[i]]; };
-    const double target = u * scan(kept, wave_d, in_order, [](int, double, double) {});
+    const double target = u * scan<kAll>(kept, wave_d, in_order, [](int, double, double) {});
     int first = kept, some = 0;  // the first that is above it; the last that has a weight, and one
-    scan(kept, wave_d, in_order, [&](int i, double run, double v) {
+    scan<kAll>(kept, wave_d, in_order, [&](int i, double run, double v) {
         if (v > 0.) some = i + 1;
         if (v > 0. && run + v > target) first = min(first, i);
     });
     for (int d = 1; d < 64; d <<= 1) first = min(first, __shfl_xor(first, d)), some = max(some, __shfl_xor(some, d));
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = first, wave_n[kWaves + (threadIdx.x >> 6)] = some;
+    if ((threadIdx.x & 63) == 0) wave_n[threadIdx.x >> 6] = first, wave_n[kAllWaves + (threadIdx.x >> 6)] = some;
     __syncthreads();
-    for (int w = 0; w < kWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kWaves + w]);
+    for (int w = 0; w < kAllWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kAllWaves + w]);
     return (int)~(uint32_t)(s.list[first < kept ? first : some - 1] >> 32);
+}
+
+// The same of few, by one wave without barriers: two to a lane, in the order
+// of their ranks.
+constexpr int kFew = 128;
+template <int T> __device__ inline int pick_few(const Task<T> &t, Sorting &s, int n, double u) {
+    const int lane = threadIdx.x & 63, k = min(n, t.top_k);
+    uint32_t index[2];
+    double w[2];
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        const int i = e * 64 + lane;
+        const uint64_t v = i < k ? s.list[i] : 0;
+        index[e] = ~(uint32_t)v;
+        w[e] = i < k ? t.row.weight((uint32_t)(v >> 32)) : 0.;
+    }
+    double run[2] = {w[0], w[1]};
+    for (int d = 1; d < 64; d <<= 1) {
+        const double a = __shfl_up(run[0], d), b = __shfl_up(run[1], d);
+        if (lane >= d) run[0] += a, run[1] += b;
+    }
+    const double half = __shfl(run[0], 63), most = (half + __shfl(run[1], 63)) * (double)t.top_p;
+    const double lower[2] = {__shfl_up(run[0], 1), __shfl_up(run[1], 1)};
+    int kept = 0;
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        const double before = (e ? half : 0.) + (lane ? lower[e] : 0.);
+        const bool in = e * 64 + lane < k && (t.top_p >= 1.f || before < most || t.top_p != t.top_p) && (!(t.min_p > 0.f) || w[e] >= (double)t.min_p);
+        kept += __popcll(__ballot(in));
+    }
+    kept = max(kept, 1);
+    // the running sums in the order of the indices
+    double sum[2] = {0., 0.}, all = 0.;
+    for (int i = 0; i < kept; i++) {
+        const uint32_t o = __builtin_amdgcn_readlane(i < 64 ? index[0] : index[1], i & 63);
+        const uint64_t b = __builtin_bit_cast(uint64_t, i < 64 ? w[0] : w[1]);
+        const double v = __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)b, i & 63) |
+                                                        (uint64_t)__builtin_amdgcn_readlane((uint32_t)(b >> 32), i & 63) << 32);
+        all += v;
+#pragma unroll
+        for (int e = 0; e < 2; e++) sum[e] += o <= index[e] ? v : 0.;
+    }
+    uint32_t past = ~0u, some = 0;  // the first index above, the last with a weight, and one
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+        if (e * 64 + lane < kept && w[e] > 0.) {
+            some = max(some, index[e] + 1);
+            if (sum[e] > u * all) past = min(past, index[e]);
+        }
+    for (int d = 1; d < 64; d <<= 1) past = min(past, (uint32_t)__shfl_xor((int)past, d)), some = max(some, (uint32_t)__shfl_xor((int)some, d));
+    return (int)(past != ~0u ? past : some - 1);
 }
 
 template <int T> __global__ __launch_bounds__(kThreads) void sample_border(SampleArgs a, Plan p) {
     typedef typename Elem<T>::type El;
-    __shared__ union {
-        Sorting sorting;
-        Shared alone;
-    } s;
-    __shared__ uint64_t wave64[kWaves];
-    __shared__ double wave_d[kWaves];
-    __shared__ int wave_n[2 * kWaves], s_n, s_base, s_last;
-    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
+    __shared__ uint64_t s_list[kStage];
+    __shared__ int s_n;
+    __shared__ uint32_t s_base;
+    const int64_t r = blockIdx.x / p.slices;
     const int slice = (int)(blockIdx.x % p.slices);
-    const Task<T> t = task_of<T>(a, p, b);
-    uint32_t *const state = p.state + r * kState;
-    const auto token = [&](int i) {
-        if (threadIdx.x == 0) a.tokens[b] = i, state[kMode] = kDone;
-    };
-    if (t.kind == kAll) return;
-    if (t.kind == kToken) {
-        if (slice == 0) token(t.token());
-        return;
-    }
-    if (t.kind == kAlone) {
-        if (slice == 0) token(search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, number_of(a, b)));
-        return;
-    }
-    const uint64_t *const bins = p.bins + r * kBins;
-    uint64_t target = (uint64_t)t.top_k, above = 0, all = 0;
-    if (t.kind == kWeight) {
-        for (int i = threadIdx.x; i < kBins; i += kThreads) all += bins[i];
-        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor((unsigned long long)all, d);
-        if ((threadIdx.x & 63) == 0) wave64[threadIdx.x >> 6] = all;
-        __syncthreads();
-        all = wave64[0] + wave64[1] + wave64[2] + wave64[3];
-        __syncthreads();
-        target = max((uint64_t)1, (uint64_t)__builtin_ceil((double)all * (double)t.top_p));
-    }
-    if (threadIdx.x == 0) s_n = 0;
-    int border = crossing([&](int i) { return bins[i]; }, target, wave64, above);
+    const Task<T> t = task_of<T>(a, p, p.row0 + r);
+    if (t.kind != kSorted && t.kind != kNumber && t.kind != kWeight) return;
+    RowState &state = p.state[r];
     const bool whole = t.kind == kSorted;
-    if (border < 0) {  // a top-k beyond the logits that there are: all of them
-        if (!whole) {
-            if (slice == 0 && threadIdx.x == 0) state[kLowest] = 1, state[kCut] = (uint32_t)a.V, state[kMode] = kBordered;
-            return;
-        }
+    int border = state.border;
+    if (border < 0) {  // all of them
+        if (!whole) return;
         border = kBins - 1;
     }
-    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8], int) {
+    uint64_t *const list = p.list + r * kList;
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8]) {
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const float z = Elem<T>::get(v[j]);
-            if (z == -INFINITY) continue;
             const int bin = bin_of(t.top, z);
-            if (bin == border || (whole && bin < border)) {
+            if (z != -INFINITY && (bin == border || (whole && bin < border))) {
                 const int n = atomicAdd(&s_n, 1);
-                if (n < kList) s.sorting.list[n] = (uint64_t)key_of<T>(v[j]) << 32 | (uint32_t)~(i + j);
+                const uint64_t what = (uint64_t)key_of<T>(v[j]) << 32 | (uint32_t)~(i + j);
+                if (n < kStage) {
+                    s_list[n] = what;
+                } else {
+                    const uint32_t at = atomicAdd(&state.listed, 1u);
+                    if (at < kList) list[at] = what;
+                }
             }
         }
     });
     __syncthreads();
-    const int mine = s_n;
-    uint64_t *const list = p.list + r * kList;
-    if (threadIdx.x == 0 && mine) s_base = (int)__hip_atomic_fetch_add(&state[kListed], (uint32_t)mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int mine = min(s_n, kStage);
+    if (mine == 0) return;
+    if (threadIdx.x == 0) s_base = atomicAdd(&state.listed, (uint32_t)mine);
     __syncthreads();
-    for (int i = threadIdx.x; i < min(mine, kList); i += kThreads)
-        if (s_base + i < kList) __hip_atomic_store(&list[s_base + i], s.sorting.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (!last_of(&state[kArrived], p.slices, &s_last)) return;
+    for (int i = threadIdx.x; i < mine; i += kThreads)
+        if (s_base + i < kList) list[s_base + i] = s_list[i];
+}
 
-    const int n = (int)at_device(&state[kListed]);
+// What the list says: the border, or the token.
+template <int T> __global__ __launch_bounds__(kAll) void sample_sorted(SampleArgs a, Plan p) {
+    __shared__ union {
+        Sorting sorting;
+        Shared alone;
+    } s;
+    __shared__ double wave_d[kAllWaves];
+    __shared__ int wave_n[2 * kAllWaves];
+    const int64_t r = blockIdx.x, b = p.row0 + r;
+    const Task<T> t = task_of<T>(a, p, b);
+    RowState &state = p.state[r];
+    if (t.kind == kEvery) return;
     const double u = number_of(a, b);
-    if (n > kList) {
-        token(search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u));
+    const int n = (int)min(state.listed, (uint32_t)kList + 1);
+    int token;
+    if (t.kind == kToken) {
+        token = t.token();
+    } else if (t.kind == kAlone || n > kList) {
+        token = search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u);
+    } else if (t.kind != kSorted && state.border < 0) {  // a top-k beyond the logits that there are: all of them
+        if (threadIdx.x == 0) state.lowest = 1, state.cut = (uint32_t)a.V, state.mode = kBordered;
         return;
-    }
-    for (int i = threadIdx.x; i < n; i += kThreads) s.sorting.list[i] = at_device(&list[i]);
-    __syncthreads();
-    sort(s.sorting.list, n);
-    if (whole) {
-        token(pick_sorted<T>(t, s.sorting, n, u, wave_d, wave_n));
-        return;
-    }
-    int kept = 0;
-    if (t.kind == kNumber) {
-        kept = (int)((uint64_t)t.top_k - above);
     } else {
-        const double most = (double)all * (double)t.top_p / kUnit, over = (double)above / kUnit;
-        scan(n, wave_d, [&](int i) { return t.row.weight((uint32_t)(s.sorting.list[i] >> 32)); },
-             [&](int, double before, double) { kept += over + before < most; });
-        kept = count(kept, wave_n);
+        const uint64_t *const list = p.list + r * kList;
+        for (int i = threadIdx.x; i < n; i += kAll) s.sorting.list[i] = list[i];
+        __syncthreads();
+        sort(s.sorting.list, n);
+        if (t.kind == kSorted && n <= kFew) {
+            if (threadIdx.x >= 64) return;
+            token = pick_few<T>(t, s.sorting, n, u);
+        } else if (t.kind == kSorted) {
+            token = pick_sorted<T>(t, s.sorting, n, u, wave_d, wave_n);
+        } else {
+            int kept = 0;
+            if (t.kind == kNumber) {
+                kept = (int)((uint64_t)t.top_k - state.above);
+            } else {
+                const double most = (double)state.all * (double)t.top_p / kUnit, over = (double)state.above / kUnit;
+                scan<kAll>(n, wave_d, [&](int i) { return t.row.weight((uint32_t)(s.sorting.list[i] >> 32)); },
+                           [&](int, double before, double) { kept += over + before < most; });
+                kept = count(kept, wave_n);
+            }
+            if (threadIdx.x == 0) {
+                const uint64_t lowest = s.sorting.list[min(max(kept, 1), n) - 1];
+                state.lowest = (uint32_t)(lowest >> 32);
+                state.cut = ~(uint32_t)lowest;
+                state.mode = kBordered;
+            }
+            return;
+        }
     }
-    if (threadIdx.x == 0) {
-        const uint64_t lowest = s.sorting.list[min(max(kept, 1), n) - 1];
-        state[kLowest] = (uint32_t)(lowest >> 32);
-        state[kCut] = ~(uint32_t)lowest;
-        state[kMode] = kBordered;
-    }
+    if (threadIdx.x == 0) a.tokens[b] = token, state.mode = kDone;
 }
 
 template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleArgs a, Plan p) {
@@ -600,15 +763,15 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleA
     const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
     const int slice = (int)(blockIdx.x % p.slices), lane = threadIdx.x & 63;
     const Task<T> t = task_of<T>(a, p, b);
-    uint32_t *const state = p.state + r * kState;
+    RowState &state = p.state[r];
     if (t.kind == kToken) {
         if (slice == 0 && threadIdx.x == 0) a.tokens[b] = t.token();
         return;
     }
-    const bool all = t.kind == kAll;
-    if (!all && state[kMode] != kBordered) return;
-    const uint32_t lowest = all ? 1 : state[kLowest];
-    const int cut = all ? a.V : (int)state[kCut];
+    const bool all = t.kind == kEvery;
+    if (!all && state.mode != kBordered) return;
+    const uint32_t lowest = all ? 1 : state.lowest;
+    const int cut = all ? a.V : (int)state.cut;
     // further below the highest than this nothing is left by min-p, whatever the rounding
     const float far = t.min_p > 0.f ? (float)(-log((double)t.min_p) / t.row.per * 1.0001 + 1e-30) : INFINITY;
     const auto weight = [&](El v, int i) {
@@ -619,21 +782,32 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleA
         return !(t.min_p > 0.f) || w >= (double)t.min_p ? w : 0.;
     };
     double *const sums = p.sums + r * p.chunks;
-    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8], int c) {
-        double sum = 0.;
+    double group[kAhead];
+    each_group<T>(t.row, p, slice, [&](int c0, int end, const El v[kAhead][8]) {
 #pragma unroll
-        for (int j = 0; j < 8; j++) sum += weight(v[j], i + j);
-        sum = wave_sum(sum);
-        if (lane == 0) __hip_atomic_store(&sums[c], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int n = 0; n < kAhead; n++) {
+            group[n] = 0.;
+            if (c0 + n * kWaves < end) {
+                const int i = index_of(t.row, c0 + n * kWaves);
+#pragma unroll
+                for (int j = 0; j < 8; j++) group[n] += weight(v[n][j], i + j);
+            }
+        }
+        for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+            for (int n = 0; n < kAhead; n++) group[n] += __shfl_xor(group[n], d);
+#pragma unroll
+        for (int n = 0; n < kAhead; n++)
+            if (lane == n && c0 + n * kWaves < end) __hip_atomic_store(&sums[c0 + n * kWaves], group[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
-    if (!last_of(&state[kPicked], p.slices, &s_last)) return;
+    if (!last_of(&state.picked, p.slices, &s_last)) return;
 
     for (int i = threadIdx.x; i < p.chunks; i += kThreads) s_sum[i] = at_device(&sums[i]);
     __syncthreads();
     const auto value = [&](int i) { return s_sum[i]; };
-    const double target = number_of(a, b) * scan(p.chunks, wave_d, value, [](int, double, double) {});
+    const double target = number_of(a, b) * scan<kThreads>(p.chunks, wave_d, value, [](int, double, double) {});
     int first = p.chunks, some = 0;
-    scan(p.chunks, wave_d, value, [&](int i, double run, double v) {
+    scan<kThreads>(p.chunks, wave_d, value, [&](int i, double run, double v) {
         if (v > 0.) some = i;
         if (v > 0. && run + v > target) first = min(first, i);
     });
@@ -643,16 +817,17 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleA
     __syncthreads();
     for (int w = 0; w < kWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kWaves + w]);
     const int chunk = first < p.chunks ? first : some;
-    scan(p.chunks, wave_d, value, [&](int i, double run, double) {
+    scan<kThreads>(p.chunks, wave_d, value, [&](int i, double run, double) {
         if (i == chunk) s_before = run;
     });
     __syncthreads();
     if (threadIdx.x >= 64) return;
     El v[8];
     double w[8], own = 0.;
-    load8(t.row, chunk * kChunk + lane * 8, v);
+    const int i0 = index_of(t.row, chunk);
+    load8(t.row, i0, v);
 #pragma unroll
-    for (int j = 0; j < 8; j++) own += w[j] = weight(v[j], chunk * kChunk + lane * 8 + j);
+    for (int j = 0; j < 8; j++) own += w[j] = weight(v[j], i0 + j);
     double sum = own;
     for (int d = 1; d < 64; d <<= 1) {
         const double o = __shfl_up(sum, d);
@@ -671,13 +846,13 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleA
     }
     const uint64_t is_past = __ballot(past < 8), is_some = __ballot(last >= 0);
     const int l = is_past ? __ffsll((unsigned long long)is_past) - 1 : is_some ? 63 - __clzll((long long)is_some) : 0;
-    if (lane == l) a.tokens[b] = chunk * kChunk + lane * 8 + (is_past ? past : max(last, 0));
+    if (lane == l) a.tokens[b] = i0 + (is_past ? past : max(last, 0));
 }
 
 // How rows are cut: into slices that together fill the GPU several times.
 Plan plan_of(int64_t rows, int V, uint8_t *ws) {
     Plan p = {};
-    p.chunks = (V + kChunk - 1) / kChunk;
+    p.chunks = (V + 7 + kChunk - 1) / kChunk;  // wherever a row begins
     const int most = (int)std::min<int64_t>({(int64_t)kMaxSlices, std::max<int64_t>(1, kSliceGroups / rows), (int64_t)(p.chunks + kWaves - 1) / kWaves});
     p.chunks_of_slice = (p.chunks + most - 1) / most;
     p.slices = (p.chunks + p.chunks_of_slice - 1) / p.chunks_of_slice;
@@ -687,7 +862,7 @@ Plan plan_of(int64_t rows, int V, uint8_t *ws) {
     p.bins = (uint64_t *)take((size_t)rows * kBins * 8);
     p.list = (uint64_t *)take((size_t)rows * kList * 8);
     p.sums = (double *)take((size_t)rows * p.chunks * 8);
-    p.state = (uint32_t *)take((size_t)rows * kState * 4);
+    p.state = (RowState *)take((size_t)rows * sizeof(RowState));
     p.row0 = (int64_t)at;  // the size, for the query
     return p;
 }
@@ -704,6 +879,7 @@ template <int T> sim_status sample_t(hipStream_t st, const SampleArgs &a, uint8_
         if (some_k || some_p) {
             sample_bins<T><<<grid, kThreads, 0, st>>>(a, p);
             sample_border<T><<<grid, kThreads, 0, st>>>(a, p);
+            sample_sorted<T><<<(uint32_t)rows, kAll, 0, st>>>(a, p);
         }
         if (!sorted) sample_pick<T><<<grid, kThreads, 0, st>>>(a, p);
     }
