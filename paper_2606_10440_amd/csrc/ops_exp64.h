@@ -15,8 +15,7 @@ __device__ inline double exp64(double x) {
     const double magic = 6755399441055744., t = __builtin_fma(x, 1.4426950408889634, magic), n = t - magic;
     // ln 2 as 24 bits, by which n is multiplied exactly, and the rest
     const double r = __builtin_fma(n, 1.904654299957768e-09, __builtin_fma(n, -0.693147182464599609375, x));
-    double p = 1. / 479001600.;
-    p = __builtin_fma(p, r, 1. / 39916800.);
+    double p = __builtin_fma(r, 1. / 479001600., 1. / 39916800.);
     p = __builtin_fma(p, r, 1. / 3628800.);
     p = __builtin_fma(p, r, 1. / 362880.);
     p = __builtin_fma(p, r, 1. / 40320.);

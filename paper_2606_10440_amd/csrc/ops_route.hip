@@ -19,7 +19,7 @@ namespace {
 constexpr int kChunk = 64;           // tokens of one workgroup
 constexpr int kThreads = 16 * kChunk;
 constexpr int kPart = 16;            // tokens of one where there are few
-constexpr int kScanChunks = 512;     // above it, counts are scanned by a kernel of their own
+constexpr int kScanChunks = 384;     // above it, counts are scanned by a kernel of their own
 
 typedef uint32_t u32_any __attribute__((aligned(1), may_alias));  // words of elements of any type
 
@@ -528,11 +528,118 @@ template <int NV> __device__ inline uint64_t top_groups(const uint32_t key[NV], 
     return keep;
 }
 
+// The choice by scores with a bias, from scores in 32 bits: as whole numbers of
+// kBits bits above the experts' complemented indices, so that a search is
+// maxima and nothing else.  It is the definition's where no two that it had to
+// tell apart, of the groups or of the experts, are nearer to each other than
+// their errors; sure says whether that is so.
+template <int NV> struct Fast {
+    static constexpr int kIndexBits = NV == 1 ? 4 : NV == 2 ? 5 : NV == 4 ? 6 : NV == 8 ? 7 : NV == 16 ? 8 : NV == 32 ? 9 : 10;
+    static constexpr int kBits = kIndexBits < 8 ? 24 : 32 - kIndexBits;
+    static constexpr uint32_t kIndex = (1u << kIndexBits) - 1;
+    // In steps of 2^-24 of the range, how far a value may be from what the
+    // definition compares: a sigmoid 4 (its exponent's argument, two results to
+    // a unit in the last place, a sum), the definition's own two roundings 2,
+    // the bias, the offset and the scale 6, and two whole steps of a conversion
+    // beside; a softmax's sum of NV + 4 terms and its division as many more.
+    // Two values that are further apart than twice that are in order.
+    static constexpr uint32_t near(uint32_t steps) { return 2 * ((steps >> (24 - kBits)) + 3); }
+    static constexpr uint32_t kNear = near(12), kNearSum = near(12 + NV + 8);
+    uint32_t k[NV];
+    uint32_t apart;  // kNear or kNearSum
+    bool sure = true;
+
+    __device__ uint32_t take() {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) m = max(m, k[i]);
+        m = max16(m);
+#pragma unroll
+        for (int i = 0; i < NV; i++) k[i] = k[i] == m ? 0 : k[i];
+        return m;
+    }
+    // groups as 64 times their value and, complemented, their index
+    __device__ static uint32_t group_key(const Two &two, uint32_t zero, int best, uint32_t g) {
+        const uint32_t v = (two.a >> kIndexBits) + (best == 1 ? 0 : two.b ? two.b >> kIndexBits : zero);
+        return two.a ? v << 6 | (63 - g) : 0;
+    }
+    __device__ void keep_groups(int E, int groups, int top, int best, uint32_t zero) {
+        const int l = threadIdx.x & 15, size = E / groups, lanes = size / NV;
+        uint64_t keep = 0;
+        uint32_t last = 0, next = 0;
+        if (lanes * NV == size && (lanes & (lanes - 1)) == 0) {
+            Two two;
+#pragma unroll
+            for (int i = 0; i < NV; i++) two.add(k[i]);
+            if (lanes >= 2) two.merge<kDppXor1>();
+            if (lanes >= 4) two.merge<kDppXor2>();
+            if (lanes >= 8) two.merge<kDppHalfMirror>();
+            if (lanes >= 16) two.merge<kDppMirror>();
+            uint32_t v = group_key(two, zero, best, l / lanes);
+            for (int j = 0; j <= top; j++) {
+                const uint32_t m = max16(v);
+                if (j < top) keep |= m ? 1ull << (63 - (m & 63)) : 0, last = m;
+                else next = m;
+                v = v == m ? 0 : v;
+            }
+            const bool kept = (keep >> (l / lanes)) & 1;
+#pragma unroll
+            for (int i = 0; i < NV; i++) k[i] = kept ? k[i] : 0;
+        } else {
+            uint32_t v[SIM_MOE_MAX_GROUPS / 16] = {};  // of groups l, l + 16, ...
+            for (int g = 0; g < groups; g++) {
+                Two two;
+#pragma unroll
+                for (int i = 0; i < NV; i++) two.add((uint32_t)(l * NV + i - g * size) < (uint32_t)size ? k[i] : 0);
+                two.merge<kDppXor1>();
+                two.merge<kDppXor2>();
+                two.merge<kDppHalfMirror>();
+                two.merge<kDppMirror>();
+#pragma unroll
+                for (int q = 0; q < SIM_MOE_MAX_GROUPS / 16; q++)
+                    if (g == q * 16 + l) v[q] = group_key(two, zero, best, g);
+            }
+            for (int j = 0; j <= top; j++) {
+                const uint32_t m = max16(max(max(v[0], v[1]), max(v[2], v[3])));
+                if (j < top) keep |= m ? 1ull << (63 - (m & 63)) : 0, last = m;
+                else next = m;
+#pragma unroll
+                for (int q = 0; q < SIM_MOE_MAX_GROUPS / 16; q++) v[q] = v[q] == m ? 0 : v[q];
+            }
+            int g = l * NV / size, in = l * NV - g * size;
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                if (!((keep >> (g & 63)) & 1)) k[i] = 0;
+                if (++in == size) in = 0, g++;
+            }
+        }
+        sure = sure && (next == 0 || (last >> 6) - (next >> 6) > best * (apart + 4));  // (the definition's sum is rounded too)
+    }
+};
+
+// Up to 16 experts, one in each of 16 lanes where had, in the order of their
+// sigmoids with the bias, from 64 bits.
+__device__ inline uint32_t rank_chosen(bool had, uint32_t e, double z, const float *__restrict__ bias) {
+    const uint32_t key = had ? order_key((float)sigmoid64(z) + bias[e]) : 0;
+    const int row = threadIdx.x & 48;
+    int place = 0;
+    for (int j = 0; j < 16; j++) {
+        const uint32_t k2 = __shfl(key, row | j), e2 = __shfl(e, row | j);
+        place += k2 > key || (k2 == key && (k2 ? e2 < e : j < (int)(threadIdx.x & 15)));
+    }
+    return (uint32_t)__builtin_amdgcn_ds_permute((row | place) << 2, (int)e);
+}
+
 // The choice by scores.  Which of two experts is higher must not depend on how
-// a score was computed, so scores are in 64 bits and rounded to 32, in which
+// a score was computed, so scores are those of 64 bits, rounded to 32, in which
 // the bias and the groups' sums are added: what is compared is the definition's
 // but where a 64-bit value lies within its own error of the middle between two
-// 32-bit ones.
+// 32-bit ones.  With a bias 32 bits are tried first, which suffice but for one
+// token in a thousand (scores of 256 experts, k = 8).
+//
+// 32768 tokens, 256 bf16 experts in 8 groups, k = 8: 33 us (49 with all scores
+// in 64 bits; 39 where a token whose choices are near to each other is done
+// anew with these, so that one wave in seventy holds up its workgroup).
 template <int T, int NV, int CH>
 __global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__restrict__ experts, float *__restrict__ weights,
                                                         uint8_t *__restrict__ hist, int32_t *__restrict__ offsets,
@@ -541,89 +648,165 @@ __global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__
     __shared__ Lists lists;
     const int l = threadIdx.x & 15, tok = threadIdx.x >> 4, E = a.E, k = a.k;
     const int64_t t = (int64_t)blockIdx.x * CH + tok;
-    const bool live = t < a.T;
+    const bool live = t < a.T, grouped = a.groups > a.top_groups, sigmoid = a.score == SIM_SCORE_SIGMOID;
     const El *const z = (const El *)a.logits + (live ? t : 0) * a.stride;
     const uint8_t *const mask = a.mask ? a.mask + (live ? t : 0) * a.mask_stride : nullptr;
     clear<CH>(lists);
-    Keys<SIM_TYPE_F32, NV> key;
-    El v[NV];
-    uint64_t ok = load_logits<T, NV>(z, mask, E, live, v);
-    uint32_t top = 0;  // the highest of the allowed logits
+    float x[NV];  // -infinity where nothing can be chosen
+    {
+        El v[NV];
+        const uint64_t ok = load_logits<T, NV>(z, mask, E, live, v);
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-        const uint32_t by = (ok >> i) & 1 ? order_key(Elem<T>::get(v[i])) : 0;
-        if (!by) ok &= ~(1ull << i);
-        key.k[i] = by;
-        top = max(top, by);
+        for (int i = 0; i < NV; i++) x[i] = (ok >> i) & 1 ? Elem<T>::get(v[i]) : -INFINITY;
     }
-    double high = 0., inv = 0.;
-    if (a.score == SIM_SCORE_SOFTMAX) {
-        high = key_value(max16(top));
-        if (a.bias || !a.renorm || (a.groups > a.top_groups && a.group_best == 2)) {
-            double sum = 0.;
-#pragma unroll
-            for (int i = 0; i < NV; i++) sum += (ok >> i) & 1 ? exp64(Elem<T>::get(v[i]) - high) : 0.;
-            inv = 1. / sum16(sum);
-        }
-    }
-    const bool grouped = a.groups > a.top_groups, by_score = a.bias || (grouped && a.group_best == 2);
-    if (by_score) {
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const double x = Elem<T>::get(v[i]);
-            const float s = (float)(a.score == SIM_SCORE_SIGMOID ? sigmoid64(x) : exp64(x - high) * inv);
-            key.k[i] = (ok >> i) & 1 ? order_key(a.bias ? s + a.bias[min(l * NV + i, E - 1)] : s) : 0;
-        }
-    }
-    if (grouped) {
-        const uint64_t keep = top_groups<NV>(key.k, E, a.groups, a.top_groups, a.group_best);
-        const int size = E / a.groups;
-        int g = l * NV / size, in = l * NV - g * size;
-#pragma unroll
-        for (int i = 0; i < NV; i++) {
-            // without a bias the logits have the scores' order, and a finer one
-            if (by_score && !a.bias && key.k[i]) key.k[i] = order_key(Elem<T>::get(v[i]));
-            if (!((keep >> (g & 63)) & 1)) key.k[i] = 0;
-            if (++in == size) in = 0, g++;
-        }
-    }
-    __syncthreads();
 
     uint32_t mine[2] = {0, 0}, mine_e[2] = {0, 0};  // the choices l and l + 16
-    for (int j = 0; j < k; j++) {
-        uint32_t e;
-        const uint32_t m = key.take(e);
-        if (l == (j & 15)) {
-            mine[j >> 4] = m;
-            mine_e[j >> 4] = e;
+    bool sure = false;
+    if (a.bias) {
+        Fast<NV> fast;
+        float b[NV], most = 0.f, all = 0.f, high = 1.f, top = -INFINITY, inv = 1.f;
+        if (l * NV + NV <= E) load_some<NV>(a.bias + l * NV, b);
+        else
+#pragma unroll
+            for (int i = 0; i < NV; i++) b[i] = a.bias[min(l * NV + i, E - 1)];
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            most = fmaxf(most, fabsf(b[i]));
+            top = fmaxf(top, x[i]);
+        }
+        most = __uint_as_float(max16(__float_as_uint(most)));
+        if (!sigmoid) {
+            top = fmaxf(top, dpp_f32<kDppXor1>(top));
+            top = fmaxf(top, dpp_f32<kDppXor2>(top));
+            top = fmaxf(top, dpp_f32<kDppHalfMirror>(top));
+            top = fmaxf(top, dpp_f32<kDppMirror>(top));
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0.f : fast_exp(x[i] - top);
+            high = inv = 1.f / sum16(sum);
+        }
+        const float scale = (float)((1 << Fast<NV>::kBits) - 16) / (high + 2.f * most);
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            const float c = sigmoid ? __builtin_amdgcn_rcpf(1.f + fast_exp(-x[i])) + b[i] : fast_exp(x[i] - top) * inv + b[i];
+            const uint32_t key = ((uint32_t)((c + most) * scale) + 1) << Fast<NV>::kIndexBits | (Fast<NV>::kIndex - (l * NV + i));
+            all += x[i] == -INFINITY ? 0.f : c;
+            fast.k[i] = x[i] == -INFINITY ? 0 : key;
+        }
+        all = sum16(all);
+        fast.apart = sigmoid ? Fast<NV>::kNear : Fast<NV>::kNearSum;
+        // nothing is infinite or NaN (most past 2^64 is left to the other way too)
+        fast.sure = fabsf(all) < 1.8446744e19f && most < 1.8446744e19f;
+        if (grouped) fast.keep_groups(E, a.groups, a.top_groups, a.group_best, (uint32_t)(most * scale) + 1);
+        // two more than are wanted: who of those that are near is higher is a
+        // question of few then, unless the last is near the last wanted too
+        const bool ranked = sigmoid && k <= 14;
+        const int n = ranked ? k + 2 : k + 1;
+        bool near = false;
+        uint32_t before = 0, wanted = 0;
+        for (int j = 0; j < n; j++) {
+            const uint32_t m = fast.take(), gap = (before >> Fast<NV>::kIndexBits) - (m >> Fast<NV>::kIndexBits);
+            near |= j && m && gap <= fast.apart;
+            before = m;
+            if (j == k - 1) wanted = m;
+            if (l == (j & 15)) {
+                mine[j >> 4] = m;
+                mine_e[j >> 4] = Fast<NV>::kIndex - (m & Fast<NV>::kIndex);
+            }
+        }
+        if (!ranked) {
+            fast.sure = fast.sure && !near;
+            if (k < 32 && l == (k & 15)) mine[k >> 4] = 0;
+        } else {
+            if (before && (wanted >> Fast<NV>::kIndexBits) - (before >> Fast<NV>::kIndexBits) <= fast.apart) fast.sure = false;
+            if (__ballot(near && live)) mine_e[0] = rank_chosen(mine[0] != 0, mine_e[0], mine[0] ? (double)Elem<T>::get(z[mine_e[0]]) : 0., a.bias);
+            if (l >= k) mine[0] = 0;
+        }
+        sure = fast.sure || !live;
+    }
+    if (__ballot(!sure)) {
+        Keys<SIM_TYPE_F32, NV> key;
+        uint32_t top = 0;  // the highest of the allowed logits
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            key.k[i] = order_key(x[i]);
+            top = max(top, key.k[i]);
+        }
+        const bool by_score = a.bias || (grouped && a.group_best == 2);
+        if (by_score) {
+            double high = 0., inv = 0.;
+            if (!sigmoid) {
+                high = key_value(max16(top));
+                double sum = 0.;
+#pragma unroll
+                for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0. : exp64(x[i] - high);
+                inv = 1. / sum16(sum);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                const float s = (float)(sigmoid ? sigmoid64(x[i]) : exp64(x[i] - high) * inv);
+                key.k[i] = x[i] == -INFINITY ? 0 : order_key(a.bias ? s + a.bias[min(l * NV + i, E - 1)] : s);
+            }
+        }
+        if (grouped) {
+            const uint64_t keep = top_groups<NV>(key.k, E, a.groups, a.top_groups, a.group_best);
+            const int size = E / a.groups;
+            int g = l * NV / size, in = l * NV - g * size;
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                // without a bias the logits have the scores' order, and a finer one
+                if (by_score && !a.bias && key.k[i]) key.k[i] = order_key(x[i]);
+                if (!((keep >> (g & 63)) & 1)) key.k[i] = 0;
+                if (++in == size) in = 0, g++;
+            }
+        }
+        for (int j = 0; j < k; j++) {
+            uint32_t e;
+            const uint32_t m = key.take(e);
+            if (l == (j & 15)) {
+                mine[j >> 4] = m;
+                mine_e[j >> 4] = e;
+            }
         }
     }
     // the weights from the chosen logits again, relative to the highest chosen
     // one where they are divided by their sum
-    double x[2], w64[2];
+    const int rows = k > 16 ? 2 : 1;
+    double high = 0., inv = 0., chosen[2] = {0., 0.}, w64[2] = {0., 0.};
     uint32_t first = 0;
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        x[q] = mine[q] ? (double)Elem<T>::get(z[mine_e[q]]) : 0.;
-        first = max(first, mine[q] ? order_key((float)x[q]) : 0u);
-    }
-    const bool sigmoid = a.score == SIM_SCORE_SIGMOID;
+    for (int q = 0; q < 2; q++)
+        if (q < rows) {
+            chosen[q] = mine[q] ? (double)Elem<T>::get(z[mine_e[q]]) : 0.;
+            first = max(first, mine[q] ? order_key((float)chosen[q]) : 0u);
+        }
     if (a.renorm) {
         high = key_value(max16(first));
         if (sigmoid && high > 0.) high = 0.;
+    } else if (!sigmoid) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) top = max(top, order_key(x[i]));
+        high = key_value(max16(top));
+        double sum = 0.;
+#pragma unroll
+        for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0. : exp64(x[i] - high);
+        inv = 1. / sum16(sum);
     }
 #pragma unroll
-    for (int q = 0; q < 2; q++) {
-        if (!mine[q]) w64[q] = 0.;
-        else if (!sigmoid) w64[q] = exp64(x[q] - high);
-        else if (a.renorm) w64[q] = exp64((x[q] > 0. ? 0. : x[q]) - high) * reciprocal(1. + exp64(-__builtin_fabs(x[q])));
-        else w64[q] = sigmoid64(x[q]);
-    }
+    for (int q = 0; q < 2; q++)
+        if (q < rows) {
+            if (!sigmoid) w64[q] = exp64(chosen[q] - high);
+            else if (a.renorm) w64[q] = exp64((chosen[q] > 0. ? 0. : chosen[q]) - high) * reciprocal(1. + exp64(-__builtin_fabs(chosen[q])));
+            else w64[q] = sigmoid64(chosen[q]);
+            if (!mine[q]) w64[q] = 0.;
+        }
     if (a.renorm) inv = 1. / sum16(w64[0] + w64[1]);
     else if (sigmoid) inv = 1.;
     float w[2];
 #pragma unroll
     for (int q = 0; q < 2; q++) w[q] = (float)(w64[q] * inv * a.scale);
+    __syncthreads();  // the lists are clear
     finish<CH>(lists, t, live, k, E, (int)min(a.T, (int64_t)CH), mine_e, mine, w, experts, weights, hist, offsets, order);
 }
 

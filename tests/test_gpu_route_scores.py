@@ -135,6 +135,31 @@ def test_infinities_and_nan(ops, score, biased):
             assert (np.abs(w - want[1][rows])[fin] <= rel * np.abs(want[1][rows][fin]) + least).all()
 
 
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,groups,top,best", [(16, 1, 1, 1), (64, 8, 3, 2), (60, 5, 2, 2), (256, 8, 4, 2), (256, 16, 5, 1), (1000, 10, 4, 2)])
+def test_values_a_rounding_apart(ops, score, E, groups, top, best):
+    # biases a few steps of 32 bits apart, in no order, on logits that are the same, or a step of theirs apart: the choice
+    # depends on the last place of a score, of its sum with the bias, and of the groups' sums
+    g = np.random.default_rng(E + best)
+    T = 40
+    b = (0.25 + g.integers(0, 12, E) * 2.0 ** -25).astype(np.float32)
+    v = np.full((T, E), 0.3, np.float32)
+    v[1::3] = g.standard_normal((len(v[1::3]), 1)).astype(np.float32)
+    v[2::3] = np.nextafter(np.float32(1.25), np.float32(2)) + g.integers(0, 6, (len(v[2::3]), E)).astype(np.float32) * np.float32(2.0 ** -23)
+    k = min(8, E // groups * top)
+    r = ops.moe_route(torch.from_numpy(v).cuda(), k, score=score, bias=torch.from_numpy(b).cuda(), groups=groups, top_groups=top, group_best=best)
+    check(r, ref.route(v.astype(np.float64), k, None, True, score, b, groups, top, best))
+
+
+@pytest.mark.parametrize("size", [1e-20, 1e3, 1e15, 1e25])
+def test_biases_of_any_size(ops, size):
+    z, v = logits(5, 60, 128, "fp32")
+    b = (np.random.default_rng(5).standard_normal(128) * size).astype(np.float32)
+    for score in ("sigmoid", "softmax"):
+        r = ops.moe_route(z, 6, score=score, bias=torch.from_numpy(b).cuda(), groups=8, top_groups=3, group_best=2)
+        check(r, ref.route(v, 6, None, True, score, b, 8, 3, 2))
+
+
 def test_every_bf16_logit_has_its_score(ops):
     bits = (np.arange(1 << 16, dtype=np.uint32) << 16).view(np.float32)
     v = bits[np.isfinite(bits)].astype(np.float64)
