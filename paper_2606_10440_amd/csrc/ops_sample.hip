@@ -5,12 +5,14 @@
 // lowest kept logit and how many of the logits that tie with it are kept, in
 // the order of their indices.  A row is read by several workgroups, a slice
 // each, in up to five launches:
-//   tops    the highest logit of each slice;
-//   bins    the numbers of logits, or the sums of their weights, by how far
-//           they are below the highest, in steps of 1/128 of that distance;
-//   border  the logits of the bin in which the border lies (with a small
-//           top-k: of all above it too) as a list;
-//   sorted  one workgroup sorts it: a small top-k's row is done with that;
+//   tops    the highest logit of each slice, and of each eight;
+//   bins    the sums of the weights, or the numbers of logits, by how far they
+//           are below the highest, in steps of 1/128 of that distance;
+//   border  the logits of the bin in which the border lies as a list;
+//   sorted  one workgroup sorts it.  For a small top-k the list is made here:
+//           where k of the eights' highest are above a border, k logits are, so
+//           that only the eights whose highest is need be read.  Such a row is
+//           done with that;
 //   pick    the sums of the kept weights of 512 logits each; the row's last
 //           workgroup finds the 512 that the token is in, and the token.
 // A row whose border bin holds more than can be sorted (logits that are nearly
@@ -270,6 +272,7 @@ struct RowState {
 // Where the rows' parts of the workspace are, and how a row is cut.
 struct Plan {
     uint64_t *tops;    // [row][slice]: key and, complemented, index of the highest
+    void *eights;      // [row][chunks * kChunk / 8]: the highest of each eight
     uint64_t *bins;    // [row][kBins]
     uint64_t *list;    // [row][kList]
     double *sums;      // [row][chunks]
@@ -281,6 +284,7 @@ struct Plan {
 enum Kind {
     kToken,   // the highest, or -1
     kSorted,  // a small top-k: all that is above its border is sorted
+    kListed,  // the same, of a row with few eights for it
     kNumber,  // a large top-k
     kWeight,  // top-p
     kEvery,   // every logit, or what min-p leaves
@@ -296,12 +300,15 @@ template <int T> struct Task {
     __device__ int token() const { return best == 0 || best >= kInfinite<T> ? -1 : first; }
 };
 
-// What is to be done with a row, from its slices' tops; the same in every wave.
-template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Plan &p, int64_t b) {
+// Whether a row has so many eights that the k-th highest of theirs leaves no
+// more logits than can be sorted (with twice k eights that is four thirds of
+// k), or so few logits that all can.
+__host__ __device__ inline bool by_eights(int V, int k) { return V <= kList || V / 16 >= k; }
+
+// What is to be done with a row, from its highest logit's key and, complemented,
+// index.
+template <int T> __device__ inline Task<T> task_from(const SampleArgs &a, int64_t b, uint64_t top) {
     typedef typename Elem<T>::type El;
-    const int lane = threadIdx.x & 63;
-    uint64_t top = lane < p.slices ? p.tops[(b - p.row0) * p.slices + lane] : 0;
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
     Task<T> t;
     t.row.z = (const El *)a.logits + b * a.stride;
     t.row.V = a.V;
@@ -316,8 +323,16 @@ template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Pl
     t.row.per = 1. / temperature;
     if (t.best == 0 || t.best >= kInfinite<T> || !(temperature > 0.f) || t.top_k == 1 || t.top_p <= 0.f || t.min_p > 1.f) t.kind = kToken;
     else if (t.top_k < 1 || t.top_k >= a.V) t.kind = t.top_p < 1.f ? kWeight : kEvery;
-    else t.kind = t.top_k <= kMaxSorted ? kSorted : t.top_p < 1.f ? kAlone : kNumber;
+    else if (t.top_k <= kMaxSorted) t.kind = by_eights(a.V, t.top_k) ? kSorted : kListed;
+    else t.kind = t.top_p < 1.f ? kAlone : kNumber;
     return t;
+}
+// The same from its slices' tops, in every wave.
+template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Plan &p, int64_t b) {
+    const int lane = threadIdx.x & 63;
+    uint64_t top = lane < p.slices ? p.tops[(b - p.row0) * p.slices + lane] : 0;
+    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
+    return task_from<T>(a, b, top);
 }
 __device__ inline double number_of(const SampleArgs &a, int64_t b) {
     return a.u[b] > 0.f ? (double)min(a.u[b], 1.f - 5.9604644775390625e-8f) : 0.;
@@ -341,22 +356,22 @@ template <int T> __device__ inline void load8(const Row<T> &row, int i, typename
 }
 constexpr int kAhead = 4;  // chunks that are loaded together
 // Calls f(first chunk, end of the slice, logits) for this wave's part of a
-// slice, every kWaves-th chunk.
-template <int T, typename F> __device__ inline void each_group(const Row<T> &row, const Plan &p, int slice, F &&f) {
+// slice, every NW-th chunk.
+template <int T, int NW, typename F> __device__ inline void each_group(const Row<T> &row, const Plan &p, int slice, F &&f) {
     const int end = min(p.chunks, (slice + 1) * p.chunks_of_slice);
-    for (int c0 = slice * p.chunks_of_slice + (int)(threadIdx.x >> 6); c0 < end; c0 += kAhead * kWaves) {
+    for (int c0 = slice * p.chunks_of_slice + (int)(threadIdx.x >> 6); c0 < end; c0 += kAhead * NW) {
         typename Elem<T>::type v[kAhead][8];
 #pragma unroll
-        for (int n = 0; n < kAhead; n++) load8(row, index_of(row, min(c0 + n * kWaves, end - 1)), v[n]);
+        for (int n = 0; n < kAhead; n++) load8(row, index_of(row, min(c0 + n * NW, end - 1)), v[n]);
         f(c0, end, v);
     }
 }
-// Calls f(index, eight logits) for each of them.
-template <int T, typename F> __device__ inline void each_chunk(const Row<T> &row, const Plan &p, int slice, F &&f) {
-    each_group<T>(row, p, slice, [&](int c0, int end, const typename Elem<T>::type v[kAhead][8]) {
+// Calls f(index, eight logits, chunk) for each of them.
+template <int T, int NW, typename F> __device__ inline void each_chunk(const Row<T> &row, const Plan &p, int slice, F &&f) {
+    each_group<T, NW>(row, p, slice, [&](int c0, int end, const typename Elem<T>::type v[kAhead][8]) {
 #pragma unroll
         for (int n = 0; n < kAhead; n++)
-            if (c0 + n * kWaves < end) f(index_of(row, c0 + n * kWaves), v[n]);
+            if (c0 + n * NW < end) f(index_of(row, c0 + n * NW), v[n], c0 + n * NW);
     });
 }
 
@@ -365,28 +380,74 @@ template <int T, typename F> __device__ inline void each_chunk(const Row<T> &row
 __device__ inline int bin_of(float top, float z) {
     return min((int)(__float_as_uint(top - z + 0.03125f) >> 16) - 0x3d00, kBins - 1);
 }
+// Weights of many logits: e^((z - top) / T) = 2^(n / 64) e^r, n the nearest whole
+// number, from a table of 2^(j / 64) in LDS and the series of e^r up to r^4 / 24
+// (r is at most ln 2 / 128, the next term below 2^-44).  A 64-bit fused operation
+// takes as long as two others here, and a constant that the compiler knows costs
+// it two moves, so constants are kept from it, in scalar registers (192 rows of
+// 131072 without top-k: @EXP@).
+constexpr int kTable = 64;
+__device__ inline double scalar(double c) {
+    asm("" : "+s"(c));
+    return c;
+}
+__device__ inline void fill(double *table) {
+    if (threadIdx.x < kTable) table[threadIdx.x] = 2. * exp64(((int)threadIdx.x - kTable) * (0.69314718055994531 / kTable));
+}
+template <int T> struct Exp {
+    const double *table;
+    double top, steps;  // 64 / (T ln 2)
+    float high, far;    // beyond this below the highest, weights are below 2^-1022: 0
+    __device__ Exp(const Row<T> &row, const double *table_) : table(table_), top(row.top), steps(row.per * (kTable * 1.4426950408889634)) {
+        high = (float)top;
+        far = (float)min(708. / row.per, 3e38);
+    }
+    __device__ bool none(float z) const { return high - z > far; }
+    // where not none(z)
+    __device__ double operator()(float z) const {
+        const double d = (double)z - top, t = __builtin_fma(d, steps, scalar(6755399441055744.)), n = t - scalar(6755399441055744.);
+        const double f = __builtin_fma(d, steps, -n);
+        const int i = (int)__builtin_bit_cast(uint64_t, t);
+        constexpr double c = 0.69314718055994531 / kTable;
+        double p = __builtin_fma(f, scalar(c * c * c * c / 24.), scalar(c * c * c / 6.));
+        p = __builtin_fma(p, f, scalar(c * c / 2.));
+        p = __builtin_fma(p, f, scalar(c));
+        const uint64_t b = __builtin_bit_cast(uint64_t, table[i & (kTable - 1)]);
+        const double s = __builtin_bit_cast(double, b + ((uint64_t)(uint32_t)((i >> 6) << 20) << 32));
+        return __builtin_fma(s * f, p, s);
+    }
+    // Eight at once, which keeps the 64-bit units busy (a branch around each left
+    // them waiting for each other's results: @EIGHT@); 0 where not in.
+    __device__ void eight(const float z[8], const bool in[8], double w[8]) const {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[j] = in[j] ? z[j] : high;
+#pragma unroll
+        for (int j = 0; j < 8; j++) w[j] = (*this)(x[j]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) w[j] = in[j] ? w[j] : 0.;
+    }
+};
+
 // A weight as a whole multiple of 1 / kUnit: it lands in the low bits of 2^52 + w kUnit
 __device__ inline uint64_t fixed(double w) {
     return __builtin_bit_cast(uint64_t, __builtin_fma(w, kUnit, 4503599627370496.)) & 0xfffffffffffffull;
 }
 
-template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleArgs a, Plan p) {
+// Key and, complemented, index of the highest logit of a wave's part of a slice;
+// eight(value, chunk) gets the highest of each eight.
+template <int T, int NW, typename F> __device__ inline uint64_t highest(const Row<T> &row, const Plan &p, int slice, F &&eight) {
     typedef typename Elem<T>::type El;
-    __shared__ uint64_t s_top[kWaves];
-    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
-    const int slice = (int)(blockIdx.x % p.slices);
-    Row<T> row;
-    row.z = (const El *)a.logits + b * a.stride;
-    row.V = a.V;
     // the highest of eight at a time; which of them it is, only where they hold
     // a lane's highest
     float best = -INFINITY;
     int at = 0;
-    each_chunk<T>(row, p, slice, [&](int i, const El v[8]) {
+    each_chunk<T, NW>(row, p, slice, [&](int i, const El v[8], int c) {
         float m = Elem<T>::get(v[0]);
 #pragma unroll
         for (int j = 1; j < 8; j++) m = __builtin_elementwise_maximum(m, Elem<T>::get(v[j]));
         if (!(m <= best) && best == best) at = i, best = __builtin_elementwise_maximum(best, m);
+        eight(m, c);
     });
     uint32_t key = 0;
     if (best != -INFINITY) {
@@ -403,6 +464,20 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleA
     }
     uint64_t top = (uint64_t)key << 32 | (uint32_t)~at;
     for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
+    return top;
+}
+
+template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleArgs a, Plan p, bool with_eights) {
+    typedef typename Elem<T>::type El;
+    __shared__ uint64_t s_top[kWaves];
+    const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
+    const int slice = (int)(blockIdx.x % p.slices);
+    Row<T> row;
+    row.z = (const El *)a.logits + b * a.stride;
+    row.V = a.V;
+    uint64_t top = highest<T, kWaves>(row, p, slice, [&](float m, int c) {
+        if (with_eights) ((El *)p.eights)[r * p.chunks * (kChunk / 8) + c * (kChunk / 8) + (threadIdx.x & 63)] = Elem<T>::put(m);
+    });
     if ((threadIdx.x & 63) == 0) s_top[threadIdx.x >> 6] = top;
     // what the launches after this one count up from
     for (int i = slice * kThreads + threadIdx.x; i < kBins; i += p.slices * kThreads) p.bins[r * kBins + i] = 0;
@@ -425,21 +500,27 @@ __device__ inline bool last_of(uint32_t *arrived, int of, int *s_last) {
 template <int T> __global__ __launch_bounds__(kThreads) void sample_bins(SampleArgs a, Plan p) {
     typedef typename Elem<T>::type El;
     __shared__ uint64_t s_bin[kBins], wave64[kWaves];
+    __shared__ double s_table[kTable];
     __shared__ int s_last;
     const int64_t r = blockIdx.x / p.slices;
     const int slice = (int)(blockIdx.x % p.slices);
     const Task<T> t = task_of<T>(a, p, p.row0 + r);
-    if (t.kind != kSorted && t.kind != kNumber && t.kind != kWeight) return;
+    if (t.kind != kListed && t.kind != kNumber && t.kind != kWeight) return;
     for (int i = threadIdx.x; i < kBins; i += kThreads) s_bin[i] = 0;
+    fill(s_table);
+    const Exp<T> weight(t.row, s_table);
+    const bool weights = t.kind == kWeight;
     __syncthreads();
-    each_chunk<T>(t.row, p, slice, [&](int, const El v[8]) {
+    each_chunk<T, kWaves>(t.row, p, slice, [&](int, const El v[8], int) {
+        float z[8];
+        bool in[8];
+        double w[8];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float z = Elem<T>::get(v[j]);
-            if (z == -INFINITY) continue;
-            const uint64_t n = t.kind == kWeight ? fixed(exp64(((double)z - t.row.top) * t.row.per)) : 1;
-            atomicAdd((unsigned long long *)&s_bin[bin_of(t.top, z)], (unsigned long long)n);
-        }
+        for (int j = 0; j < 8; j++) z[j] = Elem<T>::get(v[j]), in[j] = !(weights ? weight.none(z[j]) : z[j] == -INFINITY);
+        if (weights) weight.eight(z, in, w);
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (in[j]) atomicAdd((unsigned long long *)&s_bin[bin_of(t.top, z[j])], (unsigned long long)(weights ? fixed(w[j]) : 1));
     });
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += kThreads)
@@ -664,9 +745,9 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_border(Sampl
     const int64_t r = blockIdx.x / p.slices;
     const int slice = (int)(blockIdx.x % p.slices);
     const Task<T> t = task_of<T>(a, p, p.row0 + r);
-    if (t.kind != kSorted && t.kind != kNumber && t.kind != kWeight) return;
+    if (t.kind != kListed && t.kind != kNumber && t.kind != kWeight) return;
     RowState &state = p.state[r];
-    const bool whole = t.kind == kSorted;
+    const bool whole = t.kind == kListed;
     int border = state.border;
     if (border < 0) {  // all of them
         if (!whole) return;
@@ -675,7 +756,7 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_border(Sampl
     uint64_t *const list = p.list + r * kList;
     if (threadIdx.x == 0) s_n = 0;
     __syncthreads();
-    each_chunk<T>(t.row, p, slice, [&](int i, const El v[8]) {
+    each_chunk<T, kWaves>(t.row, p, slice, [&](int i, const El v[8], int) {
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             const float z = Elem<T>::get(v[j]);
@@ -701,6 +782,92 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_border(Sampl
         if (s_base + i < kList) list[s_base + i] = s_list[i];
 }
 
+// The list of a small top-k, from the highest of each eight; its length.
+template <int T> __device__ inline int list_by_eights(const Task<T> &t, const Plan &p, int64_t r, Sorting &s, int *s_n) {
+    typedef typename Elem<T>::type El;
+    __shared__ union {
+        uint32_t bin[kBins];
+        int32_t first[kList];  // of the eights that are read
+    } e;
+    __shared__ uint64_t wave64[kAllWaves];
+    __shared__ int s_eights;
+    constexpr int kAt = 8;  // loads under way
+    const int n = p.chunks * (kChunk / 8), before_row = (int)((uintptr_t)t.row.z / sizeof(El) % 8);
+    const El *const eights = (const El *)p.eights + r * n;
+    const auto each = [&](auto &&f) {
+        for (int g0 = threadIdx.x; g0 < n; g0 += kAt * kAll) {
+            float m[kAt];
+#pragma unroll
+            for (int x = 0; x < kAt; x++) m[x] = Elem<T>::get(eights[min(g0 + x * kAll, n - 1)]);
+#pragma unroll
+            for (int x = 0; x < kAt; x++)
+                if (g0 + x * kAll < n && m[x] != -INFINITY) f(g0 + x * kAll, bin_of(t.top, m[x]));
+        }
+    };
+    for (int i = threadIdx.x; i < kBins; i += kAll) e.bin[i] = 0;
+    if (threadIdx.x == 0) *s_n = s_eights = 0;
+    __syncthreads();
+    each([&](int, int bin) { atomicAdd(&e.bin[bin], 1u); });
+    __syncthreads();
+    uint64_t above;
+    int border = crossing<kAll>([&](int i) { return (uint64_t)e.bin[i]; }, (uint64_t)t.top_k, wave64, above);
+    if (border < 0) border = kBins - 1;  // all of them
+    __syncthreads();
+    each([&](int g, int bin) {
+        if (bin > border) return;
+        const int at = atomicAdd(&s_eights, 1);
+        if (at < kList) e.first[at] = g * 8 - before_row;
+    });
+    __syncthreads();
+    if (s_eights > kList) return kList + 1;  // of which each has one at least
+    for (int x0 = threadIdx.x; x0 < s_eights * 8; x0 += kAt * kAll) {
+        El v[kAt];
+        int at[kAt];
+#pragma unroll
+        for (int x = 0; x < kAt; x++) {
+            const int of = min(x0 + x * kAll, s_eights * 8 - 1);
+            at[x] = e.first[of / 8] + of % 8;
+            const bool in = x0 + x * kAll < s_eights * 8 && at[x] >= 0 && at[x] < t.row.V;
+            v[x] = in ? t.row.z[at[x]] : Elem<T>::put(-INFINITY);
+        }
+#pragma unroll
+        for (int x = 0; x < kAt; x++) {
+            const float z = Elem<T>::get(v[x]);
+            if (z == -INFINITY || bin_of(t.top, z) > border) continue;
+            const int n = atomicAdd(s_n, 1);
+            if (n < kList) s.list[n] = (uint64_t)key_of<T>(v[x]) << 32 | (uint32_t)~at[x];
+        }
+    }
+    __syncthreads();
+    return min(*s_n, kList + 1);
+}
+
+// The token of a row's sorted list; -2 where that has the border alone: then
+// lowest and cut are that of thread 0.  above and all: the bins' sums above the
+// border and all of them.
+template <int T>
+__device__ inline int resolve(const Task<T> &t, Sorting &s, int n, double u, uint64_t above, uint64_t all, double *wave_d, int *wave_n,
+                              uint32_t &lowest, uint32_t &cut) {
+    sort(s.list, n);
+    if (t.kind == kSorted || t.kind == kListed) {
+        if (n > kFew) return pick_sorted<T>(t, s, n, u, wave_d, wave_n);
+        return threadIdx.x < 64 ? pick_few<T>(t, s, n, u) : 0;
+    }
+    int kept = 0;
+    if (t.kind == kNumber) {
+        kept = (int)((uint64_t)t.top_k - above);
+    } else {
+        const double most = (double)all * (double)t.top_p / kUnit, over = (double)above / kUnit;
+        scan<kAll>(n, wave_d, [&](int i) { return t.row.weight((uint32_t)(s.list[i] >> 32)); },
+                   [&](int, double before, double) { kept += over + before < most; });
+        kept = count(kept, wave_n);
+    }
+    const uint64_t last = s.list[min(max(kept, 1), n) - 1];
+    lowest = (uint32_t)(last >> 32);
+    cut = ~(uint32_t)last;
+    return -2;
+}
+
 // What the list says: the border, or the token.
 template <int T> __global__ __launch_bounds__(kAll) void sample_sorted(SampleArgs a, Plan p) {
     __shared__ union {
@@ -708,145 +875,143 @@ template <int T> __global__ __launch_bounds__(kAll) void sample_sorted(SampleArg
         Shared alone;
     } s;
     __shared__ double wave_d[kAllWaves];
-    __shared__ int wave_n[2 * kAllWaves];
+    __shared__ int wave_n[2 * kAllWaves], s_n;
     const int64_t r = blockIdx.x, b = p.row0 + r;
     const Task<T> t = task_of<T>(a, p, b);
     RowState &state = p.state[r];
     if (t.kind == kEvery) return;
     const double u = number_of(a, b);
-    const int n = (int)min(state.listed, (uint32_t)kList + 1);
-    int token;
+    int n = (int)min(state.listed, (uint32_t)kList + 1);
+    if (t.kind == kSorted) n = list_by_eights<T>(t, p, r, s.sorting, &s_n);
+    int token = -2;
     if (t.kind == kToken) {
         token = t.token();
     } else if (t.kind == kAlone || n > kList) {
         token = search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u);
-    } else if (t.kind != kSorted && state.border < 0) {  // a top-k beyond the logits that there are: all of them
+    } else if (t.kind == kNumber && state.border < 0) {  // a top-k beyond the logits that there are: all of them
         if (threadIdx.x == 0) state.lowest = 1, state.cut = (uint32_t)a.V, state.mode = kBordered;
-        return;
     } else {
         const uint64_t *const list = p.list + r * kList;
-        for (int i = threadIdx.x; i < n; i += kAll) s.sorting.list[i] = list[i];
+        if (t.kind != kSorted)
+            for (int i = threadIdx.x; i < n; i += kAll) s.sorting.list[i] = list[i];
         __syncthreads();
-        sort(s.sorting.list, n);
-        if (t.kind == kSorted && n <= kFew) {
-            if (threadIdx.x >= 64) return;
-            token = pick_few<T>(t, s.sorting, n, u);
-        } else if (t.kind == kSorted) {
-            token = pick_sorted<T>(t, s.sorting, n, u, wave_d, wave_n);
-        } else {
-            int kept = 0;
-            if (t.kind == kNumber) {
-                kept = (int)((uint64_t)t.top_k - state.above);
-            } else {
-                const double most = (double)state.all * (double)t.top_p / kUnit, over = (double)state.above / kUnit;
-                scan<kAll>(n, wave_d, [&](int i) { return t.row.weight((uint32_t)(s.sorting.list[i] >> 32)); },
-                           [&](int, double before, double) { kept += over + before < most; });
-                kept = count(kept, wave_n);
-            }
-            if (threadIdx.x == 0) {
-                const uint64_t lowest = s.sorting.list[min(max(kept, 1), n) - 1];
-                state.lowest = (uint32_t)(lowest >> 32);
-                state.cut = ~(uint32_t)lowest;
-                state.mode = kBordered;
-            }
-            return;
-        }
+        uint32_t lowest, cut;
+        token = resolve<T>(t, s.sorting, n, u, state.above, state.all, wave_d, wave_n, lowest, cut);
+        if (token == -2 && threadIdx.x == 0) state.lowest = lowest, state.cut = cut, state.mode = kBordered;
     }
-    if (threadIdx.x == 0) a.tokens[b] = token, state.mode = kDone;
+    if (threadIdx.x == 0 && token != -2) a.tokens[b] = token, state.mode = kDone;
 }
 
+// The weights of what is kept of a row, 0 for the others.
+template <int T> struct Kept {
+    Row<T> row;
+    Exp<T> exp;
+    float top, far, low, min_p;
+    int cut;
+    __device__ Kept(const Task<T> &t, const double *table, bool all, uint32_t lowest, int cut_)
+        : row(t.row), exp(t.row, table), top(t.top), min_p(t.min_p) {
+        low = all ? -INFINITY : value_of<T>(lowest);
+        cut = all ? INT32_MIN : cut_;
+        // further below the highest than this nothing is left by min-p, whatever the rounding
+        far = min_p > 0.f ? min((float)(-log((double)min_p) / row.per * 1.0001 + 1e-30), exp.far) : exp.far;
+    }
+    __device__ bool in(float z, int i) const { return (z > low || (z == low && i <= cut)) && !(top - z > far); }
+    __device__ double weight(typename Elem<T>::type v, int i) const {
+        const float z = Elem<T>::get(v);
+        if (!in(z, i)) return 0.;
+        const double w = exp(z);
+        return !(min_p > 0.f) || w >= (double)min_p ? w : 0.;
+    }
+    // Of a wave's part of a slice: put(chunk, sum of its weights), by one lane.
+    template <int NW, typename F> __device__ void sums(const Plan &p, int slice, F &&put) const {
+        each_group<T, NW>(row, p, slice, [&](int c0, int end, const typename Elem<T>::type v[kAhead][8]) {
+            double sum[kAhead];
+#pragma unroll
+            for (int n = 0; n < kAhead; n++) {
+                sum[n] = 0.;
+                if (c0 + n * NW < end) {
+                    const int i = index_of(row, c0 + n * NW);
+                    float z[8];
+                    bool is[8], any = false;
+                    double w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; j++) z[j] = Elem<T>::get(v[n][j]), is[j] = in(z[j], i + j), any |= is[j];
+                    if (__ballot(any)) {
+                        exp.eight(z, is, w);
+#pragma unroll
+                        for (int j = 0; j < 8; j++) sum[n] += !(min_p > 0.f) || w[j] >= (double)min_p ? w[j] : 0.;
+                    }
+                }
+            }
+            for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+                for (int n = 0; n < kAhead; n++) sum[n] += __shfl_xor(sum[n], d);
+#pragma unroll
+            for (int n = 0; n < kAhead; n++)
+                if ((int)(threadIdx.x & 63) == n && c0 + n * NW < end) put(c0 + n * NW, sum[n]);
+        });
+    }
+    // The token, from all chunks' sums (in LDS); in all threads.
+    template <int NT> __device__ int find(const double *s_sum, int chunks, double u, double *wave_d, int *wave_n) const {
+        __shared__ double s_before;
+        const int lane = threadIdx.x & 63;
+        double target = 0., before = 0.;
+        int n = chunks, i0 = 0, at = 0;
+#pragma unroll 1
+        for (int step = 0; step < 2; step++) {  // the chunk, and the logit in it
+            const auto value = [&](int i) {
+                if (step == 0) return s_sum[i];
+                return i0 + i >= 0 && i0 + i < row.V ? weight(row.z[i0 + i], i0 + i) : 0.;
+            };
+            int first = n, some = -1;  // the first above the target; the last that has a weight
+            double before_first = 0., before_some = 0.;
+            for (int pass = step; pass < 2; pass++) {
+                const double sum = scan<NT>(n, wave_d, value, [&](int i, double run, double v) {
+                    if (pass == 0 || !(v > 0.)) return;
+                    some = i, before_some = before + run;
+                    if (first == n && before + run + v > target) first = i, before_first = before + run;
+                });
+                if (pass == 0) target = u * sum;
+            }
+            int f = first, o = some;
+            for (int d = 1; d < 64; d <<= 1) f = min(f, __shfl_xor(f, d)), o = max(o, __shfl_xor(o, d));
+            __syncthreads();
+            if (lane == 0) wave_n[threadIdx.x >> 6] = f, wave_n[NT / 64 + (threadIdx.x >> 6)] = o;
+            if (threadIdx.x == 0) s_before = before;
+            __syncthreads();
+            for (int w = 0; w < NT / 64; w++) f = min(f, wave_n[w]), o = max(o, wave_n[NT / 64 + w]);
+            at = f < n ? f : max(o, 0);
+            if (f < n ? first == f : o >= 0 && some == o) s_before = f < n ? before_first : before_some;
+            __syncthreads();
+            before = s_before;
+            if (step == 0) i0 = at * kChunk - (int)((uintptr_t)row.z / sizeof(*row.z) % 8), n = kChunk;
+        }
+        return i0 + at;
+    }
+};
+
 template <int T> __global__ __launch_bounds__(kThreads) void sample_pick(SampleArgs a, Plan p) {
-    typedef typename Elem<T>::type El;
-    __shared__ double wave_d[kWaves];
+    __shared__ double wave_d[kWaves], s_sum[kMaxChunks], s_table[kTable];
     __shared__ int wave_n[2 * kWaves], s_last;
-    __shared__ double s_before, s_sum[kMaxChunks];
     const int64_t r = blockIdx.x / p.slices, b = p.row0 + r;
-    const int slice = (int)(blockIdx.x % p.slices), lane = threadIdx.x & 63;
+    const int slice = (int)(blockIdx.x % p.slices);
     const Task<T> t = task_of<T>(a, p, b);
     RowState &state = p.state[r];
     if (t.kind == kToken) {
         if (slice == 0 && threadIdx.x == 0) a.tokens[b] = t.token();
         return;
     }
-    const bool all = t.kind == kEvery;
-    if (!all && state.mode != kBordered) return;
-    const uint32_t lowest = all ? 1 : state.lowest;
-    const int cut = all ? a.V : (int)state.cut;
-    // further below the highest than this nothing is left by min-p, whatever the rounding
-    const float far = t.min_p > 0.f ? (float)(-log((double)t.min_p) / t.row.per * 1.0001 + 1e-30) : INFINITY;
-    const auto weight = [&](El v, int i) {
-        const uint32_t k = key_of<T>(v);
-        const bool in = (k > lowest || (k == lowest && i <= cut)) && !(t.top - Elem<T>::get(v) > far);
-        if (!in) return 0.;
-        const double w = exp64(((double)Elem<T>::get(v) - t.row.top) * t.row.per);
-        return !(t.min_p > 0.f) || w >= (double)t.min_p ? w : 0.;
-    };
+    if (t.kind != kEvery && state.mode != kBordered) return;
+    fill(s_table);
+    __syncthreads();
+    const Kept<T> kept(t, s_table, t.kind == kEvery, state.lowest, (int)state.cut);
     double *const sums = p.sums + r * p.chunks;
-    double group[kAhead];
-    each_group<T>(t.row, p, slice, [&](int c0, int end, const El v[kAhead][8]) {
-#pragma unroll
-        for (int n = 0; n < kAhead; n++) {
-            group[n] = 0.;
-            if (c0 + n * kWaves < end) {
-                const int i = index_of(t.row, c0 + n * kWaves);
-#pragma unroll
-                for (int j = 0; j < 8; j++) group[n] += weight(v[n][j], i + j);
-            }
-        }
-        for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-            for (int n = 0; n < kAhead; n++) group[n] += __shfl_xor(group[n], d);
-#pragma unroll
-        for (int n = 0; n < kAhead; n++)
-            if (lane == n && c0 + n * kWaves < end) __hip_atomic_store(&sums[c0 + n * kWaves], group[n], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    });
+    kept.template sums<kWaves>(p, slice, [&](int c, double sum) { __hip_atomic_store(&sums[c], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
     if (!last_of(&state.picked, p.slices, &s_last)) return;
-
     for (int i = threadIdx.x; i < p.chunks; i += kThreads) s_sum[i] = at_device(&sums[i]);
     __syncthreads();
-    const auto value = [&](int i) { return s_sum[i]; };
-    const double target = number_of(a, b) * scan<kThreads>(p.chunks, wave_d, value, [](int, double, double) {});
-    int first = p.chunks, some = 0;
-    scan<kThreads>(p.chunks, wave_d, value, [&](int i, double run, double v) {
-        if (v > 0.) some = i;
-        if (v > 0. && run + v > target) first = min(first, i);
-    });
-    for (int d = 1; d < 64; d <<= 1) first = min(first, __shfl_xor(first, d)), some = max(some, __shfl_xor(some, d));
-    __syncthreads();
-    if (lane == 0) wave_n[threadIdx.x >> 6] = first, wave_n[kWaves + (threadIdx.x >> 6)] = some;
-    __syncthreads();
-    for (int w = 0; w < kWaves; w++) first = min(first, wave_n[w]), some = max(some, wave_n[kWaves + w]);
-    const int chunk = first < p.chunks ? first : some;
-    scan<kThreads>(p.chunks, wave_d, value, [&](int i, double run, double) {
-        if (i == chunk) s_before = run;
-    });
-    __syncthreads();
-    if (threadIdx.x >= 64) return;
-    El v[8];
-    double w[8], own = 0.;
-    const int i0 = index_of(t.row, chunk);
-    load8(t.row, i0, v);
-#pragma unroll
-    for (int j = 0; j < 8; j++) own += w[j] = weight(v[j], i0 + j);
-    double sum = own;
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
-    double run = __shfl_up(sum, 1);
-    run = s_before + (lane ? run : 0.);
-    int past = 8, last = -1;
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        run += w[j];
-        if (w[j] > 0.) {
-            last = j;
-            if (past == 8 && run > target) past = j;
-        }
-    }
-    const uint64_t is_past = __ballot(past < 8), is_some = __ballot(last >= 0);
-    const int l = is_past ? __ffsll((unsigned long long)is_past) - 1 : is_some ? 63 - __clzll((long long)is_some) : 0;
-    if (lane == l) a.tokens[b] = i0 + (is_past ? past : max(last, 0));
+    const int token = kept.template find<kThreads>(s_sum, p.chunks, number_of(a, b), wave_d, wave_n);
+    if (threadIdx.x == 0) a.tokens[b] = token;
 }
 
 // How rows are cut: into slices that together fill the GPU several times.
@@ -859,6 +1024,7 @@ Plan plan_of(int64_t rows, int V, uint8_t *ws) {
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t n = at; at += (bytes + 255) / 256 * 256; return ws + n; };
     p.tops = (uint64_t *)take((size_t)rows * p.slices * 8);
+    p.eights = take((size_t)rows * p.chunks * (kChunk / 8) * 4);
     p.bins = (uint64_t *)take((size_t)rows * kBins * 8);
     p.list = (uint64_t *)take((size_t)rows * kList * 8);
     p.sums = (double *)take((size_t)rows * p.chunks * 8);
@@ -869,19 +1035,20 @@ Plan plan_of(int64_t rows, int V, uint8_t *ws) {
 
 template <int T> sim_status sample_t(hipStream_t st, const SampleArgs &a, uint8_t *ws) {
     const bool some_k = a.top_k || (a.all_k > 1 && a.all_k < a.V), some_p = a.top_p || a.all_p < 1.f;
-    const bool sorted = !a.top_k && some_k && a.all_k <= kMaxSorted;  // every row
+    // where one top-k is for all rows, what they need is known; else all of it may be
+    const bool small = !a.top_k && some_k && a.all_k <= kMaxSorted, sorted = small && by_eights(a.V, a.all_k);
     for (int64_t row0 = 0; row0 < a.B; row0 += kRows) {
         const int64_t rows = std::min<int64_t>(kRows, a.B - row0);
         Plan p = plan_of(rows, a.V, ws);
         p.row0 = row0;
         const uint32_t grid = (uint32_t)(rows * p.slices);
-        sample_tops<T><<<grid, kThreads, 0, st>>>(a, p);
-        if (some_k || some_p) {
+        sample_tops<T><<<grid, kThreads, 0, st>>>(a, p, some_k);
+        if ((some_k || some_p) && !sorted) {
             sample_bins<T><<<grid, kThreads, 0, st>>>(a, p);
             sample_border<T><<<grid, kThreads, 0, st>>>(a, p);
-            sample_sorted<T><<<(uint32_t)rows, kAll, 0, st>>>(a, p);
         }
-        if (!sorted) sample_pick<T><<<grid, kThreads, 0, st>>>(a, p);
+        if (some_k || some_p) sample_sorted<T><<<(uint32_t)rows, kAll, 0, st>>>(a, p);
+        if (!small) sample_pick<T><<<grid, kThreads, 0, st>>>(a, p);
     }
     return SIM_OPS_LAUNCH_OK();
 }
