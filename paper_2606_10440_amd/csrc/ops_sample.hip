@@ -51,10 +51,45 @@ template <int T> __device__ inline float value_of(uint32_t key) {
 template <int T> constexpr uint32_t kInfinite = T == SIM_TYPE_F32 ? 0xff800000u : T == SIM_TYPE_BF16 ? 0xff80u : 0xfc00u;  // key of +infinity
 template <int T> constexpr int kKeyBits = T == SIM_TYPE_F32 ? 32 : 16;
 
-__device__ inline double wave_sum(double v) {
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
+// Sums over the lanes up to each, of 64-bit whole numbers or values, by moves
+// between registers (an exchange through LDS takes some 100 cycles, and there
+// are six, one after another).
+template <int CTRL, int ROWS, typename V> __device__ inline V add_from(V v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+    return v + __builtin_bit_cast(V, lo | (uint64_t)hi << 32);
 }
+template <typename V> __device__ inline V row_scan(V v) {  // of 16 lanes
+    v = add_from<0x111, 0xf>(v);                           // from the lane before
+    v = add_from<0x112, 0xf>(v);                           // two before
+    v = add_from<0x114, 0xf>(v);
+    return add_from<0x118, 0xf>(v);
+}
+template <typename V> __device__ inline V wave_scan(V v) {
+    v = row_scan(v);
+    v = add_from<0x142, 0xa>(v);     // lane 15's and 47's to the rows after
+    return add_from<0x143, 0xc>(v);  // lane 31's to the upper half
+}
+template <typename V> __device__ inline V lane_of(V v, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)b, lane) |
+                                     (uint64_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32);
+}
+// Sums over the workgroup's threads before each, and over all, from own values.
+template <int NT, typename V> __device__ inline V block_scan(V own, V *wave_sums, V &all) {
+    static_assert(NT / 64 <= 16, "a lane of a row for each wave");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const V sum = wave_scan(own);
+    __syncthreads();
+    if (lane == 63) wave_sums[wave] = sum;
+    __syncthreads();
+    const V waves = row_scan((lane & 15) < NT / 64 ? wave_sums[lane & 15] : V(0));
+    all = lane_of(waves, 15);
+    const V before = __shfl_up(sum, 1);
+    return (lane ? before : V(0)) + (wave ? lane_of(waves, wave - 1) : V(0));
+}
+__device__ inline double wave_sum(double v) { return lane_of(wave_scan(v), 63); }
 
 struct Shared {
     uint64_t bin[kBins];
@@ -80,19 +115,13 @@ template <int NT, typename Bin> __device__ inline int crossing(Bin &&bin, uint64
     constexpr int kEach = kBins / NT;
     __shared__ int s_at;
     __shared__ uint64_t s_before;
+    typedef unsigned long long u64;
     uint64_t v[kEach], own = 0;
 #pragma unroll
     for (int i = 0; i < kEach; i++) own += v[i] = bin(threadIdx.x * kEach + i);
-    uint64_t sum = own;
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)sum, d);
-        if ((int)(threadIdx.x & 63) >= d) sum += o;
-    }
-    if ((threadIdx.x & 63) == 63) wave_sums[threadIdx.x >> 6] = sum;
     if (threadIdx.x == 0) s_at = -1;
-    __syncthreads();
-    uint64_t run = sum - own;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); w++) run += wave_sums[w];
+    u64 all;
+    uint64_t run = block_scan<NT>((u64)own, (u64 *)wave_sums, all);
 #pragma unroll
     for (int i = 0; i < kEach; i++) {
         if (run < target && run + v[i] >= target) s_at = threadIdx.x * kEach + i, s_before = run;
@@ -591,7 +620,14 @@ __device__ inline void sort(uint64_t *v, int n) {
     if (n <= 128) {
         const uint64_t own = (int)threadIdx.x < n ? v[threadIdx.x] : 0;
         int place = 0;
-        for (int i = 0; i < n; i++) place += v[i] > own;
+        // (a wave that has none of them would read them all the same)
+        for (int i = 0; i < n && (int)(threadIdx.x & ~63) < n; i += 8) {
+            uint64_t o[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) o[j] = v[min(i + j, n - 1)];
+#pragma unroll
+            for (int j = 0; j < 8; j++) place += i + j < n && o[j] > own;
+        }
         __syncthreads();
         if ((int)threadIdx.x < n) v[place] = own;
         __syncthreads();
@@ -607,23 +643,10 @@ __device__ inline void sort(uint64_t *v, int n) {
 // Running sums over n values, a run of them to each thread: before(i) of each is
 // passed to f(i, before, value); returns the sum of all.
 template <int NT, typename Value, typename F> __device__ inline double scan(int n, double *wave_d, Value &&value, F &&f) {
-    const int each = (n + NT - 1) / NT, i0 = threadIdx.x * each, i1 = min(n, i0 + each), lane = threadIdx.x & 63;
+    const int each = (n + NT - 1) / NT, i0 = threadIdx.x * each, i1 = min(n, i0 + each);
     double own = 0.;
     for (int i = i0; i < i1; i++) own += value(i);
-    double sum = own;
-    for (int d = 1; d < 64; d <<= 1) {
-        const double o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
-    __syncthreads();
-    if (lane == 63) wave_d[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    double run = __shfl_up(sum, 1), all = 0.;
-    if (lane == 0) run = 0.;
-    for (int w = 0; w < NT / 64; w++) {
-        if (w < (int)(threadIdx.x >> 6)) run += wave_d[w];
-        all += wave_d[w];
-    }
+    double all, run = block_scan<NT>(own, wave_d, all);
     for (int i = i0; i < i1; i++) {
         const double v = value(i);
         f(i, run, v);
@@ -700,12 +723,8 @@ template <int T> __device__ inline int pick_few(const Task<T> &t, Sorting &s, in
         index[e] = ~(uint32_t)v;
         w[e] = i < k ? t.row.weight((uint32_t)(v >> 32)) : 0.;
     }
-    double run[2] = {w[0], w[1]};
-    for (int d = 1; d < 64; d <<= 1) {
-        const double a = __shfl_up(run[0], d), b = __shfl_up(run[1], d);
-        if (lane >= d) run[0] += a, run[1] += b;
-    }
-    const double half = __shfl(run[0], 63), most = (half + __shfl(run[1], 63)) * (double)t.top_p;
+    const double run[2] = {wave_scan(w[0]), wave_scan(w[1])};
+    const double half = lane_of(run[0], 63), most = (half + lane_of(run[1], 63)) * (double)t.top_p;
     const double lower[2] = {__shfl_up(run[0], 1), __shfl_up(run[1], 1)};
     int kept = 0;
 #pragma unroll
@@ -794,6 +813,10 @@ template <int T> __device__ inline int list_by_eights(const Task<T> &t, const Pl
     constexpr int kAt = 8;  // loads under way
     const int n = p.chunks * (kChunk / 8), before_row = (int)((uintptr_t)t.row.z / sizeof(El) % 8);
     const El *const eights = (const El *)p.eights + r * n;
+    // Of few logits the border is that of k threads' highest, one of each, which
+    // are as many logits (one row of 131072, k = 50: @THREADS@): half as many as
+    // threads leave 1024 ln 2 of them.
+    const bool by_threads = t.top_k <= kAll / 2 && n >= kAll;
     const auto each = [&](auto &&f) {
         for (int g0 = threadIdx.x; g0 < n; g0 += kAt * kAll) {
             float m[kAt];
@@ -807,7 +830,13 @@ template <int T> __device__ inline int list_by_eights(const Task<T> &t, const Pl
     for (int i = threadIdx.x; i < kBins; i += kAll) e.bin[i] = 0;
     if (threadIdx.x == 0) *s_n = s_eights = 0;
     __syncthreads();
-    each([&](int, int bin) { atomicAdd(&e.bin[bin], 1u); });
+    if (by_threads) {
+        int nearest = kBins;
+        each([&](int, int bin) { nearest = min(nearest, bin); });
+        if (nearest < kBins) atomicAdd(&e.bin[nearest], 1u);
+    } else {
+        each([&](int, int bin) { atomicAdd(&e.bin[bin], 1u); });
+    }
     __syncthreads();
     uint64_t above;
     int border = crossing<kAll>([&](int i) { return (uint64_t)e.bin[i]; }, (uint64_t)t.top_k, wave64, above);
