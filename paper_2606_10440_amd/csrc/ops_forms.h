@@ -52,6 +52,8 @@ constexpr int kFewExperts = 256;
 constexpr int kFewInputs = 24576;  // bytes of inputs that a workgroup of the first kernel keeps in LDS
 constexpr uint32_t kSlots = 512;   // workgroups of the forms for more tokens that run at once: two on each of 256 compute units
 
+constexpr int kShortList = 10;     // tokens: up to this average, one column tile
+
 enum LayerForm { kFew, kGroup1, kGroup2, kGroup4 };  // with so many column tiles of sixteen tokens
 
 inline bool few(int64_t T, int E, int64_t D, int64_t F) { return T <= kFewTokens && E <= kFewExperts && D >= 8 && F >= 8; }
@@ -74,7 +76,7 @@ inline LayerForm layer_form(int64_t T, int E, int k, int64_t D, int64_t F, bool 
     // 3520 x 545 fp16: 86 us, 62 with four)
     const int64_t mean = T * k / E, tiles = std::min<int64_t>(E, T * k) * ((F + 31) / 32);
     const bool odd = (D | F) & 1;
-    if (mean <= 10 || D < 8 || F < 8 || (tiles * ((mean + 31) / 32) <= kSlots / 8 && !odd)) return kGroup1;
+    if (mean <= kShortList || D < 8 || F < 8 || (tiles * ((mean + 31) / 32) <= kSlots / 8 && !odd)) return kGroup1;
     if (!mx4 && mean > 24 && (tiles > kSlots / 2 || odd)) return kGroup4;
     return kGroup2;
 }

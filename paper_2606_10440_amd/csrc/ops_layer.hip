@@ -651,16 +651,15 @@ __device__ inline int nth_expert(const int32_t *__restrict__ offsets, int E, int
 }
 
 // 16 RP hidden units of one expert.
+template <int WT, int RP, int CT> constexpr int kUpLds = kWaves * std::max<int>(Acts<WT, CT, (CT > 1)>::kBytes, 2 * RP * CT * 64 * sizeof(f32x4));
 template <int T, int WT, int RP, int CT, int U, int EDGE>
-__global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
-                                                           const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
-                                                           int E, int k, const int32_t *__restrict__ offsets,
-                                                           const int32_t *__restrict__ order,
-                                                           const float *__restrict__ weights, uint32_t tiles,
-                                                           __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo, int h_pitch) {
+__device__ __forceinline__ void up_tiles(uint8_t *lds, const uint16_t *__restrict__ x, int64_t x_stride, int D,
+                                         const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F, int E, int k,
+                                         const int32_t *__restrict__ offsets, const int32_t *__restrict__ order,
+                                         const float *__restrict__ weights, uint32_t tiles, __bf16 *__restrict__ h_hi,
+                                         __bf16 *__restrict__ h_lo, int h_pitch) {
     constexpr int kPart = 2 * RP * CT * 64;  // sums of a wave
     typedef Acts<WT, CT, (CT > 1)> Ac;
-    __shared__ __align__(16) uint8_t lds[kWaves * std::max<int>(Ac::kBytes, kPart * sizeof(f32x4))];
     f32x4 *const part = (f32x4 *)lds;  // once all waves have read what they staged
     typedef Weights<WT, EDGE> Wt;
     typedef Inputs<T, WT, EDGE> In;
@@ -776,17 +775,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__res
     }
 }
 
+// (4-bit weights: the registers do not suffice for staging)
+template <int WT, int CT> using DownActs = Acts<WT, CT, (CT > 1 && WT != SIM_TYPE_MX4)>;
+template <int WT, int R, int CT> constexpr int kDownLds = kWaves * std::max<int>(2 * DownActs<WT, CT>::kBytes, R * CT * 64 * sizeof(f32x4));
 template <int WT, int R, int CT, int U, int EDGE>
-__global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
-                                                          int h_pitch, int F, const void *__restrict__ w2,
-                                                          const uint8_t *__restrict__ s2, int D, int E,
-                                                          const int32_t *__restrict__ offsets,
-                                                          const int32_t *__restrict__ order, uint32_t tiles,
-                                                          float *__restrict__ out) {
+__device__ __forceinline__ void down_tiles(uint8_t *lds, const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
+                                           int h_pitch, int F, const void *__restrict__ w2, const uint8_t *__restrict__ s2,
+                                           int D, int E, const int32_t *__restrict__ offsets,
+                                           const int32_t *__restrict__ order, uint32_t tiles, float *__restrict__ out) {
     constexpr int kPart = R * CT * 64;  // sums of a wave
-    // (4-bit weights: the registers do not suffice)
-    typedef Acts<WT, CT, (CT > 1 && WT != SIM_TYPE_MX4)> Ac;
-    __shared__ __align__(16) uint8_t lds[kWaves * std::max<int>(2 * Ac::kBytes, kPart * sizeof(f32x4))];
+    typedef DownActs<WT, CT> Ac;
     f32x4 *const part = (f32x4 *)lds;  // once all waves have read what they staged
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     uint8_t *const mine = lds + wave * 2 * Ac::kBytes, *const mine_lo = mine + Ac::kBytes;
@@ -886,6 +884,46 @@ __global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__res
     }
 }
 
+// Kernels of CT column tiles.  The lists of given choices are known to the GPU
+// alone: there (EITHER) a workgroup takes one column tile where the average list
+// has at most ten tokens, the rule for choices that the layer makes (200 tokens,
+// k = 8, 32 of 256 4-bit experts of 4096 x 1536: up 58 and 63 us with one and
+// two, down 38 and 72).
+template <int WT, int CT> constexpr int kUpRows = CT == 1 && WT != SIM_TYPE_MX4 ? 1 : 2;  // tiles that share the activations' loads
+template <int WT, int CT> constexpr int kUpAhead = WT == SIM_TYPE_MX4 ? 2 : 4 / CT;       // and how far ahead all are loaded
+constexpr int kDownRows = 4;
+template <int CT> constexpr int kDownAhead = CT == 4 ? 1 : 2;
+__device__ inline bool short_lists(const int32_t *__restrict__ offsets, int E) { return offsets[E] / E <= kShortList; }
+
+template <int T, int WT, int CT, int EDGE, bool EITHER>
+__global__ __launch_bounds__(64 * kWaves, 2) void group_up(const uint16_t *__restrict__ x, int64_t x_stride, int D,
+                                                           const void *__restrict__ w13, const uint8_t *__restrict__ s13, int F,
+                                                           int E, int k, const int32_t *__restrict__ offsets,
+                                                           const int32_t *__restrict__ order,
+                                                           const float *__restrict__ weights, uint32_t tiles,
+                                                           __bf16 *__restrict__ h_hi, __bf16 *__restrict__ h_lo, int h_pitch) {
+    __shared__ __align__(16) uint8_t lds[std::max(kUpLds<WT, kUpRows<WT, CT>, CT>, EITHER ? kUpLds<WT, kUpRows<WT, CT>, 1> : 0)];
+    if (EITHER && short_lists(offsets, E))
+        up_tiles<T, WT, kUpRows<WT, CT>, 1, 2, EDGE>(lds, x, x_stride, D, w13, s13, F, E, k, offsets, order, weights, tiles, h_hi,
+                                                    h_lo, h_pitch);
+    else
+        up_tiles<T, WT, kUpRows<WT, CT>, CT, kUpAhead<WT, CT>, EDGE>(lds, x, x_stride, D, w13, s13, F, E, k, offsets, order, weights,
+                                                                    tiles, h_hi, h_lo, h_pitch);
+}
+template <int WT, int CT, int EDGE, bool EITHER>
+__global__ __launch_bounds__(64 * kWaves, 2) void group_down(const __bf16 *__restrict__ h_hi, const __bf16 *__restrict__ h_lo,
+                                                          int h_pitch, int F, const void *__restrict__ w2,
+                                                          const uint8_t *__restrict__ s2, int D, int E,
+                                                          const int32_t *__restrict__ offsets,
+                                                          const int32_t *__restrict__ order, uint32_t tiles,
+                                                          float *__restrict__ out) {
+    __shared__ __align__(16) uint8_t lds[std::max(kDownLds<WT, kDownRows, CT>, EITHER ? kDownLds<WT, kDownRows, 1> : 0)];
+    if (EITHER && short_lists(offsets, E))
+        down_tiles<WT, kDownRows, 1, kDownAhead<1>, EDGE>(lds, h_hi, h_lo, h_pitch, F, w2, s2, D, E, offsets, order, tiles, out);
+    else
+        down_tiles<WT, kDownRows, CT, kDownAhead<CT>, EDGE>(lds, h_hi, h_lo, h_pitch, F, w2, s2, D, E, offsets, order, tiles, out);
+}
+
 // A token's result: its choices in order.
 template <int T>
 __global__ __launch_bounds__(256) void layer_join(const float *__restrict__ part, const int32_t *__restrict__ experts, int k,
@@ -982,10 +1020,10 @@ template <int T, int WT, int CT> sim_status group_t(hipStream_t st, const LayerA
     const sim_status s = launch_route(st, r, experts, weights, offsets, order, ws + at.route);
     if (s != SIM_OK) return s;
     constexpr bool M = WT == SIM_TYPE_MX4;
-    // rows that share the activations' loads, and how far ahead all are loaded
-    constexpr int RP = CT == 1 && !M ? 1 : 2, UU = M ? 2 : 4 / CT, R = 4, UD = CT == 4 ? 1 : 2;
     const uint32_t lists = (uint32_t)std::min<int64_t>(r.E, r.T * r.k);
-    const uint32_t tf = (uint32_t)((a.F + 16 * RP - 1) / (16 * RP)), td = (uint32_t)((a.D + 16 * R - 1) / (16 * R)), tj = (uint32_t)((a.D + 255) / 256);
+    constexpr int kRows = 16 * kUpRows<WT, CT>;
+    const uint32_t tf = (uint32_t)((a.F + kRows - 1) / kRows), td = (uint32_t)((a.D + 16 * kDownRows - 1) / (16 * kDownRows));
+    const uint32_t tj = (uint32_t)((a.D + 255) / 256);
     // lists are shared among workgroups where these would leave compute units
     // idle, which costs another read of the weights from the caches (120
     // tokens, k = 4 of 4 4-bit experts of 2048 x 768: 68 -> 41 us; 1000, k = 2
@@ -994,17 +1032,26 @@ template <int T, int WT, int CT> sim_status group_t(hipStream_t st, const LayerA
         const uint32_t all = (uint32_t)((r.T + 16 * CT - 1) / (16 * CT));
         return dim3(lists * tiles, std::max(1u, std::min(all, kSlots / (lists * tiles))));
     };
-    by_edge<WT, CT>(a.D, [&](auto edge) {
-        group_up<T, WT, RP, CT, UU, decltype(edge)::value><<<grid(tf), 64 * kWaves, 0, st>>>(
-            (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi, lo,
-            at.pitch);
-    });
-    const auto down = [&](auto edge) {
-        group_down<WT, R, CT, UD, decltype(edge)::value><<<grid(td), 64 * kWaves, 0, st>>>(
-            hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, r.E, offsets, order, td, part);
+    const auto run = [&](auto either) {
+        constexpr bool E = decltype(either)::value;
+        by_edge<WT, CT>(a.D, [&](auto edge) {
+            group_up<T, WT, CT, decltype(edge)::value, E><<<grid(tf), 64 * kWaves, 0, st>>>(
+                (const uint16_t *)a.x, a.x_stride, (int)a.D, a.w13, a.s13, (int)a.F, r.E, r.k, offsets, order, weights, tf, hi,
+                lo, at.pitch);
+        });
+        const auto down = [&](auto edge) {
+            group_down<WT, CT, decltype(edge)::value, E><<<grid(td), 64 * kWaves, 0, st>>>(
+                hi, lo, at.pitch, (int)a.F, a.w2, a.s2, (int)a.D, r.E, offsets, order, td, part);
+        };
+        if constexpr (M) down(std::integral_constant<int, kWhole>());  // rows and hidden values are padded
+        else by_edge<WT, CT>(a.F, down);
     };
-    if constexpr (M) down(std::integral_constant<int, kWhole>());  // rows and hidden values are padded
-    else by_edge<WT, CT>(a.F, down);
+    if constexpr (CT > 1) {
+        if (r.given) run(std::true_type());
+        else run(std::false_type());
+    } else {
+        run(std::false_type());
+    }
     layer_join<T><<<(uint32_t)(r.T * tj), 256, 0, st>>>(part, experts, r.k, a.D, (typename Elem<T>::type *)a.y, a.y_stride, tj);
     return SIM_OPS_LAUNCH_OK();
 }
