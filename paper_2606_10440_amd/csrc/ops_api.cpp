@@ -380,7 +380,7 @@ bool attention_fits(int64_t B, int32_t q_heads, int32_t kv_heads, int32_t D, int
         D > SIM_CACHE_MAX_D || D % 8 || table_pages < 0 || page_size < 1 || window < 0 ||
         (int64_t)table_pages * page_size > kMaxKeys)
         return false;
-    const int64_t tiles = attend_tiles(q_heads / kv_heads, D), units = attend_units(kv_heads * tiles);
+    const int64_t tiles = attend_tiles(q_heads / kv_heads, D), units = attend_units(kv_heads * tiles, attend_resident(D, attend_heads(q_heads / kv_heads, D)));
     return (attend_max_units(B, units, (int64_t)table_pages * page_size, window) * kv_heads + 8) * tiles < kMaxGroups / 256 &&
            B * q_heads < kMaxGroups / 256;  // (a launch has 2^32 threads at most)
 }
@@ -408,7 +408,8 @@ size_t sim_cache_attention_workspace(int64_t B, int32_t q_heads, int32_t kv_head
     if (!attention_fits(B, q_heads, kv_heads, D, table_pages, page_size, window)) return 0;
     const int64_t capacity = (int64_t)table_pages * page_size;
     if (!attend_splits(capacity, window)) return 0;
-    const int64_t units = attend_units((int64_t)kv_heads * attend_tiles(q_heads / kv_heads, D));
+    const int group = q_heads / kv_heads;
+    const int64_t units = attend_units((int64_t)kv_heads * attend_tiles(group, D), attend_resident(D, attend_heads(group, D)));
     return (size_t)((attend_max_units(B, units, capacity, window) * q_heads * (D + 2) * 4 + 15) / 16 * 16);
 }
 
@@ -441,8 +442,9 @@ sim_status sim_cache_attention(void *stream, int32_t type, const void *q, int64_
     a.table = table, a.table_stride = table_stride, a.capacity = (int64_t)table_pages * page_size, a.lengths = lengths;
     a.scale_log2 = (float)(scale * 1.4426950408889634), a.window = window;
     a.out = out, a.out_stride = out_stride, a.lse = lse, a.part = (float *)workspace;
-    a.tiles = attend_tiles(q_heads / kv_heads, D), a.units = attend_units((int64_t)kv_heads * a.tiles);
+    a.tiles = attend_tiles(q_heads / kv_heads, D), a.units = attend_units((int64_t)kv_heads * a.tiles, attend_resident(D, attend_heads(q_heads / kv_heads, D)));
     a.max_units = attend_max_units(B, a.units, a.capacity, window);
+    a.splits = attend_splits(a.capacity, window);
     a.q_aligned = aligned_to(q, 16) && (B == 1 || q_stride % 8 == 0) && (q_heads == 1 || q_head_stride % 8 == 0);
     a.out_aligned = aligned_to(out, 16) && (B == 1 || out_stride % 8 == 0);
     return done(launch_attention((hipStream_t)stream, a), __func__);

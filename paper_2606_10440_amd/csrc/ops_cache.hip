@@ -111,7 +111,7 @@ __device__ inline int scan_units(const AttendArgs &a, int64_t b0, int unit) {
 // fp16 weights are 2^15 times as large as the highest's 1, so that small ones,
 // of which a long sequence may have many, are not lost.
 template <int T, int DP, int HT, bool PAGE16>
-__global__ __launch_bounds__(64 * kWaves, DP * HT > 128 ? 2 : 3) void attend(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void attend(AttendArgs a) {
     constexpr int CH = DP / 32;                // 32 d of keys
     constexpr int NV = DP == 64 ? 4 : 8;       // consecutive d of values in a lane
     constexpr int NH = DP / (16 * NV);         // times that
@@ -126,10 +126,10 @@ __global__ __launch_bounds__(64 * kWaves, DP * HT > 128 ? 2 : 3) void attend(Att
     const int kvh = at % a.kv_heads, u = at / a.kv_heads;
 
     // the unit's sequence
-    int64_t b = -1;
-    int before = 0, n_units = 0;
-    const int unit = __builtin_amdgcn_readfirstlane(steps_of_unit(a));
-    for (int64_t b0 = 0, base = 0; b0 < a.B; b0 += 64) {
+    int64_t b = a.splits || u >= a.B ? -1 : u;
+    int before = u, n_units = 1, unit = kAttendWhole;
+    if (a.splits) unit = __builtin_amdgcn_readfirstlane(steps_of_unit(a));
+    for (int64_t b0 = 0, base = 0; a.splits && b0 < a.B; b0 += 64) {
         const int n = scan_units(a, b0, unit);
         const uint64_t past = __ballot((int64_t)u < base + n);
         if (past) {
@@ -502,7 +502,7 @@ template <int T> sim_status attention_t(hipStream_t st, const AttendArgs &a) {
     if (a.D <= 64) heads == 16 ? attend_t<T, 64, 1>(st, a) : attend_t<T, 64, 2>(st, a);
     else if (a.D <= 128) heads == 16 ? attend_t<T, 128, 1>(st, a) : attend_t<T, 128, 2>(st, a);
     else attend_t<T, 256, 1>(st, a);
-    if (attend_splits(a.capacity, a.window)) attend_join<T><<<(uint32_t)(a.B * a.q_heads), 256, 0, st>>>(a);
+    if (a.splits) attend_join<T><<<(uint32_t)(a.B * a.q_heads), 256, 0, st>>>(a);
     return SIM_OPS_LAUNCH_OK();
 }
 

@@ -172,7 +172,7 @@ struct AttendArgs {
     float *lse, *part;
     int64_t units, max_units;
     int tiles;
-    bool q_aligned, out_aligned;
+    bool q_aligned, out_aligned, splits;
 };
 sim_status launch_attention(hipStream_t st, const AttendArgs &a);
 struct SampleArgs {

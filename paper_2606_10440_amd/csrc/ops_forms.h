@@ -85,8 +85,8 @@ inline LayerForm layer_form(int64_t T, int E, int k, int64_t D, int64_t F, bool 
 
 constexpr int kAttendKeys = 32;       // keys of one step of a wave
 constexpr int kAttendMinUnit = 4;     // steps of a unit: one for each wave
+constexpr int kAttendWhole = 16;      // sequences of so many are not cut: joining costs more than three steps of a wave
 constexpr int kAttendGoodUnit = 16;
-constexpr int64_t kAttendSlots = 768; // workgroups that run at once: three on each of 256 compute units
 constexpr int kAttendRounds = 4;
 
 // Heads of one workgroup, of those that share a kv head: each sixteen cost D /
@@ -94,8 +94,16 @@ constexpr int kAttendRounds = 4;
 constexpr int attend_heads(int group, int D) { return group > 16 && D <= 128 ? 32 : 16; }
 constexpr int attend_tiles(int group, int D) { return (group + attend_heads(group, D) - 1) / attend_heads(group, D); }
 
+// Workgroups on a compute unit, by the registers of a wave: keys and values of
+// a step and the results take 192 at D = 128, more of which in flight gain less
+// than values that the registers do not hold cost (64 sequences of up to 8192, D
+// = 128: 217 us with two workgroups, 255 with three).
+constexpr int attend_resident(int D, int heads) { return D > 128 ? 1 : D <= 64 && heads == 16 ? 3 : 2; }
+
 // Units that fill the GPU once, with so many workgroups to a unit.
-constexpr int64_t attend_units(int64_t workgroups) { return workgroups >= kAttendSlots ? 1 : kAttendSlots / workgroups; }
+constexpr int64_t attend_units(int64_t workgroups, int resident) {
+    return workgroups >= 256 * resident ? 1 : 256 * resident / workgroups;
+}
 
 // Steps of a unit where all sequences have total: what fills the GPU once, if
 // that is little; else small enough that the last ones to run are a small part
@@ -110,12 +118,12 @@ constexpr int64_t attend_steps(int64_t capacity, int32_t window) {
     const int64_t all = (capacity + kAttendKeys - 1) / kAttendKeys, in = (int64_t)window / kAttendKeys + 2;
     return window > 0 && in < all ? in : all;
 }
-constexpr bool attend_splits(int64_t capacity, int32_t window) { return attend_steps(capacity, window) > kAttendMinUnit; }
+constexpr bool attend_splits(int64_t capacity, int32_t window) { return attend_steps(capacity, window) > kAttendWhole; }
 // Units that B sequences have at most: one each and what the cuts add, and as
 // many as the smallest units would be.
 constexpr int64_t attend_max_units(int64_t B, int64_t units, int64_t capacity, int32_t window) {
     const int64_t each = (attend_steps(capacity, window) + kAttendMinUnit - 1) / kAttendMinUnit, cut = B + units * kAttendRounds;
-    return each <= 1 ? B : each < (cut + B - 1) / B ? B * each : cut;
+    return !attend_splits(capacity, window) ? B : each < (cut + B - 1) / B ? B * each : cut;
 }
 
 }  // namespace simops

@@ -79,7 +79,7 @@ int main() {
     for (int i = 0; i < 20000; i++) {
         const int64_t B = 1 + upto(i % 3 ? 8 : 300), cap = 1 + upto((int64_t)1 << (4 + upto(16)));
         const int32_t window = i % 4 ? 0 : 1 + (int32_t)upto(4000);
-        const int64_t units = attend_units(1 + upto(i % 5 ? 16 : 2000)), most = attend_max_units(B, units, cap, window);
+        const int64_t units = attend_units(1 + upto(i % 5 ? 16 : 2000), 1 + (int)upto(3)), most = attend_max_units(B, units, cap, window);
         int64_t total = 0, n = 0;
         std::vector<int64_t> steps(B);
         for (auto &s : steps) {
@@ -89,9 +89,9 @@ int main() {
             total += s;
         }
         const int unit = attend_unit(total, units);
-        for (int64_t s : steps) {
+        for (int64_t s : steps) if (!attend_splits(cap, window)) n++; else {
             n += std::max<int64_t>(1, (s + unit - 1) / unit);
-            if (s > unit && !attend_splits(cap, window)) return 2;
+            if (s > kAttendWhole && !attend_splits(cap, window)) return 2;
         }
         if (n > most) { printf("%ld %ld %d %ld\\n", (long)B, (long)cap, window, (long)units); return 3; }
     }
