@@ -88,6 +88,7 @@ constexpr int kAttendMinUnit = 4;     // steps of a unit: one for each wave
 constexpr int kAttendWhole = 16;      // sequences of so many are not cut: joining costs more than three steps of a wave
 constexpr int kAttendGoodUnit = 16;
 constexpr int kAttendRounds = 4;
+constexpr int kAttendMostSteps = 1 << 26;  // a sequence has at most 2^30 tokens
 
 // Heads of one workgroup, of those that share a kv head: each sixteen cost D /
 // 2 registers for their results.
@@ -110,7 +111,8 @@ constexpr int64_t attend_units(int64_t workgroups, int resident) {
 // of the whole.
 constexpr int attend_unit(int64_t total, int64_t units) {
     const int64_t once = (total + units - 1) / units, part = (total + units * kAttendRounds - 1) / (units * kAttendRounds);
-    return (int)(once <= kAttendGoodUnit ? (once > kAttendMinUnit ? once : kAttendMinUnit) : part > kAttendGoodUnit ? part : kAttendGoodUnit);
+    const int64_t unit = once <= kAttendGoodUnit ? (once > kAttendMinUnit ? once : kAttendMinUnit) : part > kAttendGoodUnit ? part : kAttendGoodUnit;
+    return unit < kAttendMostSteps ? (int)unit : kAttendMostSteps;  // no sequence has more
 }
 
 // Steps that a sequence has at most.

@@ -475,7 +475,7 @@ struct Two {
         a = max(a, a2);
     }
     // of a group, as a key; 0 where nothing of it can be chosen
-    __device__ uint32_t value(int best) const { return best == 1 || !b ? a : order_key(key_value(a) + key_value(b)); }
+    __device__ uint32_t value(int best) const { return best == 1 || !b ? a : max(1u, order_key(key_value(a) + key_value(b))); }
 };
 
 // Which groups a token keeps, a bit for each, from its experts' keys.  Where a

@@ -506,7 +506,7 @@ PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, w
         need(o.n == q.n && o.heads == q.heads && o.D == q.D && o.type == q.type && o.dev == q.dev, "out must be as q");
         need((o.heads == 1 || o.head_stride == o.D) && (o.n <= 1 || o.stride >= o.heads * o.D), "out's heads must be contiguous and must not overlap");
         need(!out.requires_grad() || !c10::GradMode::is_enabled(), "out must not require a gradient: the result has none");
-        need(!out.is_alias_of(THPVariable_Unpack(a[0])), "out must not be q");
+        need(!out.is_alias_of(THPVariable_Unpack(a[0])), "out must not share q's memory");
     } else {
         out = fresh({q.n, q.heads, q.D}, q.type, q.dev);
     }

@@ -74,6 +74,8 @@ def test_units_fit_the_workspace(lib, tmp_path):
 #include <random>
 using namespace simops;
 int main() {
+    // however many steps there are together, a unit is a number of them, and one is enough for any sequence
+    if (attend_unit((int64_t)1 << 50, 1) != kAttendMostSteps || attend_steps((int64_t)1 << 30, 0) > kAttendMostSteps) return 4;
     std::mt19937_64 rng(1);
     const auto upto = [&](int64_t n) { return (int64_t)(rng() % (uint64_t)n); };
     for (int i = 0; i < 20000; i++) {
@@ -89,8 +91,8 @@ int main() {
             total += s;
         }
         const int unit = attend_unit(total, units);
-        for (int64_t s : steps) if (!attend_splits(cap, window)) n++; else {
-            n += std::max<int64_t>(1, (s + unit - 1) / unit);
+        for (int64_t s : steps) {
+            n += attend_splits(cap, window) ? std::max<int64_t>(1, (s + unit - 1) / unit) : 1;
             if (s > kAttendWhole && !attend_splits(cap, window)) return 2;
         }
         if (n > most) { printf("%ld %ld %d %ld\\n", (long)B, (long)cap, window, (long)units); return 3; }
