@@ -810,6 +810,170 @@ __global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__
     finish<CH>(lists, t, live, k, E, (int)min(a.T, (int64_t)CH), mine_e, mine, w, experts, weights, hist, offsets, order);
 }
 
+// The same for a decode step's few tokens, where one wave's chain of operations
+// is all of the time: a wave for a token, so that a lane has a quarter of the
+// experts, and scores in 64 bits at once (256 fp32 experts in 8 groups, k = 8:
+// one token 6.8 us, 15.7 by route_scored; 16 tokens 10.3 and 14.8).
+constexpr int kRouteFew = 16;
+
+__device__ inline uint32_t max64(uint32_t v) {
+    v = max16(v);
+    const auto row = [&](int r) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 16 * r); };
+    return max(max(row(0), row(1)), max(row(2), row(3)));
+}
+__device__ inline double sum64(double v) {
+    v = sum16(v);
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const auto row = [&](int r) {
+        return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)b, 16 * r) |
+                                              (uint64_t)__builtin_amdgcn_readlane((int)(b >> 32), 16 * r) << 32);
+    };
+    return (row(0) + row(1)) + (row(2) + row(3));
+}
+
+template <int T, int NV>
+__global__ __launch_bounds__(64 * kRouteFew) void route_few(RouteArgs a, int32_t *__restrict__ experts, float *__restrict__ weights,
+                                                           int32_t *__restrict__ offsets, int32_t *__restrict__ order) {
+    typedef typename Elem<T>::type El;
+    static_assert(64 * kRouteFew == kThreads, "a thread for each expert");
+    __shared__ Lists lists;
+    const int l = threadIdx.x & 63, t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), E = a.E, k = a.k, e0 = l * NV;
+    const bool live = t < a.T, grouped = a.groups > a.top_groups, sigmoid = a.score == SIM_SCORE_SIGMOID;
+    clear<kChunk>(lists);
+    __syncthreads();
+    int mine = -1;
+    if (live) {
+        const El *const z = (const El *)a.logits + t * a.stride;
+        const uint8_t *const mask = a.mask ? a.mask + t * a.mask_stride : nullptr;
+        El raw[NV];
+        uint8_t m[NV];
+        if (e0 + NV <= E) {
+            load_some<NV>(z + e0, raw);
+            if (mask) load_some<NV>(mask + e0, m);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                raw[i] = e0 + i < E ? z[e0 + i] : Elem<T>::put(-INFINITY);
+                m[i] = mask && e0 + i < E ? mask[e0 + i] : 0;
+            }
+        }
+        float x[NV];  // -infinity where nothing can be chosen
+        uint32_t key[NV], top = 0;
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+            x[i] = e0 + i < E && (!mask || m[i]) ? Elem<T>::get(raw[i]) : -INFINITY;
+            key[i] = order_key(x[i]);
+            top = max(top, key[i]);
+        }
+        const bool by_score = a.bias || (grouped && a.group_best == 2);
+        double high = 0., inv = 1.;
+        if (!sigmoid && (by_score || !a.renorm)) {
+            high = key_value(max64(top));
+            double sum = 0.;
+#pragma unroll
+            for (int i = 0; i < NV; i++) sum += x[i] == -INFINITY ? 0. : exp64(x[i] - high);
+            inv = 1. / sum64(sum);
+        }
+        if (by_score) {
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                const float s = (float)(sigmoid ? sigmoid64(x[i]) : exp64(x[i] - high) * inv);
+                key[i] = x[i] == -INFINITY ? 0 : order_key(a.bias ? s + a.bias[min(e0 + i, E - 1)] : s);
+            }
+        }
+        if (grouped) {
+            // a group's value in one lane each: its first where it is a whole
+            // number of lanes, a power of two up to 16, else lane g
+            const int size = E / a.groups, lanes = size / NV;
+            const bool whole = lanes * NV == size && (lanes & (lanes - 1)) == 0 && lanes <= 16;
+            uint32_t v = 0;
+            if (whole) {
+                Two two;
+#pragma unroll
+                for (int i = 0; i < NV; i++) two.add(key[i]);
+                if (lanes >= 2) two.merge<kDppXor1>();
+                if (lanes >= 4) two.merge<kDppXor2>();
+                if (lanes >= 8) two.merge<kDppHalfMirror>();
+                if (lanes >= 16) two.merge<kDppMirror>();
+                v = l % lanes ? 0 : two.value(a.group_best);
+            }
+            for (int g = whole ? a.groups : 0; g < a.groups; g++) {
+                Two two;
+#pragma unroll
+                for (int i = 0; i < NV; i++) two.add((uint32_t)(e0 + i - g * size) < (uint32_t)size ? key[i] : 0);
+                two.merge<kDppXor1>();
+                two.merge<kDppXor2>();
+                two.merge<kDppHalfMirror>();
+                two.merge<kDppMirror>();
+                Two all;
+#pragma unroll
+                for (int r = 0; r < 4; r++) {
+                    all.add((uint32_t)__builtin_amdgcn_readlane((int)two.a, 16 * r));
+                    all.add((uint32_t)__builtin_amdgcn_readlane((int)two.b, 16 * r));
+                }
+                if (l == g) v = all.value(a.group_best);
+            }
+            uint64_t keep = 0;
+            for (int j = 0; j < a.top_groups; j++) {
+                const uint32_t best = max64(v);
+                if (!best) break;
+                const int from = __ffsll((unsigned long long)__ballot(v == best)) - 1;
+                keep |= 1ull << (whole ? from / lanes : from);
+                v = l == from ? 0 : v;
+            }
+            int g = e0 / size, in = e0 - g * size;
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                // without a bias the logits have the scores' order, and a finer one
+                if (by_score && !a.bias && key[i]) key[i] = order_key(x[i]);
+                if (!((keep >> (g & 63)) & 1)) key[i] = 0;
+                if (++in == size) in = 0, g++;
+            }
+        }
+        for (int j = 0; j < k; j++) {
+            uint32_t best = 0;
+            int at = 0;  // the first of equal ones has the lowest index, in the lane and among the lanes
+#pragma unroll
+            for (int i = 0; i < NV; i++) {
+                at = key[i] > best ? i : at;
+                best = max(best, key[i]);
+            }
+            const uint32_t all = max64(best);
+            if (!all) break;
+            const int from = __ffsll((unsigned long long)__ballot(best == all)) - 1, e = from * NV + __builtin_amdgcn_readlane(at, from);
+            mine = l == j ? e : mine;
+#pragma unroll
+            for (int i = 0; i < NV; i++) key[i] = e0 + i == e ? 0 : key[i];
+        }
+        // the weights, as in route_scored
+        const double chosen = mine >= 0 ? (double)Elem<T>::get(z[mine]) : 0.;
+        if (a.renorm) {
+            high = key_value(max64(mine >= 0 ? order_key((float)chosen) : 0u));
+            if (sigmoid && high > 0.) high = 0.;
+        }
+        double w;
+        if (!sigmoid) w = exp64(chosen - high);
+        else if (a.renorm) w = exp64((chosen > 0. ? 0. : chosen) - high) * reciprocal(1. + exp64(-__builtin_fabs(chosen)));
+        else w = sigmoid64(chosen);
+        w = mine >= 0 ? w : 0.;
+        if (a.renorm) inv = 1. / sum64(w);
+        if (l < k) {
+            experts[t * k + l] = mine;
+            weights[t * k + l] = mine >= 0 ? (float)(w * inv * a.scale) : 0.f;
+            if (mine >= 0 && order) mark(lists.chose, mine, t);
+        }
+    }
+    if (!order) return;
+    __syncthreads();
+    int total;
+    lists.base[threadIdx.x] = block_scan(__popcll(lists.chose[threadIdx.x]), lists.wave_sum, total);
+    if ((int)threadIdx.x < E) offsets[threadIdx.x] = lists.base[threadIdx.x];
+    if (threadIdx.x == 0) offsets[E] = total;
+    __syncthreads();
+    if (mine >= 0) order[lists.base[mine] + before_in(lists.chose[mine], t)] = t * k + l;
+    for (int i = total + threadIdx.x; i < (int)a.T * k; i += kThreads) order[i] = -1;
+}
+
 // Gradient of sigmoid weights: at the chosen experts only.  As in route_grad,
 // lane l has the choices l and l + 16.
 template <int T, int NV>
@@ -912,6 +1076,17 @@ sim_status route_t(hipStream_t st, const RouteArgs &a, int32_t *experts, float *
             (const typename Elem<T>::type *)a.logits, a.T, a.E, a.stride, a.mask, a.mask_stride, a.k, a.renorm, experts,
             weights, hist, offsets, order);
     };
+    if (a.scored && a.T <= kRouteFew) {
+        const auto few = [&](auto nv) {
+            route_few<T, decltype(nv)::value><<<1, 64 * kRouteFew, 0, st>>>(a, experts, weights, offsets, order);
+        };
+        if (a.E <= 64) few(std::integral_constant<int, 1>());
+        else if (a.E <= 128) few(std::integral_constant<int, 2>());
+        else if (a.E <= 256) few(std::integral_constant<int, 4>());
+        else if (a.E <= 512) few(std::integral_constant<int, 8>());
+        else few(std::integral_constant<int, 16>());
+        return SIM_OPS_LAUNCH_OK();
+    }
     if (a.given) {
         if (rows > chunks) route_given<kPart><<<rows, 16 * kPart, 0, st>>>(a, experts, weights, hist, offsets, order);
         else route_given<kChunk><<<chunks, kThreads, 0, st>>>(a, experts, weights, hist, offsets, order);
