@@ -275,7 +275,8 @@ sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, in
  *   the token is the first kept i, in the order of the indices, up to and with
  *     which the kept weights' sum is above u times the sum of all of them.
  * Weights and sums are in 64 bits, so that only values that close to a border
- * depend on the order of summation.  A temperature that is not above 0 means
+ * depend on the order of summation; a weight below 2^-1022 is 0, and so is that
+ * of a logit more than 3.4e38 below the highest.  A temperature that is not above 0 means
  * the highest logit's first index; top_k below 1 or above V, a top_p of 1 or
  * more or NaN, and a min_p that is not above 0 keep all; a top_p of 0 or less
  * and a min_p above 1 keep the highest.  u below 0 or NaN counts as 0, above 1

@@ -1,7 +1,9 @@
 """Operators of an expert-parallel step on the GPU, next to the traffic that
 ``sim`` simulates: 4-bit microscaled tensors (what travels, and the products of
-linear layers), the router with the experts' token lists (who gets it), and
-the experts' layer for few tokens (what is computed there).
+linear layers), the router with the experts' token lists (who gets it), the
+experts' layer for few tokens (what is computed there), and what a decode step
+has around them: attention over a paged key-value cache, and the choice of the
+next token.
 
 Functions marshal torch tensors for the C ABI of ``include/simgpu_ops.h``
 (there the layouts, formulas and limits are stated), by way of
