@@ -18,6 +18,13 @@
 // A row whose border bin holds more than can be sorted (logits that are nearly
 // all the same, say) is searched by one workgroup alone, digit by digit of a
 // key that orders as the logits do.
+//
+// One row of 131072 fp32, top-k 50 and top-p 0.95: 18 us (tops 4, sorted 14, which
+// is one workgroup's chain of barriers and of 64-bit operations); all of its
+// logits kept 15.  192 rows of 100003 bf16, each with settings of its own: 103 us (tops 11,
+// bins 22, border 13, sorted 34, pick 25) for 38 MB, 7.4 us of memory: the 64-bit
+// weights of the rows without top-k, and the sorted lists, of 700 where top-k is
+// 500, take the rest.
 #include "ops_exp64.h"
 
 namespace simops {
@@ -49,6 +56,7 @@ template <int T> __device__ inline float value_of(uint32_t key) {
     else return Elem<T>::get(__builtin_bit_cast(typename Elem<T>::type, (uint16_t)(key & 0x8000 ? key & 0x7fff : ~key)));
 }
 template <int T> constexpr uint32_t kInfinite = T == SIM_TYPE_F32 ? 0xff800000u : T == SIM_TYPE_BF16 ? 0xff80u : 0xfc00u;  // key of +infinity
+template <int T> constexpr uint32_t kLowest = T == SIM_TYPE_F32 ? 0x800000u : T == SIM_TYPE_BF16 ? 0x80u : 0x400u;  // of the lowest finite value
 template <int T> constexpr int kKeyBits = T == SIM_TYPE_F32 ? 32 : 16;
 
 // Sums over the lanes up to each, of 64-bit whole numbers or values, by moves
@@ -429,7 +437,7 @@ template <int T> struct Exp {
     float high, far;    // beyond this below the highest, weights are below 2^-1022: 0
     __device__ Exp(const Row<T> &row, const double *table_) : table(table_), top(row.top), steps(row.per * (kTable * 1.4426950408889634)) {
         high = (float)top;
-        far = (float)min(708. / row.per, 3e38);
+        far = (float)min(708. / row.per, 3.4028234e38);
     }
     __device__ bool none(float z) const { return high - z > far; }
     // where not none(z)
@@ -908,7 +916,7 @@ template <int T> __global__ __launch_bounds__(kAll) void sample_sorted(SampleArg
     } else if (t.kind == kAlone || n > kList) {
         token = search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u);
     } else if (t.kind == kNumber && state.border < 0) {  // a top-k beyond the logits that there are: all of them
-        if (threadIdx.x == 0) state.lowest = 1, state.cut = (uint32_t)a.V, state.mode = kBordered;
+        if (threadIdx.x == 0) state.lowest = kLowest<T>, state.cut = (uint32_t)a.V, state.mode = kBordered;
     } else {
         const uint64_t *const list = p.list + r * kList;
         if (t.kind != kSorted)

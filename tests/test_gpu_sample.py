@@ -126,6 +126,20 @@ def test_masked_logits_and_rows_without_a_token(ops, kind):
     assert got[5] == got[7] == got[8] == -1 and got[6] == 1234
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("left", [1, 2100, 2999])
+def test_large_top_k_beyond_the_logits_that_are_left(ops, kind, left):
+    # more than are sorted, of 6001 logits of which fewer are above -infinity: all of these are kept, the lowest finite one too
+    z, v = rows(left, 4, 6001, kind)
+    g = np.random.default_rng(left)
+    for b in range(4):
+        v[b, g.permutation(6001)[left:]] = -np.inf
+    v[3, np.isfinite(v[3]).argmax()] = -np.float64(torch.finfo(TYPES[kind]).max)
+    z.copy_(torch.from_numpy(v).to(TYPES[kind]))
+    for n, how in enumerate([dict(top_k=3000), dict(top_k=3000, temperature=1e30), dict(top_k=3000, min_p=0.01), dict(top_k=3000, top_p=0.9)]):
+        check(ops, z, v, uniform(n, 4), **how)
+
+
 def test_random_numbers_at_and_past_the_ends(ops):
     V = 4000
     z, v = rows(11, 6, V, "fp32")
