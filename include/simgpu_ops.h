@@ -249,7 +249,7 @@ sim_status sim_cache_append(void *hip_stream, int32_t type, const void *k, int64
  * An infinity among the V makes the results that it enters infinite or NaN, and
  * no others.
  *   q, out [B, q_heads, D] of type, out's heads contiguous; kv_heads divides
- *   q_heads; table [B, table_pages] i32; lengths [B] i32;
+ *   q_heads; scale up to 2e38; table [B, table_pages] i32; lengths [B] i32;
  *   lse NULL or [B, q_heads] f32: log of the sum over j of e^(scale q . K_j),
  *   -infinity where nothing is left; by it, parts of a sequence that different
  *   calls attend to can be joined.
@@ -275,8 +275,10 @@ sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, in
  *   the token is the first kept i, in the order of the indices, up to and with
  *     which the kept weights' sum is above u times the sum of all of them.
  * Weights and sums are in 64 bits, so that only values that close to a border
- * depend on the order of summation; a weight below 2^-1022 is 0, and so is that
- * of a logit more than 3.4e38 below the highest.  A temperature that is not above 0 means
+ * depend on the order of summation; but top_p's sums over more logits than a
+ * top_k of 2048 count each weight to the nearest 2^-44 (the highest is 1).  A
+ * weight below 2^-1022 is 0, and so is that of a logit more than 3.4e38 below
+ * the highest.  A temperature that is not above 0 means
  * the highest logit's first index; top_k below 1 or above V, a top_p of 1 or
  * more or NaN, and a min_p that is not above 0 keep all; a top_p of 0 or less
  * and a min_p above 1 keep the highest.  u below 0 or NaN counts as 0, above 1

@@ -423,7 +423,8 @@ sim_status sim_cache_attention(void *stream, int32_t type, const void *q, int64_
         return refuse(SIM_ERR_INVALID_ARG, __func__, why);
     NEED(B >= 0 && table_pages >= 0 && window >= 0, "negative size");
     NEED(q_heads >= 1 && q_heads % kv_heads == 0, "kv_heads must divide q_heads");
-    NEED(std::isfinite(scale), "scale must be finite");
+    const float scale_log2 = (float)(scale * 1.4426950408889634);
+    NEED(std::isfinite(scale_log2), "scale must be finite, 2e38 at most");
     NEED(q_stride >= 0 && q_head_stride >= 0 && table_stride >= 0, "negative stride");
     FITS((int64_t)table_pages * page_size <= kMaxKeys, "a row of the table has room for more than 2^30 tokens");
     if (B == 0) return done(SIM_OK, __func__);
@@ -440,7 +441,7 @@ sim_status sim_cache_attention(void *stream, int32_t type, const void *q, int64_
     a.k_cache = k_cache, a.v_cache = v_cache, a.k_page_stride = k_page_stride, a.v_page_stride = v_page_stride;
     a.pages = pages, a.page_size = page_size;
     a.table = table, a.table_stride = table_stride, a.capacity = (int64_t)table_pages * page_size, a.lengths = lengths;
-    a.scale_log2 = (float)(scale * 1.4426950408889634), a.window = window;
+    a.scale_log2 = scale_log2, a.window = window;
     a.out = out, a.out_stride = out_stride, a.lse = lse, a.part = (float *)workspace;
     a.tiles = attend_tiles(q_heads / kv_heads, D), a.units = attend_units((int64_t)kv_heads * a.tiles, attend_resident(D, attend_heads(q_heads / kv_heads, D)));
     a.max_units = attend_max_units(B, a.units, a.capacity, window);

@@ -469,6 +469,7 @@ PyObject *append(PyObject *const *a) {  // cache, k, v, slots
     need(k.n == v.n && k.heads == c.heads && v.heads == c.heads && k.D == c.D && v.D == c.D, "k and v must be [T, kv heads, D]");
     need(k.type == c.type && v.type == c.type, "k and v must have the cache's type");
     need(slots.dim() == 1 && slots.size(0) == k.n && slots.scalar_type() == at::kLong && slots.is_contiguous(), "slots must be contiguous int64 [T]");
+    need(c.pages == 0 || c.k != c.v, "keys and values must be written to places of their own");
     need(k.dev == c.dev && v.dev == c.dev && slots.device() == c.dev, "tensors are on different GPUs");
     for (int i = 0; i < 2; i++)
         need(!c10::GradMode::is_enabled() || !THPVariable_Unpack(PyTuple_GET_ITEM(a[0], i)).requires_grad(),
@@ -506,7 +507,8 @@ PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, w
         need(o.n == q.n && o.heads == q.heads && o.D == q.D && o.type == q.type && o.dev == q.dev, "out must be as q");
         need((o.heads == 1 || o.head_stride == o.D) && (o.n <= 1 || o.stride >= o.heads * o.D), "out's heads must be contiguous and must not overlap");
         need(!out.requires_grad() || !c10::GradMode::is_enabled(), "out must not require a gradient: the result has none");
-        need(!out.is_alias_of(THPVariable_Unpack(a[0])), "out must not share q's memory");
+        for (PyObject *o : {(PyObject *)a[0], PyTuple_GET_ITEM(a[1], 0), PyTuple_GET_ITEM(a[1], 1)})
+            need(!out.is_alias_of(THPVariable_Unpack(o)), "out must not share memory with q or the cache");
     } else {
         out = fresh({q.n, q.heads, q.D}, q.type, q.dev);
     }

@@ -386,3 +386,14 @@ def test_refusals(ops):
                 dict(slots=slots.cpu()), dict(k=k.cpu()), dict(cache=P(torch.zeros_like(c.cache.k).requires_grad_(), c.cache.v))]:
         with pytest.raises(SimError):
             ops.cache_append(**{**dict(cache=c.cache, k=k, v=k, slots=slots), **bad})
+
+
+def test_results_in_memory_that_is_read_are_refused(ops):
+    from paper_2606_10440_amd import SimError
+    c = Case(ops, [20, 30])
+    k = torch.zeros(2, *c.cache.k.shape[1::2], dtype=c.cache.k.dtype, device="cuda")
+    for part in c.cache:
+        with pytest.raises(SimError, match="share"):
+            ops.cache_attention(c.q, c.cache, c.dtable, c.dlengths, out=part.reshape(-1)[:c.q.numel()].view_as(c.q))
+    with pytest.raises(SimError, match="own"):
+        ops.cache_append(ops.PagedCache(c.cache.k, c.cache.k), k, k, torch.zeros(2, dtype=torch.int64, device="cuda"))

@@ -45,7 +45,7 @@ ATTEND = [("type", 2), ("q", P), ("q_stride", 1024), ("q_head", 128), ("B", 3), 
 @pytest.mark.parametrize("change,want", CACHE_BAD + [
     (dict(heads=0), INVALID), (dict(heads=3), INVALID), (dict(q_heads=0), INVALID), (dict(B=-1), INVALID),
     (dict(table_pages=-1), INVALID), (dict(window=-1), INVALID), (dict(scale=float("nan")), INVALID),
-    (dict(scale=float("inf")), INVALID), (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(lengths=None), INVALID),
+    (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID), (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(lengths=None), INVALID),
     (dict(table=None), INVALID), (dict(q=P + 1), INVALID), (dict(out=P + 1), INVALID), (dict(table=P + 2), INVALID),
     (dict(lengths=P + 2), INVALID), (dict(lse=P + 2), INVALID), (dict(out_stride=1023), INVALID), (dict(q_stride=-1), INVALID),
     (dict(table_stride=-1), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 4), INVALID), (dict(ws_bytes=64), INVALID),
