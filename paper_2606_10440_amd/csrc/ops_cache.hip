@@ -118,8 +118,8 @@ __device__ inline int scan_units(const AttendArgs &a, int64_t b0, int unit) {
 // joining the units.  More heads to a kv head than 16 (32 up to D = 128) read the
 // keys again from the caches: 64 heads on one of D = 256, 330 us for 0.5 GB.  One
 // sequence of 300: 8 us, the chain of lengths, table, keys and values and the
-// waves' joint.  Pages of no whole 16 tokens exchange a row's offset for each key
-// (D = 80, 24 tokens a page: 2.4 TB/s).
+// waves' joint.  Pages of no whole 16 tokens exchange a row's offset for each key,
+// which costs 2 to 4 % (64 sequences of up to 8192: 221 us, pages of 24 and 216 of 16).
 template <int T, int DP, int HT, bool PAGE16>
 __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void attend(AttendArgs a) {
     constexpr int CH = DP / 32;                // 32 d of keys

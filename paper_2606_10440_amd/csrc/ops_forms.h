@@ -86,7 +86,8 @@ inline LayerForm layer_form(int64_t T, int E, int k, int64_t D, int64_t F, bool 
 constexpr int kAttendKeys = 32;       // keys of one step of a wave
 constexpr int kAttendMinUnit = 4;     // steps of a unit: one for each wave
 constexpr int kAttendWhole = 16;      // sequences of so many are not cut: joining costs more than three steps of a wave
-constexpr int kAttendGoodUnit = 16;
+constexpr int kAttendGoodUnit = 16;   // where units fill the GPU more than once they are no shorter
+constexpr int kAttendLongUnit = 32;   // up to which they fill it once
 constexpr int kAttendRounds = 4;
 constexpr int kAttendMostSteps = 1 << 26;  // a sequence has at most 2^30 tokens
 
@@ -108,11 +109,16 @@ constexpr int64_t attend_units(int64_t workgroups, int resident) {
 
 // Steps of a unit where all sequences have total: what fills the GPU once, if
 // that is little; else small enough that the last ones to run are a small part
-// of the whole.
+// of the whole.  Once up to 32 steps, since somewhat more than once is the worst
+// of both (16 sequences of up to 4096, 32 heads on 8, D = 128: 38 us, 46 with the
+// limit at 16 steps; 16 of 8192, 128 heads on 4: 64 and 75).  A whole number for
+// each wave: the last part of one takes as long (30 sequences, a window of 1000:
+// 31.8 us, 34.4 without).
 constexpr int attend_unit(int64_t total, int64_t units) {
     const int64_t once = (total + units - 1) / units, part = (total + units * kAttendRounds - 1) / (units * kAttendRounds);
-    const int64_t unit = once <= kAttendGoodUnit ? (once > kAttendMinUnit ? once : kAttendMinUnit) : part > kAttendGoodUnit ? part : kAttendGoodUnit;
-    return unit < kAttendMostSteps ? (int)unit : kAttendMostSteps;  // no sequence has more
+    const int64_t unit = once <= kAttendLongUnit ? (once > kAttendMinUnit ? once : kAttendMinUnit) : part > kAttendGoodUnit ? part : kAttendGoodUnit;
+    const int64_t whole = (unit + kAttendMinUnit - 1) / kAttendMinUnit * kAttendMinUnit;
+    return whole < kAttendMostSteps ? (int)whole : kAttendMostSteps;  // no sequence has more
 }
 
 // Steps that a sequence has at most.
