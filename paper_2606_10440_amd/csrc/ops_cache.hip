@@ -59,9 +59,18 @@ template <int T> __device__ inline float half_of(uint32_t w, int i) {
     return Elem<T>::get(__builtin_bit_cast(typename Elem<T>::type, (uint16_t)(i ? w >> 16 : w)));
 }
 
-__device__ inline int wave_sum(int v) {
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return v;
+// Sums over the lanes up to each, by moves between registers: every workgroup
+// begins with two of them.
+template <int CTRL, int ROWS> __device__ inline uint32_t add_from(uint32_t v) {
+    return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+__device__ inline uint32_t wave_scan(uint32_t v) {
+    v = add_from<0x111, 0xf>(v);  // from the lane before, of its row of 16
+    v = add_from<0x112, 0xf>(v);
+    v = add_from<0x114, 0xf>(v);
+    v = add_from<0x118, 0xf>(v);
+    v = add_from<0x142, 0xa>(v);     // lane 15's and 47's to the rows after
+    return add_from<0x143, 0xc>(v);  // lane 31's to the upper half
 }
 
 // Where a sequence's keys lie: steps of kKeys from first_step on.
@@ -83,19 +92,15 @@ __device__ inline Span span_of(const AttendArgs &a, int64_t b) {
 __device__ inline int steps_of_unit(const AttendArgs &a) {
     const int lane = threadIdx.x & 63;
     int64_t total = 0;
-    for (int64_t b0 = 0; b0 < a.B; b0 += 64) total += wave_sum(b0 + lane < a.B ? span_of(a, b0 + lane).steps : 0);
+    for (int64_t b0 = 0; b0 < a.B; b0 += 64)  // (64 times 2^25 fit 32 bits without a sign)
+        total += (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(b0 + lane < a.B ? span_of(a, b0 + lane).steps : 0), 63);
     return attend_unit(total, a.units);
 }
 __device__ inline int units_of(int steps, int unit) { return max(1, (steps + unit - 1) / unit); }
 // The units before sequence b0's lanes: inclusive sums over the wave.
 __device__ inline int scan_units(const AttendArgs &a, int64_t b0, int unit) {
     const int lane = threadIdx.x & 63;
-    int n = b0 + lane < a.B ? units_of(span_of(a, b0 + lane).steps, unit) : 0;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(n, d);
-        if (lane >= d) n += o;
-    }
-    return n;
+    return (int)wave_scan(b0 + lane < a.B ? units_of(span_of(a, b0 + lane).steps, unit) : 0);
 }
 
 // One unit of one sequence and kv head, for up to 16 HT of the heads that

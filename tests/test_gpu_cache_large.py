@@ -76,3 +76,20 @@ def test_many_heads_and_no_pages(ops):
     lengths = torch.tensor([2000, 5, 1999], dtype=torch.int32, device="cuda")
     out, lse = ops.cache_attention(q, ops.PagedCache(k, k.clone()), table, lengths, return_lse=True)
     assert not out.any() and (lse == float("-inf")).all()
+
+
+def test_lengths_that_add_up_past_31_bits(ops):
+    # 64 sequences of 2^30 tokens, 2^31 steps of 32, on pages that are not there but for one of 2^20 tokens
+    page, D = 1 << 20, 8
+    k = torch.zeros(1, 1, page, D, dtype=torch.bfloat16, device="cuda")
+    table = torch.full((64, (1 << 30) // page), -1, dtype=torch.int32, device="cuda")
+    table[5, 0] = table[63, -1] = 0
+    lengths = torch.full((64,), 1 << 30, dtype=torch.int32, device="cuda")
+    q = torch.ones(64, 1, D, dtype=torch.bfloat16, device="cuda")
+    out, lse = ops.cache_attention(q, ops.PagedCache(k, torch.ones_like(k)), table, lengths, return_lse=True)
+    some = torch.zeros(64, dtype=torch.bool)
+    some[[5, 63]] = True
+    out, lse = out.cpu().float(), lse.cpu()
+    assert (out[some] == 1).all() and not out[~some].any()  # sums of ones up to 2^20 are exact
+    assert (lse[~some] == float("-inf")).all()
+    assert ((lse[some].double() - 20 * np.log(2)).abs() <= 4 * 20 * np.log(2) * 2.0 ** -24).all()  # a logarithm, a constant, a product
