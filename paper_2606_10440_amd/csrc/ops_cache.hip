@@ -79,6 +79,7 @@ struct Span {
 };
 __device__ inline Span span_of(const AttendArgs &a, int64_t b) {
     Span s;
+    b = min(b, a.B - 1);
     s.end = (int)min((int64_t)max(a.lengths[b], 0), a.capacity);
     s.start = a.window > 0 ? max(0, s.end - a.window) : 0;
     s.first_step = s.start / kKeys;
@@ -88,19 +89,21 @@ __device__ inline Span span_of(const AttendArgs &a, int64_t b) {
 
 // How the sequences are cut: into units of so many steps, the same for all,
 // so that long sequences among short ones are shared alike; a sequence has one
-// unit at least.  Every wave works that out from all lengths by itself.
-__device__ inline int steps_of_unit(const AttendArgs &a) {
+// unit at least.  Every wave works that out from all lengths by itself; first
+// is what lane holds of the first 64, which are not loaded twice.
+__device__ inline int steps_of_unit(const AttendArgs &a, const Span &first) {
     const int lane = threadIdx.x & 63;
     int64_t total = 0;
-    for (int64_t b0 = 0; b0 < a.B; b0 += 64)  // (64 times 2^25 fit 32 bits without a sign)
-        total += (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(b0 + lane < a.B ? span_of(a, b0 + lane).steps : 0), 63);
+    for (int64_t b0 = 0; b0 < a.B; b0 += 64) {  // (64 times 2^25 fit 32 bits without a sign)
+        const int steps = b0 ? span_of(a, b0 + lane).steps : first.steps;
+        total += (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(b0 + lane < a.B ? steps : 0), 63);
+    }
     return attend_unit(total, a.units);
 }
 __device__ inline int units_of(int steps, int unit) { return max(1, (steps + unit - 1) / unit); }
-// The units before sequence b0's lanes: inclusive sums over the wave.
-__device__ inline int scan_units(const AttendArgs &a, int64_t b0, int unit) {
-    const int lane = threadIdx.x & 63;
-    return (int)wave_scan(b0 + lane < a.B ? units_of(span_of(a, b0 + lane).steps, unit) : 0);
+// The units up to sequence b0 + lane from b0 on, whose span is s.
+__device__ inline int scan_units(const AttendArgs &a, int64_t b0, const Span &s, int unit) {
+    return (int)wave_scan(b0 + (int)(threadIdx.x & 63) < a.B ? units_of(s.steps, unit) : 0);
 }
 
 // One unit of one sequence and kv head, for up to 16 HT of the heads that
@@ -143,24 +146,28 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
     // the unit's sequence
     int64_t b = a.splits || u >= a.B ? -1 : u;
     int before = u, n_units = 1, unit = kAttendWhole;
-    if (a.splits) unit = __builtin_amdgcn_readfirstlane(steps_of_unit(a));
+    const Span first = span_of(a, a.splits ? lane : u);
+    Span sp = first;
+    if (a.splits) unit = __builtin_amdgcn_readfirstlane(steps_of_unit(a, first));
     for (int64_t b0 = 0, base = 0; a.splits && b0 < a.B; b0 += 64) {
-        const int n = scan_units(a, b0, unit);
+        const Span s = b0 ? span_of(a, b0 + lane) : first;
+        const int n = scan_units(a, b0, s, unit);
         const uint64_t past = __ballot((int64_t)u < base + n);
         if (past) {
             const int l = __ffsll((unsigned long long)past) - 1;
             b = b0 + l;
-            before = (int)base + (l ? __shfl(n, l - 1) : 0);
-            n_units = (int)base + __shfl(n, l) - before;
+            const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            sp = {of(s.start), of(s.end), of(s.first_step), of(s.steps)};
+            before = (int)base + (l ? __builtin_amdgcn_readlane(n, l - 1) : 0);
+            n_units = (int)base + of(n) - before;
             break;
         }
-        base += __shfl(n, 63);
+        base += __builtin_amdgcn_readlane(n, 63);
     }
     if (b < 0) return;  // the whole workgroup: no such unit
     b = __builtin_amdgcn_readfirstlane((int)b);
     before = __builtin_amdgcn_readfirstlane(before);
     n_units = __builtin_amdgcn_readfirstlane(n_units);
-    Span sp = span_of(a, b);
     sp.start = __builtin_amdgcn_readfirstlane(sp.start);
     sp.end = __builtin_amdgcn_readfirstlane(sp.end);
     const int step_end = sp.first_step + min(sp.steps, (u - before + 1) * unit);
@@ -447,12 +454,13 @@ template <int T> __global__ __launch_bounds__(256) void attend_join(AttendArgs a
     constexpr float kShift = T == SIM_TYPE_F16 ? 15.f : 0.f;
     const int64_t b = blockIdx.x / a.q_heads;
     const int h = (int)(blockIdx.x % a.q_heads), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D;
-    const int unit = steps_of_unit(a), n = units_of(span_of(a, b).steps, unit);
+    const Span first = span_of(a, lane);
+    const int unit = steps_of_unit(a, first), n = units_of(span_of(a, b).steps, unit);
     if (n == 1) return;  // it is written
     int u0 = 0;
     for (int64_t b0 = 0; b0 < b; b0 += 64) {
-        const int s = scan_units(a, b0, unit);
-        u0 += __shfl(s, (int)min((int64_t)63, b - 1 - b0));
+        const int s = scan_units(a, b0, b0 ? span_of(a, b0 + lane) : first, unit);
+        u0 += __builtin_amdgcn_readlane(s, (int)min((int64_t)63, b - 1 - b0));
     }
     const float *const part = a.part + ((int64_t)u0 * a.q_heads + h) * D;
     const float *const stat = a.part + (int64_t)a.max_units * a.q_heads * D + ((int64_t)u0 * a.q_heads + h) * 2;
