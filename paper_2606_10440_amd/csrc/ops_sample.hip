@@ -62,12 +62,13 @@ template <int T> constexpr int kKeyBits = T == SIM_TYPE_F32 ? 32 : 16;
 // Sums over the lanes up to each, of 64-bit whole numbers or values, by moves
 // between registers (an exchange through LDS takes some 100 cycles, and there
 // are six, one after another).
-template <int CTRL, int ROWS, typename V> __device__ inline V add_from(V v) {
+template <int CTRL, int ROWS, typename V> __device__ inline V moved(V v) {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
-    return v + __builtin_bit_cast(V, lo | (uint64_t)hi << 32);
+    return __builtin_bit_cast(V, lo | (uint64_t)hi << 32);
 }
+template <int CTRL, int ROWS, typename V> __device__ inline V add_from(V v) { return v + moved<CTRL, ROWS>(v); }
 template <typename V> __device__ inline V row_scan(V v) {  // of 16 lanes
     v = add_from<0x111, 0xf>(v);                           // from the lane before
     v = add_from<0x112, 0xf>(v);                           // two before
@@ -83,6 +84,14 @@ template <typename V> __device__ inline V lane_of(V v, int lane) {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     return __builtin_bit_cast(V, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)b, lane) |
                                      (uint64_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32);
+}
+__device__ inline uint64_t wave_max(uint64_t v) {
+    v = max(v, moved<0x111, 0xf>(v));
+    v = max(v, moved<0x112, 0xf>(v));
+    v = max(v, moved<0x114, 0xf>(v));
+    v = max(v, moved<0x118, 0xf>(v));
+    v = max(v, moved<0x142, 0xa>(v));
+    return lane_of(max(v, moved<0x143, 0xc>(v)), 63);
 }
 // Sums over the workgroup's threads before each, and over all, from own values.
 template <int NT, typename V> __device__ inline V block_scan(V own, V *wave_sums, V &all) {
@@ -367,9 +376,7 @@ template <int T> __device__ inline Task<T> task_from(const SampleArgs &a, int64_
 // The same from its slices' tops, in every wave.
 template <int T> __device__ inline Task<T> task_of(const SampleArgs &a, const Plan &p, int64_t b) {
     const int lane = threadIdx.x & 63;
-    uint64_t top = lane < p.slices ? p.tops[(b - p.row0) * p.slices + lane] : 0;
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
-    return task_from<T>(a, b, top);
+    return task_from<T>(a, b, wave_max(lane < p.slices ? p.tops[(b - p.row0) * p.slices + lane] : 0));
 }
 __device__ inline double number_of(const SampleArgs &a, int64_t b) {
     return a.u[b] > 0.f ? (double)min(a.u[b], 1.f - 5.9604644775390625e-8f) : 0.;
@@ -499,9 +506,7 @@ template <int T, int NW, typename F> __device__ inline uint64_t highest(const Ro
         }
         at += first;
     }
-    uint64_t top = (uint64_t)key << 32 | (uint32_t)~at;
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (uint64_t)__shfl_xor((unsigned long long)top, d));
-    return top;
+    return wave_max((uint64_t)key << 32 | (uint32_t)~at);
 }
 
 template <int T> __global__ __launch_bounds__(kThreads) void sample_tops(SampleArgs a, Plan p, bool with_eights) {
@@ -569,7 +574,7 @@ template <int T> __global__ __launch_bounds__(kThreads) void sample_bins(SampleA
     uint64_t target = (uint64_t)t.top_k, above = 0, all = 0;
     if (t.kind == kWeight) {
         for (int i = threadIdx.x; i < kBins; i += kThreads) all += s_bin[i];
-        for (int d = 1; d < 64; d <<= 1) all += __shfl_xor((unsigned long long)all, d);
+        all = lane_of(wave_scan(all), 63);
         if ((threadIdx.x & 63) == 0) wave64[threadIdx.x >> 6] = all;
         __syncthreads();
         all = wave64[0] + wave64[1] + wave64[2] + wave64[3];
@@ -970,9 +975,8 @@ template <int T> struct Kept {
                     }
                 }
             }
-            for (int d = 1; d < 64; d <<= 1)
 #pragma unroll
-                for (int n = 0; n < kAhead; n++) sum[n] += __shfl_xor(sum[n], d);
+            for (int n = 0; n < kAhead; n++) sum[n] = wave_sum(sum[n]);
 #pragma unroll
             for (int n = 0; n < kAhead; n++)
                 if ((int)(threadIdx.x & 63) == n && c0 + n * NW < end) put(c0 + n * NW, sum[n]);
