@@ -15,7 +15,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // A thread moves one piece of PIECE elements: sixteen bytes where the rows are
 // aligned to that.  It is a copy, bound by memory: 20011 tokens of 8 x 128, 164 MB
-// read and written, 27 us (6 TB/s); 64 tokens 2.9 us, launch.
+// read and written, 27 us (6 TB/s); 64 tokens 3.0 us, launch.
 template <int PIECE>
 __global__ __launch_bounds__(256) void append_rows(AppendArgs a, int pieces_of_row, int64_t pieces) {
     const bool is_v = blockIdx.y;
@@ -121,13 +121,13 @@ __device__ inline int scan_units(const AttendArgs &a, int64_t b0, const Span &s,
 // fp16 weights are 2^15 times as large as the highest's 1, so that small ones,
 // of which a long sequence may have many, are not lost.
 //
-// Memory bounds it: 64 sequences of up to 8192 tokens, 8 heads of 128 for 32, 190
-// us for 1.1 GB; two of 131072, 64 heads, 179 us (5.8 TB/s), and 8 to 10 us for
+// Memory bounds it: 64 sequences of up to 8192 tokens, 8 heads of 128 for 32, 183
+// us for 1.1 GB; two of 131072, 64 heads, 175 us (5.9 TB/s), and 7 to 8 us for
 // joining the units.  More heads to a kv head than 16 (32 up to D = 128) read the
-// keys again from the caches: 64 heads on one of D = 256, 330 us for 0.5 GB.  One
+// keys again from the caches: 64 heads on one of D = 256, 296 us for 0.5 GB.  One
 // sequence of 300: 8 us, the chain of lengths, table, keys and values and the
 // waves' joint.  Pages of no whole 16 tokens exchange a row's offset for each key,
-// which costs 2 to 4 % (64 sequences of up to 8192: 221 us, pages of 24 and 216 of 16).
+// which costs 2 to 4 % (64 sequences of up to 8192, fresh ones: 221 us, pages of 24, and 216 of 16).
 template <int T, int DP, int HT, bool PAGE16>
 __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void attend(AttendArgs a) {
     constexpr int CH = DP / 32;                // 32 d of keys

@@ -84,6 +84,20 @@ def test_many_tokens(ops, kind, score):
     check(r, ref.route(v, 2, None, True, score, b, 4, 2, 2))
 
 
+@pytest.mark.parametrize("T,E,k", [(4096, 1024, 2), (4097, 1024, 2), (6976, 600, 3), (6977, 600, 3), (20928, 200, 4), (20929, 200, 4), (24576, 33, 5), (24577, 33, 5)])
+def test_lists_on_both_sides_of_the_scan(ops, T, E, k):
+    z, v = logits(T, T, E, "bf16")
+    mask, _ = masks(E, T, E, "token")
+    for how in (dict(), dict(score="sigmoid", scale=2.0)):
+        r = ops.moe_route(z, k, mask, **how)
+        flat = r.experts.reshape(-1)
+        slots = (flat >= 0).nonzero().reshape(-1)
+        n = len(slots)
+        assert torch.equal(r.order[:n].long(), slots[torch.argsort(flat[slots], stable=True)]) and (r.order[n:] == -1).all()
+        count = torch.zeros(E, dtype=torch.int64, device="cuda").scatter_add_(0, flat[slots].long(), torch.ones_like(slots))
+        assert r.offsets[0] == 0 and torch.equal(r.offsets[1:].long(), count.cumsum(0))
+
+
 @pytest.mark.parametrize("best", [1, 2])
 @pytest.mark.parametrize("biased", [False, True])
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
