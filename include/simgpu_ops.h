@@ -276,7 +276,7 @@ sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, in
  *     which the kept weights' sum is above u times the sum of all of them.
  * Weights and sums are in 64 bits, so that only values that close to a border
  * depend on the order of summation; but top_p's sums over more logits than a
- * top_k of 2048 count each weight to the nearest 2^-44 (the highest is 1).  A
+ * top_k of 2048 count each weight to the nearest 2^-43 (the highest is 1).  A
  * weight below 2^-1022 is 0, and so is that of a logit more than 3.4e38 below
  * the highest.  A temperature that is not above 0 means
  * the highest logit's first index; top_k below 1 or above V, a top_p of 1 or

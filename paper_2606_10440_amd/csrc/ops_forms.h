@@ -134,4 +134,10 @@ constexpr int64_t attend_max_units(int64_t B, int64_t units, int64_t capacity, i
     return !attend_splits(capacity, window) ? B : each < (cut + B - 1) / B ? B * each : cut;
 }
 
+// ------------------------------------------------------------------ sampling
+
+// Weights are at most 1: as whole multiples of 2^-43, their sums over a row of
+// 2^20 fit 64 bits, and do not depend on the order in which they are added.
+constexpr double kWeightUnit = 8796093022208.;
+
 }  // namespace simops

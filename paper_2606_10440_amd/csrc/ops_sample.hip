@@ -36,9 +36,8 @@ constexpr int kAll = 1024;     // of one that has what is left of a row, or all 
 constexpr int kAllWaves = kAll / 64;
 constexpr int kDigit = 11;
 constexpr int kBins = 1 << kDigit;
-// Weights are at most 1: as whole multiples of 2^-44, of 2^20 of them, their
-// sums fit 64 bits, and do not depend on the order in which they are added.
-constexpr double kUnit = 17592186044416.;
+constexpr double kUnit = kWeightUnit;
+static_assert(kUnit * SIM_SAMPLE_MAX_V < 18446744073709551616., "the sum of a row's weights fits 64 bits");
 
 // Keys that order as logits do: NaN above everything, -infinity 0.
 template <int T> __device__ inline uint32_t key_of(typename Elem<T>::type v) {
@@ -920,7 +919,7 @@ template <int T> __global__ __launch_bounds__(kAll) void sample_sorted(SampleArg
         token = t.token();
     } else if (t.kind == kAlone || n > kList) {
         token = search_row<T>(t.row, s.alone, t.top_k, t.top_p, t.min_p, u);
-    } else if (t.kind == kNumber && state.border < 0) {  // a top-k beyond the logits that there are: all of them
+    } else if (t.kind != kListed && state.border < 0) {  // a top-k beyond the logits that there are: all of them
         if (threadIdx.x == 0) state.lowest = kLowest<T>, state.cut = (uint32_t)a.V, state.mode = kBordered;
     } else {
         const uint64_t *const list = p.list + r * kList;
