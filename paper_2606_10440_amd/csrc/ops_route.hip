@@ -725,14 +725,13 @@ __global__ __launch_bounds__(16 * CH) void route_scored(RouteArgs a, int32_t *__
             near |= j && m && gap <= fast.apart;
             before = m;
             if (j == k - 1) wanted = m;
-            if (l == (j & 15)) {
+            if ((j < k || ranked) && l == (j & 15)) {  // (of 32 and one more the last has no place)
                 mine[j >> 4] = m;
                 mine_e[j >> 4] = Fast<NV>::kIndex - (m & Fast<NV>::kIndex);
             }
         }
         if (!ranked) {
             fast.sure = fast.sure && !near;
-            if (k < 32 && l == (k & 15)) mine[k >> 4] = 0;
         } else {
             if (before && (wanted >> Fast<NV>::kIndexBits) - (before >> Fast<NV>::kIndexBits) <= fast.apart) fast.sure = false;
             if (__ballot(near && live)) mine_e[0] = rank_chosen(mine[0] != 0, mine_e[0], mine[0] ? (double)Elem<T>::get(z[mine_e[0]]) : 0., a.bias);
