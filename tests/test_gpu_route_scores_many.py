@@ -1,12 +1,12 @@
-"""The router with scores where there are more tokens than one workgroup takes a wave each for: large k;
-choices and lists exactly."""
+"""The router with scores where there are more tokens than one workgroup takes a wave each for: large k, many experts, groups
+of every kind; choices and lists exactly."""
 from __future__ import annotations
 
 import numpy as np
 import pytest
 
 from tests import route_reference as ref
-from tests.test_gpu_route_scores import check, logits, masks
+from tests.test_gpu_route_scores import TYPES, check, logits, masks
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -38,6 +38,24 @@ def test_large_k(ops, T, E, k, score, biased):
     run(ops, T, E, 1, 1, 1, k, "bf16", score, biased, "token", False)
     if E % 4 == 0 and E // 2 >= k:
         run(ops, T, E, 4, 2, 2, k, "fp32", score, biased)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("biased", [True, False])
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("T", [17, 70])
+@pytest.mark.parametrize("shape", [(8, 4, 2, 2, 3), (16, 16, 5, 2, 5), (30, 30, 4, 2, 4), (36, 2, 1, 2, 18), (60, 5, 2, 2, 4), (64, 64, 10, 2, 10), (96, 3, 2, 2, 7),
+                                   (160, 8, 3, 1, 6), (256, 16, 5, 1, 9), (512, 64, 9, 2, 17), (640, 64, 6, 1, 9), (700, 7, 3, 2, 17), (1024, 16, 3, 2, 32),
+                                   (1024, 64, 10, 1, 32)])
+def test_shapes(ops, kind, score, biased, T, shape):
+    E, groups, top_groups, best, k = shape
+    run(ops, T, E, groups, top_groups, best, k, kind, score, biased, "token" if T == 70 else "", T == 17)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("k", [15, 32])
+def test_many_tokens_with_many_choices(ops, score, k):
+    run(ops, 4200, 64, 4, 3, 2, k, "fp32", score, True, "token")
 
 
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
