@@ -943,8 +943,9 @@ template <int T> struct Kept {
         : row(t.row), exp(t.row, table), top(t.top), min_p(t.min_p) {
         low = all ? -INFINITY : value_of<T>(lowest);
         cut = all ? INT32_MIN : cut_;
-        // further below the highest than this nothing is left by min-p, whatever the rounding
-        far = min_p > 0.f ? min((float)(-log((double)min_p) / row.per * 1.0001 + 1e-30), exp.far) : exp.far;
+        // further below the highest than this nothing is left by min-p, whatever the rounding (a weight of 1 - 10^-9
+        // is below 1, one of 1 - 10^-17 is not: of a min-p of 1 a high temperature may leave all)
+        far = min_p > 0.f ? (float)min((1e-9 - log((double)min_p) * 1.0001) / row.per, (double)exp.far) : exp.far;
     }
     __device__ bool in(float z, int i) const { return (z > low || (z == low && i <= cut)) && !(top - z > far); }
     __device__ double weight(typename Elem<T>::type v, int i) const {
