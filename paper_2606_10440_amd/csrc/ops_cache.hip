@@ -59,6 +59,10 @@ template <int T> __device__ inline float half_of(uint32_t w, int i) {
     return Elem<T>::get(__builtin_bit_cast(typename Elem<T>::type, (uint16_t)(i ? w >> 16 : w)));
 }
 
+// What the highest weight is.
+template <int T> constexpr float kLog2Times = T == SIM_TYPE_F16 ? 15.f : 0.f;
+template <int T> constexpr float kTimes = T == SIM_TYPE_F16 ? 32768.f : 1.f;
+
 // Sums over the lanes up to each, by moves between registers: every workgroup
 // begins with two of them.
 template <int CTRL, int ROWS> __device__ inline uint32_t add_from(uint32_t v) {
@@ -119,7 +123,9 @@ __device__ inline int scan_units(const AttendArgs &a, int64_t b0, const Span &s,
 // Weights are rounded in two parts, which keep 16 bits (bf16) or 22 (fp16) of
 // them: rounded once they would add as much error as rounding the result does.
 // fp16 weights are 2^15 times as large as the highest's 1, so that small ones,
-// of which a long sequence may have many, are not lost.
+// of which a long sequence may have many, are not lost: multiplied by that, since
+// a distance of 15 would be rounded with the scores (from 2^24 on to 16, whose 2^16
+// fp16 does not hold).
 //
 // Memory bounds it: 64 sequences of up to 8192 tokens, 8 heads of 128 for 32, 183
 // us for 1.1 GB; two of 131072, 64 heads, 175 us (5.9 TB/s), and 7 to 8 us for
@@ -133,7 +139,6 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
     constexpr int CH = DP / 32;                // 32 d of keys
     constexpr int NV = DP == 64 ? 4 : 8;       // consecutive d of values in a lane
     constexpr int NH = DP / (16 * NV);         // times that
-    constexpr float kShift = T == SIM_TYPE_F16 ? 15.f : 0.f;
     constexpr int kPitch = DP + 4;
     __shared__ float s_o[kWaves][16][kPitch];
     __shared__ float s_m[kWaves][HT * 16], s_l[kWaves][HT * 16];
@@ -342,9 +347,9 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
             for (int e = 0; e < 8; e++) top = fmaxf(top, v[e]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float off = top == -INFINITY ? 0.f : top - kShift;
+            const float off = top == -INFINITY ? 0.f : top;
             if (__ballot(top > m[t])) {
-                const float less = __builtin_amdgcn_exp2f(m[t] == -INFINITY ? -INFINITY : m[t] - kShift - off);
+                const float less = __builtin_amdgcn_exp2f(m[t] - off);
                 m[t] = top;
                 l[t] *= less;
 #pragma unroll
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                v[e] = __builtin_amdgcn_exp2f(v[e] - off);
+                v[e] = __builtin_amdgcn_exp2f(v[e] - off) * kTimes<T>;
                 l[t] += v[e];
             }
 #pragma unroll
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
 #pragma unroll
                     for (int i = 0; i < 8; i++) p[i] = (uint16_t)(out[i / 2] >> (16 * (i & 1)));
                 }
-                if (a.lse && d == 0) a.lse[b * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718056f;
+                if (a.lse && d == 0) a.lse[b * a.q_heads + qh] = sum == 0.f ? -INFINITY : (top + (log2f(sum) - kLog2Times<T>)) * 0.69314718056f;
             } else {
                 float *p = part + ((int64_t)u * a.q_heads + qh) * D + d;
                 *(f32x4 *)p = f32x4{v[0], v[1], v[2], v[3]};
@@ -451,7 +456,6 @@ __global__ __launch_bounds__(64 * kWaves, attend_resident(DP, 16 * HT)) void att
 template <int T> __global__ __launch_bounds__(256) void attend_join(AttendArgs a) {
     __shared__ f32x4 s_v[256];
     __shared__ float s_top[4];
-    constexpr float kShift = T == SIM_TYPE_F16 ? 15.f : 0.f;
     const int64_t b = blockIdx.x / a.q_heads;
     const int h = (int)(blockIdx.x % a.q_heads), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.D;
     const Span first = span_of(a, lane);
@@ -513,7 +517,7 @@ template <int T> __global__ __launch_bounds__(256) void attend_join(AttendArgs a
         for (int i = 0; i < 4; i++) p[i] = (uint16_t)(out[i / 2] >> (16 * (i & 1)));
     }
     if (a.lse && threadIdx.x == 0)
-        a.lse[b * a.q_heads + h] = sum == 0.f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718056f;
+        a.lse[b * a.q_heads + h] = sum == 0.f ? -INFINITY : (top + (log2f(sum) - kLog2Times<T>)) * 0.69314718056f;
 }
 
 template <int T, int DP, int HT> void attend_t(hipStream_t st, const AttendArgs &a) {
