@@ -454,6 +454,7 @@ Paged paged(PyObject *o) {
     need(k.is_cuda() && v.device() == k.device(), "the cache must be on one GPU");
     const int64_t pages = k.size(0), heads = k.size(1), size = k.size(2), D = k.size(3);
     need(heads > 0 && heads < 1 << 20 && size > 0 && size < (int64_t)1 << 31, "bad sizes of the cache");
+    need(D > 0 && D <= SIM_CACHE_MAX_D, "D must be a multiple of 8 up to 256");
     const auto whole_pages = [&](const Tensor &t) {
         return (D <= 1 || t.stride(3) == 1) && (size == 1 || t.stride(2) == D) && (heads == 1 || t.stride(1) == size * D);
     };
@@ -497,7 +498,6 @@ PyObject *attention(PyObject *const *a) {  // q, cache, table, lengths, scale, w
     const int64_t window = whole(a[5]);
     need(window >= 0 && window < (int64_t)1 << 31, "window must not be negative");
     const bool want_lse = truth(a[6]);
-    need(c.D > 0, "D must be a multiple of 8 up to 256");
     const double scale = a[4] == Py_None ? 1 / std::sqrt((double)c.D) : number(a[4]);
     Tensor out, lse;
     const bool given = a[7] != Py_None;
