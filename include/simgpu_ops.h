@@ -226,7 +226,9 @@ sim_status sim_moe_experts(void *hip_stream, const void *x, int32_t type, int64_
  * cache is skipped, and so is its token.  Tokens must differ in their slots:
  * where two have the same, each 16 bytes that it holds after the call are of
  * one of them.  Strides between tokens and heads count elements; a row of D is
- * contiguous and may lie anywhere its type may.
+ * contiguous and may lie anywhere its type may, in the cache too where no slot
+ * is written, but not where one is.  The pages of keys and those of values must
+ * not share memory: arrays that reach into each other have one page stride.
  */
 #define SIM_CACHE_MAX_D 256
 sim_status sim_cache_append(void *hip_stream, int32_t type, const void *k, int64_t k_stride, int64_t k_head_stride,

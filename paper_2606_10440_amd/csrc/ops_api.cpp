@@ -398,6 +398,9 @@ sim_status sim_cache_append(void *stream, int32_t type, const void *k, int64_t k
     if (T == 0 || pages == 0) return done(SIM_OK, __func__);
     NEED(k && v && slots, "null array");
     NEED(aligned_to(k, 2) && aligned_to(v, 2) && aligned_to(slots, 8), "array not aligned to its type");
+    NEED(!pages_meet((uintptr_t)k_cache, (uint64_t)k_page_stride * 2, (uintptr_t)v_cache, (uint64_t)v_page_stride * 2, (uint64_t)pages,
+                     (uint64_t)kv_heads * page_size * D * 2),
+         "keys and values must be written to places of their own");
     const AppendArgs a = {k, v, k_stride, k_head_stride, v_stride, v_head_stride, T, kv_heads, D, slots, k_cache, v_cache,
                           k_page_stride, v_page_stride, pages, page_size};
     return done(launch_append((hipStream_t)stream, a), __func__);

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <utility>
 
 namespace simops {
 
@@ -79,6 +80,24 @@ inline LayerForm layer_form(int64_t T, int E, int k, int64_t D, int64_t F, bool 
     if (mean <= kShortList || D < 8 || F < 8 || (tiles * ((mean + 31) / 32) <= kSlots / 8 && !odd)) return kGroup1;
     if (!mx4 && mean > 24 && (tiles > kSlots / 2 || odd)) return kGroup4;
     return kGroup2;
+}
+
+// ------------------------------------------------------------------ paged cache
+
+// Whether the pages of two arrays share memory: of so many bytes each, at a, a +
+// a_stride, ... and b, b + b_stride, ..., none within its own array.  Arrays of
+// one stride may lie between each other; of two that reach into each other with
+// different strides none is known to be apart.
+inline bool pages_meet(uint64_t a, uint64_t a_stride, uint64_t b, uint64_t b_stride, uint64_t pages, uint64_t page) {
+    typedef unsigned __int128 u128;
+    if (pages == 0) return false;
+    if (b < a) std::swap(a, b), std::swap(a_stride, b_stride);
+    if (b - a >= (u128)(pages - 1) * a_stride + page) return false;  // behind it
+    if (pages == 1) return true;
+    if (a_stride != b_stride) return true;
+    // a's last page that begins before b, and the next one
+    const uint64_t i = (b - a) / a_stride, before = (b - a) % a_stride;
+    return before < page || (i + 1 < pages && a_stride - before < page);
 }
 
 // ------------------------------------------------------------------ attention over a paged cache

@@ -470,7 +470,6 @@ PyObject *append(PyObject *const *a) {  // cache, k, v, slots
     need(k.n == v.n && k.heads == c.heads && v.heads == c.heads && k.D == c.D && v.D == c.D, "k and v must be [T, kv heads, D]");
     need(k.type == c.type && v.type == c.type, "k and v must have the cache's type");
     need(slots.dim() == 1 && slots.size(0) == k.n && slots.scalar_type() == at::kLong && slots.is_contiguous(), "slots must be contiguous int64 [T]");
-    need(c.pages == 0 || c.k != c.v, "keys and values must be written to places of their own");
     need(k.dev == c.dev && v.dev == c.dev && slots.device() == c.dev, "tensors are on different GPUs");
     for (int i = 0; i < 2; i++)
         need(!c10::GradMode::is_enabled() || !THPVariable_Unpack(PyTuple_GET_ITEM(a[0], i)).requires_grad(),

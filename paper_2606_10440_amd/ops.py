@@ -261,7 +261,9 @@ class PagedCache(NamedTuple):
 def cache_append(cache: PagedCache, k, v, slots):
     """Writes the rows k and v [T, kv heads, D] of T tokens into the cache, at
     ``slots`` [T] (int64): page * page size + place in the page.  Tokens whose
-    slot is not in the cache (-1 say) are skipped; no two may have the same."""
+    slot is not in the cache (-1 say) are skipped; no two may have the same.
+    The rows may be the cache's own, but not where a slot is written.  The
+    cache carries no gradients, whatever k and v require."""
     _c().append(cache, k, v, slots)
 
 
