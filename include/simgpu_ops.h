@@ -244,12 +244,13 @@ sim_status sim_cache_append(void *hip_stream, int32_t type, const void *k, int64
  *   max(0, n - window) <= j < n = lengths[b]  (window 0: from 0 on).
  * lengths count the new token where its row is in the cache; below 0 they
  * count as 0, above table_pages * page_size (at most 2^30) as that.  Tokens on
- * a page that is not one of the cache's (-1 say) are left out, and so is a
- * score of -infinity; where nothing is left, out is 0.  What other places of
- * the cache hold has no effect.  Scores, weights and sums are in 32 bits (the
- * products' operands: q, K and V as they are, the weights in two parts of type).
- * An infinity among the V makes the results that it enters infinite or NaN, and
- * no others.
+ * a page that is not one of the cache's (-1 say) are left out.  A score of
+ * -infinity has no weight; where nothing has any, out is 0.  What other places
+ * of the cache hold has no effect.  Scores, weights and sums are in 32 bits (the
+ * products' operands: q, K and V as they are, the weights in two parts of type);
+ * V are summed before the division, so V whose sum passes 3.4e38 give infinities.
+ * An infinity among the V of tokens that are not left out makes the results that
+ * it enters infinite or NaN, with a weight of 0 too, and no others.
  *   q, out [B, q_heads, D] of type, out's heads contiguous; kv_heads divides
  *   q_heads; scale up to 2e38; table [B, table_pages] i32; lengths [B] i32;
  *   lse NULL or [B, q_heads] f32: log of the sum over j of e^(scale q . K_j),
@@ -276,8 +277,8 @@ sim_status sim_cache_attention(void *hip_stream, int32_t type, const void *q, in
  *     and of these the ones with w_i >= min_p; the highest always is;
  *   the token is the first kept i, in the order of the indices, up to and with
  *     which the kept weights' sum is above u times the sum of all of them.
- * Weights and sums are in 64 bits, so that only values that close to a border
- * depend on the order of summation; but top_p's sums over more logits than a
+ * Weights and sums are in 64 bits, a weight good to 2^-42 of itself, so that only
+ * values that close to a border depend on how it is computed; but top_p's sums over more logits than a
  * top_k of 2048 count each weight to the nearest 2^-43 (the highest is 1).  A
  * weight below 2^-1022 is 0, and so is that of a logit more than 3.4e38 below
  * the highest.  A temperature that is not above 0 means

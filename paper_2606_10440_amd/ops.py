@@ -275,7 +275,8 @@ def cache_attention(q, cache: PagedCache, table, lengths, scale=None, window=0, 
     head of the cache.  ``scale`` is D ** -0.5 unless given.  Returns [B, q
     heads, D], 0 where there is nothing to attend to; with ``return_lse`` also
     the logarithm of each head's sum of weights, float32 [B, q heads].  ``out``
-    may have strided rows.  The result carries no gradients."""
+    may have strided rows; it may not be of the storage of q or the cache.
+    The result carries no gradients."""
     return _c().attention(q, cache, table, lengths, scale, window, return_lse, out)
 
 
